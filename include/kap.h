@@ -508,6 +508,151 @@ kap_status kap_materialize_view(
     void* cuda_stream);
 
 /*
+ * kap_append_kv_rope - kap_append_kv with the position rotation applied on the way.  The pool holds
+ * keys encoded at their logical index and the attention calls expect queries encoded at theirs
+ * (the paper's logical-position preservation, Section 2.1); this call takes q, k and v as a
+ * projection leaves them, rotates q and k, and places k and v into their slots exactly as
+ * kap_append_kv does (same token order, block table, ctx_len rule and layouts).
+ *   angle of pair i of a head at row r:  pos(axis_i, r) * inv_freq[i],  i < rotary_dim / 2
+ *   (a, b) -> (a cos - b sin, b cos + a sin) on columns (i, i + rotary_dim / 2), or with
+ *   interleaved != 0 on columns (2 i, 2 i + 1); columns from rotary_dim on are copied.
+ * Angles are formed and reduced in 64 bits, the rotation runs in fp32, each result is rounded to
+ * bf16 once.
+ *   positions == NULL   every axis is the token's logical index ctx_len[b] + j, plus
+ *                       position_offset[b] when that is given (a sequence whose positions run
+ *                       behind or ahead of its cache index).
+ *   positions           int32 [num_axes][positions_stride >= total_rows]: row r's position on each
+ *                       axis (time, height, width of image and video tokens); freq_axis[i] names the
+ *                       axis of pair i (NULL: axis 0).  It does not move the slot of k and v.
+ * q, k_new and v_new are rows of [heads][128]; the strides count elements from one token row to the
+ * next (views of one fused projection are fine).  q_out may be q itself (in place); it must not
+ * overlap q otherwise, nor k_new or v_new.  q == NULL: only k and v are handled.
+ * Rows outside new_indptr[0] .. new_indptr[batch] - 1 belong to no sequence: nothing is written for
+ * them.  A token without a page, with a page outside the pool or of a sequence with a negative ctx_len is
+ * reported in *device_status (1 << KAP_ERR_DEVICE_INDEX); its k and v are not written, its q_out is.
+ * With new_indptr == NULL one kernel does everything; with it, advance != 0 adds a second one that
+ * moves ctx_len.  Asynchronous on cuda_stream; can be captured into a CUDA graph.
+ * Errors: KAP_ERR_UNSUPPORTED (head_dim, page_size; rotary_dim not a multiple of 16 in 16 .. 128),
+ * KAP_ERR_INVALID_ARG (NULL or misaligned pointer or stride, total_rows != batch without new_indptr,
+ * axes without positions, freq_axis[i] >= num_axes), KAP_ERR_CUDA.
+ */
+kap_status kap_append_kv_rope(
+    const void* q, int64_t q_stride,          /* DEVICE bf16 [total_rows][Hq][d] or NULL */
+    const void* k_new, int64_t k_stride,      /* DEVICE bf16 [total_rows][Hkv][d] */
+    const void* v_new, int64_t v_stride,      /* DEVICE bf16 [total_rows][Hkv][d] */
+    void* q_out, int64_t q_out_stride,        /* DEVICE bf16 [total_rows][Hq][d] */
+    const int32_t* new_indptr,                /* DEVICE [batch+1], or NULL: one new token per sequence */
+    int32_t total_rows,
+    const float* inv_freq,                    /* DEVICE [rotary_dim / 2] */
+    int32_t rotary_dim, int32_t interleaved,
+    const int32_t* positions,                 /* DEVICE [num_axes][positions_stride] or NULL */
+    int64_t positions_stride, int32_t num_axes,
+    const uint8_t* freq_axis,                 /* HOST [rotary_dim / 2] or NULL */
+    const int32_t* position_offset,           /* DEVICE [batch] or NULL */
+    void* kv_pool, int64_t num_pool_pages,
+    const int32_t* bt_indptr,                 /* DEVICE [batch+1] CSR block table */
+    const int32_t* bt_pages,                  /* DEVICE */
+    int32_t* ctx_len,                         /* DEVICE [batch], read; updated when advance != 0 */
+    int32_t advance,
+    int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+    int32_t kv_layout,                        /* KAP_KV_HND or KAP_KV_NHD */
+    int32_t* device_status,                   /* DEVICE int32 or NULL */
+    void* cuda_stream);
+
+/*
+ * kap_shared_prefix_attn - kap_verify_attn for a batch whose sequences come in groups that share
+ * the first pages of their block tables (one document or instruction, many requests on it).  Same
+ * arguments, same rows, same visibility rule (row j of sequence b sees t <= ctx_len[b] - n_q + j),
+ * same result; the shared pages are read once per group, for all of its query rows together
+ * (n_q = 1: one decoding step of the batch).  The paper has no counterpart.
+ *
+ * kap_schedule_shared_prefix (HOST arrays) makes the work list, like kap_schedule: group i is the
+ * sequences group_indptr[i] .. group_indptr[i+1]-1 (every sequence belongs to one group; a group of
+ * one, or prefix_pages[i] == 0, shares nothing), whose block tables begin with the same
+ * prefix_pages[i] physical pages; list_len[b] counts all pages of sequence b, the shared ones
+ * included, and must cover every context length the schedule will serve.  The shared pages are
+ * read through the block table of the group's first sequence.  The schedule serves every layer and
+ * every step whose counts are unchanged; ctx_len may grow up to 16 list_len[b].
+ * The workspace's partial buffer of max_items * max_rows_per_item rows is used as a whole:
+ * kap_shared_prefix_items (HOST only) gives the max_items that a workspace with this
+ * max_rows_per_item needs for such a schedule on a device of cta_slots SMs.  A workspace holds one schedule of
+ * either kind at a time.
+ *
+ * Every token below a sequence's ctx_len must hold finite K and V; what lies behind the longest
+ * context of a group may hold anything.  A context shorter than its group's shared prefix is allowed (the rows
+ * see what lies below their own position) as long as the shared pages hold finite values.
+ * A row that sees no token gets out = 0, lse = -inf.  out rows beyond q_indptr[batch] are left alone.
+ * Errors: as kap_schedule and kap_verify_attn, plus KAP_ERR_INVALID_ARG for groups that do not
+ * cover the batch in order, a prefix longer than a sequence's list, or an sm_scale that is not a positive number.
+ */
+kap_status kap_shared_prefix_items(
+    int32_t batch, const int32_t* list_len, const int32_t* n_q,       /* HOST [batch] */
+    int32_t n_groups, const int32_t* group_indptr,                    /* HOST [n_groups+1] */
+    const int32_t* prefix_pages,                                      /* HOST [n_groups] */
+    int32_t num_q_heads, int32_t num_kv_heads, int32_t max_rows_per_item, int32_t cta_slots,
+    int32_t* max_items);
+
+kap_status kap_schedule_shared_prefix(
+    kap_workspace* ws, int32_t batch,
+    const int32_t* list_len,           /* HOST [batch] pages of each sequence, shared ones included */
+    const int32_t* n_q,                /* HOST [batch] query rows of each sequence */
+    int32_t n_groups,
+    const int32_t* group_indptr,       /* HOST [n_groups+1] */
+    const int32_t* prefix_pages,       /* HOST [n_groups] pages that the group shares */
+    int32_t num_q_heads, int32_t num_kv_heads, void* cuda_stream);
+
+kap_status kap_shared_prefix_attn(
+    const void* q,                     /* DEVICE bf16 [sum n_q, Hq, d], a sequence's rows contiguous */
+    const int32_t* q_indptr,           /* DEVICE [batch+1] */
+    const void* kv_pool, int64_t num_pool_pages,
+    const int32_t* bt_indptr,          /* DEVICE [batch+1] CSR full block table */
+    const int32_t* bt_pages,           /* DEVICE */
+    const int32_t* ctx_len,            /* DEVICE [batch] */
+    int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+    float sm_scale,
+    void* out,                         /* DEVICE bf16 [sum n_q, Hq, d] */
+    float* lse,                        /* DEVICE fp32 [sum n_q, Hq] or NULL */
+    kap_workspace* ws, void* cuda_stream);
+
+/* element type of kap_sample_tokens' logits */
+enum {
+    KAP_LOGITS_F32 = 0,
+    KAP_LOGITS_BF16 = 1
+};
+
+/*
+ * kap_sample_tokens - draw one token per logits row with given random numbers (the proposal steps'
+ * next token, or the carry of a verification window, when decoding is not greedy; the paper fixes
+ * no sampling rule).  Row r, with x its logits, T = temperature[r], u = uniform[r]:
+ *   w_i = exp((x_i - max x) / T);  tokens rank by logit descending, lower index first on equal ones
+ *   top_k[r] > 0      only the first top_k[r] ranks stay
+ *   top_p[r] < 1      of those, rank n stays iff the weight of the ranks before it is below top_p[r]
+ *                     times the weight of all of them (rank 0 always stays)
+ *   min_p[r] > 0      of those, tokens with (x_i - max x) / T >= ln min_p[r] stay (the best always does for min_p <= 1)
+ *   token[r]          the lowest index i such that the kept weights of tokens 0 .. i sum to more
+ *                     than u times the sum of all kept weights (u in [0, 1))
+ *   logprob[r]        ln(w_token / sum of kept weights)
+ * Sums and comparisons are in 64 bits.  T <= 0 (or NaN): the lowest index of the largest logit,
+ * logprob 0.  NaN and -inf logits have no weight; if +inf occurs only the +inf tokens do.  A row
+ * without any token of weight (all -inf or NaN) gives token -1, logprob -inf.  A parameter array
+ * that is NULL switches its filter off for all rows (temperature: 1).  Results do not depend on
+ * timing or on the other rows.
+ * Errors: KAP_ERR_INVALID_ARG (NULL or misaligned pointer, vocab < 1, row_stride < vocab, negative rows),
+ * KAP_ERR_UNSUPPORTED (logits_type), KAP_ERR_CUDA.  Asynchronous on cuda_stream.
+ */
+kap_status kap_sample_tokens(
+    const void* logits,                /* DEVICE, row r starts at element r * row_stride */
+    int32_t logits_type, int64_t row_stride, int32_t rows, int32_t vocab,
+    const float* temperature,          /* DEVICE [rows] or NULL */
+    const int32_t* top_k,              /* DEVICE [rows] or NULL */
+    const float* top_p,                /* DEVICE [rows] or NULL */
+    const float* min_p,                /* DEVICE [rows] or NULL */
+    const float* uniform,              /* DEVICE [rows] */
+    int32_t* token,                    /* DEVICE out [rows] */
+    float* logprob,                    /* DEVICE out [rows] or NULL */
+    void* cuda_stream);
+
+/*
  * kap_selected_decode_attn_static - the proposal-path attention of kap_selected_decode_attn for
  * callers that are not allowed to allocate device memory.  (The paper has no counterpart: this is
  * a packaging of the same computation, not another operation.)

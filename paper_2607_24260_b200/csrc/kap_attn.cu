@@ -285,6 +285,8 @@ kap_status check_shape(int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_
     if (batch != ws->batch || hq != ws->num_q_heads || hkv != ws->num_kv_heads)
         return fail(KAP_ERR_INVALID_ARG, "call shape (batch %d, heads %d/%d) differs from the schedule "
                     "(batch %d, heads %d/%d)", batch, hq, hkv, ws->batch, ws->num_q_heads, ws->num_kv_heads);
+    if (ws->shared_prefix)
+        return fail(KAP_ERR_INVALID_ARG, "the workspace holds a shared-prefix schedule: use kap_shared_prefix_attn");
     if (verify != (ws->has_nq != 0))
         return fail(KAP_ERR_INVALID_ARG, verify ? "verification needs a schedule made with n_q"
                                                 : "the proposal path needs a schedule made without n_q");
@@ -466,6 +468,7 @@ extern "C" kap_status kap_schedule(kap_workspace* ws, int32_t batch, const int32
     ws->batch = batch; ws->n_items = (int32_t)items.size(); ws->n_groups = (int32_t)groups.size();
     ws->n_merge_groups = n_merge; ws->max_chunk = max_chunk; ws->row_tiles = row_tiles;
     ws->num_q_heads = num_q_heads; ws->num_kv_heads = num_kv_heads; ws->has_nq = n_q != nullptr;
+    ws->shared_prefix = 0;
     ws->total_rows = total_rows; ws->cluster_size = cluster; ws->umma = umma ? 1 : 0; ws->max_splits = max_splits;
     int32_t mq = 1;
     for (int32_t b = 0; b < batch; ++b) mq = std::max(mq, n_q ? n_q[b] : 1);

@@ -17,6 +17,7 @@ from . import build as _build
 OK, ERR_INVALID_ARG, ERR_CAPACITY, ERR_UNSUPPORTED, ERR_CUDA, ERR_TIMEOUT, ERR_DEVICE_INDEX = range(7)
 PLAN_FULL, PLAN_OVER_BUDGET, PLAN_S_HIGH, PLAN_MOVES_WITH_LENGTH = 1, 2, 4, 8
 KV_HND, KV_NHD = 0, 1
+LOGITS_F32, LOGITS_BF16 = 0, 1
 
 _i32p, _f32p, _u8p, _vp = C.POINTER(C.c_int32), C.POINTER(C.c_float), C.POINTER(C.c_uint8), C.c_void_p
 
@@ -60,6 +61,18 @@ SIGNATURES = {
                                       C.POINTER(C.c_double)]),
     "kap_materialize_view": (C.c_int, [_vp, C.c_int64, _vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
                                        _vp, C.c_int64, _vp, _vp, _vp]),
+    "kap_append_kv_rope": (C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int32,
+                                     _vp, C.c_int32, C.c_int32, _vp, C.c_int64, C.c_int32, _u8p, _vp, _vp,
+                                     C.c_int64, _vp, _vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                     C.c_int32, C.c_int32, C.c_int32, _vp, _vp]),
+    "kap_shared_prefix_items": (C.c_int, [C.c_int32, _i32p, _i32p, C.c_int32, _i32p, _i32p, C.c_int32,
+                                          C.c_int32, C.c_int32, C.c_int32, _i32p]),
+    "kap_schedule_shared_prefix": (C.c_int, [_vp, C.c_int32, _i32p, _i32p, C.c_int32, _i32p, _i32p, C.c_int32,
+                                             C.c_int32, _vp]),
+    "kap_shared_prefix_attn": (C.c_int, [_vp, _vp, _vp, C.c_int64, _vp, _vp, _vp, C.c_int32, C.c_int32,
+                                         C.c_int32, C.c_int32, C.c_int32, C.c_float, _vp, _vp, _vp, _vp]),
+    "kap_sample_tokens": (C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp, _vp,
+                                    _vp, _vp, _vp]),
     "kap_device_sm_rates": (C.c_int, [C.c_int32, C.c_int32, _f32p, _i32p]),
     "kap_workspace_check": (C.c_int, [_vp, _vp]),
     "kap_set_launch_options": (C.c_int, [C.c_int32] * 5),
@@ -286,6 +299,18 @@ class Workspace:
         _check(lib().kap_workspace_set_kv_layout(self._h, int(kv_layout)))
         self.kv_layout = int(kv_layout)
 
+    def schedule_shared_prefix(self, list_len, n_q, group_indptr, prefix_pages, num_q_heads=32,
+                               num_kv_heads=8, stream=None):
+        """kap_schedule_shared_prefix on host arrays (see kap.h); shared_prefix_items gives the
+        max_items the workspace needs."""
+        list_len, n_q = _np(list_len, np.int32), _np(n_q, np.int32)
+        group_indptr, prefix_pages = _np(group_indptr, np.int32), _np(prefix_pages, np.int32)
+        _check_groups(list_len, n_q, group_indptr, prefix_pages)
+        _check(lib().kap_schedule_shared_prefix(
+            self._h, int(list_len.shape[0]), _ptr(list_len, C.c_int32), _ptr(n_q, C.c_int32),
+            int(prefix_pages.shape[0]), _ptr(group_indptr, C.c_int32), _ptr(prefix_pages, C.c_int32),
+            num_q_heads, num_kv_heads, _stream_ptr(stream)))
+
     def info(self):
         v = [C.c_int32(0) for _ in range(5)]
         _check(lib().kap_schedule_info(self._h, *[C.byref(x) for x in v]))
@@ -324,6 +349,41 @@ def verify_attn(q, q_indptr, kv_pool, bt_indptr, bt_pages, ctx_len, out, ws: Wor
     return out
 
 
+def _check_groups(list_len, n_q, group_indptr, prefix_pages):
+    if n_q.shape != list_len.shape or group_indptr.shape != (prefix_pages.shape[0] + 1,):
+        raise KapError(ERR_INVALID_ARG, f"{list_len.shape[0]} list lengths, {n_q.shape[0]} row counts, "
+                       f"{group_indptr.shape[0]} group offsets, {prefix_pages.shape[0]} prefixes")
+
+
+def shared_prefix_items(list_len, n_q, group_indptr, prefix_pages, num_q_heads=32, num_kv_heads=8,
+                        max_rows_per_item=64, cta_slots=148):
+    """kap_shared_prefix_items: the max_items of a Workspace (with this max_rows_per_item) that can
+    hold the schedule of schedule_shared_prefix on a device of cta_slots SMs."""
+    list_len, n_q = _np(list_len, np.int32), _np(n_q, np.int32)
+    group_indptr, prefix_pages = _np(group_indptr, np.int32), _np(prefix_pages, np.int32)
+    _check_groups(list_len, n_q, group_indptr, prefix_pages)
+    n = C.c_int32(0)
+    _check(lib().kap_shared_prefix_items(
+        int(list_len.shape[0]), _ptr(list_len, C.c_int32), _ptr(n_q, C.c_int32), int(prefix_pages.shape[0]),
+        _ptr(group_indptr, C.c_int32), _ptr(prefix_pages, C.c_int32), num_q_heads, num_kv_heads,
+        int(max_rows_per_item), int(cta_slots), C.byref(n)))
+    return n.value
+
+
+def shared_prefix_attn(q, q_indptr, kv_pool, bt_indptr, bt_pages, ctx_len, out, ws: Workspace, lse=None,
+                       sm_scale=None, stream=None):
+    """kap_shared_prefix_attn on torch CUDA tensors: the arguments and the result of verify_attn, for a
+    workspace scheduled with schedule_shared_prefix."""
+    _, Hq, d = q.shape
+    pages, Hkv, P = _pool_shape(kv_pool, ws)
+    sm_scale = float(d) ** -0.5 if sm_scale is None else float(sm_scale)
+    _check(lib().kap_shared_prefix_attn(
+        _dptr(q), _dptr(q_indptr), _dptr(kv_pool), int(pages), _dptr(bt_indptr), _dptr(bt_pages),
+        _dptr(ctx_len), int(ctx_len.shape[0]), Hq, Hkv, d, P, sm_scale, _dptr(out), _dptr(lse),
+        ws._h, _stream_ptr(stream)))
+    return out
+
+
 def selected_decode_attn_static(q, kv_pool, plan_indptr, plan_phys_pages, plan_logical_pages, ctx_len,
                                 out, num_splits, lse=None, device_status=None, sm_scale=None,
                                 stream=None):
@@ -353,6 +413,77 @@ def append_kv(k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, new_indptr=No
                                _dptr(bt_indptr), _dptr(bt_pages), _dptr(ctx_len), int(bool(advance)),
                                int(ctx_len.shape[0]), Hkv, d, P, int(kv_layout), _dptr(device_status),
                                _stream_ptr(stream)))
+
+
+def _head_rows(name, t, rows, heads):
+    """the row stride of a bf16 [rows, heads, d] tensor whose heads are contiguous within a row"""
+    import torch
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or tuple(t.shape[:2]) != (rows, heads):
+        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)}, expected bfloat16 [{rows}, {heads}, d]")
+    d = t.shape[2]
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise KapError(ERR_INVALID_ARG, f"{name} has strides {t.stride()}: the heads of a row must be contiguous")
+    return heads * d if rows <= 1 else int(t.stride(0))
+
+
+def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_freq, q_out=None,
+                   new_indptr=None, positions=None, freq_axis=None, position_offset=None,
+                   interleaved=False, advance=True, device_status=None, stream=None, kv_layout=KV_HND):
+    """kap_append_kv_rope: rotate q and k_new (bf16 [rows, heads, d], any row stride) by
+    position * inv_freq (fp32 [rotary_dim / 2]) and write k and v_new into the paged pool like
+    append_kv.  q_out None rotates q in place; q None handles k and v only.  positions None: the
+    logical index (+ position_offset[b]); else int32 [rows] or [axes, rows], freq_axis naming the axis
+    of each pair (host sequence)."""
+    import torch
+    if kv_layout == KV_NHD:
+        pages, _, P, Hkv, d = kv_pool.shape
+    else:
+        pages, _, Hkv, P, d = kv_pool.shape
+    rows, Hq = int(k_new.shape[0]), 0
+    ks, vs = _head_rows("k_new", k_new, rows, Hkv), _head_rows("v_new", v_new, rows, Hkv)
+    qs = os_ = 0
+    if q is not None:
+        Hq = int(q.shape[1])
+        q_out = q if q_out is None else q_out
+        qs, os_ = _head_rows("q", q, rows, Hq), _head_rows("q_out", q_out, rows, Hq)
+    axes, pos_stride = 0, 0
+    if positions is not None:
+        positions = positions.view(1, -1) if positions.dim() == 1 else positions
+        if positions.dtype != torch.int32 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
+            raise KapError(ERR_INVALID_ARG, f"positions {positions.dtype} {tuple(positions.shape)} for {rows} rows")
+        axes, pos_stride = int(positions.shape[0]), int(positions.stride(0))
+        pos_stride = max(pos_stride, rows) if axes == 1 else pos_stride
+    rot = 2 * int(inv_freq.shape[0])
+    axis = _np(freq_axis, np.uint8)
+    if axis is not None and axis.shape != (rot // 2,):
+        raise KapError(ERR_INVALID_ARG, f"freq_axis names {axis.size} pairs, inv_freq {rot // 2}")
+    _check(lib().kap_append_kv_rope(
+        _dptr(q), qs, _dptr(k_new), ks, _dptr(v_new), vs, _dptr(q_out) if q is not None else None, os_,
+        _dptr(new_indptr), rows, _dptr(inv_freq), rot, int(bool(interleaved)), _dptr(positions), pos_stride,
+        axes, _ptr(axis, C.c_uint8), _dptr(position_offset), _dptr(kv_pool), int(pages), _dptr(bt_indptr),
+        _dptr(bt_pages), _dptr(ctx_len), int(bool(advance)), int(ctx_len.shape[0]), Hq, int(Hkv), int(d), int(P),
+        int(kv_layout), _dptr(device_status), _stream_ptr(stream)))
+
+
+def sample_tokens(logits, uniform, token, logprob=None, temperature=None, top_k=None, top_p=None,
+                  min_p=None, stream=None):
+    """kap_sample_tokens on torch CUDA tensors: logits fp32 or bf16 [rows, vocab] (any row stride), uniform
+    fp32 [rows]; outputs int32 token [rows] and optional fp32 logprob [rows].  temperature, top_p,
+    min_p (fp32 [rows]) and top_k (int32 [rows]) are optional; None switches a filter off."""
+    import torch
+    kinds = {torch.float32: LOGITS_F32, torch.bfloat16: LOGITS_BF16}
+    if logits.dtype not in kinds or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise KapError(ERR_INVALID_ARG, f"logits are {logits.dtype} {tuple(logits.shape)} with strides {logits.stride()}")
+    rows, vocab = logits.shape
+    for name, t, dt in (("uniform", uniform, torch.float32), ("token", token, torch.int32),
+                        ("logprob", logprob, torch.float32), ("temperature", temperature, torch.float32),
+                        ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if t is not None and (t.dtype != dt or t.numel() != rows or not t.is_contiguous()):
+            raise KapError(ERR_INVALID_ARG, f"{name} must be a contiguous {dt} tensor of {rows}")
+    stride = vocab if rows <= 1 else int(logits.stride(0))
+    _check(lib().kap_sample_tokens(
+        _dptr(logits), kinds[logits.dtype], stride, int(rows), int(vocab), _dptr(temperature), _dptr(top_k),
+        _dptr(top_p), _dptr(min_p), _dptr(uniform), _dptr(token), _dptr(logprob), _stream_ptr(stream)))
 
 
 def top3_accept(logits, row_indptr, proposed, top3, accepted, next_token, stream=None, ctx_len=None):
