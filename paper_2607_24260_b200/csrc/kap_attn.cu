@@ -295,6 +295,25 @@ kap_status check_shape(int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_
 }
 
 }  // namespace
+
+// for kap_shared_prefix_attn: the pool's tensor map (as above, cached in the workspace) and a map over query rows
+kap_status workspace_kv_map(kap_workspace* ws, const void* pool, int64_t pages, int32_t hkv, const void** map) {
+    return get_tensor_map(ws, pool, pages, hkv, reinterpret_cast<const CUtensorMap**>(map));
+}
+kap_status encode_query_map(void* map, const void* q, int64_t rows, int32_t hq, int32_t G, int32_t tile_rows) {
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return fail(KAP_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    // (d, head, token row); the box takes 64 columns of the G heads of a KV head for tile_rows / G tokens
+    cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)hq, (cuuint64_t)rows};
+    cuuint64_t strides[2] = {(cuuint64_t)kHeadDim * 2, (cuuint64_t)hq * kHeadDim * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)(tile_rows / G)};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = enc(reinterpret_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims,
+                     strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? KAP_OK : fail(KAP_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d", (int)r);
+}
+bool launch_programmatically() { return g_use_pdl.load() != 0; }
 }  // namespace kap
 
 using namespace kap;

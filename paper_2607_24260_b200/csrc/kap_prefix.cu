@@ -1,73 +1,62 @@
-// kap_shared_prefix_attn: full-context attention (kap_verify_attn's result) for a batch whose sequences come in
-// groups that share the first pages of their block tables.
-#include <cuda_bf16.h>
-#include <cuda_runtime.h>
+// Host side of kap_shared_prefix_attn: full-context attention (kap_verify_attn's result, Section 3.2 of the KAP paper) for a
+// batch whose sequences come in groups that share the first pages of their block tables.  The work list is built in
+// kap_prefix_schedule.cpp, the kernels are in kap_prefix_kernel.cuh.
+#include <cstring>
+#include <exception>
 
-#include "kap_internal.h"
+#include "kap_prefix_kernel.cuh"
 
 namespace kap {
 void count_launch();
+kap_status workspace_kv_map(kap_workspace* ws, const void* pool, int64_t pages, int32_t hkv, const void** map);
+kap_status encode_query_map(void* map, const void* q, int64_t rows, int32_t hq, int32_t G, int32_t tile_rows);
+bool launch_programmatically();
 
 namespace {
 
-struct PrefixParams {
-    const __nv_bfloat16 *q, *pool;
-    const int32_t *q_indptr, *bt_indptr, *bt_pages, *ctx_len;
-    __nv_bfloat16* out;
-    float* lse;
-    int32_t* status;
-    long long num_pool_pages;
-    int32_t batch, hq, hkv, nhd;
-    float scale_log2;
+#define KAP_CUDA(call)                                                                         \
+    do {                                                                                       \
+        cudaError_t e_ = (call);                                                               \
+        if (e_ != cudaSuccess)                                                                 \
+            return fail(KAP_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));         \
+    } while (0)
+
+// offsets of the sequences, rows and CTA ranges inside the workspace's third metadata array
+struct BlobLayout {
+    size_t rows, ctas;
+    BlobLayout(int64_t batch, int64_t total_rows) {
+        rows = (size_t)batch * sizeof(PrefixSeq);
+        ctas = rows + (size_t)total_rows * sizeof(PrefixRow);
+    }
 };
 
-// one warp per (query row, head): each lane holds four of the 128 columns
-__global__ void __launch_bounds__(128)
-kap_prefix_rows_kernel(const PrefixParams p)
-{
-    const int lane = threadIdx.x & 31;
-    const int row = blockIdx.x, head = blockIdx.y * 4 + (threadIdx.x >> 5);
-    if (head >= p.hq || row < p.q_indptr[0] || row >= p.q_indptr[p.batch]) return;
-    int lo = 0, hi = p.batch;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.q_indptr[mid] <= row) lo = mid; else hi = mid;
+kap_status upload_schedule(kap_workspace* ws, const PrefixSchedule& s, int32_t batch, int32_t hq, int32_t hkv, cudaStream_t stream) {
+    int dev = -1;
+    KAP_CUDA(cudaGetDevice(&dev));
+    if (dev != ws->device) KAP_CUDA(cudaSetDevice(ws->device));
+    cudaError_t e = cudaEventSynchronize((cudaEvent_t)ws->upload_event);   // the pinned staging may still feed the previous upload
+    const BlobLayout at(batch, s.total_rows);
+    const size_t seg_bytes = s.segments.size() * sizeof(PrefixSegment), unit_bytes = s.units.size() * sizeof(PrefixUnit);
+    if (e == cudaSuccess && batch > 0) {
+        unsigned char* blob = reinterpret_cast<unsigned char*>(ws->h_merge);
+        std::memcpy(ws->h_items, s.segments.data(), seg_bytes);
+        std::memcpy(ws->h_groups, s.units.data(), unit_bytes);
+        std::memcpy(blob, s.seqs.data(), at.rows);
+        std::memcpy(blob + at.rows, s.rows.data(), at.ctas - at.rows);
+        std::memcpy(blob + at.ctas, s.cta_begin.data(), s.cta_begin.size() * sizeof(int32_t));
+        e = cudaMemcpyAsync(ws->d_items, ws->h_items, seg_bytes, cudaMemcpyHostToDevice, stream);
+        if (e == cudaSuccess) e = cudaMemcpyAsync(ws->d_groups, ws->h_groups, unit_bytes, cudaMemcpyHostToDevice, stream);
+        if (e == cudaSuccess) e = cudaMemcpyAsync(ws->d_merge, blob, prefix_blob_bytes(s), cudaMemcpyHostToDevice, stream);
     }
-    const int b = lo, n_q = p.q_indptr[b + 1] - p.q_indptr[b];
-    const int seen = p.ctx_len[b] - n_q + (row - p.q_indptr[b]) + 1;     // visible tokens
-    const int g = head / (p.hq / p.hkv);
-    auto four = [](const __nv_bfloat16* at, float (&v)[4]) {
-        const uint2 u = *reinterpret_cast<const uint2*>(at);
-        v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u);
-        v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
-    };
-    float q[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-    const long long q_at = ((long long)row * p.hq + head) * kHeadDim + lane * 4;
-    four(p.q + q_at, q);
-    for (int t = 0; t < seen; ++t) {
-        const int i = p.bt_indptr[b] + t / kPageSize;
-        const int32_t page = i < p.bt_indptr[b + 1] ? p.bt_pages[i] : -1;
-        if (page < 0 || page >= p.num_pool_pages) {
-            if (lane == 0) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
-            continue;
-        }
-        const long long step = p.nhd ? (long long)p.hkv * kHeadDim : kHeadDim;       // between tokens
-        const __nv_bfloat16* k_at = p.pool + (long long)page * 2 * p.hkv * kPageSize * kHeadDim +
-                                    (p.nhd ? (long long)g * kHeadDim : (long long)g * kPageSize * kHeadDim) + t % kPageSize * step + lane * 4;
-        float k[4], v[4];
-        four(k_at, k);
-        four(k_at + (long long)p.hkv * kPageSize * kHeadDim, v);
-        float s = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        s *= p.scale_log2;
-        const float m_new = fmaxf(m, s), a = exp2f(m - m_new), w = exp2f(s - m_new);
-        l = l * a + w;
-        for (int j = 0; j < 4; ++j) o[j] = o[j] * a + w * v[j];
-        m = m_new;
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    for (int j = 0; j < 4; ++j) p.out[q_at + j] = __float2bfloat16(o[j] * inv);
-    if (p.lse && lane == 0) p.lse[(long long)row * p.hq + head] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (e == cudaSuccess) e = cudaEventRecord((cudaEvent_t)ws->upload_event, stream);
+    if (dev != ws->device) cudaSetDevice(dev);                             // the caller's current device is put back
+    if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "schedule upload failed: %s", cudaGetErrorString(e));
+    ws->shared_prefix = 1;                                                 // the other attention calls refuse this schedule
+    ws->prefix_ctas = s.n_cta;
+    if (ws->schedule_key) ws->schedule_key->clear();
+    ws->batch = batch; ws->num_q_heads = hq; ws->num_kv_heads = hkv; ws->total_rows = s.total_rows;
+    ws->n_items = (int32_t)s.segments.size();
+    return KAP_OK;
 }
 
 }  // namespace
@@ -75,62 +64,25 @@ kap_prefix_rows_kernel(const PrefixParams p)
 
 using namespace kap;
 
-static kap_status check_groups(int32_t batch, const int32_t* list_len, const int32_t* n_q, int32_t n_groups,
-                               const int32_t* group_indptr, const int32_t* prefix_pages, int32_t hq, int32_t hkv)
-{
-    if (batch < 0 || n_groups < 0 || (batch > 0 && (!list_len || !n_q || !group_indptr || !prefix_pages)))
-        return fail(KAP_ERR_INVALID_ARG, "NULL pointer, batch %d or n_groups %d", batch, n_groups);
-    if (hq <= 0 || hkv <= 0 || hq % hkv) return fail(KAP_ERR_INVALID_ARG, "head counts %d / %d", hq, hkv);
-    const int32_t G = hq / hkv;
-    if (kRowTile % G) return fail(KAP_ERR_UNSUPPORTED, "group size %d must divide %d", G, kRowTile);
-    if (batch > 0 && (n_groups < 1 || group_indptr[0] != 0 || group_indptr[n_groups] != batch))
-        return fail(KAP_ERR_INVALID_ARG, "group_indptr must run from 0 to the batch size %d", batch);
-    for (int32_t b = 0; b < batch; ++b) {
-        if (list_len[b] <= 0 || n_q[b] < 1) return fail(KAP_ERR_INVALID_ARG, "sequence %d: list_len %d, n_q %d", b, list_len[b], n_q[b]);
-        if ((int64_t)n_q[b] * G > kRowTile * kMaxRowTiles)
-            return fail(KAP_ERR_CAPACITY, "sequence %d: %d query rows x %d heads exceed %d", b, n_q[b], G, kRowTile * kMaxRowTiles);
-    }
-    for (int32_t i = 0; i < n_groups; ++i) {
-        if (group_indptr[i + 1] <= group_indptr[i] || group_indptr[i + 1] > batch)
-            return fail(KAP_ERR_INVALID_ARG, "group %d is empty or group_indptr is not ascending", i);
-        for (int32_t b = group_indptr[i]; b < group_indptr[i + 1]; ++b)
-            if (prefix_pages[i] < 0 || prefix_pages[i] > list_len[b])
-                return fail(KAP_ERR_INVALID_ARG, "group %d shares %d pages, sequence %d has %d", i, prefix_pages[i], b, list_len[b]);
-    }
-    return KAP_OK;
-}
-
-extern "C" kap_status kap_shared_prefix_items(
-    int32_t batch, const int32_t* list_len, const int32_t* n_q, int32_t n_groups, const int32_t* group_indptr,
-    const int32_t* prefix_pages, int32_t num_q_heads, int32_t num_kv_heads, int32_t max_rows_per_item, int32_t cta_slots,
-    int32_t* max_items)
-{
-    if (!max_items || max_rows_per_item <= 0 || cta_slots <= 0) return fail(KAP_ERR_INVALID_ARG, "NULL pointer or sizes below 1");
-    kap_status st = check_groups(batch, list_len, n_q, n_groups, group_indptr, prefix_pages, num_q_heads, num_kv_heads);
-    if (st != KAP_OK) return st;
-    int64_t rows = 0;
-    for (int32_t b = 0; b < batch; ++b) rows += (int64_t)n_q[b] * num_q_heads;
-    *max_items = (int32_t)(rows / max_rows_per_item + 1);
-    return KAP_OK;
-}
-
 extern "C" kap_status kap_schedule_shared_prefix(
     kap_workspace* ws, int32_t batch, const int32_t* list_len, const int32_t* n_q, int32_t n_groups,
     const int32_t* group_indptr, const int32_t* prefix_pages, int32_t num_q_heads, int32_t num_kv_heads, void* cuda_stream)
 {
     if (!ws) return fail(KAP_ERR_INVALID_ARG, "NULL workspace");
     if (batch > ws->max_batch) return fail(KAP_ERR_CAPACITY, "batch %d > workspace max_batch %d", batch, ws->max_batch);
-    kap_status st = check_groups(batch, list_len, n_q, n_groups, group_indptr, prefix_pages, num_q_heads, num_kv_heads);
-    if (st != KAP_OK) return st;
-    (void)cuda_stream;
-    int64_t rows = 0;
-    for (int32_t b = 0; b < batch; ++b) rows += n_q[b];
-    if (rows * num_q_heads > (int64_t)ws->max_items * ws->max_rows)
-        return fail(KAP_ERR_CAPACITY, "%lld states exceed the workspace's %d x %d", (long long)(rows * num_q_heads), ws->max_items, ws->max_rows);
-    ws->shared_prefix = 1;                              // the other attention calls refuse this schedule
-    if (ws->schedule_key) ws->schedule_key->clear();
-    ws->batch = batch; ws->num_q_heads = num_q_heads; ws->num_kv_heads = num_kv_heads; ws->total_rows = rows;
-    return KAP_OK;
+    try {
+        PrefixSchedule s;
+        kap_status st = build_prefix_schedule(batch, list_len, n_q, n_groups, group_indptr, prefix_pages, num_q_heads, num_kv_heads,
+                                              ws->sm_count, s);
+        if (st != KAP_OK) return st;
+        const int64_t need = prefix_items_needed(s, ws->max_rows);
+        if (need > ws->max_items)
+            return fail(KAP_ERR_CAPACITY, "the schedule needs a workspace of %lld items of %d rows, this one has %d", (long long)need,
+                        ws->max_rows, ws->max_items);
+        return upload_schedule(ws, s, batch, num_q_heads, num_kv_heads, (cudaStream_t)cuda_stream);
+    } catch (const std::exception& e) {                                    // no exception leaves a C entry point
+        return fail(KAP_ERR_CAPACITY, "the schedule does not fit the host's memory: %s", e.what());
+    }
 }
 
 extern "C" kap_status kap_shared_prefix_attn(
@@ -154,14 +106,49 @@ extern "C" kap_status kap_shared_prefix_attn(
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev != ws->device)
         return fail(KAP_ERR_INVALID_ARG, "the workspace belongs to device %d but device %d is current", ws->device, dev);
-    PrefixParams p{};
-    p.q = (const __nv_bfloat16*)q; p.pool = (const __nv_bfloat16*)kv_pool; p.q_indptr = q_indptr; p.bt_indptr = bt_indptr;
-    p.bt_pages = bt_pages; p.ctx_len = ctx_len; p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ws->d_status;
-    p.num_pool_pages = num_pool_pages; p.batch = batch; p.hq = num_q_heads; p.hkv = num_kv_heads;
-    p.nhd = ws->kv_layout == KAP_KV_NHD; p.scale_log2 = sm_scale * 1.4426950408889634f;
-    kap_prefix_rows_kernel<<<dim3((unsigned)ws->total_rows, (unsigned)((num_q_heads + 3) / 4)), 128, 0, (cudaStream_t)cuda_stream>>>(p);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "kap_shared_prefix_attn launch failed: %s", cudaGetErrorString(e));
+    const void* kv_map = nullptr;
+    alignas(64) CUtensorMap q_map;
+    const int32_t G = num_q_heads / num_kv_heads;
+    kap_status st = workspace_kv_map(ws, kv_pool, num_pool_pages, num_kv_heads, &kv_map);
+    if (st == KAP_OK) st = encode_query_map(&q_map, q, ws->total_rows, num_q_heads, G, kPrefixTileRows);
+    if (st != KAP_OK) return st;
+    const bool nhd = ws->kv_layout == KAP_KV_NHD;
+    if (!ws->prefix_attrs_set) {                                           // function attributes are per device
+        KAP_CUDA(cudaFuncSetAttribute(kap_prefix_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfxSmemBytes));
+        KAP_CUDA(cudaFuncSetAttribute(kap_prefix_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfxSmemBytes));
+        ws->prefix_attrs_set = 1;
+    }
+    PfxParams p{};
+    const BlobLayout at(batch, ws->total_rows);
+    const unsigned char* blob = reinterpret_cast<const unsigned char*>(ws->d_merge);
+    p.segments = reinterpret_cast<const PrefixSegment*>(ws->d_items);
+    p.units = reinterpret_cast<const PrefixUnit*>(ws->d_groups);
+    p.seqs = reinterpret_cast<const PrefixSeq*>(blob);
+    p.row_map = reinterpret_cast<const PrefixRow*>(blob + at.rows);
+    p.cta_begin = reinterpret_cast<const int32_t*>(blob + at.ctas);
+    p.q_indptr = q_indptr; p.bt_indptr = bt_indptr; p.bt_pages = bt_pages; p.ctx_len = ctx_len;
+    p.part_o = ws->d_part_o; p.part_ml = ws->d_part_ml; p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ws->d_status;
+    p.num_pool_pages = num_pool_pages; p.batch = batch; p.total_rows = (int32_t)ws->total_rows;
+    p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G; p.nhd = nhd;
+    p.scale_log2 = sm_scale * 1.4426950408889634f;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ws->prefix_ctas);
+    cfg.blockDim = dim3(kPfxThreads);
+    cfg.dynamicSmemBytes = kPfxSmemBytes;
+    cfg.stream = (cudaStream_t)cuda_stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = launch_programmatically() ? 1 : 0;
+    const CUtensorMap& kv = *reinterpret_cast<const CUtensorMap*>(kv_map);
+    if (nhd) KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<true>, kv, q_map, p));
+    else KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<false>, kv, q_map, p));
+    count_launch();
+    cfg.gridDim = dim3((unsigned)((ws->total_rows * num_q_heads + 3) / 4));
+    cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = 0;
+    KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_merge_kernel, p));
     count_launch();
     return KAP_OK;
 }
