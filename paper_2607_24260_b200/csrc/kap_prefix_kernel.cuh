@@ -13,8 +13,8 @@
 // row tiles from one copy in shared memory, and the two tiles' softmax must overlap the other's products.  One CTA per SM:
 //   warps 0-3, 4-7  softmax of stream 0 and stream 1: one query row per thread (TMEM lane), 64 scores at a time
 //   warp 8          TMA: query tiles, then K / V steps through a ring of five 32 KiB stages
-//   warp 9          issues the MMAs: S of work n before O += P V of work n - 2, works alternating between the streams, so
-//                   scores are ready before a softmax warp group asks and the tensor core never waits for one group alone
+//   warps 9, 11     issue the MMAs of stream 0 and stream 1: S of a work before O += P V of the one before it, so scores are
+//                   ready before the softmax warps ask for them
 //   warp 10         reads the CTA's segment list ahead and hands it to the others through shared memory
 // A pair segment gives each stream its own row tile and both the same K / V stage; a solo segment (at most 128 rows)
 // alternates its steps between the streams.  Tensor memory: 512 columns, per stream two S / P buffers of 64 columns (the
@@ -57,7 +57,7 @@ struct PfxControl {
     unsigned long long kv_full[kPfxStages], kv_free[kPfxStages];
     unsigned long long q_full[2], q_free[2];
     unsigned long long s_ready[4], p_ready[4], pv_done[4];             // [stream * 2 + buffer]
-    unsigned long long drained;
+    unsigned long long drained[2];
     uint32_t tmem_base;
     int32_t timed_out;
 };
@@ -82,8 +82,8 @@ struct PfxParams {
     float scale_log2;
 };
 
-// Position in the two-stream order.  Works alternate strictly between the streams across all segments of a CTA, except that
-// a pair always ends with the stream it did not begin with; so of any three consecutive works two streams are present.
+// Which stream a segment begins with: not the one that the segment before it ended with, so that runs of short segments keep
+// both streams busy.
 struct PfxOrder {
     int last = 1;
     __device__ __forceinline__ int begin() const { return last ^ 1; }
@@ -109,17 +109,17 @@ kap_prefix_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_const
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&c->seg_full[i]), 1);
-            mbar_init(smem_u32(&c->seg_free[i]), 10);                  // eight softmax warps, the TMA warp, the MMA warp
+            mbar_init(smem_u32(&c->seg_free[i]), 11);                  // eight softmax warps, the TMA warp, two MMA warps
             mbar_init(smem_u32(&c->q_full[i]), 1);
-            mbar_init(smem_u32(&c->q_free[i]), 1);
+            mbar_init(smem_u32(&c->q_free[i]), 2);                     // both MMA warps
+            mbar_init(smem_u32(&c->drained[i]), 1);
         }
-        for (int i = 0; i < kPfxStages; ++i) { mbar_init(smem_u32(&c->kv_full[i]), 1); mbar_init(smem_u32(&c->kv_free[i]), 1); }
+        for (int i = 0; i < kPfxStages; ++i) { mbar_init(smem_u32(&c->kv_full[i]), 1); mbar_init(smem_u32(&c->kv_free[i]), 2); }
         for (int i = 0; i < 4; ++i) {
             mbar_init(smem_u32(&c->s_ready[i]), 1);
             mbar_init(smem_u32(&c->p_ready[i]), 4);
             mbar_init(smem_u32(&c->pv_done[i]), 1);
         }
-        mbar_init(smem_u32(&c->drained), 1);
         c->timed_out = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&kv_map) : "memory");
@@ -244,82 +244,100 @@ kap_prefix_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_const
             for (int s = 0; s < 2; ++s)
                 if (q_use[s]) mbar_wait(smem_u32(&c->q_full[s]), (uint32_t)(q_use[s] - 1) & 1u, last, &more);
         }
-    } else if (warp == 9) {
-        // ---- tensor core.  All lanes walk along (the segment list is read by whole warps), lane 0 waits and issues.
+    } else if (warp == 9 || warp == 11) {
+        // ---- tensor core: one warp per stream, because a group of products keeps its issuer waiting for about as long as
+        // they take (the queue is short), so whatever the issuer does in between is lost unless another one issues then.
+        // The whole warp walks along with warp-uniform values (operands computed by a single lane have to be moved to the
+        // uniform registers for every product); one elected lane issues.
+        const int stream = warp == 9 ? 0 : 1;
         constexpr uint32_t idesc_s = umma_idesc(kPrefixTileRows, kPrefixStepTokens, false), idesc_o = umma_idesc(kPrefixTileRows, kHeadDim, true);
-        struct Work { int stream, count, stage, pages, first, frees; };
-        Work older{}, newer{};                                         // the works whose P V is still to be issued
-        int n_pend = 0, step = 0, q_use[2] = {0, 0}, q_slot = 0, count0 = 0, count1 = 0;
+        // descriptors of the first query tile, of K and of V in the first stage; other places add their distance / 16
+        const uint64_t q_desc = umma_smem_desc(smem_u32(q_tiles), 16, 1024), k_desc = umma_smem_desc(smem_u32(stages), 16, 1024);
+        // V: 16 tokens (K) x 128 columns (N), N contiguous; columns 64-127 one plane further, 8 tokens = 1 KiB
+        const uint64_t v_desc = umma_smem_desc(smem_u32(stages) + 2 * kPfxPlaneBytes, kPfxPlaneBytes, 1024);
+        const uint32_t t_s = tmem + stream * 256, t_o = t_s + 128;
+        int stage = 0, q_slot = 0, count = 0;
+        uint32_t stage_parity = 0, q_parity = 0;                       // of the ring; bit i: of query slot i
+        int held = -1, held_pages = 0, held_first = 0;                 // stage of the work whose P V is still to be issued
         bool ok = true;
         PfxOrder order;
-        auto issue_pv = [&](const Work& w) {
-            const int b = w.stream * 2 + (w.count & 1);
-            if (!wait(c->p_ready[b], (uint32_t)(w.count >> 1) & 1u)) return false;
+        auto all_wait = [&](unsigned long long& bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+        auto issue_pv = [&](int n) {                                   // of work n, the held one
+            const int b = stream * 2 + (n & 1);
+            if (!all_wait(c->p_ready[b], (uint32_t)(n >> 1) & 1u)) return false;
             tc_fence_after();
-            const uint32_t o = tmem + w.stream * 256 + 128, s = tmem + w.stream * 256 + (w.count & 1) * 64;
-            const uint32_t v = smem_u32(stages + w.stage * kPfxStageBytes + 2 * kPfxPlaneBytes);
-            // V: 16 tokens (K) x 128 columns (N), N contiguous; columns 64-127 one plane further, 8 tokens = 1 KiB
-            for (int pg = 0; pg < w.pages; ++pg)
-                umma_ts(o, s + pg * 8, umma_smem_desc(v + pg * kHalfTileBytes, kPfxPlaneBytes, 1024), idesc_o, !w.first || pg > 0);
-            umma_commit(smem_u32(&c->pv_done[b]));
-            if (w.frees) umma_commit(smem_u32(&c->kv_free[w.stage]));
+            const uint64_t v = v_desc + (uint32_t)held * (kPfxStageBytes / 16);
+            const uint32_t s = t_s + (n & 1) * 64;
+            if (elect_one()) {
+#pragma unroll
+                for (int pg = 0; pg < kPrefixStepPages; ++pg)
+                    if (pg < held_pages) umma_ts(t_o, s + pg * 8, v + pg * (kHalfTileBytes / 16), idesc_o, !held_first || pg > 0);
+                umma_commit(smem_u32(&c->pv_done[b]));
+                umma_commit(smem_u32(&c->kv_free[held]));
+            }
+            __syncwarp();
+            held = -1;
             return true;
         };
-        auto issue_s = [&](int stream, int n, int stage, uint32_t q_at) {
+        auto issue_s = [&](int n, int slot) {
             const int b = stream * 2 + (n & 1);
-            // the weights of this stream's work n - 2 lie over this buffer: its products must be done
-            if (n >= 2 && !wait(c->pv_done[b], (uint32_t)((n - 2) >> 1) & 1u)) return false;
+            // the weights of work n - 2 lie over this buffer: its products must be done
+            if (n >= 2 && !all_wait(c->pv_done[b], (uint32_t)((n - 2) >> 1) & 1u)) return false;
             tc_fence_after();
-            const uint32_t k_at = smem_u32(stages + stage * kPfxStageBytes), s = tmem + stream * 256 + (n & 1) * 64;
+            const uint64_t q = q_desc + (uint32_t)slot * (kPfxQBytes / 16), kd = k_desc + (uint32_t)stage * (kPfxStageBytes / 16);
+            const uint32_t s = t_s + (n & 1) * 64;
+            if (elect_one()) {
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-                umma_ss(s, umma_smem_desc(q_at + (ks >> 2) * kPfxQHalfBytes + (ks & 3) * 32, 16, 1024),
-                        umma_smem_desc(k_at + (ks >> 2) * kPfxPlaneBytes + (ks & 3) * 32, 16, 1024), idesc_s, ks > 0);
-            umma_commit(smem_u32(&c->s_ready[b]));
+                for (int ks = 0; ks < 8; ++ks)
+                    umma_ss(s, q + ((ks >> 2) * kPfxQHalfBytes + (ks & 3) * 32) / 16, kd + ((ks >> 2) * kPfxPlaneBytes + (ks & 3) * 32) / 16,
+                            idesc_s, ks > 0);
+                umma_commit(smem_u32(&c->s_ready[b]));
+            }
+            __syncwarp();
             return true;
         };
         for (int k = 0; k < n_seg && ok; ++k) {
             PfxDesc d;
             if (!(ok = open_segment(k, d))) break;
-            if (lane == 0 && d.n_steps > 0) {
-                const bool pair = d.flags & kSegPair;
-                const int start = order.begin();
-                const int slot = pair ? 0 : q_slot;
-                ok = wait(c->q_full[slot], (uint32_t)q_use[slot] & 1u) && (!pair || wait(c->q_full[1], (uint32_t)q_use[1] & 1u));
-                for (int j = 0; j < d.n_steps && ok; ++j, ++step) {
-                    const int stage = step % kPfxStages;
-                    ok = wait(c->kv_full[stage], (uint32_t)(step / kPfxStages) & 1u);
-                    for (int t = 0; t < (pair ? 2 : 1) && ok; ++t) {
-                        const int stream = pair ? start ^ t : start ^ (j & 1);
-                        const int count = stream ? count1 : count0;
-                        ok = issue_s(stream, count, stage, smem_u32(q_tiles + (pair ? stream : slot) * kPfxQBytes));
+            const int n_steps = __shfl_sync(0xffffffffu, d.n_steps, 0), n_pages = __shfl_sync(0xffffffffu, d.n_pages, 0);
+            const int pair = __shfl_sync(0xffffffffu, d.flags & kSegPair, 0) ? 1 : 0;
+            if (n_steps > 0) {
+                const int start = order.begin(), slot = pair ? stream : q_slot, used = pair ? 3 : 1 << q_slot;
+                // both issuers wait for every query tile and every stage, and both give each back: what one does not use
+                // itself it gives back at once
+                for (int i = 0; i < 2 && ok; ++i)
+                    if (used >> i & 1) ok = all_wait(c->q_full[i], (q_parity >> i) & 1u);
+                int mine = 0;
+                for (int j = 0; j < n_steps && ok; ++j) {
+                    ok = all_wait(c->kv_full[stage], stage_parity);
+                    if (!ok) break;
+                    if (pair || (start ^ (j & 1)) == stream) {
+                        ok = issue_s(count, slot);
+                        if (ok && held >= 0) ok = issue_pv(count - 1);
                         if (!ok) break;
-                        if (n_pend == 2) { ok = issue_pv(older); n_pend = 1; }
-                        const bool first = pair ? j == 0 : j < 2;
-                        older = newer;
-                        newer = Work{stream, count, stage, min(kPrefixStepPages, d.n_pages - j * kPrefixStepPages), first, !pair || t == 1};
-                        ++n_pend;
-                        if (stream) ++count1; else ++count0;
+                        held = stage; held_pages = min(kPrefixStepPages, n_pages - j * kPrefixStepPages); held_first = mine == 0;
+                        ++count; ++mine;
+                    } else if (elect_one()) {
+                        mbar_arrive(smem_u32(&c->kv_free[stage]));
                     }
+                    __syncwarp();
+                    if (++stage == kPfxStages) { stage = 0; stage_parity ^= 1u; }
                 }
-                if (ok) {                                              // the query tiles may be replaced when these products are done
+                if (ok && elect_one()) {                               // the query tiles may be replaced when these products are done
                     umma_commit(smem_u32(&c->q_free[slot]));
-                    if (pair) umma_commit(smem_u32(&c->q_free[1]));
+                    if (pair) umma_commit(smem_u32(&c->q_free[slot ^ 1]));
                 }
-                ++q_use[slot];
-                if (pair) ++q_use[1]; else q_slot ^= 1;
-                order.done(pair, d.n_steps);
+                __syncwarp();
+                if (ok && held >= 0) ok = issue_pv(count - 1);         // nothing of the next segment can be scored meanwhile: O is read first
+                q_parity ^= used;
+                if (!pair) q_slot ^= 1;
+                order.done(pair, n_steps);
             }
-            ok = __shfl_sync(0xffffffffu, (int)ok, 0);
             close_segment(k);
         }
-        if (lane == 0) {
-            if (n_pend == 2 && ok) ok = issue_pv(older);
-            if (n_pend > 0 && ok) issue_pv(newer);
-            umma_commit(smem_u32(&c->drained));                        // everything issued, whatever happened
-            int32_t more = 0;
-            mbar_wait(smem_u32(&c->drained), 0, global_ns() + kWaitBudgetNs, &more);
-        }
+        if (elect_one()) umma_commit(smem_u32(&c->drained[stream]));   // everything issued, whatever happened
+        int32_t more = 0;
+        mbar_wait(smem_u32(&c->drained[stream]), 0, global_ns() + kWaitBudgetNs, &more);
         __syncwarp();
     } else if (warp < 8) {
         // ---- softmax: stream = warp group, one query row per thread
