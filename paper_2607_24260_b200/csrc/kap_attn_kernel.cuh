@@ -86,6 +86,7 @@ struct AttnParams {
     int32_t cluster, early_kv;       // CTAs per work item (cluster size); early KV prefetch
     int32_t ring_slots;              // page slots in the shared-memory ring (8, 12, 16 or 24)
     float scale_log2;                // sm_scale * log2(e)
+    const int2* row_map;             // mode 3: a token row's (sequence, place in it minus n_q - 1)
 #ifdef KAP_TRACE
     unsigned long long* trace;       // [8192 records][8] timestamps of this launch (debug builds)
 #endif
@@ -151,7 +152,10 @@ __device__ __forceinline__ void merge_group_cell(const AttnParams& p, const Merg
 //
 // kMode: 0 = general; 1 = push-style cluster reduction (kPush above); 2 = plain lists (kPlain: the
 // caller gave neither logical page indices nor token masks - the verification path and the
-// full-context fallback - so a CTA keeps only physical page ids and can hold 2.5 times as many).
+// full-context fallback - so a CTA keeps only physical page ids and can hold 2.5 times as many);
+// 3 = the parts of shared-prefix attention (plain lists too): the rows' positions come from row_map, because the rows of a
+// shared prefix (item.group = 1) belong to several sequences; items always leave a partial state, at row item.split of the
+// partial buffer, and item.n_splits is their first row of q; row sums add the unrounded weights, so that lse keeps fp32 accuracy for short parts as well.
 template <int kMode, bool kNhd>
 __global__ void __launch_bounds__(kThreads, 3)
 kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnParams p)
@@ -192,7 +196,7 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     const int n_item = item.page_end - item.page_begin;      // pages of the whole item
     const int slice0 = rank * (n_item / C) + min(rank, n_item % C);
     int n_local = n_item / C + (rank < n_item % C ? 1 : 0);  // pages of this CTA
-    constexpr bool kPush = kMode == 1, kPlain = kMode == 2;
+    constexpr bool kPush = kMode == 1, kPlain = kMode >= 2, kParts = kMode == 3;
     constexpr int kIdCap = kPush ? kPushIds : kPlain ? kPlainIds : kMaxIds;
     if (n_local > kIdCap) {                                  // the scheduler caps a CTA's share at 512
         if (tid == 0) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
@@ -225,7 +229,7 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     if (push) cluster_arrive();
     const int64_t list0 = (int64_t)offs[item.seq] + item.page_begin;
     const int64_t list_end = offs[item.seq + 1];
-    const int64_t q_row0 = p.q_indptr ? offs[p.batch + 1 + item.seq] : item.seq;
+    const int64_t q_row0 = kParts ? item.n_splits : p.q_indptr ? offs[p.batch + 1 + item.seq] : item.seq;
     for (int j = tid; j < n_local; j += kThreads) {
         const int i = slice0 + j;                            // entry of the item
         // the three loads are independent of one another: one round trip
@@ -320,7 +324,8 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     KAP_TRACE_POINT(blockIdx.x, 2);
     if (producer)
         for (; filled < depth; ++filled) fill(grp * depth + filled, filled);
-    const int L = p.ctx_len[item.seq];
+    // (a shared prefix is full pages: none of its tokens lies behind a context)
+    const int L = kParts && item.group ? 0x3fffffff : p.ctx_len[item.seq];
     const uint64_t deadline = global_ns() + kWaitBudgetNs;
     // second half of the prologue's cluster barrier: by now every peer has long arrived, so this
     // costs nothing here, and the epilogue may push without any further synchronisation
@@ -331,7 +336,12 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     int pos_row[2];                                          // logical position of rows gid, gid+8
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-        pos_row[half] = L - item.n_q + q_tok[half];
+        if constexpr (kParts) {
+            const int2 row = p.row_map[q_row0 + q_tok[half]];
+            pos_row[half] = p.ctx_len[row.x] + row.y - 1;
+        } else {
+            pos_row[half] = L - item.n_q + q_tok[half];
+        }
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
             qf[ks][half] = q_src[half] ? __ldg(q_src[half] + ks * 8 + tid4) : 0u;          // cols 16ks + 2tid4
@@ -348,7 +358,8 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     // P V product uses, so out = sum(p v) / sum(p) stays a true weighted mean).
     float l_acc[4] = {0.f, 0.f, 0.f, 0.f};                   // [0] row gid, [2] row gid + 8
     const float sc = p.scale_log2;
-    const int full_vis_limit = L - item.n_q;                 // tokens <= this are visible to all rows
+    // tokens <= this are visible to all rows
+    const int full_vis_limit = kParts ? __reduce_min_sync(0xffffffffu, min(pos_row[0], pos_row[1])) : L - item.n_q;
 
     // per-lane ldmatrix row addressing inside a tile (row = token, 128-byte rows, 16-byte chunk
     // index xor (row & 7) = the TMA 128-byte swizzle)
@@ -425,10 +436,21 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
             m_run[h] = mn;
         }
         uint32_t pa[4];      // P as the A operand of P V (rows gid / gid+8, tokens 0-7 / 8-15)
+        float part[2] = {0.f, 0.f};                          // mode 3: this lane's share of the two row sums
+        if constexpr (kParts) {
+            float w[2][4];
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { w[nt][e] = ex2(fmaf(sacc[nt][e], sc, -mu[e >> 1])); part[e >> 1] += w[nt][e]; }
+            pa[0] = pack_bf16(w[0][0], w[0][1]); pa[1] = pack_bf16(w[0][2], w[0][3]);
+            pa[2] = pack_bf16(w[1][0], w[1][1]); pa[3] = pack_bf16(w[1][2], w[1][3]);
+        } else {
         pa[0] = pack_bf16(ex2(fmaf(sacc[0][0], sc, -mu[0])), ex2(fmaf(sacc[0][1], sc, -mu[0])));
         pa[1] = pack_bf16(ex2(fmaf(sacc[0][2], sc, -mu[1])), ex2(fmaf(sacc[0][3], sc, -mu[1])));
         pa[2] = pack_bf16(ex2(fmaf(sacc[1][0], sc, -mu[0])), ex2(fmaf(sacc[1][1], sc, -mu[0])));
         pa[3] = pack_bf16(ex2(fmaf(sacc[1][2], sc, -mu[1])), ex2(fmaf(sacc[1][3], sc, -mu[1])));
+        }
         if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
 #pragma unroll
             for (int n = 0; n < 16; ++n) {
@@ -438,7 +460,8 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
             l_acc[0] *= corr[0]; l_acc[1] *= corr[0];
             l_acc[2] *= corr[1]; l_acc[3] *= corr[1];
         }
-        mma_bf16(l_acc, pa, ones_bf16, ones_bf16);
+        if constexpr (kParts) { l_acc[0] += part[0]; l_acc[2] += part[1]; }
+        else mma_bf16(l_acc, pa, ones_bf16, ones_bf16);
         // O += P V   (16 n-tiles of 8 output columns, two per ldmatrix)
 #pragma unroll
         for (int n2 = 0; n2 < 8; ++n2) {
@@ -468,6 +491,13 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     KAP_TRACE_POINT(blockIdx.x, 4);
 
     // ------------------------------------------------ combine the four warps' states, write out
+    if constexpr (kParts) {                            // the four lanes of a row hold a quarter of its sum each
+#pragma unroll
+        for (int d = 1; d <= 2; d <<= 1) {
+            l_acc[0] += __shfl_xor_sync(0xffffffffu, l_acc[0], d);
+            l_acc[2] += __shfl_xor_sync(0xffffffffu, l_acc[2], d);
+        }
+    }
     const float l_run[2] = {l_acc[0], l_acc[2]};       // complete row sums (every column of P x ones)
     __syncthreads();                                   // all tile reads done: the ring is scratch now
     float* scratch = reinterpret_cast<float*>(ring) + warp * (kRowTile * kScratchStride);
@@ -489,7 +519,7 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     float* all = reinterpret_cast<float*>(ring);
     float* m_flat = tail->cta_m;
     float* l_flat = tail->cta_l;
-    const bool single = item.n_splits == 1;
+    const bool single = !kParts && item.n_splits == 1;
     // Combine the warp groups: the CTA-level state of row R ends up in scratch row R (the region
     // of warp R / 16 of group 0, which only this cell's thread reads) and cta_m[R], cta_l[R]; with
     // one CTA per item it goes straight to global memory instead.

@@ -56,9 +56,8 @@ struct kap_workspace {
     int32_t kv_layout = 0;         // KAP_KV_HND / KAP_KV_NHD: layout of the pools given to the attention calls
     int32_t plain_next = 0;        // the page lists were just rewritten on the device: launch the
                                    // next attention kernel as an ordinary (fully ordered) one
-    int32_t shared_prefix = 0;     // the schedule was made by kap_schedule_shared_prefix ...
-    int32_t prefix_attrs_set = 0;
-    int32_t prefix_ctas = 0;       // ... for so many CTAs (d_items: segments, d_groups: units, d_merge: the rest)
+    int32_t shared_prefix = 0;     // the schedule was made by kap_schedule_shared_prefix (its arrays: kap_prefix.h)
+    int32_t prefix_attrs_set = 0, prefix_ctas = 0, prefix_segments = 0;
     int64_t total_rows = 0;        // sum over sequences of n_q
     unsigned long long bulk_overflows_seen = 0;   // see kv_written_in_bulk() in kap_attn.cu
     // host (pinned) staging and device copies

@@ -11,6 +11,9 @@ void count_launch();
 kap_status workspace_kv_map(kap_workspace* ws, const void* pool, int64_t pages, int32_t hkv, const void** map);
 kap_status encode_query_map(void* map, const void* q, int64_t rows, int32_t hq, int32_t G, int32_t tile_rows);
 bool launch_programmatically();
+kap_status launch_prefix_parts(kap_workspace* ws, const void* kv_map, const void* q, const int32_t* bt_indptr, const int32_t* bt_pages,
+                               const int32_t* ctx_len, const WorkItem* items, int32_t n_items, const void* row_map,
+                               int64_t num_pool_pages, int32_t batch, int32_t hq, int32_t hkv, float scale_log2, cudaStream_t stream);
 
 namespace {
 
@@ -21,32 +24,24 @@ namespace {
             return fail(KAP_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));         \
     } while (0)
 
-// offsets of the sequences, rows and CTA ranges inside the workspace's third metadata array
-struct BlobLayout {
-    size_t rows, ctas;
-    BlobLayout(int64_t batch, int64_t total_rows) {
-        rows = (size_t)batch * sizeof(PrefixSeq);
-        ctas = rows + (size_t)total_rows * sizeof(PrefixRow);
-    }
-};
-
 kap_status upload_schedule(kap_workspace* ws, const PrefixSchedule& s, int32_t batch, int32_t hq, int32_t hkv, cudaStream_t stream) {
     int dev = -1;
     KAP_CUDA(cudaGetDevice(&dev));
     if (dev != ws->device) KAP_CUDA(cudaSetDevice(ws->device));
     cudaError_t e = cudaEventSynchronize((cudaEvent_t)ws->upload_event);   // the pinned staging may still feed the previous upload
-    const BlobLayout at(batch, s.total_rows);
-    const size_t seg_bytes = s.segments.size() * sizeof(PrefixSegment), unit_bytes = s.units.size() * sizeof(PrefixUnit);
+    const PrefixLayout at = prefix_layout(s);
     if (e == cudaSuccess && batch > 0) {
-        unsigned char* blob = reinterpret_cast<unsigned char*>(ws->h_merge);
-        std::memcpy(ws->h_items, s.segments.data(), seg_bytes);
-        std::memcpy(ws->h_groups, s.units.data(), unit_bytes);
-        std::memcpy(blob, s.seqs.data(), at.rows);
-        std::memcpy(blob + at.rows, s.rows.data(), at.ctas - at.rows);
-        std::memcpy(blob + at.ctas, s.cta_begin.data(), s.cta_begin.size() * sizeof(int32_t));
-        e = cudaMemcpyAsync(ws->d_items, ws->h_items, seg_bytes, cudaMemcpyHostToDevice, stream);
-        if (e == cudaSuccess) e = cudaMemcpyAsync(ws->d_groups, ws->h_groups, unit_bytes, cudaMemcpyHostToDevice, stream);
-        if (e == cudaSuccess) e = cudaMemcpyAsync(ws->d_merge, blob, prefix_blob_bytes(s), cudaMemcpyHostToDevice, stream);
+        unsigned char* first = reinterpret_cast<unsigned char*>(ws->h_items);
+        unsigned char* third = reinterpret_cast<unsigned char*>(ws->h_merge);
+        std::memcpy(first, s.items.data(), at.segments);
+        std::memcpy(first + at.segments, s.segments.data(), at.first_bytes - at.segments);
+        std::memcpy(ws->h_groups, s.units.data(), at.second_bytes);
+        std::memcpy(third, s.seqs.data(), at.rows);
+        std::memcpy(third + at.rows, s.rows.data(), at.ctas - at.rows);
+        std::memcpy(third + at.ctas, s.cta_begin.data(), s.cta_begin.size() * sizeof(int32_t));
+        e = cudaMemcpyAsync(ws->d_items, first, at.first_bytes, cudaMemcpyHostToDevice, stream);
+        if (e == cudaSuccess) e = cudaMemcpyAsync(ws->d_groups, ws->h_groups, at.second_bytes, cudaMemcpyHostToDevice, stream);
+        if (e == cudaSuccess) e = cudaMemcpyAsync(ws->d_merge, third, at.third_bytes, cudaMemcpyHostToDevice, stream);
     }
     if (e == cudaSuccess) e = cudaEventRecord((cudaEvent_t)ws->upload_event, stream);
     if (dev != ws->device) cudaSetDevice(dev);                             // the caller's current device is put back
@@ -55,7 +50,7 @@ kap_status upload_schedule(kap_workspace* ws, const PrefixSchedule& s, int32_t b
     ws->prefix_ctas = s.n_cta;
     if (ws->schedule_key) ws->schedule_key->clear();
     ws->batch = batch; ws->num_q_heads = hq; ws->num_kv_heads = hkv; ws->total_rows = s.total_rows;
-    ws->n_items = (int32_t)s.segments.size();
+    ws->n_items = (int32_t)s.items.size(); ws->n_groups = (int32_t)s.units.size(); ws->prefix_segments = (int32_t)s.segments.size();
     return KAP_OK;
 }
 
@@ -119,18 +114,25 @@ extern "C" kap_status kap_shared_prefix_attn(
         ws->prefix_attrs_set = 1;
     }
     PfxParams p{};
-    const BlobLayout at(batch, ws->total_rows);
-    const unsigned char* blob = reinterpret_cast<const unsigned char*>(ws->d_merge);
-    p.segments = reinterpret_cast<const PrefixSegment*>(ws->d_items);
+    const PrefixLayout at((size_t)ws->n_items, (size_t)ws->prefix_segments, (size_t)ws->n_groups, (size_t)batch, (size_t)ws->total_rows, (size_t)ws->prefix_ctas);
+    const unsigned char* first = reinterpret_cast<const unsigned char*>(ws->d_items);
+    const unsigned char* third = reinterpret_cast<const unsigned char*>(ws->d_merge);
+    p.segments = reinterpret_cast<const PrefixSegment*>(first + at.segments);
     p.units = reinterpret_cast<const PrefixUnit*>(ws->d_groups);
-    p.seqs = reinterpret_cast<const PrefixSeq*>(blob);
-    p.row_map = reinterpret_cast<const PrefixRow*>(blob + at.rows);
-    p.cta_begin = reinterpret_cast<const int32_t*>(blob + at.ctas);
+    p.seqs = reinterpret_cast<const PrefixSeq*>(third);
+    p.row_map = reinterpret_cast<const PrefixRow*>(third + at.rows);
+    p.cta_begin = reinterpret_cast<const int32_t*>(third + at.ctas);
     p.q_indptr = q_indptr; p.bt_indptr = bt_indptr; p.bt_pages = bt_pages; p.ctx_len = ctx_len;
     p.part_o = ws->d_part_o; p.part_ml = ws->d_part_ml; p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ws->d_status;
-    p.num_pool_pages = num_pool_pages; p.batch = batch; p.total_rows = (int32_t)ws->total_rows;
-    p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G; p.nhd = nhd;
+    p.num_pool_pages = num_pool_pages; p.total_rows = (int32_t)ws->total_rows;
+    p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G;
     p.scale_log2 = sm_scale * 1.4426950408889634f;
+    // the sequences' own pages and small prefixes, then the large prefixes, then the join of their states
+    if (ws->n_items > 0) {
+        st = launch_prefix_parts(ws, kv_map, q, bt_indptr, bt_pages, ctx_len, ws->d_items, ws->n_items, p.row_map, num_pool_pages, batch,
+                                 num_q_heads, num_kv_heads, p.scale_log2, (cudaStream_t)cuda_stream);
+        if (st != KAP_OK) return st;
+    }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -142,9 +144,11 @@ extern "C" kap_status kap_shared_prefix_attn(
     cfg.attrs = attr;
     cfg.numAttrs = launch_programmatically() ? 1 : 0;
     const CUtensorMap& kv = *reinterpret_cast<const CUtensorMap*>(kv_map);
-    if (nhd) KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<true>, kv, q_map, p));
-    else KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<false>, kv, q_map, p));
-    count_launch();
+    if (ws->prefix_ctas > 0) {
+        if (nhd) KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<true>, kv, q_map, p));
+        else KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<false>, kv, q_map, p));
+        count_launch();
+    }
     cfg.gridDim = dim3((unsigned)((ws->total_rows * num_q_heads + 3) / 4));
     cfg.blockDim = dim3(128);
     cfg.dynamicSmemBytes = 0;

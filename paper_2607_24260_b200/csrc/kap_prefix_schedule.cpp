@@ -1,10 +1,9 @@
 // The work list of kap_shared_prefix_attn (host code, no GPU).
 //
-// Units of work: a shared prefix for one KV head and up to 256 of the group's query rows (two tiles of 128),
-// or one sequence's own pages for one KV head.  A unit is a run of steps of 64 tokens (four pages); all units
-// laid end to end form a tape, which is cut into one piece per CTA of nearly equal cost, so that a long prefix is
-// spread over the whole device and many short own parts are dealt out in runs.  What a CTA gets of one unit is
-// a segment; every segment leaves un-normalised states (m, l, O) that the merge pass joins.
+// A group's shared pages are read once per KV head for all of the group's query rows.  With more than 64 rows they go to
+// the tcgen05 kernel, in blocks of up to 256 rows (two tiles of 128) and steps of 80 tokens; with fewer, and for the pages that a
+// sequence has of its own, to the split kernel, whose unit is one (rows, KV head, slice of a page list).  Every piece leaves
+// un-normalised states (m, l, O) that the merge pass joins.
 #include <algorithm>
 #include <exception>
 
@@ -14,20 +13,45 @@ namespace kap {
 
 namespace {
 
-struct Unit {
-    int32_t seq, kv_head, first_page, n_pages, tok_row0, rows, flags, n_q, merge_unit;
-    int32_t steps() const { return (n_pages + kPrefixStepPages - 1) / kPrefixStepPages; }
+// Row counts up to which the split kernel takes a prefix: what its warps can hold.
+constexpr int32_t kSplitRows = kRowTile * kMaxRowTiles;
+constexpr int32_t kSplitCtasPerSm = 3;
+constexpr int32_t kMinSplitPages = 4;                          // a page for each of a CTA's warps
+constexpr int32_t kMaxSplitPages = 1024;                       // page ids a CTA holds: 1600
+// A segment of the tcgen05 kernel pays for its query tiles, the pipeline's fill and its states about as much as for two steps.
+constexpr int64_t kSegmentSteps = 2;
+
+struct Unit {                                                  // of the tcgen05 kernel
+    int32_t seq, kv_head, n_pages, tok_row0, rows, unit;
+};
+struct Tape {                                                  // row blocks that walk over the same pages side by side
+    int32_t steps, first_unit, n_units;                        // consecutive entries of the unit list
 };
 
-// Costs in thirds of a 64-token step of two row tiles (about 1300 cycles of the tensor core).  A step of a single
-// tile is bound by its 32 KiB from memory; a segment pays for its query tile, the pipeline's fill and its states.
-constexpr int64_t kPairCost = 3, kSoloCost = 3, kSegmentCost = 6;
+// CTAs that walk over the same pages side by side, for different row blocks, so that the pages come from memory once: the
+// largest width up to eight that wastes at most 3 % more CTA time than the best one (blocks that do not fill the last
+// bundle, SMs that do not fill one).
+int32_t bundle_width(const std::vector<std::pair<int32_t, int64_t>>& groups /* (row blocks, steps) */, int32_t sm_count) {
+    double waste[9], best = 1e300;
+    for (int32_t w = 1; w <= 8; ++w) {
+        double used = 0, need = 0;
+        for (const auto& g : groups) {
+            used += (double)((g.first + w - 1) / w * w) * (double)g.second;
+            need += (double)g.first * (double)g.second;
+        }
+        waste[w] = w > sm_count || need == 0 ? 1e300 : used / need * sm_count / (sm_count / w * w);
+        best = std::min(best, waste[w]);
+    }
+    for (int32_t w = 8; w > 1; --w)
+        if (waste[w] <= 1.03 * best) return w;
+    return 1;
+}
 
 }  // namespace
 
 kap_status build_prefix_schedule(int32_t batch, const int32_t* list_len, const int32_t* n_q, int32_t n_groups,
                                  const int32_t* group_indptr, const int32_t* prefix_pages, int32_t hq, int32_t hkv,
-                                 int32_t cta_slots, PrefixSchedule& out)
+                                 int32_t sm_count, PrefixSchedule& out)
 {
     if (batch < 0 || n_groups < 0 || (batch > 0 && (!list_len || !n_q || !group_indptr || !prefix_pages)))
         return fail(KAP_ERR_INVALID_ARG, "NULL pointer, batch %d or n_groups %d", batch, n_groups);
@@ -50,96 +74,143 @@ kap_status build_prefix_schedule(int32_t batch, const int32_t* list_len, const i
     }
 
     out = PrefixSchedule();
-    std::vector<Unit> units;
-    auto add = [&](Unit u) {
-        u.merge_unit = (int32_t)units.size();
-        units.push_back(u);
-    };
     out.seqs.resize((size_t)batch);
+    std::vector<Unit> tc;
+    std::vector<std::pair<int32_t, int64_t>> widths;
+    struct Part { int32_t seq, kv_head, first_page, n_pages, rows, n_q, prefix, row0, unit; };
+    std::vector<Part> parts;                                   // of the split kernel
+    std::vector<int32_t> blocks_of;                            // per tcgen05 group: row blocks
     int32_t row = 0;
     for (int32_t i = 0; i < n_groups && batch > 0; ++i) {
         const int32_t b0 = group_indptr[i], b1 = group_indptr[i + 1], row0 = row;
+        // a prefix that only one sequence reads is part of that sequence's own pages
+        const int32_t shared = b1 - b0 > 1 ? prefix_pages[i] : 0;
         for (int32_t b = b0; b < b1; ++b) {
-            PrefixSeq& s = out.seqs[(size_t)b];
-            s = PrefixSeq{row, n_q[b], -1, -1, 0, row0, list_len[b], 0};
+            out.seqs[(size_t)b] = PrefixSeq{row, list_len[b], -1, -1, 0, 1, row0, 0};
             for (int32_t j = 0; j < n_q[b]; ++j) out.rows.push_back(PrefixRow{b, j + 1 - n_q[b]});
             row += n_q[b];
         }
-        // a prefix that only one sequence reads is part of that sequence's own pages
-        const int32_t shared = b1 - b0 > 1 ? prefix_pages[i] : 0;
         if (shared > 0) {
-            const int32_t rows = (row - row0) * G, pairs = (rows + kPrefixUnitRows - 1) / kPrefixUnitRows;
+            const int32_t rows = (row - row0) * G;
+            const bool split = rows <= kSplitRows;
+            const int32_t block = split ? rows : kPrefixUnitRows, blocks = (rows + block - 1) / block;
             for (int32_t b = b0; b < b1; ++b) {
-                out.seqs[(size_t)b].prefix_unit0 = (int32_t)units.size();
-                out.seqs[(size_t)b].n_pairs = pairs;
+                PrefixSeq& s = out.seqs[(size_t)b];
+                s.prefix_unit0 = (int32_t)out.units.size(); s.n_blocks = blocks; s.block_rows = block;
             }
             for (int32_t g = 0; g < hkv; ++g)
-                for (int32_t p = 0; p < pairs; ++p) {
-                    const int32_t r0 = p * kPrefixUnitRows, n = std::min(kPrefixUnitRows, rows - r0);
-                    add(Unit{b0, g, 0, shared, row0 + r0 / G, n, kSegPrefix | (n > kPrefixTileRows ? kSegPair : 0), 0, 0});
+                for (int32_t k = 0; k < blocks; ++k) {
+                    const int32_t n = std::min(block, rows - k * block), unit = (int32_t)out.units.size();
+                    out.units.push_back(PrefixUnit{0, n, 0, 0});
+                    if (split) parts.push_back(Part{b0, g, 0, shared, n, row - row0, 1, row0, unit});
+                    else tc.push_back(Unit{b0, g, shared, row0 + k * block / G, n, unit});
                 }
+            if (!split) {
+                widths.emplace_back(blocks, (int64_t)hkv * ((shared + kPrefixStepPages - 1) / kPrefixStepPages));
+                for (int32_t g = 0; g < hkv; ++g) blocks_of.push_back(blocks);
+            }
         }
         for (int32_t b = b0; b < b1; ++b) {
-            PrefixSeq& s = out.seqs[(size_t)b];
             if (list_len[b] <= shared) continue;
-            s.own_unit0 = (int32_t)units.size();
-            for (int32_t g = 0; g < hkv; ++g)
-                add(Unit{b, g, shared, list_len[b] - shared, s.row0, n_q[b] * G, 0, n_q[b], 0});
+            out.seqs[(size_t)b].own_unit0 = (int32_t)out.units.size();
+            for (int32_t g = 0; g < hkv; ++g) {
+                parts.push_back(Part{b, g, shared, list_len[b] - shared, n_q[b] * G, n_q[b], 0, out.seqs[(size_t)b].row0, (int32_t)out.units.size()});
+                out.units.push_back(PrefixUnit{0, n_q[b] * G, 0, 0});
+            }
         }
     }
     out.total_rows = row;
-    out.units.resize(units.size());
-
-    // shared prefixes first (long, bound by the tensor cores), then the own parts
-    std::stable_sort(units.begin(), units.end(), [](const Unit& a, const Unit& b) { return (a.flags & kSegPrefix) > (b.flags & kSegPrefix); });
-    auto step_cost = [](const Unit& u) { return u.flags & kSegPair ? kPairCost : kSoloCost; };
-    int64_t cost = 0, steps = 0;
-    for (const Unit& u : units) { cost += u.steps() * step_cost(u) + kSegmentCost; steps += u.steps(); }
-    const int32_t n_cta = (int32_t)std::max<int64_t>(1, std::min<int64_t>(cta_slots, steps));
-    cost += (n_cta - 1) * kSegmentCost;                        // a cut unit starts once more
-    int64_t spent = 0;                                         // cost of everything handed out so far
-    int32_t cta = 0;
-    out.cta_begin.push_back(0);
     int64_t state_rows = 0;
-    for (const Unit& u : units) {
-        PrefixUnit& mu = out.units[(size_t)u.merge_unit];
-        mu.state_row0 = (int32_t)state_rows; mu.rows = u.rows; mu.n_states = 0; mu.pad = 0;
-        for (int32_t at = 0; at < u.steps();) {
-            // steps that still fit this CTA's share; the last CTA takes what is left
-            int64_t end = cost * (cta + 1) / n_cta;
-            int64_t fit = (end - spent - kSegmentCost + step_cost(u) / 2) / step_cost(u);
-            if (cta + 1 < n_cta && fit < 1 && spent > cost * cta / n_cta) {   // not even one: the next CTA's
-                ++cta;
-                out.cta_begin.push_back((int32_t)out.segments.size());
-                continue;
-            }
-            const int32_t n = cta + 1 == n_cta ? u.steps() - at : (int32_t)std::min<int64_t>(std::max<int64_t>(fit, 1), u.steps() - at);
-            const bool two = !(u.flags & kSegPair) && n > 1;   // a single tile's steps alternate between the two streams
-            PrefixSegment s{};
-            s.seq = u.seq; s.kv_head = u.kv_head; s.flags = u.flags | (two ? kSegTwoStates : 0);
-            s.first_page = u.first_page; s.n_pages = u.n_pages; s.step_begin = at; s.step_end = at + n;
-            s.tok_row0 = u.tok_row0; s.rows = u.rows; s.n_q = u.n_q;
-            s.state_row0 = (int32_t)(state_rows + (int64_t)mu.n_states * u.rows);
-            mu.n_states += two ? 2 : 1;
-            out.segments.push_back(s);
-            at += n;
-            spent += n * step_cost(u) + kSegmentCost;
+
+    // ---- split kernel: near-equal slices that fill the device once, the longest first
+    int64_t pages = 0;
+    for (const Part& p : parts) pages += p.n_pages;
+    const int64_t slots = (int64_t)sm_count * kSplitCtasPerSm;
+    const int32_t chunk = (int32_t)std::min<int64_t>(kMaxSplitPages, std::max<int64_t>(kMinSplitPages, (pages + slots - 1) / slots));
+    for (const Part& p : parts) {
+        const int32_t n = (p.n_pages + chunk - 1) / chunk;
+        PrefixUnit& u = out.units[(size_t)p.unit];
+        u.state_row0 = (int32_t)state_rows; u.n_states = n;
+        for (int32_t k = 0; k < n; ++k) {
+            const int32_t from = (int32_t)((int64_t)p.n_pages * k / n), to = (int32_t)((int64_t)p.n_pages * (k + 1) / n);
+            out.items.push_back(WorkItem{p.seq, p.kv_head, p.first_page + from, p.first_page + to, p.prefix, (int32_t)(state_rows + (int64_t)k * p.rows), p.row0, p.n_q});
         }
-        state_rows += (int64_t)mu.n_states * u.rows;
+        state_rows += (int64_t)n * p.rows;
         if (state_rows > 0x7fffffff) return fail(KAP_ERR_CAPACITY, "the schedule needs %lld state rows", (long long)state_rows);
     }
-    out.cta_begin.push_back((int32_t)out.segments.size());
-    out.n_cta = (int32_t)out.cta_begin.size() - 1;
+    std::stable_sort(out.items.begin(), out.items.end(), [](const WorkItem& a, const WorkItem& b) { return a.page_end - a.page_begin > b.page_end - b.page_begin; });
+
+    // ---- tcgen05 kernel: the tapes of all (group, KV head, bundle of row blocks) end to end, cut into equal pieces; bundle b of
+    // `width` CTAs takes piece b, CTA p of it row block p
+    if (!tc.empty()) {
+        const int32_t width = bundle_width(widths, sm_count);
+        std::vector<Tape> tapes;
+        int64_t cost = 0, steps = 0;
+        for (size_t at = 0, k = 0; at < tc.size(); ++k) {
+            const int32_t blocks = blocks_of[k];
+            for (int32_t j = 0; j < blocks; j += width) {
+                Tape t{(tc[at].n_pages + kPrefixStepPages - 1) / kPrefixStepPages, (int32_t)at + j, std::min(width, blocks - j)};
+                cost += t.steps + kSegmentSteps;
+                steps += t.steps;
+                tapes.push_back(t);
+            }
+            at += (size_t)blocks;
+        }
+        const int32_t bundles = (int32_t)std::max<int64_t>(1, std::min<int64_t>(sm_count / width, steps));
+        cost += (bundles - 1) * kSegmentSteps;                 // a cut tape starts once more
+        std::vector<std::vector<PrefixSegment>> per_cta((size_t)bundles * width);
+        int64_t spent = 0;
+        int32_t bundle = 0;
+        for (const Tape& t : tapes) {
+            std::vector<int64_t> first((size_t)t.n_units, -1);
+            for (int32_t at = 0; at < t.steps;) {
+                const int64_t fit = cost * (bundle + 1) / bundles - spent - kSegmentSteps;   // steps that still fit this bundle's share
+                if (bundle + 1 < bundles && fit < 1 && spent > cost * bundle / bundles) { ++bundle; continue; }
+                const int32_t n = bundle + 1 == bundles ? t.steps - at : (int32_t)std::min<int64_t>(std::max<int64_t>(fit, 1), t.steps - at);
+                for (int32_t p = 0; p < t.n_units; ++p) {
+                    const Unit& u = tc[(size_t)(t.first_unit + p)];
+                    const bool pair = u.rows > kPrefixTileRows, two = !pair && n > 1;   // a single tile's steps alternate between the streams
+                    PrefixSegment s{};
+                    s.seq = u.seq; s.kv_head = u.kv_head; s.flags = (pair ? kSegPair : 0) | (two ? kSegTwoStates : 0);
+                    s.n_pages = u.n_pages; s.step_begin = at; s.step_end = at + n; s.tok_row0 = u.tok_row0; s.rows = u.rows;
+                    s.state_row0 = out.units[(size_t)u.unit].n_states;     // the state's number for now
+                    s.pad[0] = u.unit;
+                    out.units[(size_t)u.unit].n_states += two ? 2 : 1;
+                    per_cta[(size_t)bundle * width + p].push_back(s);
+                }
+                at += n;
+                spent += n + kSegmentSteps;
+            }
+        }
+        for (const Unit& u : tc) {
+            PrefixUnit& mu = out.units[(size_t)u.unit];
+            mu.state_row0 = (int32_t)state_rows;
+            state_rows += (int64_t)mu.n_states * mu.rows;
+            if (state_rows > 0x7fffffff) return fail(KAP_ERR_CAPACITY, "the schedule needs %lld state rows", (long long)state_rows);
+        }
+        out.n_cta = bundles * width;
+        out.cta_begin.push_back(0);
+        for (auto& list : per_cta) {
+            for (PrefixSegment& s : list) {
+                const PrefixUnit& mu = out.units[(size_t)s.pad[0]];
+                s.state_row0 = mu.state_row0 + s.state_row0 * mu.rows;
+                s.pad[0] = 0;
+                out.segments.push_back(s);
+            }
+            out.cta_begin.push_back((int32_t)out.segments.size());
+        }
+    }
     out.state_rows = state_rows;
     return KAP_OK;
 }
 
 int64_t prefix_items_needed(const PrefixSchedule& s, int32_t max_rows) {
-    auto up = [](int64_t bytes) { return (bytes + (int64_t)sizeof(WorkItem) - 1) / (int64_t)sizeof(WorkItem); };
+    auto up = [](size_t bytes) { return (int64_t)((bytes + sizeof(WorkItem) - 1) / sizeof(WorkItem)); };
+    const PrefixLayout at = prefix_layout(s);
     int64_t n = std::max<int64_t>(1, (s.state_rows + max_rows - 1) / max_rows);
-    n = std::max(n, up((int64_t)(s.segments.size() * sizeof(PrefixSegment))));
-    n = std::max(n, up((int64_t)(s.units.size() * sizeof(PrefixUnit))));
-    return std::max(n, up((int64_t)prefix_blob_bytes(s)));
+    n = std::max(n, up(at.first_bytes));
+    n = std::max(n, up(at.second_bytes));
+    return std::max(n, up(at.third_bytes));
 }
 
 }  // namespace kap

@@ -93,6 +93,55 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Two fp32 operations in one instruction (sm_100a); a pair is one 64-bit register pair.
+__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_rm_f32x2(uint64_t a, uint64_t b) {      // rounded towards -inf
+    uint64_t d;
+    asm("add.rm.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 2^x for two x in [-inf, 127) on the FMA pipe: x = n + f with n = floor(x) (a sum with 1.5 2^23 rounded down holds n in
+// its low bits), 2^f by a degree-4 polynomial of least largest relative error on [0, 1) (2.7e-6; fitted by iteratively reweighted
+// least squares), n added to the exponent.  Below 2^-126 the result is 2^-126.
+__device__ __forceinline__ void exp2_poly(uint64_t x2, float& lo, float& hi) {
+    float a, b;
+    unpack_f32x2(x2, a, b);
+    const uint64_t x = pack_f32x2(fmaxf(a, -126.f), fmaxf(b, -126.f));
+    const uint64_t magic = pack_f32x2(12582912.f, 12582912.f), minus_magic = pack_f32x2(-12582912.f, -12582912.f);
+    const uint64_t t = add_rm_f32x2(x, magic);
+    const uint64_t f = fma_f32x2(add_f32x2(t, minus_magic), pack_f32x2(-1.f, -1.f), x);
+    uint64_t y = fma_f32x2(pack_f32x2(0.0135341678f, 0.0135341678f), f, pack_f32x2(0.0520114601f, 0.0520114601f));
+    y = fma_f32x2(y, f, pack_f32x2(0.241442755f, 0.241442755f));
+    y = fma_f32x2(y, f, pack_f32x2(0.693003833f, 0.693003833f));
+    y = fma_f32x2(y, f, pack_f32x2(1.00000262f, 1.00000262f));
+    float y0, y1, t0, t1;
+    unpack_f32x2(y, y0, y1);
+    unpack_f32x2(t, t0, t1);
+    lo = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(t0) << 23));
+    hi = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(t1) << 23));
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t*>(&v);

@@ -149,6 +149,14 @@ def test_long_prefix():
     Case(7, [(700, [(4, 40 + 3 * i) for i in range(48)])], 32, 8).check()
 
 
+@pytest.mark.parametrize("layout", [kap.KV_HND, kap.KV_NHD])
+@pytest.mark.parametrize("members", [17, 18, 24, 33, 39, 45, 70, 72, 97])
+def test_partly_filled_tiles_over_many_steps(members, layout):
+    # 68 rows (one tile) to 388 (a pair and a single tile): softmax warps with all, some and none of their rows
+    rng = np.random.default_rng(members)
+    Case(30, [(403, [(1, int(t)) for t in rng.integers(1, 60, members)]), (130, [(1, int(t)) for t in rng.integers(1, 60, 20)])], 8, 2, layout).check()
+
+
 def test_windows_longer_than_the_own_part():
     # a sequence whose rows reach back into the shared pages, and one with nothing of its own
     Case(8, [(4, [(3, 1), (1, 0), (6, 2), (1, 9)])]).check()
