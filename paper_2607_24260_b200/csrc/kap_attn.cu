@@ -322,18 +322,18 @@ kap_status launch_prefix_parts(kap_workspace* ws, const void* kv_map, const void
     p.q = (const __nv_bfloat16*)q; p.list_indptr = bt_indptr; p.phys_pages = bt_pages; p.ctx_len = ctx_len;
     p.items = items; p.part_o = ws->d_part_o; p.part_ml = ws->d_part_ml; p.status = ws->d_status;
     p.num_pool_pages = num_pool_pages; p.Hq = hq; p.Hkv = hkv; p.G = hq / hkv; p.rows_cap = 1; p.batch = batch;
-    p.cluster = 1; p.early_kv = 0; p.ring_slots = kDefaultSlots; p.scale_log2 = scale_log2;
+    p.cluster = 1; p.early_kv = 0; p.ring_slots = ws->ring_slots; p.scale_log2 = scale_log2;
     p.row_map = (const int2*)row_map;
     const bool nhd = ws->kv_layout == KAP_KV_NHD;
     KAP_CUDA(cudaFuncSetAttribute(nhd ? kap_attn_split_kernel<3, true> : kap_attn_split_kernel<3, false>,
-                                  cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes_for(kDefaultSlots)));
+                                  cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes_for(kMaxSlots)));
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)n_items);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem_bytes_for(kDefaultSlots);
+    cfg.dynamicSmemBytes = smem_bytes_for(ws->ring_slots);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = launch_programmatically() ? 1 : 0;

@@ -154,7 +154,8 @@ __device__ __forceinline__ void merge_group_cell(const AttnParams& p, const Merg
 // caller gave neither logical page indices nor token masks - the verification path and the
 // full-context fallback - so a CTA keeps only physical page ids and can hold 2.5 times as many);
 // 3 = the parts of shared-prefix attention (plain lists too): the rows' positions come from row_map, because the rows of a
-// shared prefix (item.group = 1) belong to several sequences; items always leave a partial state, at row item.split of the
+// shared prefix (bit 0 of item.group) belong to several sequences; short parts of few rows may share a CTA (bit 1: warp i takes
+// the whole list for KV head item.kv_head + i, because one CTA for each of many short lists is mostly start-up); items always leave a partial state, at row item.split of the
 // partial buffer, and item.n_splits is their first row of q; row sums add the unrounded weights, so that lse keeps fp32 accuracy for short parts as well.
 template <int kMode, bool kNhd>
 __global__ void __launch_bounds__(kThreads, 3)
@@ -168,7 +169,7 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     unsigned char* ring = smem_base + kTailBytes;
     const int n_slots = p.ring_slots;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    pdl_launch_dependents();
+    if constexpr (kMode != 3) pdl_launch_dependents();       // (mode 3: behind the wait)
     KAP_TRACE_POINT(blockIdx.x, 0);
 
     // ---- prologue on static metadata only (work list, page lists, q_indptr): with programmatic
@@ -250,28 +251,30 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
 
     const int depth = n_slots / n_groups;                    // ring slots per group
     const int grp = warp / RT, rt = warp % RT;
+    const bool by_head = kParts && (item.group & 2);          // RT = 1: a warp is a group
+    const int kv_head = by_head ? item.kv_head + warp : item.kv_head;
     const bool producer = (rt == 0) && (lane == 0);           // fills the group's ring at the start
     const int rows_per_page = 2 * p.Hkv * kPageSize;
     const int v_row_off = p.Hkv * kPageSize;
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-    const int group_pages = (n_local - grp + n_groups - 1) / n_groups;   // pages of this warp group
+    const int group_pages = by_head ? n_local : (n_local - grp + n_groups - 1) / n_groups;   // pages of this warp group
     // put the group's k-th page into ring slot s, or publish "no more pages" there
     auto fill = [&](int s, int k) {
         const uint32_t bar = smem_u32(&tail->full[s]);
-        const int idx = k * n_groups + grp;                  // local id
+        const int idx = by_head ? k : k * n_groups + grp;    // local id
         if (k < group_pages) {
             tail->slot_page[s] = idx;
             const uint32_t dst = smem_u32(ring + s * kPageHeadBytes);
             mbar_expect_tx(bar, kPageHeadBytes);
             if (kNhd) {
                 const int z = id_phys[idx] * (2 * kPageSize);            // token row of the page's K
-                tma_load_3d(dst, &kv_map, 0, item.kv_head, z, bar, policy);
-                tma_load_3d(dst + kHalfTileBytes, &kv_map, 64, item.kv_head, z, bar, policy);
-                tma_load_3d(dst + kTileBytes, &kv_map, 0, item.kv_head, z + kPageSize, bar, policy);
-                tma_load_3d(dst + kTileBytes + kHalfTileBytes, &kv_map, 64, item.kv_head, z + kPageSize, bar, policy);
+                tma_load_3d(dst, &kv_map, 0, kv_head, z, bar, policy);
+                tma_load_3d(dst + kHalfTileBytes, &kv_map, 64, kv_head, z, bar, policy);
+                tma_load_3d(dst + kTileBytes, &kv_map, 0, kv_head, z + kPageSize, bar, policy);
+                tma_load_3d(dst + kTileBytes + kHalfTileBytes, &kv_map, 64, kv_head, z + kPageSize, bar, policy);
             } else {
-                const int y = id_phys[idx] * rows_per_page + item.kv_head * kPageSize;
+                const int y = id_phys[idx] * rows_per_page + kv_head * kPageSize;
                 tma_load_2d(dst, &kv_map, 0, y, bar, policy);
                 tma_load_2d(dst + kHalfTileBytes, &kv_map, 64, y, bar, policy);
                 tma_load_2d(dst + kTileBytes, &kv_map, 0, y + v_row_off, bar, policy);
@@ -315,17 +318,19 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
         const bool valid = R < rows;
         q_tok[half] = valid ? R / p.G : item.n_q - 1;
         q_src[half] = valid ? reinterpret_cast<const uint32_t*>(
-            p.q + ((q_row0 + q_tok[half]) * p.Hq + item.kv_head * p.G + R % p.G) * kHeadDim) : nullptr;
+            p.q + ((q_row0 + q_tok[half]) * p.Hq + kv_head * p.G + R % p.G) * kHeadDim) : nullptr;
         if (valid && tid4 < 2)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(q_src[half] + tid4 * 32) : "memory");
     }
     // ---- nothing else produced by earlier kernels (Q, fresh KV, partial buffers) is touched above
     pdl_wait();
+    // mode 3: the kernel behind may start once every CTA here knows that the kernels in front are complete: it does not wait itself
+    if constexpr (kParts) pdl_launch_dependents();
     KAP_TRACE_POINT(blockIdx.x, 2);
     if (producer)
         for (; filled < depth; ++filled) fill(grp * depth + filled, filled);
     // (a shared prefix is full pages: none of its tokens lies behind a context)
-    const int L = kParts && item.group ? 0x3fffffff : p.ctx_len[item.seq];
+    const int L = kParts && (item.group & 1) ? 0x3fffffff : p.ctx_len[item.seq];
     const uint64_t deadline = global_ns() + kWaitBudgetNs;
     // second half of the prologue's cluster barrier: by now every peer has long arrived, so this
     // costs nothing here, and the epilogue may push without any further synchronisation
@@ -524,6 +529,16 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     // of warp R / 16 of group 0, which only this cell's thread reads) and cta_m[R], cta_l[R]; with
     // one CTA per item it goes straight to global memory instead.
     KAP_TRACE_POINT(blockIdx.x, 6);
+    if (by_head) {                                      // nothing to combine: warp w holds the state of head item.kv_head + w
+        for (int idx = tid; idx < kWarps * rows * 32; idx += kThreads) {
+            const int w = idx / (rows * 32), R = (idx >> 5) % rows, c4 = idx & 31;
+            const int64_t prow = (int64_t)item.split + w * rows + R;
+            *(reinterpret_cast<float4*>(p.part_o + prow * kHeadDim) + c4) =
+                *reinterpret_cast<const float4*>(all + (w * kRowTile + R) * kScratchStride + c4 * 4);
+            if (c4 == 0) *reinterpret_cast<float2*>(p.part_ml + prow * 2) = make_float2(tail->m[w][R], tail->l[w][R]);
+        }
+        return;
+    }
     for (int idx = tid; idx < rows * 32; idx += kThreads) {
         const int R = idx >> 5, c4 = idx & 31;
         const int t = R / kRowTile, r = R % kRowTile;

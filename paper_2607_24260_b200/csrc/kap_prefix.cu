@@ -1,6 +1,7 @@
 // Host side of kap_shared_prefix_attn: full-context attention (kap_verify_attn's result, Section 3.2 of the KAP paper) for a
 // batch whose sequences come in groups that share the first pages of their block tables.  The work list is built in
 // kap_prefix_schedule.cpp, the kernels are in kap_prefix_kernel.cuh.
+#include <algorithm>
 #include <cstring>
 #include <exception>
 
@@ -23,6 +24,8 @@ namespace {
         if (e_ != cudaSuccess)                                                                 \
             return fail(KAP_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));         \
     } while (0)
+
+constexpr int32_t kWideMergeStates = 5;            // states of one row from which four warps share them
 
 kap_status upload_schedule(kap_workspace* ws, const PrefixSchedule& s, int32_t batch, int32_t hq, int32_t hkv, cudaStream_t stream) {
     int dev = -1;
@@ -51,6 +54,9 @@ kap_status upload_schedule(kap_workspace* ws, const PrefixSchedule& s, int32_t b
     if (ws->schedule_key) ws->schedule_key->clear();
     ws->batch = batch; ws->num_q_heads = hq; ws->num_kv_heads = hkv; ws->total_rows = s.total_rows;
     ws->n_items = (int32_t)s.items.size(); ws->n_groups = (int32_t)s.units.size(); ws->prefix_segments = (int32_t)s.segments.size();
+    ws->ring_slots = s.ring_slots;
+    ws->max_splits = 1;
+    for (const PrefixUnit& u : s.units) ws->max_splits = std::max(ws->max_splits, u.n_states);
     return KAP_OK;
 }
 
@@ -125,7 +131,7 @@ extern "C" kap_status kap_shared_prefix_attn(
     p.q_indptr = q_indptr; p.bt_indptr = bt_indptr; p.bt_pages = bt_pages; p.ctx_len = ctx_len;
     p.part_o = ws->d_part_o; p.part_ml = ws->d_part_ml; p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ws->d_status;
     p.num_pool_pages = num_pool_pages; p.total_rows = (int32_t)ws->total_rows;
-    p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G;
+    p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G; p.behind_parts = ws->n_items > 0;
     p.scale_log2 = sm_scale * 1.4426950408889634f;
     // the sequences' own pages and small prefixes, then the large prefixes, then the join of their states
     if (ws->n_items > 0) {
@@ -149,10 +155,16 @@ extern "C" kap_status kap_shared_prefix_attn(
         else KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<false>, kv, q_map, p));
         count_launch();
     }
-    cfg.gridDim = dim3((unsigned)((ws->total_rows * num_q_heads + 3) / 4));
+    // four heads a warp where a group has them; four warps a set when many states have to be read and the sets are one wave of CTAs
+    const int H = G >= 4 ? 4 : G;
+    const int64_t sets = ws->total_rows * (num_q_heads / H);
+    const bool wide = ws->max_splits >= kWideMergeStates && sets <= (int64_t)ws->sm_count * 6;
+    cfg.gridDim = dim3((unsigned)(wide ? sets : (sets + 3) / 4));
     cfg.blockDim = dim3(128);
     cfg.dynamicSmemBytes = 0;
-    KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_merge_kernel, p));
+    if (H == 4) KAP_CUDA(cudaLaunchKernelEx(&cfg, wide ? kap_prefix_merge_kernel<4, true> : kap_prefix_merge_kernel<4, false>, p));
+    else if (H == 2) KAP_CUDA(cudaLaunchKernelEx(&cfg, wide ? kap_prefix_merge_kernel<2, true> : kap_prefix_merge_kernel<2, false>, p));
+    else KAP_CUDA(cudaLaunchKernelEx(&cfg, wide ? kap_prefix_merge_kernel<1, true> : kap_prefix_merge_kernel<1, false>, p));
     count_launch();
     return KAP_OK;
 }

@@ -34,11 +34,13 @@ struct PrefixRow { int32_t seq, back; };               // a token row's sequence
 struct PrefixSchedule {
     std::vector<PrefixSegment> segments;               // of the tcgen05 kernel
     std::vector<int32_t> cta_begin;                    // [n_cta + 1], n_cta = 0: nothing for it
-    std::vector<WorkItem> items;                       // of the split kernel: group = 1 for a prefix; split = first state row; n_splits = first row of q
+    std::vector<WorkItem> items;                       // of the split kernel: group: 1 a prefix, 2 one warp per KV head;
+                                                       // split = first state row; n_splits = first row of q
     std::vector<PrefixUnit> units;
     std::vector<PrefixSeq> seqs;
     std::vector<PrefixRow> rows;
     int32_t n_cta = 0, total_rows = 0;
+    int32_t ring_slots = 8;                            // of the split kernel
     int64_t state_rows = 0;
 };
 // Places of the arrays inside the workspace's metadata: items and segments in the first array, units in the second, sequences,

@@ -69,6 +69,7 @@ struct PfxParams {
     int32_t* status;
     long long num_pool_pages;
     int32_t total_rows, hq, hkv, G;
+    int32_t behind_parts;                                              // the split kernel ran just before, on the same stream
     float scale_log2;
 };
 
@@ -162,7 +163,9 @@ kap_prefix_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_const
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = c->tmem_base;
-    pdl_wait();                                                        // nothing of the caller's is read above
+    // Nothing of the caller's is read above.  Behind the split kernel there is nothing to wait for either: it lets this one start when
+    // the kernels in front of both are complete, and their results do not meet before the merge pass (see the end).
+    if (!p.behind_parts) pdl_wait();
     pdl_launch_dependents();
     const uint64_t deadline = global_ns() + kWaitBudgetNs;
     volatile int32_t* const late = &c->timed_out;
@@ -422,9 +425,10 @@ kap_prefix_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_const
                         tmem_ld16_nowait(t_o + i + 16, o[1]);
                         tmem_wait_ld();
                         if (valid) {
-                            uint4* dst = reinterpret_cast<uint4*>(p.part_o + row * kHeadDim + i);
+                            // 32-byte stores: each lane has a row of its own, so an instruction touches 32 lines whatever its width
+                            float* dst = p.part_o + row * kHeadDim + i;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[e >> 2][4 * (e & 3)], o[e >> 2][4 * (e & 3) + 1], o[e >> 2][4 * (e & 3) + 2], o[e >> 2][4 * (e & 3) + 3]);
+                            for (int e = 0; e < 4; ++e) store_32b(dst + 8 * e, &o[e >> 1][8 * (e & 1)]);
                         }
                     }
                     if (valid) *reinterpret_cast<float2*>(p.part_ml + row * 2) = make_float2(m_ref, l);
@@ -438,24 +442,29 @@ kap_prefix_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_const
     tc_fence_before();
     __syncthreads();
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+    pdl_wait();                                                        // complete only when the split kernel is: the merge pass waits for this one
 }
 
-// ---- joins the states of every (query row, head): one warp each, a lane holds four columns.  Bound by latency and by the
-// states' bytes (520 each, mostly still in L2).
+// ---- joins the states of every (query row, head).  A warp takes H heads of a KV head's group, whose states lie next to each other; a
+// lane holds four columns of each.  Bound by latency (the chain row -> units -> states, then batches of loads) and by the
+// states' bytes (520 each, mostly still in L2).  kWide: the four warps of a CTA share the states of one such set and join
+// theirs through shared memory.
+template <int H, bool kWide>
 __global__ void __launch_bounds__(128)
 kap_prefix_merge_kernel(const PfxParams p)
 {
-    const int lane = threadIdx.x & 31;
-    const long long cell = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (cell >= (long long)p.total_rows * p.hq) { pdl_wait(); return; }
-    const int row = (int)(cell / p.hq), head = (int)(cell % p.hq), g = head / p.G, h = head % p.G;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long set = kWide ? blockIdx.x : (long long)blockIdx.x * 4 + warp;
+    const int per_row = p.hq / H;
+    if (set >= (long long)p.total_rows * per_row) { pdl_wait(); return; }
+    const int row = (int)(set / per_row), head = (int)(set % per_row) * H, g = head / p.G, h = head % p.G;
     const PrefixRow where = p.row_map[row];                            // the schedule's arrays: final before the kernel in front
     const PrefixSeq s = p.seqs[where.seq];
     int n[2] = {0, 0};
     long long at[2] = {0, 0};
     int stride[2] = {0, 0};
     if (s.prefix_unit0 >= 0) {
-        const int R = (row - s.group_row0) * p.G + h;
+        const int R = (row - s.group_row0) * p.G + h;                  // (H heads never straddle a block: H divides G, G divides 256)
         const PrefixUnit u = p.units[s.prefix_unit0 + g * s.n_blocks + R / s.block_rows];
         n[0] = u.n_states; stride[0] = u.rows; at[0] = u.state_row0 + R % s.block_rows;
     }
@@ -465,33 +474,62 @@ kap_prefix_merge_kernel(const PfxParams p)
     }
     pdl_wait();
     // not the scheduled rows, or a context that outgrew the schedule or its block table
-    if (lane == 0) {
+    if (lane == 0 && (!kWide || warp == 0)) {
         const int most = min(s.list_pages, p.bt_indptr[where.seq + 1] - p.bt_indptr[where.seq]);
         if (p.q_indptr[where.seq] != s.row0 || p.ctx_len[where.seq] > (long long)most * kPageSize) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
     }
-    Merged acc; acc.m = -INFINITY; acc.l = 0.f; acc.o = make_float4(0.f, 0.f, 0.f, 0.f);
+    Merged acc[H];
+#pragma unroll
+    for (int e = 0; e < H; ++e) { acc[e].m = -INFINITY; acc[e].l = 0.f; acc[e].o = make_float4(0.f, 0.f, 0.f, 0.f); }
     const int total = n[0] + n[1];
-    constexpr int kBatch = 8;
-    for (int i0 = 0; i0 < total; i0 += kBatch) {
-        float2 ml[kBatch];
-        float4 o[kBatch];
+    constexpr int kBatch = 8 / H, kStep = kWide ? 4 : 1;
+    for (int i0 = kWide ? warp : 0; i0 < total; i0 += kBatch * kStep) {
+        float2 ml[kBatch][H];
+        float4 o[kBatch][H];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-            const int i = min(i0 + j, total - 1), part = i < n[0] ? 0 : 1;
+            const int i = min(i0 + j * kStep, total - 1), part = i < n[0] ? 0 : 1;
             const long long r = at[part] + (long long)(i - part * n[0]) * stride[part];
-            ml[j] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + r * 2));
-            o[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + r * kHeadDim) + lane);
+#pragma unroll
+            for (int e = 0; e < H; ++e) {
+                ml[j][e] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + (r + e) * 2));
+                o[j][e] = __ldcg(reinterpret_cast<const float4*>(p.part_o + (r + e) * kHeadDim) + lane);
+            }
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
-            if (i0 + j < total && ml[j].y > 0.f) merge_into(acc, ml[j].x, ml[j].y, o[j]);   // an empty state's O was never written
+#pragma unroll
+            for (int e = 0; e < H; ++e)                                // (an empty state's O was never written)
+                if (i0 + j * kStep < total && ml[j][e].y > 0.f) merge_into(acc[e], ml[j][e].x, ml[j][e].y, o[j][e]);
     }
-    const float inv = acc.l > 0.f ? 1.f / acc.l : 0.f;
-    uint2 v;
-    v.x = pack_bf16(acc.o.x * inv, acc.o.y * inv);
-    v.y = pack_bf16(acc.o.z * inv, acc.o.w * inv);
-    *reinterpret_cast<uint2*>(p.out + cell * kHeadDim + lane * 4) = v;
-    if (p.lse && lane == 0) p.lse[cell] = acc.l > 0.f ? (acc.m + log2f(acc.l)) * 0.6931471805599453f : -INFINITY;
+    if constexpr (kWide) {
+        __shared__ float4 other_o[3][H][32];
+        __shared__ float2 other_ml[3][H];
+        if (warp > 0) {
+#pragma unroll
+            for (int e = 0; e < H; ++e) {
+                other_o[warp - 1][e][lane] = acc[e].o;
+                if (lane == 0) other_ml[warp - 1][e] = make_float2(acc[e].m, acc[e].l);
+            }
+        }
+        __syncthreads();
+        if (warp > 0) return;
+#pragma unroll
+        for (int w = 0; w < 3; ++w)                                    // in a fixed order: results do not depend on timing
+#pragma unroll
+            for (int e = 0; e < H; ++e)
+                if (other_ml[w][e].y > 0.f) merge_into(acc[e], other_ml[w][e].x, other_ml[w][e].y, other_o[w][e][lane]);
+    }
+#pragma unroll
+    for (int e = 0; e < H; ++e) {
+        const long long cell = (long long)row * p.hq + head + e;
+        const float inv = acc[e].l > 0.f ? 1.f / acc[e].l : 0.f;
+        uint2 v;
+        v.x = pack_bf16(acc[e].o.x * inv, acc[e].o.y * inv);
+        v.y = pack_bf16(acc[e].o.z * inv, acc[e].o.w * inv);
+        *reinterpret_cast<uint2*>(p.out + cell * kHeadDim + lane * 4) = v;
+        if (p.lse && lane == 0) p.lse[cell] = acc[e].l > 0.f ? (acc[e].m + log2f(acc[e].l)) * 0.6931471805599453f : -INFINITY;
+    }
 }
 
 }  // namespace kap

@@ -1,11 +1,12 @@
 // The work list of kap_shared_prefix_attn (host code, no GPU).
 //
-// A group's shared pages are read once per KV head for all of the group's query rows.  With more than 64 rows they go to
+// A group's shared pages are read once per KV head for all of the group's query rows.  With more than 32 rows they go to
 // the tcgen05 kernel, in blocks of up to 256 rows (two tiles of 128) and steps of 80 tokens; with fewer, and for the pages that a
 // sequence has of its own, to the split kernel, whose unit is one (rows, KV head, slice of a page list).  Every piece leaves
 // un-normalised states (m, l, O) that the merge pass joins.
 #include <algorithm>
 #include <exception>
+#include <functional>
 
 #include "kap_prefix.h"
 
@@ -13,11 +14,19 @@ namespace kap {
 
 namespace {
 
-// Row counts up to which the split kernel takes a prefix: what its warps can hold.
-constexpr int32_t kSplitRows = kRowTile * kMaxRowTiles;
+// Row counts up to which the split kernel takes a prefix.  Measured on B200 (8 KV heads, one group; split / tcgen05, us a call): 16 rows
+// 10.8 / 12.4 at 512 tokens, 37.8 / 42.9 at 32K; 32 rows 13.4 / 12.8 and 41.4 / 43.3; 64 rows 15.4 / 15.8 and 58.4 / 46.0.
+constexpr int32_t kSplitRows = 2 * kRowTile;
 constexpr int32_t kSplitCtasPerSm = 3;
 constexpr int32_t kMinSplitPages = 4;                          // a page for each of a CTA's warps
 constexpr int32_t kMaxSplitPages = 1024;                       // page ids a CTA holds: 1600
+// Short parts of at most 16 rows may go four KV heads to a CTA, one per warp, instead of a CTA each: for many short lists a CTA is
+// mostly start-up.  A warp alone takes about a microsecond a page, so long lists do not belong there.
+constexpr int32_t kByHeadPages = 48;
+// What a CTA of the split kernel takes, in pages that one warp group streams (about a microsecond each): its start and its end as much
+// as five.  Measured on B200: 384 slices of 16 pages of 32 rows (two groups, one wave) 14.5 us, 768 of 8 pages 21.5; 384 of 16 pages
+// of 4 rows (four groups) 8.
+constexpr int32_t kSliceTime = 5;
 // A segment of the tcgen05 kernel pays for its query tiles, the pipeline's fill and its states about as much as for two steps.
 constexpr int64_t kSegmentSteps = 2;
 
@@ -122,23 +131,71 @@ kap_status build_prefix_schedule(int32_t batch, const int32_t* list_len, const i
     out.total_rows = row;
     int64_t state_rows = 0;
 
-    // ---- split kernel: near-equal slices that fill the device once, the longest first
-    int64_t pages = 0;
-    for (const Part& p : parts) pages += p.n_pages;
+    // ---- split kernel: near-equal slices, the longest first, cut where a simulated run ends soonest
     const int64_t slots = (int64_t)sm_count * kSplitCtasPerSm;
-    const int32_t chunk = (int32_t)std::min<int64_t>(kMaxSplitPages, std::max<int64_t>(kMinSplitPages, (pages + slots - 1) / slots));
-    for (const Part& p : parts) {
-        const int32_t n = (p.n_pages + chunk - 1) / chunk;
-        PrefixUnit& u = out.units[(size_t)p.unit];
-        u.state_row0 = (int32_t)state_rows; u.n_states = n;
+    struct Plan { int32_t chunk, limit; };                     // pages a slice; pages up to which parts go four heads to a CTA
+    auto slices = [](const Part& p, int32_t chunk) { return (p.n_pages + chunk - 1) / chunk; };
+    auto shares_cta = [&](const Part& p, int32_t limit) { return hkv % 4 == 0 && !p.prefix && p.rows <= kRowTile && p.n_pages <= limit; };
+    std::vector<int32_t> times;
+    std::vector<int64_t> ends;
+    auto makespan = [&](const Plan& plan) {
+        times.clear();
+        int64_t total = 0;
+        for (size_t i = 0; i < parts.size(); ++i) {
+            const Part& p = parts[i];
+            const bool by_head = shares_cta(p, plan.limit);
+            if (by_head && p.kv_head % 4) continue;
+            const int32_t tiles = (p.rows + kRowTile - 1) / kRowTile, groups = by_head ? 1 : tiles == 1 ? 4 : tiles == 2 ? 2 : 1;
+            const int32_t n = by_head ? 1 : slices(p, plan.chunk), most = (p.n_pages + n - 1) / n;
+            for (int32_t k = 0; k < n; ++k) times.push_back(kSliceTime + (most + groups - 1) / groups);
+            total += (int64_t)n * times.back();
+        }
+        if ((int64_t)times.size() > 8 * slots) return total / slots + kSliceTime;       // many waves: the sum decides
+        std::sort(times.begin(), times.end(), std::greater<int32_t>());
+        ends.assign((size_t)slots, 0);                         // a heap: the CTA place that is free first takes the next slice
+        int64_t last = 0;
+        for (int32_t t : times) {
+            std::pop_heap(ends.begin(), ends.end(), std::greater<int64_t>());
+            ends.back() += t;
+            last = std::max(last, ends.back());
+            std::push_heap(ends.begin(), ends.end(), std::greater<int64_t>());
+        }
+        return last;
+    };
+    Plan plan{kMaxSplitPages, 0};
+    if (!parts.empty()) {
+        int64_t best = makespan(plan);
+        for (int32_t limit = 0; limit <= kByHeadPages; limit += limit < 16 ? 4 : 16)
+            for (int32_t chunk = kMinSplitPages; chunk <= kMaxSplitPages; chunk += std::max(2, chunk / 3)) {
+                const Plan other{chunk, limit};
+                const int64_t t = makespan(other);
+                if (t < best) { best = t; plan = other; }
+            }
+    }
+    struct Timed { WorkItem item; int32_t pages; };            // pages that the busiest warp streams
+    std::vector<Timed> timed;
+    for (size_t i = 0; i < parts.size();) {
+        const Part& p = parts[i];
+        const bool by_head = shares_cta(p, plan.limit);
+        const int32_t n = by_head ? 1 : slices(p, plan.chunk), heads = by_head ? 4 : 1;   // (a part's heads follow one another)
+        for (int32_t h = 0; h < heads; ++h) {
+            PrefixUnit& u = out.units[(size_t)parts[i + (size_t)h].unit];
+            u.state_row0 = (int32_t)(state_rows + (int64_t)h * p.rows); u.n_states = n;
+        }
         for (int32_t k = 0; k < n; ++k) {
             const int32_t from = (int32_t)((int64_t)p.n_pages * k / n), to = (int32_t)((int64_t)p.n_pages * (k + 1) / n);
-            out.items.push_back(WorkItem{p.seq, p.kv_head, p.first_page + from, p.first_page + to, p.prefix, (int32_t)(state_rows + (int64_t)k * p.rows), p.row0, p.n_q});
+            const int32_t group = (p.prefix ? 1 : 0) | (by_head ? 2 : 0);
+            timed.push_back(Timed{WorkItem{p.seq, p.kv_head, p.first_page + from, p.first_page + to, group,
+                                           (int32_t)(state_rows + (int64_t)k * p.rows), p.row0, p.n_q}, by_head ? to - from : (to - from + 3) / 4});
         }
-        state_rows += (int64_t)n * p.rows;
+        state_rows += (int64_t)n * heads * p.rows;
         if (state_rows > 0x7fffffff) return fail(KAP_ERR_CAPACITY, "the schedule needs %lld state rows", (long long)state_rows);
+        i += (size_t)heads;
     }
-    std::stable_sort(out.items.begin(), out.items.end(), [](const WorkItem& a, const WorkItem& b) { return a.page_end - a.page_begin > b.page_end - b.page_begin; });
+    std::stable_sort(timed.begin(), timed.end(), [](const Timed& a, const Timed& b) { return a.pages > b.pages; });
+    for (const Timed& t : timed) out.items.push_back(t.item);
+    // fewer CTAs than fit: deeper rings
+    out.ring_slots = (int64_t)timed.size() <= sm_count ? 24 : (int64_t)timed.size() <= 2 * (int64_t)sm_count ? 12 : 8;
 
     // ---- tcgen05 kernel: the tapes of all (group, KV head, bundle of row blocks) end to end, cut into equal pieces; bundle b of
     // `width` CTAs takes piece b, CTA p of it row block p

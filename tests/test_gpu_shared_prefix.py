@@ -157,6 +157,15 @@ def test_partly_filled_tiles_over_many_steps(members, layout):
     Case(30, [(403, [(1, int(t)) for t in rng.integers(1, 60, members)]), (130, [(1, int(t)) for t in rng.integers(1, 60, 20)])], 8, 2, layout).check()
 
 
+@pytest.mark.parametrize("layout", [kap.KV_HND, kap.KV_NHD])
+@pytest.mark.parametrize("prefix", [0, 33])
+def test_crowded_batches(prefix, layout):
+    # more short own parts than CTAs fit the device at once, with some long ones and some windows of many rows among them
+    rng = np.random.default_rng(prefix)
+    members = [(int(rng.integers(1, 5)), int(t)) for t in rng.integers(4, 300, 62)] + [(1, 1), (1, 2000), (16, 40), (9, 790), (4, 768), (1, 769)]
+    Case(31, [(prefix, members)], 32, 8, layout).check()
+
+
 def test_windows_longer_than_the_own_part():
     # a sequence whose rows reach back into the shared pages, and one with nothing of its own
     Case(8, [(4, [(3, 1), (1, 0), (6, 2), (1, 9)])]).check()
