@@ -25,8 +25,6 @@ namespace {
             return fail(KAP_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));         \
     } while (0)
 
-constexpr int32_t kWideMergeStates = 5;            // states of one row from which four warps share them
-
 kap_status upload_schedule(kap_workspace* ws, const PrefixSchedule& s, int32_t batch, int32_t hq, int32_t hkv, cudaStream_t stream) {
     int dev = -1;
     KAP_CUDA(cudaGetDevice(&dev));
@@ -155,10 +153,12 @@ extern "C" kap_status kap_shared_prefix_attn(
         else KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<false>, kv, q_map, p));
         count_launch();
     }
-    // four heads a warp where a group has them; four warps a set when many states have to be read and the sets are one wave of CTAs
-    const int H = G >= 4 ? 4 : G;
-    const int64_t sets = ws->total_rows * (num_q_heads / H);
-    const bool wide = ws->max_splits >= kWideMergeStates && sets <= (int64_t)ws->sm_count * 6;
+    // Few cells: one a warp, and four warps a cell when its states are more than one batch of loads.  Many: four heads a warp (one
+    // metadata chain for all of them), four warps a set while the sets are one wave of CTAs.
+    const int64_t cells = ws->total_rows * num_q_heads, one_wave = (int64_t)ws->sm_count * 6;
+    const int H = cells <= one_wave ? 1 : G >= 4 ? 4 : G;
+    const int64_t sets = cells / H;
+    const bool wide = ws->max_splits > (H == 1 ? 8 : 4) && sets <= one_wave;
     cfg.gridDim = dim3((unsigned)(wide ? sets : (sets + 3) / 4));
     cfg.blockDim = dim3(128);
     cfg.dynamicSmemBytes = 0;
