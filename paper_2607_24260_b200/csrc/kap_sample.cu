@@ -3,177 +3,440 @@
 // Mathematics, for a row x with temperature T > 0:  w_i = exp((x_i - max x) / T);  top-k keeps the k largest
 // logits, top-p of those the shortest prefix by descending value whose weight reaches p of theirs, min-p those
 // with w_i >= min_p;  the token is the first index, in vocabulary order, whose running sum of kept weights
-// exceeds u times their total.  Equal logits rank by index.  A sort is not needed: each filter is a threshold
-// on the logit (found by bisection on an order-preserving integer image, counting or summing what lies above)
-// plus the number of logits equal to it that still count.  Sums are held in 64 bits: the token is decided by
-// comparing long sums, and 32-bit ones over 128 256 weights would move a border in every few hundred rows.
-#include <cuda_bf16.h>
-#include <cuda_runtime.h>
+// exceeds u times their total.  Equal logits rank by index.
+//
+// A sort is not needed: each filter is a threshold on the logit plus the number of logits equal to it that still
+// count.  With I(x) an order-preserving integer image of the logit, a threshold is found on the distance
+// I(max) - I(x) by a search of 1024 intervals at a time (a histogram of counts in shared memory; integer counts, so the
+// order of the atomics does not matter): two or three levels instead of 32 bisections.  For top-p the counts give bounds of
+// the weight in every interval; the weight above the remaining range is summed exactly.
+//
+// All sums are held in 64 bits and added in an order that the row's length alone fixes: the token is decided by comparing long
+// sums, and 32-bit ones over 128 256 weights would move a border in every few hundred rows.  exp is a
+// 64-bit polynomial of degree 11 on [-1/2, 1/2] after reduction to a power of two (2e-14 of the value; the Taylor
+// coefficients ln 2^k / k!).
+//
+// Layout: one cluster of up to 16 CTAs per row, 512 threads each; the row is read once, into the shared memory of the
+// cluster, as images.  A thread owns an odd number of consecutive logits (conflict-free, and in index order).  CTAs exchange
+// partial results by writing to all peers' shared memory, one cluster barrier per exchange.
+#include <cmath>
 
-#include "kap_internal.h"
+#include "kap_ptx.cuh"
 
 namespace kap {
 void count_launch();
 
 namespace {
 
-constexpr int kSampleThreads = 1024;
+constexpr int kSampleThreads = 512;
+constexpr int kSampleWarps = kSampleThreads / 32;
+constexpr int kBins = 1024;
 constexpr uint32_t kImageMinusInf = 0x007fffffu;   // image of -inf; nothing at or below it has weight
+constexpr int kMaxRounds = 96;                     // of a search: at most 11 widths of interval, four windows each
+constexpr int kMaxStrip = 99;                      // logits a thread owns at most: 512 x 99 x 4 bytes of shared memory
 
-__device__ __forceinline__ uint32_t logit_image(float v) {          // NaN lowest, -0 = +0
+__device__ __forceinline__ uint32_t logit_image(float v) {          // NaN like -inf, -0 = +0
     const uint32_t u = __float_as_uint(v + 0.0f);
-    return v != v ? 0u : u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+    return v != v ? kImageMinusInf : u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ float image_logit(uint32_t u) {
     return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu));
 }
-__device__ __forceinline__ float load_logit(const float* x, int i) { return x[i]; }
-__device__ __forceinline__ float load_logit(const __nv_bfloat16* x, int i) { return __bfloat162float(x[i]); }
-
-// the sum (in a fixed order) over the block, in every thread
-template <typename V>
-__device__ V block_sum(V v, V* scratch) {
-    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = scratch[threadIdx.x & 31];
-    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    return v;
+// 2^t for t <= 0 in 64 bits; below the smallest normal number: 0
+__device__ __forceinline__ double exp2_f64(double t) {
+    if (!(t > -1022.0)) return 0.0;
+    const double n = rint(t), f = t - n;
+    double y = 4.4455382718708116e-10;              // ln 2^11 / 11!, and on to ln 2^0 / 0!
+    y = fma(y, f, 7.054911620801123e-09);
+    y = fma(y, f, 1.01780860092397e-07);
+    y = fma(y, f, 1.321548679014431e-06);
+    y = fma(y, f, 1.5252733804059841e-05);
+    y = fma(y, f, 0.0001540353039338161);
+    y = fma(y, f, 0.0013333558146428443);
+    y = fma(y, f, 0.009618129107628477);
+    y = fma(y, f, 0.05550410866482158);
+    y = fma(y, f, 0.24022650695910072);
+    y = fma(y, f, 0.6931471805599453);
+    y = fma(y, f, 1.0);
+    return __longlong_as_double(__double_as_longlong(y) + ((long long)(int)n << 52));
 }
 
 struct SampleParams {
     const void* logits;
     long long row_stride;
-    int32_t vocab;
+    int32_t vocab, slice, strip, cluster;          // logits of a row, of a CTA, of a thread; CTAs of a row
     const float *temperature, *top_p, *min_p, *uniform;
     const int32_t* top_k;
     int32_t* token;
     float* logprob;
 };
 
+struct SampleShared {
+    uint32_t hist[2][kBins];
+    // filled by all CTAs of the cluster, one entry each
+    unsigned long long best[kMaxCluster];
+    int32_t finite[kMaxCluster];
+    double level_sum[2][kMaxCluster], kept_sum[kMaxCluster];
+    int32_t ties[kMaxCluster];
+    // this CTA
+    double warp_d[kSampleWarps][2];
+    unsigned long long warp_u[kSampleWarps];
+    int32_t warp_i[kSampleWarps];
+    int32_t bin[2];
+    int32_t before[2];
+    uint32_t bin_count;
+    double edge;
+};
+
+__device__ __forceinline__ void put_remote(uint32_t addr, unsigned long long v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+__device__ __forceinline__ void put_remote(uint32_t addr, int32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void put_remote(uint32_t addr, double v) { put_remote(addr, (unsigned long long)__double_as_longlong(v)); }
+__device__ __forceinline__ uint32_t get_remote(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+    return v;
+}
+
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+
 template <typename T>
-__global__ void __launch_bounds__(kSampleThreads)
+__global__ void __launch_bounds__(kSampleThreads, 2)
 kap_sample_rows_kernel(const SampleParams p)
 {
-    __shared__ double scratch[33];
-    __shared__ double scan[kSampleThreads + 1];
-    __shared__ int tie_scan[kSampleThreads + 1];
-    __shared__ unsigned long long best;
-    const int r = blockIdx.x, tid = threadIdx.x, V = p.vocab;
-    const T* x = reinterpret_cast<const T*>(p.logits) + (long long)r * p.row_stride;
-    if (tid == 0) best = 0ull;
-    __syncthreads();
-    unsigned long long mine = 0ull;
-    for (int i = tid; i < V; i += kSampleThreads) {
-        const unsigned long long k = ((unsigned long long)logit_image(load_logit(x, i)) << 32) | (uint32_t)~i;
-        mine = k > mine ? k : mine;
+    extern __shared__ __align__(16) unsigned char smem[];
+    SampleShared& sh = *reinterpret_cast<SampleShared*>(smem);
+    uint32_t* const img = reinterpret_cast<uint32_t*>(smem + (sizeof(SampleShared) + 15) / 16 * 16);
+    const int C = p.cluster, r = blockIdx.x / C, rank = blockIdx.x % C, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int first = min(p.vocab, rank * p.slice), n = min(p.vocab, first + p.slice) - first;      // this CTA's logits
+    const T* x = reinterpret_cast<const T*>(p.logits) + (long long)r * p.row_stride + first;
+    const int room = p.strip * kSampleThreads;
+
+    auto to_all = [&](auto* slot, auto v) {                        // slot[rank] of every CTA's shared memory; threads 0 .. C - 1 call
+        put_remote(map_to_cta(smem_u32(slot + rank), tid), v);
+    };
+    auto meet = [&] { if (C > 1) cluster_sync(); else __syncthreads(); };
+
+    // ---- read the slice once; the row's largest logit (lowest index among equals) and how many logits have weight at all
+    unsigned long long best = 0ull;
+    int finite = 0;
+    auto take = [&](int i, float v) {
+        const uint32_t u = logit_image(v);
+        img[i] = u;
+        const unsigned long long k = ((unsigned long long)u << 32) | (uint32_t)~(first + i);
+        best = k > best ? k : best;
+        finite += u > kImageMinusInf;
+    };
+    constexpr int kVec = 16 / (int)sizeof(T);
+    const int head = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / sizeof(T)));
+    const int n_vec = (n - head) / kVec;
+    for (int i = tid; i < head; i += kSampleThreads) take(i, as_float(x[i]));
+    constexpr int kInFlight = 4;
+    for (int j0 = tid; j0 < n_vec; j0 += kInFlight * kSampleThreads) {
+        uint4 v[kInFlight];
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u)
+            if (j0 + u * kSampleThreads < n_vec) v[u] = __ldcs(reinterpret_cast<const uint4*>(x + head) + j0 + u * kSampleThreads);
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u)
+            if (j0 + u * kSampleThreads < n_vec) {
+                const T* e = reinterpret_cast<const T*>(&v[u]);
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) take(head + (j0 + u * kSampleThreads) * kVec + k, as_float(e[k]));
+            }
     }
-    atomicMax(&best, mine);
-    __syncthreads();
+    for (int i = head + n_vec * kVec + tid; i < n; i += kSampleThreads) take(i, as_float(x[i]));
+    for (int i = n + tid; i < room; i += kSampleThreads) img[i] = 0u;
+    for (int i = tid; i < 2 * kBins; i += kSampleThreads) (&sh.hist[0][0])[i] = 0u;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        const unsigned long long o = __shfl_xor_sync(0xffffffffu, best, d);
+        best = o > best ? o : best;
+        finite += __shfl_xor_sync(0xffffffffu, finite, d);
+    }
+    if (lane == 0) { sh.warp_u[warp] = best; sh.warp_i[warp] = finite; }
+    if (C > 1) cluster_sync(); else __syncthreads();               // (and every peer runs before anybody writes to it)
+    if (tid < C) {
+        best = 0ull; finite = 0;
+        for (int w = 0; w < kSampleWarps; ++w) { best = sh.warp_u[w] > best ? sh.warp_u[w] : best; finite += sh.warp_i[w]; }
+        to_all(sh.best, best);
+        to_all(sh.finite, finite);
+    }
+    meet();
+    best = 0ull; finite = 0;
+    for (int c = 0; c < C; ++c) { best = sh.best[c] > best ? sh.best[c] : best; finite += sh.finite[c]; }
     const uint32_t top = (uint32_t)(best >> 32);
-    const int top_index = (int)~(uint32_t)best;
     const float t = p.temperature ? p.temperature[r] : 1.f;
-    if (top <= kImageMinusInf || !(t > 0.f)) {                    // no token at all / greedy
-        if (tid == 0) {
+    if (top <= kImageMinusInf || !(t > 0.f)) {                     // no token at all / greedy
+        if (rank == 0 && tid == 0) {
             const bool none = top <= kImageMinusInf;
-            p.token[r] = none ? -1 : top_index;
+            p.token[r] = none ? -1 : (int)~(uint32_t)best;
             if (p.logprob) p.logprob[r] = none ? -INFINITY : 0.f;
         }
         return;
     }
-    const double x_max = (double)image_logit(top), td = (double)t;
-    auto scaled = [&](uint32_t img) { return img == top ? 0.0 : ((double)image_logit(img) - x_max) / td; };
-    auto weight = [&](uint32_t img) { return img <= kImageMinusInf ? 0.0 : exp(scaled(img)); };
+    const double x_max = (double)image_logit(top), per_bit = 1.4426950408889634 / (double)t;
+    // weights by distance d = top - image: 2^((x - max) / T / ln 2)
+    auto log2_weight = [&](uint32_t d) { return d == 0 ? 0.0 : ((double)image_logit(top - d) - x_max) * per_bit; };
+    auto weight = [&](uint32_t d) { return top - d <= kImageMinusInf ? 0.0 : exp2_f64(log2_weight(d)); };
+    auto distance = [&](uint32_t u) { return top - u; };
+    const uint32_t* const mine = img + tid * p.strip;
 
-    // the threshold (image, how many equal to it count) of top-k
-    uint32_t cut = 0;                                             // everything above it counts ...
-    int quota = V;                                                // ... and so many equal to it, lowest index first
-    const int k = p.top_k ? p.top_k[r] : 0;
-    if (k > 0 && k < V) {
-        for (int bit = 31; bit >= 0; --bit) {                     // the largest image with at least k at or above it
-            const uint32_t c = cut | (1u << bit);
-            int n = 0;
-            for (int i = tid; i < V; i += kSampleThreads) n += logit_image(load_logit(x, i)) >= c;
-            if (block_sum<int>(n, (int*)scratch) >= k) cut = c;
-        }
-        int above = 0;
-        for (int i = tid; i < V; i += kSampleThreads) above += logit_image(load_logit(x, i)) > cut;
-        quota = k - block_sum<int>(above, (int*)scratch);
-    }
-    auto sum_above = [&](uint32_t c) {                            // weight strictly above the image c
-        double s = 0.0;
-        for (int i = tid; i < V; i += kSampleThreads) {
-            const uint32_t u = logit_image(load_logit(x, i));
-            if (u > c) s += weight(u);
-        }
-        return block_sum<double>(s, scratch);
+    // sum over the block in a fixed order, in every thread
+    auto block_sum = [&](double v) {
+#pragma unroll
+        for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        __syncthreads();
+        if (lane == 0) sh.warp_d[warp][0] = v;
+        __syncthreads();
+        v = 0.0;
+        for (int w = 0; w < kSampleWarps; ++w) v += sh.warp_d[w][0];
+        return v;
     };
+    int level = 0;                                                 // of all searches of the row: parity selects the buffers
+    // One level: counts of the distances base + [b << shift, (b + 1) << shift) over the whole row, two bins a thread; `partial` is
+    // summed over the row along the way.
+    auto count_level = [&](uint64_t base, int shift, double partial, uint32_t (&bins)[2]) {
+        const int buf = level & 1;
+        for (int i = 0; i < p.strip; ++i) {
+            const uint64_t d = (uint64_t)distance(mine[i]) - base;
+            if (mine[i] > kImageMinusInf && distance(mine[i]) >= base && (d >> shift) < kBins) atomicAdd(&sh.hist[buf][d >> shift], 1u);
+        }
+        const double sum = block_sum(partial);
+        if (tid < C) to_all(sh.level_sum[buf], sum);
+        meet();
+        double total = 0.0;
+        for (int c = 0; c < C; ++c) total += sh.level_sum[buf][c];
+        bins[0] = bins[1] = 0u;
+        for (int c = 0; c < C; ++c) {
+            const uint32_t at = map_to_cta(smem_u32(&sh.hist[buf][2 * tid]), c);
+            bins[0] += get_remote(at);
+            bins[1] += get_remote(at + 4);
+        }
+        // the other buffer was last read before this barrier: clear it for the next level
+        sh.hist[buf ^ 1][2 * tid] = 0u; sh.hist[buf ^ 1][2 * tid + 1] = 0u;
+        ++level;
+        return total;
+    };
+
+    // The cut: distances below it are kept, and `quota` of those equal to it (lowest index first).
+    uint32_t cut = 0xffffffffu;
+    int quota = 0x7fffffff, ties_at_cut = 0;
+    const int k = p.top_k ? p.top_k[r] : 0;
+    if (k > 0 && k < finite) {
+        uint64_t base = 0;
+        int shift = 14, above = 0;                                 // two octaves below the largest logit at first
+        for (int rounds = 0; rounds < kMaxRounds; ++rounds) {      // (ends by itself; the bound is for a mistake in this argument)
+            uint32_t bins[2];
+            count_level(base, shift, 0.0, bins);
+            // inclusive running count; the bin in which the k-th falls
+            const int both = (int)(bins[0] + bins[1]);
+            int run = both;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, run, d); if (lane >= d) run += o; }
+            if (lane == 31) sh.warp_i[warp] = run;
+            if (tid == 0) sh.bin[0] = -1;
+            __syncthreads();
+            int total = 0;
+            for (int w = 0; w < kSampleWarps; ++w) { if (w < warp) run += sh.warp_i[w]; total += sh.warp_i[w]; }
+            const int start = above + run - both;                  // before this thread's first bin
+            if (start < k && above + run >= k) {
+                const bool second = start + (int)bins[0] < k;
+                sh.bin[0] = 2 * tid + second;
+                sh.before[0] = start + (second ? (int)bins[0] : 0);
+                sh.bin_count = bins[second ? 1 : 0];
+            }
+            __syncthreads();
+            const int b = sh.bin[0];
+            if (b < 0) {                                           // further down: wider bins
+                above += total;
+                base += (uint64_t)kBins << shift;
+                shift = min(shift + 3, 22);
+                __syncthreads();
+                continue;
+            }
+            above = sh.before[0];
+            const int in_bin = (int)sh.bin_count;
+            base += (uint64_t)b << shift;
+            __syncthreads();
+            if (above + in_bin == k) { cut = (uint32_t)min(base + ((uint64_t)1 << shift) - 1, (uint64_t)0xffffffffu); break; }     // the whole bin
+            if (shift == 0) { cut = (uint32_t)base; quota = k - above; ties_at_cut = in_bin; break; }
+            shift = max(0, shift - 10);
+        }
+    }
+
     const float top_p = p.top_p ? p.top_p[r] : 1.f;
     if (top_p < 1.f) {
-        int ties = 0;
-        for (int i = tid; i < V; i += kSampleThreads) ties += logit_image(load_logit(x, i)) == cut;
-        ties = min(block_sum<int>(ties, (int*)scratch), quota);
-        const double target = (double)top_p * (sum_above(cut) + ties * weight(cut));
-        // the smallest image, not below the present cut, such that less than the target lies above it
-        uint32_t lo = cut, hi = top;                              // sum_above(top) = 0 < target, or top alone stays
-        while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (sum_above(mid) < target) hi = mid; else lo = mid + 1;
+        // the threshold lies where weights still matter: N exp(-R / T) < 1 - p leaves less than 1 - p of the whole behind R
+        const double reach = (double)t * (log((double)p.vocab) - log(1.0 - fmax((double)top_p, 0.0))) * (1.0 + 1e-9) + 1e-30;
+        const uint32_t far = logit_image(__double2float_rd(x_max - reach));
+        const uint32_t last = min(far < top ? top - far : 0u, cut);
+        auto shift_for = [&](uint64_t range) { int s = 0; while (((range - 1) >> s) >= kBins) ++s; return s; };
+        int shift = shift_for((uint64_t)last + 1);
+        uint64_t base = 0;
+        double part = 0.0;                                         // the whole: weights of everything kept so far
+        for (int i = 0; i < p.strip; ++i) {
+            const uint32_t d = distance(mine[i]);
+            if (mine[i] > kImageMinusInf && (d < cut || (d == cut && quota == 0x7fffffff))) part += weight(d);
         }
-        const double w = weight(lo), left = target - sum_above(lo);
-        const int most = lo == cut ? quota : V;
-        const double n = w > 0.0 ? ceil(left / w) : (double)most;
-        quota = n < 1.0 ? 1 : n < (double)most ? (int)n : most;
-        cut = lo;
-    }
-    const float min_p = p.min_p ? p.min_p[r] : 0.f;
-    const double floor_z = min_p > 0.f ? log((double)min_p) : -INFINITY;
-
-    // running sums in vocabulary order: thread t owns a contiguous strip
-    const int per = (V + kSampleThreads - 1) / kSampleThreads;
-    const int i0 = min(V, tid * per), i1 = min(V, i0 + per);
-    int ties = 0;
-    for (int i = i0; i < i1; ++i) ties += logit_image(load_logit(x, i)) == cut;
-    tie_scan[tid + 1] = ties;
-    __syncthreads();
-    if (tid == 0) {
-        tie_scan[0] = 0;
-        for (int j = 1; j <= kSampleThreads; ++j) tie_scan[j] += tie_scan[j - 1];
-    }
-    __syncthreads();
-    // sum of the strip's kept weights; *found: the first index past the target, or (the same sum in another
-    // order may fall a rounding short of it) the last one with weight
-    auto walk = [&](double from, double target, int* found) {
-        int rank = tie_scan[tid];
-        for (int i = i0; i < i1; ++i) {
-            const uint32_t u = logit_image(load_logit(x, i));
-            const bool in = u > cut || (u == cut && rank++ < quota);
-            if (!in || u <= kImageMinusInf || !(scaled(u) >= floor_z)) continue;
-            const double w = weight(u);
-            from += w;
-            if (found && w > 0.0) {
-                *found = i;
-                if (from > target) return from;
+        double target = 0.0, above = 0.0;                          // p times the whole; weight of distances below base
+        const double cut_part = quota == 0x7fffffff ? 0.0 : (double)quota * weight(cut);
+        for (int rounds = 0; rounds < kMaxRounds; ++rounds) {
+            uint32_t bins[2];
+            const double sum = count_level(base, shift, part, bins);
+            if (rounds == 0) target = (double)top_p * (sum + cut_part); else above += sum;
+            double lo[2], hi[2];                                   // bounds of the weight in this thread's two bins
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint64_t from = base + ((uint64_t)(2 * tid + e) << shift), to = from + ((uint64_t)1 << shift) - 1;
+                int c = (int)bins[e];
+                if (from > cut) c = 0;
+                else if (quota != 0x7fffffff && cut <= to) c -= ties_at_cut - quota;   // of the equal ones only some are left
+                // (a bin that holds the cut may hold distances behind it as well: its bounds are too high then, but the
+                // threshold does not lie behind it, whatever they say)
+                bins[e] = (uint32_t)max(c, 0);
+                lo[e] = c > 0 ? c * weight((uint32_t)min(to, (uint64_t)(top - kImageMinusInf - 1u))) : 0.0;
+                hi[e] = c > 0 ? (shift == 0 ? lo[e] : c * weight((uint32_t)from)) : 0.0;
             }
+            double run_lo = lo[0] + lo[1], run_hi = hi[0] + hi[1];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const double a = __shfl_up_sync(0xffffffffu, run_lo, d), b = __shfl_up_sync(0xffffffffu, run_hi, d);
+                if (lane >= d) { run_lo += a; run_hi += b; }
+            }
+            __syncthreads();
+            if (lane == 31) { sh.warp_d[warp][0] = run_lo; sh.warp_d[warp][1] = run_hi; }
+            if (tid == 0) sh.bin[0] = sh.bin[1] = kBins;
+            __syncthreads();
+            double before_lo = above, before_hi = above;
+            for (int w = 0; w < warp; ++w) { before_lo += sh.warp_d[w][0]; before_hi += sh.warp_d[w][1]; }
+            run_lo += before_lo; run_hi += before_hi;
+            // the first bin whose end may reach the target and the first one whose end must; at single distances the sums are exact
+            const double slack = shift == 0 ? 0.0 : 1e-12 * target;
+            const double mid_lo = run_lo - lo[1], mid_hi = run_hi - hi[1];
+            if (bins[0] && mid_hi >= target - slack) atomicMin(&sh.bin[0], 2 * tid);
+            else if (bins[1] && run_hi >= target - slack) atomicMin(&sh.bin[0], 2 * tid + 1);
+            if (bins[0] && mid_lo >= target + slack) atomicMin(&sh.bin[1], 2 * tid);
+            else if (bins[1] && run_lo >= target + slack) atomicMin(&sh.bin[1], 2 * tid + 1);
+            __syncthreads();
+            const int b1 = sh.bin[0], b2 = sh.bin[1];
+            if (b1 < kBins && (b1 >> 1) == tid) {                  // weight before it, and how many logits it holds
+                const int e = b1 & 1;
+                sh.edge = e ? mid_lo : mid_lo - lo[0];
+                sh.bin_count = bins[e];
+            }
+            __syncthreads();
+            const int in_bin = (int)sh.bin_count;
+            const double edge = sh.edge;
+            uint64_t next;
+            if (b1 == kBins) {                                     // not within this window: on to the next one
+                next = base + ((uint64_t)kBins << shift);
+                if (next > last) {                                 // (a rounding short of the end: all that there is)
+                    if (last < cut) { cut = last; quota = 0x7fffffff; }
+                    break;
+                }
+            } else if (shift == 0) {
+                const uint32_t d = (uint32_t)(base + (uint64_t)b1);
+                const double w = weight(d), m = w > 0.0 ? ceil((target - edge) / w) : 1.0;
+                const int keep = m < 1.0 ? 1 : m < (double)in_bin ? (int)m : in_bin;
+                const bool all = keep == in_bin && !(d == cut && quota != 0x7fffffff);
+                if (d != cut || quota == 0x7fffffff) ties_at_cut = in_bin;
+                quota = all ? 0x7fffffff : keep;
+                cut = d;
+                break;
+            } else {
+                next = base + ((uint64_t)b1 << shift);
+                const uint64_t end = next + ((uint64_t)1 << shift) - 1;
+                if (b1 == b2 && in_bin == 1 && end < cut) {        // the one logit in it belongs to the prefix
+                    cut = (uint32_t)end;
+                    quota = 0x7fffffff;
+                    break;
+                }
+            }
+            // what lies between the old base and the new one is above the range from now on
+            part = 0.0;
+            for (int i = 0; i < p.strip; ++i) {
+                const uint32_t d = distance(mine[i]);
+                if (mine[i] > kImageMinusInf && d >= base && d < next) part += weight(d);
+            }
+            base = next;
+            // finer by at least two bits, so that the search ends; windows that do not cover the range follow one another
+            if (b1 < kBins) shift = max(0, min(shift - 2, b2 < kBins ? shift_for((uint64_t)(b2 - b1 + 1) << shift) : shift));
         }
-        return from;
+    }
+
+    // ---- the draw: running sums in index order over threads, CTAs, and then inside one thread's strip
+    const float min_p = p.min_p ? p.min_p[r] : 0.f;
+    const double least = min_p > 0.f ? x_max + (double)t * log((double)min_p) : -INFINITY;
+    int tie_rank = 0;                                              // equal ones before this thread's strip
+    if (quota != 0x7fffffff) {
+        int ties = 0;
+        for (int i = 0; i < p.strip; ++i) ties += distance(mine[i]) == cut;
+        int run = ties;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, run, d); if (lane >= d) run += o; }
+        __syncthreads();
+        if (lane == 31) sh.warp_i[warp] = run;
+        __syncthreads();
+        int total = 0;
+        for (int w = 0; w < kSampleWarps; ++w) { if (w < warp) run += sh.warp_i[w]; total += sh.warp_i[w]; }
+        if (tid < C) to_all(sh.ties, total);
+        meet();
+        tie_rank = run - ties;
+        for (int c = 0; c < rank; ++c) tie_rank += sh.ties[c];
+    }
+    auto kept = [&](uint32_t u, int& rank_of_tie) {
+        const uint32_t d = distance(u);
+        if (u <= kImageMinusInf || d > cut) return false;
+        if (d == cut && quota != 0x7fffffff && rank_of_tie++ >= quota) return false;
+        return min_p > 0.f ? (double)image_logit(u) >= least : true;
     };
-    scan[tid + 1] = walk(0.0, 0.0, nullptr);
-    __syncthreads();
-    if (tid == 0) {
-        scan[0] = 0.0;
-        for (int j = 1; j <= kSampleThreads; ++j) scan[j] += scan[j - 1];
+    double sum = 0.0;
+    {
+        int tr = tie_rank;
+        for (int i = 0; i < p.strip; ++i)
+            if (kept(mine[i], tr)) sum += weight(distance(mine[i]));
+    }
+    // Running sums one after the other, so that a thread without weight ends exactly where the one before it does, and the end of a
+    // warp or a CTA is the same number as the start of the next: one thread, with weight, holds the target.
+    double run = 0.0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const double s = __shfl_sync(0xffffffffu, sum, j);
+        if (lane >= j) run += s;
     }
     __syncthreads();
-    const double total = scan[kSampleThreads];
+    if (lane == 31) sh.warp_d[warp][0] = run;
+    __syncthreads();
+    double block = 0.0, offset = 0.0;
+    for (int w = 0; w < kSampleWarps; ++w) { if (w == warp) offset = block; block += sh.warp_d[w][0]; }
+    if (tid < C) to_all(sh.kept_sum, block);
+    meet();
+    double total = 0.0, before = 0.0, cta_end = 0.0;
+    for (int c = 0; c < C; ++c) { if (c == rank) before = total; total += sh.kept_sum[c]; if (c == rank) cta_end = total; }
     const double u01 = (double)p.uniform[r];
     const double target = u01 >= 0.0 ? fmin(u01 * total, total * 0.99999999999999978) : 0.0;
-    if (scan[tid] <= target && scan[tid + 1] > target) {
-        int found = -1;
-        walk(scan[tid], target, &found);
-        p.token[r] = found;
-        if (p.logprob) p.logprob[r] = (float)(scaled(logit_image(load_logit(x, found))) - log(total));
+    if (!(before <= target && target < cta_end)) return;           // another CTA's (no remote access from here on)
+    const double inner = offset + run, prev = __shfl_up_sync(0xffffffffu, inner, 1);
+    const double start = before + (lane == 0 ? offset : prev), end = before + inner;
+    if (start <= target && target < end) {
+        double at = start;
+        int found = -1, tr = tie_rank;
+        for (int i = 0; i < p.strip; ++i) {
+            if (!kept(mine[i], tr)) continue;
+            const double w = weight(distance(mine[i]));
+            at += w;
+            if (w > 0.0) {                                         // (the same sum in another order may fall a rounding short: the last one then)
+                found = i;
+                if (at > target) break;
+            }
+        }
+        p.token[r] = first + tid * p.strip + found;
+        if (p.logprob) p.logprob[r] = (float)((log2_weight(distance(mine[found])) - log2(total)) * 0.69314718055994531);
     }
 }
 
@@ -190,16 +453,39 @@ extern "C" kap_status kap_sample_tokens(
         return fail(KAP_ERR_UNSUPPORTED, "logits_type %d (KAP_LOGITS_F32 = 0, KAP_LOGITS_BF16 = 1)", logits_type);
     if (rows < 0 || vocab < 1 || row_stride < vocab)
         return fail(KAP_ERR_INVALID_ARG, "rows %d, vocab %d, row_stride %lld", rows, vocab, (long long)row_stride);
+    constexpr int kMost = kMaxCluster * kSampleThreads * kMaxStrip;
+    if (vocab > kMost) return fail(KAP_ERR_UNSUPPORTED, "vocab %d (at most %d: a row stays in a cluster's shared memory)", vocab, kMost);
     if (rows == 0) return KAP_OK;
     if (!logits || !uniform || !token) return fail(KAP_ERR_INVALID_ARG, "NULL pointer");
     if (reinterpret_cast<uintptr_t>(logits) & (logits_type == KAP_LOGITS_F32 ? 3 : 1))
         return fail(KAP_ERR_INVALID_ARG, "logits are not aligned to their type");
-    SampleParams p{logits, row_stride, vocab, temperature, top_p, min_p, uniform, top_k, token, logprob};
-    if (logits_type == KAP_LOGITS_F32)
-        kap_sample_rows_kernel<float><<<(unsigned)rows, kSampleThreads, 0, (cudaStream_t)cuda_stream>>>(p);
-    else
-        kap_sample_rows_kernel<__nv_bfloat16><<<(unsigned)rows, kSampleThreads, 0, (cudaStream_t)cuda_stream>>>(p);
-    cudaError_t e = cudaGetLastError();
+    // CTAs of a row: as many as keep two CTAs on an SM (33 logits a thread), and more while there are SMs to spare
+    auto strip_of = [&](int c) { const int s = ((vocab + c - 1) / c + kSampleThreads - 1) / kSampleThreads; return s | 1; };
+    int C = 1;
+    while (C < kMaxCluster && strip_of(C) > 33) C *= 2;
+    while (C < kMaxCluster && strip_of(C) > 5 && (int64_t)rows * C * 2 <= 148) C *= 2;
+    SampleParams p{logits, row_stride, vocab, 0, strip_of(C), C, temperature, top_p, min_p, uniform, top_k, token, logprob};
+    p.slice = p.strip * kSampleThreads;
+    if (rows > 0x7fffffff / C) return fail(KAP_ERR_UNSUPPORTED, "%d rows", rows);
+    auto smem_for = [](int slice) { return (sizeof(SampleShared) + 15) / 16 * 16 + (size_t)slice * sizeof(uint32_t); };
+    static_assert((sizeof(SampleShared) + 15) / 16 * 16 + (size_t)kSampleThreads * kMaxStrip * 4 <= 232448, "more than 227 KiB of shared memory");
+    const void* fn = logits_type == KAP_LOGITS_F32 ? (const void*)kap_sample_rows_kernel<float> : (const void*)kap_sample_rows_kernel<__nv_bfloat16>;
+    // (attributes belong to the current device; setting them again costs less than a microsecond)
+    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_for(kSampleThreads * kMaxStrip));
+    if (e == cudaSuccess && C > 8) e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)rows * (unsigned)C);
+    cfg.blockDim = dim3(kSampleThreads);
+    cfg.dynamicSmemBytes = smem_for(p.slice);
+    cfg.stream = (cudaStream_t)cuda_stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = C > 1 ? 1 : 0;
+    if (e == cudaSuccess)
+        e = logits_type == KAP_LOGITS_F32 ? cudaLaunchKernelEx(&cfg, kap_sample_rows_kernel<float>, p)
+                                          : cudaLaunchKernelEx(&cfg, kap_sample_rows_kernel<__nv_bfloat16>, p);
     if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "kap_sample_tokens launch failed: %s", cudaGetErrorString(e));
     count_launch();
     return KAP_OK;
