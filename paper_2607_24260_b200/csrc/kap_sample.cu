@@ -13,8 +13,7 @@
 //
 // All sums are held in 64 bits and added in an order that the row's length alone fixes: the token is decided by comparing long
 // sums, and 32-bit ones over 128 256 weights would move a border in every few hundred rows.  exp is a
-// 64-bit polynomial of degree 11 on [-1/2, 1/2] after reduction to a power of two (2e-14 of the value; the Taylor
-// coefficients ln 2^k / k!).
+// 64-bit polynomial after reduction to a power of two (exp2_f64 below).
 //
 // Layout: one cluster of up to 16 CTAs per row, 512 threads each; the row is read once, into the shared memory of the
 // cluster, as images.  A thread owns an odd number of consecutive logits (conflict-free, and in index order).  CTAs exchange
@@ -42,23 +41,28 @@ __device__ __forceinline__ uint32_t logit_image(float v) {          // NaN like 
 __device__ __forceinline__ float image_logit(uint32_t u) {
     return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu));
 }
-// 2^t for t <= 0 in 64 bits; below the smallest normal number: 0
+// float -> double by moving bits: the conversion instruction runs at a quarter of the rate of these
+__device__ __forceinline__ double widen(float v) {
+    const uint32_t u = __float_as_uint(v), e = u & 0x7f800000u;
+    if (e == 0u || e == 0x7f800000u) return (double)v;                 // zero, subnormal, infinite
+    return __hiloint2double((int)((u & 0x80000000u) | (((u & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(u << 29));
+}
+// 2^t for t <= 0 in 64 bits; below the smallest normal number: 0.  t = n + f with |f| <= 1/2 (a sum with 1.5 2^52 holds n in its
+// low word), 2^f by the polynomial of degree 9 of least largest relative error there (1.3e-14; Remez exchange).
 __device__ __forceinline__ double exp2_f64(double t) {
-    if (!(t > -1022.0)) return 0.0;
-    const double n = rint(t), f = t - n;
-    double y = 4.4455382718708116e-10;              // ln 2^11 / 11!, and on to ln 2^0 / 0!
-    y = fma(y, f, 7.054911620801123e-09);
-    y = fma(y, f, 1.01780860092397e-07);
-    y = fma(y, f, 1.321548679014431e-06);
-    y = fma(y, f, 1.5252733804059841e-05);
-    y = fma(y, f, 0.0001540353039338161);
-    y = fma(y, f, 0.0013333558146428443);
-    y = fma(y, f, 0.009618129107628477);
-    y = fma(y, f, 0.05550410866482158);
-    y = fma(y, f, 0.24022650695910072);
-    y = fma(y, f, 0.6931471805599453);
-    y = fma(y, f, 1.0);
-    return __longlong_as_double(__double_as_longlong(y) + ((long long)(int)n << 52));
+    if ((uint32_t)__double2hiint(t) > 0xc08ff000u) return 0.0;         // t < -1022
+    const double s = t + 6755399441055744.0, f = t - (s - 6755399441055744.0);
+    double y = 1.0150336270671598e-07;
+    y = fma(y, f, 1.3259405604554393e-06);
+    y = fma(y, f, 1.5252984841153802e-05);
+    y = fma(y, f, 0.00015403434948094166);
+    y = fma(y, f, 0.0013333557617599588);
+    y = fma(y, f, 0.009618129192067212);
+    y = fma(y, f, 0.055504108668685645);
+    y = fma(y, f, 0.24022650695649653);
+    y = fma(y, f, 0.693147180559871);
+    y = fma(y, f, 1.0000000000000127);
+    return __hiloint2double(__double2hiint(y) + (__double2loint(s) << 20), __double2loint(y));
 }
 
 struct SampleParams {
@@ -95,9 +99,9 @@ __device__ __forceinline__ void put_remote(uint32_t addr, int32_t v) {
     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 __device__ __forceinline__ void put_remote(uint32_t addr, double v) { put_remote(addr, (unsigned long long)__double_as_longlong(v)); }
-__device__ __forceinline__ uint32_t get_remote(uint32_t addr) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+__device__ __forceinline__ uint2 get_remote(uint32_t addr) {
+    uint2 v;
+    asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
     return v;
 }
 
@@ -115,6 +119,7 @@ kap_sample_rows_kernel(const SampleParams p)
     const int first = min(p.vocab, rank * p.slice), n = min(p.vocab, first + p.slice) - first;      // this CTA's logits
     const T* x = reinterpret_cast<const T*>(p.logits) + (long long)r * p.row_stride + first;
     const int room = p.strip * kSampleThreads;
+    if (C > 1) cluster_arrive();                                   // (its wait: every peer runs before anybody writes to it)
 
     auto to_all = [&](auto* slot, auto v) {                        // slot[rank] of every CTA's shared memory; threads 0 .. C - 1 call
         put_remote(map_to_cta(smem_u32(slot + rank), tid), v);
@@ -159,7 +164,8 @@ kap_sample_rows_kernel(const SampleParams p)
         finite += __shfl_xor_sync(0xffffffffu, finite, d);
     }
     if (lane == 0) { sh.warp_u[warp] = best; sh.warp_i[warp] = finite; }
-    if (C > 1) cluster_sync(); else __syncthreads();               // (and every peer runs before anybody writes to it)
+    __syncthreads();
+    if (C > 1) cluster_wait();
     if (tid < C) {
         best = 0ull; finite = 0;
         for (int w = 0; w < kSampleWarps; ++w) { best = sh.warp_u[w] > best ? sh.warp_u[w] : best; finite += sh.warp_i[w]; }
@@ -181,7 +187,7 @@ kap_sample_rows_kernel(const SampleParams p)
     }
     const double x_max = (double)image_logit(top), per_bit = 1.4426950408889634 / (double)t;
     // weights by distance d = top - image: 2^((x - max) / T / ln 2)
-    auto log2_weight = [&](uint32_t d) { return d == 0 ? 0.0 : ((double)image_logit(top - d) - x_max) * per_bit; };
+    auto log2_weight = [&](uint32_t d) { return d == 0 ? 0.0 : (widen(image_logit(top - d)) - x_max) * per_bit; };
     auto weight = [&](uint32_t d) { return top - d <= kImageMinusInf ? 0.0 : exp2_f64(log2_weight(d)); };
     auto distance = [&](uint32_t u) { return top - u; };
     const uint32_t* const mine = img + tid * p.strip;
@@ -202,9 +208,10 @@ kap_sample_rows_kernel(const SampleParams p)
     // summed over the row along the way.
     auto count_level = [&](uint64_t base, int shift, double partial, uint32_t (&bins)[2]) {
         const int buf = level & 1;
+        const uint32_t from = (uint32_t)base;                      // (a search ends before its base passes 32 bits)
         for (int i = 0; i < p.strip; ++i) {
-            const uint64_t d = (uint64_t)distance(mine[i]) - base;
-            if (mine[i] > kImageMinusInf && distance(mine[i]) >= base && (d >> shift) < kBins) atomicAdd(&sh.hist[buf][d >> shift], 1u);
+            const uint32_t u = mine[i], d = top - u, b = (d - from) >> shift;
+            if (u > kImageMinusInf && d >= from && b < kBins) atomicAdd(&sh.hist[buf][b], 1u);
         }
         const double sum = block_sum(partial);
         if (tid < C) to_all(sh.level_sum[buf], sum);
@@ -212,10 +219,14 @@ kap_sample_rows_kernel(const SampleParams p)
         double total = 0.0;
         for (int c = 0; c < C; ++c) total += sh.level_sum[buf][c];
         bins[0] = bins[1] = 0u;
-        for (int c = 0; c < C; ++c) {
-            const uint32_t at = map_to_cta(smem_u32(&sh.hist[buf][2 * tid]), c);
-            bins[0] += get_remote(at);
-            bins[1] += get_remote(at + 4);
+        const uint32_t at = smem_u32(&sh.hist[buf][2 * tid]);
+        for (int c0 = 0; c0 < C; c0 += 4) {                        // four peers' counts under way together
+            uint2 v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = get_remote(map_to_cta(at, min(c0 + e, C - 1)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c0 + e < C) { bins[0] += v[e].x; bins[1] += v[e].y; }
         }
         // the other buffer was last read before this barrier: clear it for the next level
         sh.hist[buf ^ 1][2 * tid] = 0u; sh.hist[buf ^ 1][2 * tid + 1] = 0u;
@@ -393,7 +404,7 @@ kap_sample_rows_kernel(const SampleParams p)
         const uint32_t d = distance(u);
         if (u <= kImageMinusInf || d > cut) return false;
         if (d == cut && quota != 0x7fffffff && rank_of_tie++ >= quota) return false;
-        return min_p > 0.f ? (double)image_logit(u) >= least : true;
+        return min_p > 0.f ? widen(image_logit(u)) >= least : true;
     };
     double sum = 0.0;
     {
@@ -423,20 +434,34 @@ kap_sample_rows_kernel(const SampleParams p)
     if (!(before <= target && target < cta_end)) return;           // another CTA's (no remote access from here on)
     const double inner = offset + run, prev = __shfl_up_sync(0xffffffffu, inner, 1);
     const double start = before + (lane == 0 ? offset : prev), end = before + inner;
-    if (start <= target && target < end) {
-        double at = start;
-        int found = -1, tr = tie_rank;
-        for (int i = 0; i < p.strip; ++i) {
-            if (!kept(mine[i], tr)) continue;
-            const double w = weight(distance(mine[i]));
-            at += w;
-            if (w > 0.0) {                                         // (the same sum in another order may fall a rounding short: the last one then)
-                found = i;
-                if (at > target) break;
-            }
+    const uint32_t holder = __ballot_sync(0xffffffffu, start <= target && target < end);
+    if (!holder) return;
+    // the warp walks through the strip of the thread that holds the target, 32 logits at a time
+    const int who = __ffs(holder) - 1;
+    const uint32_t* const strip = img + (warp * 32 + who) * p.strip;
+    double at = __shfl_sync(0xffffffffu, start, who);
+    int ties_before = __shfl_sync(0xffffffffu, tie_rank, who), found = -1;
+    for (int i0 = 0; i0 < p.strip; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t u = i < p.strip ? strip[i] : 0u, d = distance(u);
+        const uint32_t tied = __ballot_sync(0xffffffffu, d == cut && quota != 0x7fffffff);
+        int my_rank = ties_before + __popc(tied & ((1u << lane) - 1u));
+        ties_before += __popc(tied);
+        const double w = kept(u, my_rank) ? weight(d) : 0.0;
+        double upto = at;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const double o = __shfl_sync(0xffffffffu, w, j);
+            if (lane >= j) upto += o;
         }
-        p.token[r] = first + tid * p.strip + found;
-        if (p.logprob) p.logprob[r] = (float)((log2_weight(distance(mine[found])) - log2(total)) * 0.69314718055994531);
+        const uint32_t weighed = __ballot_sync(0xffffffffu, w > 0.0), past = __ballot_sync(0xffffffffu, w > 0.0 && upto > target);
+        if (past) { found = i0 + __ffs(past) - 1; break; }
+        if (weighed) found = i0 + 31 - __clz(weighed);             // (the same sum in another order may fall a rounding short: the last one then)
+        at = __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (lane == 0) {
+        p.token[r] = first + (warp * 32 + who) * p.strip + found;
+        if (p.logprob) p.logprob[r] = (float)((log2_weight(distance(strip[found])) - log2(total)) * 0.69314718055994531);
     }
 }
 
