@@ -31,6 +31,7 @@ constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 1024;
 constexpr uint32_t kImageMinusInf = 0x007fffffu;   // image of -inf; nothing at or below it has weight
+constexpr uint32_t kImagePlusInf = 0xff800000u;
 constexpr int kMaxRounds = 96;                     // of a search: at most 11 widths of interval, four windows each
 constexpr int kMaxStrip = 99;                      // logits a thread owns at most: 512 x 99 x 4 bytes of shared memory
 
@@ -41,11 +42,12 @@ __device__ __forceinline__ uint32_t logit_image(float v) {          // NaN like 
 __device__ __forceinline__ float image_logit(uint32_t u) {
     return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu));
 }
-// float -> double by moving bits: the conversion instruction runs at a quarter of the rate of these
-__device__ __forceinline__ double widen(float v) {
-    const uint32_t u = __float_as_uint(v), e = u & 0x7f800000u;
-    if (e == 0u || e == 0x7f800000u) return (double)v;                 // zero, subnormal, infinite
-    return __hiloint2double((int)((u & 0x80000000u) | (((u & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(u << 29));
+// The logit of an image as a double, by moving bits (the conversion instruction runs at a quarter of the rate of these).  Subnormal
+// logits and zero come out within 2^-126 of themselves and +inf as 2^128; the order is kept.
+__device__ __forceinline__ double wide_logit(uint32_t u) {
+    const uint32_t flip = ~(uint32_t)((int)u >> 31);                    // all ones for a negative logit
+    const uint32_t mag = (u ^ flip) & 0x7fffffffu;
+    return __hiloint2double((int)(((mag >> 3) + 0x38000000u) | (flip & 0x80000000u)), (int)(mag << 29));
 }
 // 2^t for t <= 0 in 64 bits; below the smallest normal number: 0.  t = n + f with |f| <= 1/2 (a sum with 1.5 2^52 holds n in its
 // low word), 2^f by the polynomial of degree 9 of least largest relative error there (1.3e-14; Remez exchange).
@@ -78,13 +80,12 @@ struct SampleParams {
 struct SampleShared {
     uint32_t hist[2][kBins];
     // filled by all CTAs of the cluster, one entry each
-    unsigned long long best[kMaxCluster];
-    int32_t finite[kMaxCluster];
+    int32_t best[kMaxCluster], finite[kMaxCluster];
     double level_sum[2][kMaxCluster], kept_sum[kMaxCluster];
     int32_t ties[kMaxCluster];
     // this CTA
     double warp_d[kSampleWarps][2];
-    unsigned long long warp_u[kSampleWarps];
+    uint32_t warp_u[kSampleWarps];
     int32_t warp_i[kSampleWarps];
     int32_t bin[2];
     int32_t before[2];
@@ -114,7 +115,7 @@ kap_sample_rows_kernel(const SampleParams p)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     SampleShared& sh = *reinterpret_cast<SampleShared*>(smem);
-    uint32_t* const img = reinterpret_cast<uint32_t*>(smem + (sizeof(SampleShared) + 15) / 16 * 16);
+    uint32_t* const space = reinterpret_cast<uint32_t*>(smem + (sizeof(SampleShared) + 15) / 16 * 16);
     const int C = p.cluster, r = blockIdx.x / C, rank = blockIdx.x % C, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int first = min(p.vocab, rank * p.slice), n = min(p.vocab, first + p.slice) - first;      // this CTA's logits
     const T* x = reinterpret_cast<const T*>(p.logits) + (long long)r * p.row_stride + first;
@@ -126,20 +127,22 @@ kap_sample_rows_kernel(const SampleParams p)
     };
     auto meet = [&] { if (C > 1) cluster_sync(); else __syncthreads(); };
 
-    // ---- read the slice once; the row's largest logit (lowest index among equals) and how many logits have weight at all
-    unsigned long long best = 0ull;
-    int finite = 0;
-    auto take = [&](int i, float v) {
-        const uint32_t u = logit_image(v);
-        img[i] = u;
-        const unsigned long long k = ((unsigned long long)u << 32) | (uint32_t)~(first + i);
-        best = k > best ? k : best;
-        finite += u > kImageMinusInf;
-    };
+    // ---- read the slice once; the row's largest logit, and with top-k how many logits have weight at all
+    const int k = p.top_k ? p.top_k[r] : 0;
+    const bool counted = k > 0 && k < p.vocab;
     constexpr int kVec = 16 / (int)sizeof(T);
     const int head = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / sizeof(T)));
     const int n_vec = (n - head) / kVec;
-    for (int i = tid; i < head; i += kSampleThreads) take(i, as_float(x[i]));
+    uint32_t* const img = space + ((4 - head) & 3);                    // image `head` on a 16-byte boundary
+    uint32_t best = 0u;
+    int finite = 0;
+    auto image_of = [&](float v) {
+        const uint32_t u = logit_image(v);
+        best = max(best, u);
+        if (counted) finite += u > kImageMinusInf;
+        return u;
+    };
+    for (int i = tid; i < head; i += kSampleThreads) img[i] = image_of(as_float(x[i]));
     constexpr int kInFlight = 4;
     for (int j0 = tid; j0 < n_vec; j0 += kInFlight * kSampleThreads) {
         uint4 v[kInFlight];
@@ -150,48 +153,74 @@ kap_sample_rows_kernel(const SampleParams p)
         for (int u = 0; u < kInFlight; ++u)
             if (j0 + u * kSampleThreads < n_vec) {
                 const T* e = reinterpret_cast<const T*>(&v[u]);
+                uint4* to = reinterpret_cast<uint4*>(img + head + (j0 + u * kSampleThreads) * kVec);
 #pragma unroll
-                for (int k = 0; k < kVec; ++k) take(head + (j0 + u * kSampleThreads) * kVec + k, as_float(e[k]));
+                for (int q = 0; q < kVec / 4; ++q)
+                    to[q] = make_uint4(image_of(as_float(e[4 * q])), image_of(as_float(e[4 * q + 1])), image_of(as_float(e[4 * q + 2])), image_of(as_float(e[4 * q + 3])));
             }
     }
-    for (int i = head + n_vec * kVec + tid; i < n; i += kSampleThreads) take(i, as_float(x[i]));
+    for (int i = head + n_vec * kVec + tid; i < n; i += kSampleThreads) img[i] = image_of(as_float(x[i]));
     for (int i = n + tid; i < room; i += kSampleThreads) img[i] = 0u;
     for (int i = tid; i < 2 * kBins; i += kSampleThreads) (&sh.hist[0][0])[i] = 0u;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) {
-        const unsigned long long o = __shfl_xor_sync(0xffffffffu, best, d);
-        best = o > best ? o : best;
-        finite += __shfl_xor_sync(0xffffffffu, finite, d);
-    }
+    best = __reduce_max_sync(0xffffffffu, best);
+    finite = __reduce_add_sync(0xffffffffu, finite);
     if (lane == 0) { sh.warp_u[warp] = best; sh.warp_i[warp] = finite; }
     __syncthreads();
     if (C > 1) cluster_wait();
     if (tid < C) {
-        best = 0ull; finite = 0;
-        for (int w = 0; w < kSampleWarps; ++w) { best = sh.warp_u[w] > best ? sh.warp_u[w] : best; finite += sh.warp_i[w]; }
-        to_all(sh.best, best);
+        best = 0u; finite = 0;
+        for (int w = 0; w < kSampleWarps; ++w) { best = max(best, sh.warp_u[w]); finite += sh.warp_i[w]; }
+        to_all(sh.best, (int32_t)best);
         to_all(sh.finite, finite);
     }
     meet();
-    best = 0ull; finite = 0;
-    for (int c = 0; c < C; ++c) { best = sh.best[c] > best ? sh.best[c] : best; finite += sh.finite[c]; }
-    const uint32_t top = (uint32_t)(best >> 32);
+    uint32_t top = 0u;
+    finite = 0;
+    for (int c = 0; c < C; ++c) { top = max(top, (uint32_t)sh.best[c]); finite += sh.finite[c]; }
+    const uint32_t* const mine = img + tid * p.strip;
     const float t = p.temperature ? p.temperature[r] : 1.f;
-    if (top <= kImageMinusInf || !(t > 0.f)) {                     // no token at all / greedy
+    if (top <= kImageMinusInf) {                                       // no token at all
         if (rank == 0 && tid == 0) {
-            const bool none = top <= kImageMinusInf;
-            p.token[r] = none ? -1 : (int)~(uint32_t)best;
-            if (p.logprob) p.logprob[r] = none ? -INFINITY : 0.f;
+            p.token[r] = -1;
+            if (p.logprob) p.logprob[r] = -INFINITY;
         }
         return;
     }
-    const double x_max = (double)image_logit(top), per_bit = 1.4426950408889634 / (double)t;
-    // weights by distance d = top - image: 2^((x - max) / T / ln 2)
-    auto log2_weight = [&](uint32_t d) { return d == 0 ? 0.0 : (widen(image_logit(top - d)) - x_max) * per_bit; };
-    auto weight = [&](uint32_t d) { return top - d <= kImageMinusInf ? 0.0 : exp2_f64(log2_weight(d)); };
-    auto distance = [&](uint32_t u) { return top - u; };
-    const uint32_t* const mine = img + tid * p.strip;
+    if (!(t > 0.f)) {                                                  // greedy: the first CTA with a largest logit, the first place in it
+        int c = 0;
+        while ((uint32_t)sh.best[c] != top) ++c;
+        if (c != rank) return;
+        int at = 0x7fffffff;
+        for (int i = p.strip - 1; i >= 0; --i)
+            if (mine[i] == top) at = tid * p.strip + i;
+        at = __reduce_min_sync(0xffffffffu, at);
+        __syncthreads();
+        if (lane == 0) sh.warp_i[warp] = at;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 1; w < kSampleWarps; ++w) at = min(at, sh.warp_i[w]);
+            p.token[r] = first + at;
+            if (p.logprob) p.logprob[r] = 0.f;
+        }
+        return;
+    }
+    const double x_max = wide_logit(top), per_bit = 1.4426950408889634 / (double)t;
+    // logarithm of a weight and the weight: 2^((x - max) / T / ln 2)
+    auto log2_weight = [&](uint32_t u) { return (wide_logit(u) - x_max) * per_bit; };
+    auto weight = [&](uint32_t u) { return exp2_f64(log2_weight(u)); };
+    // weights of the distances from .. from + span - 1 in this thread's strip
+    auto strip_weight = [&](uint32_t from, uint32_t span) {
+        const uint32_t high = top - from;
+        double s = 0.0;
+#pragma unroll 3
+        for (int i = 0; i < p.strip; ++i) {
+            const uint32_t u = mine[i];
+            if (high - u < span) s += weight(u);
+        }
+        return s;
+    };
 
+    const uint32_t furthest = top == kImagePlusInf ? 0u : top - kImageMinusInf - 1u;
     // sum over the block in a fixed order, in every thread
     auto block_sum = [&](double v) {
 #pragma unroll
@@ -208,10 +237,12 @@ kap_sample_rows_kernel(const SampleParams p)
     // summed over the row along the way.
     auto count_level = [&](uint64_t base, int shift, double partial, uint32_t (&bins)[2]) {
         const int buf = level & 1;
-        const uint32_t from = (uint32_t)base;                      // (a search ends before its base passes 32 bits)
+        // (a search ends before its base passes the last distance that has weight)
+        const uint32_t high = top - (uint32_t)base, span = (uint32_t)min((uint64_t)kBins << shift, (uint64_t)furthest + 1 - base);
+#pragma unroll 3
         for (int i = 0; i < p.strip; ++i) {
-            const uint32_t u = mine[i], d = top - u, b = (d - from) >> shift;
-            if (u > kImageMinusInf && d >= from && b < kBins) atomicAdd(&sh.hist[buf][b], 1u);
+            const uint32_t d = high - mine[i];
+            if (d < span) atomicAdd(&sh.hist[buf][d >> shift], 1u);
         }
         const double sum = block_sum(partial);
         if (tid < C) to_all(sh.level_sum[buf], sum);
@@ -234,11 +265,11 @@ kap_sample_rows_kernel(const SampleParams p)
         return total;
     };
 
-    // The cut: distances below it are kept, and `quota` of those equal to it (lowest index first).
-    uint32_t cut = 0xffffffffu;
+    // The cut: distances below it are kept, and `quota` of those equal to it (lowest index first).  At first all that have weight:
+    // behind +inf nothing has.
+    uint32_t cut = furthest;
     int quota = 0x7fffffff, ties_at_cut = 0;
-    const int k = p.top_k ? p.top_k[r] : 0;
-    if (k > 0 && k < finite) {
+    if (counted && k < finite) {
         uint64_t base = 0;
         int shift = 14, above = 0;                                 // two octaves below the largest logit at first
         for (int rounds = 0; rounds < kMaxRounds; ++rounds) {      // (ends by itself; the bound is for a mistake in this argument)
@@ -268,13 +299,14 @@ kap_sample_rows_kernel(const SampleParams p)
                 base += (uint64_t)kBins << shift;
                 shift = min(shift + 3, 22);
                 __syncthreads();
+                if (base > furthest) break;                        // (fewer than k at +inf: they are all that has weight)
                 continue;
             }
             above = sh.before[0];
             const int in_bin = (int)sh.bin_count;
             base += (uint64_t)b << shift;
             __syncthreads();
-            if (above + in_bin == k) { cut = (uint32_t)min(base + ((uint64_t)1 << shift) - 1, (uint64_t)0xffffffffu); break; }     // the whole bin
+            if (above + in_bin == k) { cut = (uint32_t)min(base + ((uint64_t)1 << shift) - 1, (uint64_t)furthest); break; }     // the whole bin
             if (shift == 0) { cut = (uint32_t)base; quota = k - above; ties_at_cut = in_bin; break; }
             shift = max(0, shift - 10);
         }
@@ -289,13 +321,9 @@ kap_sample_rows_kernel(const SampleParams p)
         auto shift_for = [&](uint64_t range) { int s = 0; while (((range - 1) >> s) >= kBins) ++s; return s; };
         int shift = shift_for((uint64_t)last + 1);
         uint64_t base = 0;
-        double part = 0.0;                                         // the whole: weights of everything kept so far
-        for (int i = 0; i < p.strip; ++i) {
-            const uint32_t d = distance(mine[i]);
-            if (mine[i] > kImageMinusInf && (d < cut || (d == cut && quota == 0x7fffffff))) part += weight(d);
-        }
+        double part = strip_weight(0u, quota == 0x7fffffff ? cut + 1u : cut);   // the whole: everything kept so far
         double target = 0.0, above = 0.0;                          // p times the whole; weight of distances below base
-        const double cut_part = quota == 0x7fffffff ? 0.0 : (double)quota * weight(cut);
+        const double cut_part = quota == 0x7fffffff ? 0.0 : (double)quota * weight(top - cut);
         for (int rounds = 0; rounds < kMaxRounds; ++rounds) {
             uint32_t bins[2];
             const double sum = count_level(base, shift, part, bins);
@@ -310,8 +338,8 @@ kap_sample_rows_kernel(const SampleParams p)
                 // (a bin that holds the cut may hold distances behind it as well: its bounds are too high then, but the
                 // threshold does not lie behind it, whatever they say)
                 bins[e] = (uint32_t)max(c, 0);
-                lo[e] = c > 0 ? c * weight((uint32_t)min(to, (uint64_t)(top - kImageMinusInf - 1u))) : 0.0;
-                hi[e] = c > 0 ? (shift == 0 ? lo[e] : c * weight((uint32_t)from)) : 0.0;
+                lo[e] = c > 0 ? c * weight(top - (uint32_t)min(to, (uint64_t)furthest)) : 0.0;
+                hi[e] = c > 0 ? (shift == 0 ? lo[e] : c * weight(top - (uint32_t)from)) : 0.0;
             }
             double run_lo = lo[0] + lo[1], run_hi = hi[0] + hi[1];
 #pragma unroll
@@ -352,7 +380,7 @@ kap_sample_rows_kernel(const SampleParams p)
                 }
             } else if (shift == 0) {
                 const uint32_t d = (uint32_t)(base + (uint64_t)b1);
-                const double w = weight(d), m = w > 0.0 ? ceil((target - edge) / w) : 1.0;
+                const double w = weight(top - d), m = w > 0.0 ? ceil((target - edge) / w) : 1.0;
                 const int keep = m < 1.0 ? 1 : m < (double)in_bin ? (int)m : in_bin;
                 const bool all = keep == in_bin && !(d == cut && quota != 0x7fffffff);
                 if (d != cut || quota == 0x7fffffff) ties_at_cut = in_bin;
@@ -369,11 +397,7 @@ kap_sample_rows_kernel(const SampleParams p)
                 }
             }
             // what lies between the old base and the new one is above the range from now on
-            part = 0.0;
-            for (int i = 0; i < p.strip; ++i) {
-                const uint32_t d = distance(mine[i]);
-                if (mine[i] > kImageMinusInf && d >= base && d < next) part += weight(d);
-            }
+            part = strip_weight((uint32_t)base, (uint32_t)(next - base));
             base = next;
             // finer by at least two bits, so that the search ends; windows that do not cover the range follow one another
             if (b1 < kBins) shift = max(0, min(shift - 2, b2 < kBins ? shift_for((uint64_t)(b2 - b1 + 1) << shift) : shift));
@@ -381,12 +405,16 @@ kap_sample_rows_kernel(const SampleParams p)
     }
 
     // ---- the draw: running sums in index order over threads, CTAs, and then inside one thread's strip
-    const float min_p = p.min_p ? p.min_p[r] : 0.f;
-    const double least = min_p > 0.f ? x_max + (double)t * log((double)min_p) : -INFINITY;
+    const float min_p = p.min_p ? fminf(p.min_p[r], 1.f) : 0.f;
+    if (min_p > 0.f) {                                             // a cut of its own: logits from the least float with weight enough on
+        const uint32_t least = logit_image(__double2float_ru(x_max + (double)t * log((double)min_p)));
+        const uint32_t d = least < top ? top - least : 0u;
+        if (d < cut) { cut = d; quota = 0x7fffffff; }
+    }
     int tie_rank = 0;                                              // equal ones before this thread's strip
     if (quota != 0x7fffffff) {
         int ties = 0;
-        for (int i = 0; i < p.strip; ++i) ties += distance(mine[i]) == cut;
+        for (int i = 0; i < p.strip; ++i) ties += mine[i] == top - cut;
         int run = ties;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, run, d); if (lane >= d) run += o; }
@@ -400,17 +428,17 @@ kap_sample_rows_kernel(const SampleParams p)
         tie_rank = run - ties;
         for (int c = 0; c < rank; ++c) tie_rank += sh.ties[c];
     }
-    auto kept = [&](uint32_t u, int& rank_of_tie) {
-        const uint32_t d = distance(u);
-        if (u <= kImageMinusInf || d > cut) return false;
-        if (d == cut && quota != 0x7fffffff && rank_of_tie++ >= quota) return false;
-        return min_p > 0.f ? widen(image_logit(u)) >= least : true;
-    };
-    double sum = 0.0;
-    {
+    // (images below top - cut, the padding's 0 among them, are cut)
+    double sum;
+    if (quota == 0x7fffffff) {
+        sum = strip_weight(0u, cut + 1u);
+    } else {
+        sum = 0.0;
         int tr = tie_rank;
-        for (int i = 0; i < p.strip; ++i)
-            if (kept(mine[i], tr)) sum += weight(distance(mine[i]));
+        for (int i = 0; i < p.strip; ++i) {
+            const uint32_t d = top - mine[i];
+            if (d < cut || (d == cut && tr++ < quota)) sum += weight(mine[i]);
+        }
     }
     // Running sums one after the other, so that a thread without weight ends exactly where the one before it does, and the end of a
     // warp or a CTA is the same number as the start of the next: one thread, with weight, holds the target.
@@ -443,11 +471,11 @@ kap_sample_rows_kernel(const SampleParams p)
     int ties_before = __shfl_sync(0xffffffffu, tie_rank, who), found = -1;
     for (int i0 = 0; i0 < p.strip; i0 += 32) {
         const int i = i0 + lane;
-        const uint32_t u = i < p.strip ? strip[i] : 0u, d = distance(u);
-        const uint32_t tied = __ballot_sync(0xffffffffu, d == cut && quota != 0x7fffffff);
-        int my_rank = ties_before + __popc(tied & ((1u << lane) - 1u));
+        const uint32_t u = i < p.strip ? strip[i] : 0u, d = top - u;
+        const uint32_t tied = __ballot_sync(0xffffffffu, i < p.strip && d == cut);
+        const int my_rank = ties_before + __popc(tied & ((1u << lane) - 1u));
         ties_before += __popc(tied);
-        const double w = kept(u, my_rank) ? weight(d) : 0.0;
+        const double w = i < p.strip && (d < cut || (d == cut && my_rank < quota)) ? weight(u) : 0.0;
         double upto = at;
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
@@ -461,7 +489,7 @@ kap_sample_rows_kernel(const SampleParams p)
     }
     if (lane == 0) {
         p.token[r] = first + (warp * 32 + who) * p.strip + found;
-        if (p.logprob) p.logprob[r] = (float)((log2_weight(distance(strip[found])) - log2(total)) * 0.69314718055994531);
+        if (p.logprob) p.logprob[r] = (float)((log2_weight(strip[found]) - log2(total)) * 0.69314718055994531);
     }
 }
 
@@ -492,8 +520,8 @@ extern "C" kap_status kap_sample_tokens(
     SampleParams p{logits, row_stride, vocab, 0, strip_of(C), C, temperature, top_p, min_p, uniform, top_k, token, logprob};
     p.slice = p.strip * kSampleThreads;
     if (rows > 0x7fffffff / C) return fail(KAP_ERR_UNSUPPORTED, "%d rows", rows);
-    auto smem_for = [](int slice) { return (sizeof(SampleShared) + 15) / 16 * 16 + (size_t)slice * sizeof(uint32_t); };
-    static_assert((sizeof(SampleShared) + 15) / 16 * 16 + (size_t)kSampleThreads * kMaxStrip * 4 <= 232448, "more than 227 KiB of shared memory");
+    auto smem_for = [](int slice) { return (sizeof(SampleShared) + 15) / 16 * 16 + ((size_t)slice + 4) * sizeof(uint32_t); };
+    static_assert((sizeof(SampleShared) + 15) / 16 * 16 + ((size_t)kSampleThreads * kMaxStrip + 4) * 4 <= 232448, "more than 227 KiB of shared memory");
     const void* fn = logits_type == KAP_LOGITS_F32 ? (const void*)kap_sample_rows_kernel<float> : (const void*)kap_sample_rows_kernel<__nv_bfloat16>;
     // (attributes belong to the current device; setting them again costs less than a microsecond)
     cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_for(kSampleThreads * kMaxStrip));
