@@ -49,21 +49,17 @@ __device__ __forceinline__ double wide_logit(uint32_t u) {
     const uint32_t mag = (u ^ flip) & 0x7fffffffu;
     return __hiloint2double((int)(((mag >> 3) + 0x38000000u) | (flip & 0x80000000u)), (int)(mag << 29));
 }
-// 2^t for t <= 0 in 64 bits; below the smallest normal number: 0.  t = n + f with |f| <= 1/2 (a sum with 1.5 2^52 holds n in its
-// low word), 2^f by the polynomial of degree 9 of least largest relative error there (1.3e-14; Remez exchange).
+// 2^t for t <= 0 in 64 bits, to be discarded below the smallest normal number (`vanishes`).  t = n + f with |f| <= 1/2 (a sum with
+// 1.5 2^52 holds n in its low word), 2^f by the polynomial of degree 9 of least largest relative error there (1.3e-14; Remez
+// exchange), its coefficients in constant memory, from where the products take them without a register.
+__constant__ double kExp2[10] = {1.0150336270671598e-07, 1.3259405604554393e-06, 1.5252984841153802e-05, 0.00015403434948094166, 0.0013333557617599588,
+                                 0.009618129192067212, 0.055504108668685645, 0.24022650695649653, 0.693147180559871, 1.0000000000000127};
+__device__ __forceinline__ bool vanishes(double t) { return (uint32_t)__double2hiint(t) > 0xc08ff000u; }       // t < -1022
 __device__ __forceinline__ double exp2_f64(double t) {
-    if ((uint32_t)__double2hiint(t) > 0xc08ff000u) return 0.0;         // t < -1022
     const double s = t + 6755399441055744.0, f = t - (s - 6755399441055744.0);
-    double y = 1.0150336270671598e-07;
-    y = fma(y, f, 1.3259405604554393e-06);
-    y = fma(y, f, 1.5252984841153802e-05);
-    y = fma(y, f, 0.00015403434948094166);
-    y = fma(y, f, 0.0013333557617599588);
-    y = fma(y, f, 0.009618129192067212);
-    y = fma(y, f, 0.055504108668685645);
-    y = fma(y, f, 0.24022650695649653);
-    y = fma(y, f, 0.693147180559871);
-    y = fma(y, f, 1.0000000000000127);
+    double y = kExp2[0];
+#pragma unroll
+    for (int i = 1; i < 10; ++i) y = fma(y, f, kExp2[i]);
     return __hiloint2double(__double2hiint(y) + (__double2loint(s) << 20), __double2loint(y));
 }
 
@@ -207,15 +203,32 @@ kap_sample_rows_kernel(const SampleParams p)
     const double x_max = wide_logit(top), per_bit = 1.4426950408889634 / (double)t;
     // logarithm of a weight and the weight: 2^((x - max) / T / ln 2)
     auto log2_weight = [&](uint32_t u) { return (wide_logit(u) - x_max) * per_bit; };
-    auto weight = [&](uint32_t u) { return exp2_f64(log2_weight(u)); };
-    // weights of the distances from .. from + span - 1 in this thread's strip
-    auto strip_weight = [&](uint32_t from, uint32_t span) {
+    auto weight = [&](uint32_t u) {
+        const double e = log2_weight(u);
+        return vanishes(e) ? 0.0 : exp2_f64(e);
+    };
+    // Weights of the distances from .. from + span - 1 in this thread's strip.  Without a branch where most of them are wanted: three
+    // chains of products side by side; one logit at a time where few are.
+    auto strip_weight = [&](uint32_t from, uint32_t span, bool most) {
         const uint32_t high = top - from;
         double s = 0.0;
-#pragma unroll 3
-        for (int i = 0; i < p.strip; ++i) {
-            const uint32_t u = mine[i];
-            if (high - u < span) s += weight(u);
+        if (most) {
+            for (int i = 0; i < p.strip; i += 3) {
+                uint32_t u[3];
+                double e[3], w[3];
+#pragma unroll
+                for (int j = 0; j < 3; ++j) u[j] = i + j < p.strip ? mine[i + j] : 0u;
+#pragma unroll
+                for (int j = 0; j < 3; ++j) { e[j] = log2_weight(u[j]); w[j] = exp2_f64(e[j]); }
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                    if (high - u[j] < span && !vanishes(e[j])) s += w[j];
+            }
+        } else {
+            for (int i = 0; i < p.strip; ++i) {
+                const uint32_t u = mine[i];
+                if (high - u < span) s += weight(u);
+            }
         }
         return s;
     };
@@ -321,7 +334,7 @@ kap_sample_rows_kernel(const SampleParams p)
         auto shift_for = [&](uint64_t range) { int s = 0; while (((range - 1) >> s) >= kBins) ++s; return s; };
         int shift = shift_for((uint64_t)last + 1);
         uint64_t base = 0;
-        double part = strip_weight(0u, quota == 0x7fffffff ? cut + 1u : cut);   // the whole: everything kept so far
+        double part = strip_weight(0u, quota == 0x7fffffff ? cut + 1u : cut, cut == furthest);   // the whole: everything kept so far
         double target = 0.0, above = 0.0;                          // p times the whole; weight of distances below base
         const double cut_part = quota == 0x7fffffff ? 0.0 : (double)quota * weight(top - cut);
         for (int rounds = 0; rounds < kMaxRounds; ++rounds) {
@@ -397,7 +410,7 @@ kap_sample_rows_kernel(const SampleParams p)
                 }
             }
             // what lies between the old base and the new one is above the range from now on
-            part = strip_weight((uint32_t)base, (uint32_t)(next - base));
+            part = strip_weight((uint32_t)base, (uint32_t)(next - base), false);
             base = next;
             // finer by at least two bits, so that the search ends; windows that do not cover the range follow one another
             if (b1 < kBins) shift = max(0, min(shift - 2, b2 < kBins ? shift_for((uint64_t)(b2 - b1 + 1) << shift) : shift));
@@ -431,7 +444,7 @@ kap_sample_rows_kernel(const SampleParams p)
     // (images below top - cut, the padding's 0 among them, are cut)
     double sum;
     if (quota == 0x7fffffff) {
-        sum = strip_weight(0u, cut + 1u);
+        sum = strip_weight(0u, cut + 1u, cut == furthest);
     } else {
         sum = 0.0;
         int tr = tie_rank;
