@@ -62,7 +62,7 @@ SIGNATURES = {
     "kap_materialize_view": (C.c_int, [_vp, C.c_int64, _vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
                                        _vp, C.c_int64, _vp, _vp, _vp]),
     "kap_append_kv_rope": (C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int32,
-                                     _vp, C.c_int32, C.c_int32, _vp, C.c_int64, C.c_int32, _u8p, _vp, _vp,
+                                     _vp, C.c_int32, C.c_int32, _vp, C.c_int64, C.c_int32, _vp, _vp, _vp,
                                      C.c_int64, _vp, _vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                      C.c_int32, C.c_int32, C.c_int32, _vp, _vp]),
     "kap_shared_prefix_items": (C.c_int, [C.c_int32, _i32p, _i32p, C.c_int32, _i32p, _i32p, C.c_int32,
@@ -252,14 +252,23 @@ def schedule_host(list_len, n_q, num_q_heads, num_kv_heads, cta_slots, max_chunk
 
 
 # ------------------------------------------------------------------------- workspace + attention
+_torch = None
+
+
+def _torch_module():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _stream_ptr(stream=None):
-    import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return C.c_void_p(s.cuda_stream)
+    return (_torch_module().cuda.current_stream() if stream is None else stream).cuda_stream
 
 
 def _dptr(t):
-    return None if t is None else C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _pool_shape(kv_pool, ws):
@@ -417,13 +426,12 @@ def append_kv(k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, new_indptr=No
 
 def _head_rows(name, t, rows, heads):
     """the row stride of a bf16 [rows, heads, d] tensor whose heads are contiguous within a row"""
-    import torch
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or tuple(t.shape[:2]) != (rows, heads):
-        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)}, expected bfloat16 [{rows}, {heads}, d]")
-    d = t.shape[2]
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
-        raise KapError(ERR_INVALID_ARG, f"{name} has strides {t.stride()}: the heads of a row must be contiguous")
-    return heads * d if rows <= 1 else int(t.stride(0))
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not _torch.bfloat16 or len(shape) != 3 or shape[0] != rows or shape[1] != heads:
+        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(shape)}, expected bfloat16 [{rows}, {heads}, d]")
+    if stride[2] != 1 or (heads > 1 and stride[1] != shape[2]):
+        raise KapError(ERR_INVALID_ARG, f"{name} has strides {stride}: the heads of a row must be contiguous")
+    return heads * shape[2] if rows <= 1 else stride[0]
 
 
 def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_freq, q_out=None,
@@ -434,35 +442,44 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
     append_kv.  q_out None rotates q in place; q None handles k and v only.  positions None: the
     logical index (+ position_offset[b]); else int32 [rows] or [axes, rows], freq_axis naming the axis
     of each pair (host sequence)."""
-    import torch
+    torch = _torch_module()
     if kv_layout == KV_NHD:
         pages, _, P, Hkv, d = kv_pool.shape
     else:
         pages, _, Hkv, P, d = kv_pool.shape
-    rows, Hq = int(k_new.shape[0]), 0
+    rows, Hq = k_new.shape[0], 0
     ks, vs = _head_rows("k_new", k_new, rows, Hkv), _head_rows("v_new", v_new, rows, Hkv)
     qs = os_ = 0
-    if q is not None:
-        Hq = int(q.shape[1])
-        q_out = q if q_out is None else q_out
-        qs, os_ = _head_rows("q", q, rows, Hq), _head_rows("q_out", q_out, rows, Hq)
+    if q is None:
+        q_out = None
+    else:
+        Hq = q.shape[1]
+        qs = _head_rows("q", q, rows, Hq)
+        if q_out is None:
+            q_out, os_ = q, qs
+        else:
+            os_ = _head_rows("q_out", q_out, rows, Hq)
     axes, pos_stride = 0, 0
     if positions is not None:
-        positions = positions.view(1, -1) if positions.dim() == 1 else positions
-        if positions.dtype != torch.int32 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
+        if positions.dim() == 1:
+            positions = positions.view(1, -1)
+        if positions.dtype is not torch.int32 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
             raise KapError(ERR_INVALID_ARG, f"positions {positions.dtype} {tuple(positions.shape)} for {rows} rows")
-        axes, pos_stride = int(positions.shape[0]), int(positions.stride(0))
-        pos_stride = max(pos_stride, rows) if axes == 1 else pos_stride
-    rot = 2 * int(inv_freq.shape[0])
-    axis = _np(freq_axis, np.uint8)
-    if axis is not None and axis.shape != (rot // 2,):
-        raise KapError(ERR_INVALID_ARG, f"freq_axis names {axis.size} pairs, inv_freq {rot // 2}")
+        axes, pos_stride = positions.shape[0], positions.stride(0)
+        if axes == 1:
+            pos_stride = max(pos_stride, rows)
+    rot = 2 * inv_freq.shape[0]
+    axis = None
+    if freq_axis is not None:
+        axis = bytes(freq_axis) if type(freq_axis) in (list, tuple, bytes) else _np(freq_axis, np.uint8).tobytes()
+        if len(axis) != rot // 2:
+            raise KapError(ERR_INVALID_ARG, f"freq_axis names {len(axis)} pairs, inv_freq {rot // 2}")
     _check(lib().kap_append_kv_rope(
-        _dptr(q), qs, _dptr(k_new), ks, _dptr(v_new), vs, _dptr(q_out) if q is not None else None, os_,
-        _dptr(new_indptr), rows, _dptr(inv_freq), rot, int(bool(interleaved)), _dptr(positions), pos_stride,
-        axes, _ptr(axis, C.c_uint8), _dptr(position_offset), _dptr(kv_pool), int(pages), _dptr(bt_indptr),
-        _dptr(bt_pages), _dptr(ctx_len), int(bool(advance)), int(ctx_len.shape[0]), Hq, int(Hkv), int(d), int(P),
-        int(kv_layout), _dptr(device_status), _stream_ptr(stream)))
+        _dptr(q), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, _dptr(q_out), os_, _dptr(new_indptr), rows,
+        inv_freq.data_ptr(), rot, 1 if interleaved else 0, _dptr(positions), pos_stride, axes, axis,
+        _dptr(position_offset), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
+        ctx_len.data_ptr(), 1 if advance else 0, ctx_len.shape[0], Hq, Hkv, d, P, kv_layout,
+        _dptr(device_status), _stream_ptr(stream)))
 
 
 def sample_tokens(logits, uniform, token, logprob=None, temperature=None, top_k=None, top_p=None,
@@ -470,20 +487,24 @@ def sample_tokens(logits, uniform, token, logprob=None, temperature=None, top_k=
     """kap_sample_tokens on torch CUDA tensors: logits fp32 or bf16 [rows, vocab] (any row stride), uniform
     fp32 [rows]; outputs int32 token [rows] and optional fp32 logprob [rows].  temperature, top_p,
     min_p (fp32 [rows]) and top_k (int32 [rows]) are optional; None switches a filter off."""
-    import torch
-    kinds = {torch.float32: LOGITS_F32, torch.bfloat16: LOGITS_BF16}
-    if logits.dtype not in kinds or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    torch = _torch_module()
+    kind = LOGITS_F32 if logits.dtype is torch.float32 else LOGITS_BF16 if logits.dtype is torch.bfloat16 else None
+    if kind is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise KapError(ERR_INVALID_ARG, f"logits are {logits.dtype} {tuple(logits.shape)} with strides {logits.stride()}")
     rows, vocab = logits.shape
-    for name, t, dt in (("uniform", uniform, torch.float32), ("token", token, torch.int32),
-                        ("logprob", logprob, torch.float32), ("temperature", temperature, torch.float32),
-                        ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
-        if t is not None and (t.dtype != dt or t.numel() != rows or not t.is_contiguous()):
+
+    def ptr(name, t, dt):
+        if t is None:
+            return None
+        if t.dtype is not dt or t.numel() != rows or not t.is_contiguous():
             raise KapError(ERR_INVALID_ARG, f"{name} must be a contiguous {dt} tensor of {rows}")
-    stride = vocab if rows <= 1 else int(logits.stride(0))
+        return t.data_ptr()
+
+    f32, i32 = torch.float32, torch.int32
     _check(lib().kap_sample_tokens(
-        _dptr(logits), kinds[logits.dtype], stride, int(rows), int(vocab), _dptr(temperature), _dptr(top_k),
-        _dptr(top_p), _dptr(min_p), _dptr(uniform), _dptr(token), _dptr(logprob), _stream_ptr(stream)))
+        logits.data_ptr(), kind, vocab if rows <= 1 else logits.stride(0), rows, vocab,
+        ptr("temperature", temperature, f32), ptr("top_k", top_k, i32), ptr("top_p", top_p, f32), ptr("min_p", min_p, f32),
+        ptr("uniform", uniform, f32), ptr("token", token, i32), ptr("logprob", logprob, f32), _stream_ptr(stream)))
 
 
 def top3_accept(logits, row_indptr, proposed, top3, accepted, next_token, stream=None, ctx_len=None):
