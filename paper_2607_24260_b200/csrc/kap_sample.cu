@@ -246,17 +246,10 @@ kap_sample_rows_kernel(const SampleParams p)
         return v;
     };
     int level = 0;                                                 // of all searches of the row: parity selects the buffers
-    // One level: counts of the distances base + [b << shift, (b + 1) << shift) over the whole row, two bins a thread; `partial` is
-    // summed over the row along the way.
-    auto count_level = [&](uint64_t base, int shift, double partial, uint32_t (&bins)[2]) {
+    // One level: the CTAs' histograms (of the distances base + [b << shift, (b + 1) << shift), by count_level) summed over the row, two
+    // bins a thread; `partial` is summed over the row along the way.
+    auto gather_level = [&](double partial, uint32_t (&bins)[2]) {
         const int buf = level & 1;
-        // (a search ends before its base passes the last distance that has weight)
-        const uint32_t high = top - (uint32_t)base, span = (uint32_t)min((uint64_t)kBins << shift, (uint64_t)furthest + 1 - base);
-#pragma unroll 3
-        for (int i = 0; i < p.strip; ++i) {
-            const uint32_t d = high - mine[i];
-            if (d < span) atomicAdd(&sh.hist[buf][d >> shift], 1u);
-        }
         const double sum = block_sum(partial);
         if (tid < C) to_all(sh.level_sum[buf], sum);
         meet();
@@ -276,6 +269,17 @@ kap_sample_rows_kernel(const SampleParams p)
         sh.hist[buf ^ 1][2 * tid] = 0u; sh.hist[buf ^ 1][2 * tid + 1] = 0u;
         ++level;
         return total;
+    };
+
+    auto count_level = [&](uint64_t base, int shift, double partial, uint32_t (&bins)[2]) {
+        // (a search ends before its base passes the last distance that has weight)
+        const uint32_t high = top - (uint32_t)base, span = (uint32_t)min((uint64_t)kBins << shift, (uint64_t)furthest + 1 - base);
+#pragma unroll 3
+        for (int i = 0; i < p.strip; ++i) {
+            const uint32_t d = high - mine[i];
+            if (d < span) atomicAdd(&sh.hist[level & 1][d >> shift], 1u);
+        }
+        return gather_level(partial, bins);
     };
 
     // The cut: distances below it are kept, and `quota` of those equal to it (lowest index first).  At first all that have weight:
@@ -332,28 +336,11 @@ kap_sample_rows_kernel(const SampleParams p)
         const uint32_t far = logit_image(__double2float_rd(x_max - reach));
         const uint32_t last = min(far < top ? top - far : 0u, cut);
         auto shift_for = [&](uint64_t range) { int s = 0; while (((range - 1) >> s) >= kBins) ++s; return s; };
-        int shift = shift_for((uint64_t)last + 1);
-        uint64_t base = 0;
-        double part = strip_weight(0u, quota == 0x7fffffff ? cut + 1u : cut, cut == furthest);   // the whole: everything kept so far
         double target = 0.0, above = 0.0;                          // p times the whole; weight of distances below base
-        const double cut_part = quota == 0x7fffffff ? 0.0 : (double)quota * weight(top - cut);
-        for (int rounds = 0; rounds < kMaxRounds; ++rounds) {
-            uint32_t bins[2];
-            const double sum = count_level(base, shift, part, bins);
-            if (rounds == 0) target = (double)top_p * (sum + cut_part); else above += sum;
-            double lo[2], hi[2];                                   // bounds of the weight in this thread's two bins
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint64_t from = base + ((uint64_t)(2 * tid + e) << shift), to = from + ((uint64_t)1 << shift) - 1;
-                int c = (int)bins[e];
-                if (from > cut) c = 0;
-                else if (quota != 0x7fffffff && cut <= to) c -= ties_at_cut - quota;   // of the equal ones only some are left
-                // (a bin that holds the cut may hold distances behind it as well: its bounds are too high then, but the
-                // threshold does not lie behind it, whatever they say)
-                bins[e] = (uint32_t)max(c, 0);
-                lo[e] = c > 0 ? c * weight(top - (uint32_t)min(to, (uint64_t)furthest)) : 0.0;
-                hi[e] = c > 0 ? (shift == 0 ? lo[e] : c * weight(top - (uint32_t)from)) : 0.0;
-            }
+        int b1, b2, in_bin;                                        // bins found; logits in the first one
+        double edge;                                               // weight before that one
+        // the first bin whose end may reach the target, by upper bounds of the bins' weights, and the first one whose end must
+        auto find = [&](const uint32_t (&bins)[2], const double (&lo)[2], const double (&hi)[2], double slack) {
             double run_lo = lo[0] + lo[1], run_hi = hi[0] + hi[1];
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -367,23 +354,82 @@ kap_sample_rows_kernel(const SampleParams p)
             double before_lo = above, before_hi = above;
             for (int w = 0; w < warp; ++w) { before_lo += sh.warp_d[w][0]; before_hi += sh.warp_d[w][1]; }
             run_lo += before_lo; run_hi += before_hi;
-            // the first bin whose end may reach the target and the first one whose end must; at single distances the sums are exact
-            const double slack = shift == 0 ? 0.0 : 1e-12 * target;
             const double mid_lo = run_lo - lo[1], mid_hi = run_hi - hi[1];
             if (bins[0] && mid_hi >= target - slack) atomicMin(&sh.bin[0], 2 * tid);
             else if (bins[1] && run_hi >= target - slack) atomicMin(&sh.bin[0], 2 * tid + 1);
             if (bins[0] && mid_lo >= target + slack) atomicMin(&sh.bin[1], 2 * tid);
             else if (bins[1] && run_lo >= target + slack) atomicMin(&sh.bin[1], 2 * tid + 1);
             __syncthreads();
-            const int b1 = sh.bin[0], b2 = sh.bin[1];
-            if (b1 < kBins && (b1 >> 1) == tid) {                  // weight before it, and how many logits it holds
+            b1 = sh.bin[0]; b2 = sh.bin[1];
+            if (b1 < kBins && (b1 >> 1) == tid) {
                 const int e = b1 & 1;
                 sh.edge = e ? mid_lo : mid_lo - lo[0];
                 sh.bin_count = bins[e];
             }
             __syncthreads();
-            const int in_bin = (int)sh.bin_count;
-            const double edge = sh.edge;
+            in_bin = (int)sh.bin_count;
+            edge = sh.edge;
+        };
+        double part = strip_weight(0u, quota == 0x7fffffff ? cut + 1u : cut, cut == furthest);   // the whole: everything kept so far
+        const double cut_part = quota == 0x7fffffff ? 0.0 : (double)quota * weight(top - cut);
+        uint64_t base = 0, end = last;                             // distances between which the threshold lies
+        const bool even = top != kImagePlusInf && last >= kBins;   // (few distances: their own intervals at once)
+        if (even) {
+            // First level by value, in equal intervals of what lies before R: intervals of the distance are narrow around zero and
+            // wide away from it, so that a flat row would meet in a few of them.  The value of a bin's ends is known to a part in
+            // 10^6 (three roundings to 32 bits); one part in 10^5 is allowed for.
+            const double depth = fmin(reach, x_max - wide_logit(top - last)) * (1.0 + 1e-5) + 1e-30;
+            const float high = image_logit(top), per_value = __double2float_rd((double)kBins / depth);
+            const bool usable = per_value > 0.f && per_value < 1e37f;
+#pragma unroll 3
+            for (int i = 0; i < p.strip; ++i) {
+                const uint32_t u = mine[i];
+                const float b = (high - image_logit(u)) * per_value;
+                if (usable && top - u <= cut && b < (float)kBins) atomicAdd(&sh.hist[level & 1][(int)b], 1u);
+            }
+            uint32_t bins[2];
+            target = (double)top_p * (gather_level(part, bins) + cut_part);
+            double lo[2], hi[2];
+            const double bin_value = 1.0 / (double)per_value;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const double near = (double)(2 * tid + e) * bin_value * (1.0 - 1e-5), far_end = (double)(2 * tid + e + 1) * bin_value * (1.0 + 1e-5);
+                const double a = -near * per_bit, b = -far_end * per_bit;
+                hi[e] = bins[e] ? (vanishes(a) ? 0.0 : bins[e] * exp2_f64(a)) : 0.0;
+                lo[e] = bins[e] ? (vanishes(b) ? 0.0 : bins[e] * exp2_f64(b)) : 0.0;
+            }
+            find(bins, lo, hi, 1e-12 * target);
+            if (b1 < kBins) {
+                const uint32_t from = logit_image(__double2float_ru(x_max - (double)b1 * bin_value * (1.0 - 1e-5)));
+                base = from < top ? top - from : 0u;
+                if (b2 < kBins) {
+                    const uint32_t to = logit_image(__double2float_rd(x_max - (double)(b2 + 1) * bin_value * (1.0 + 1e-5)));
+                    end = min(end, (uint64_t)(top - to));
+                }
+                base = min(base, end);
+                part = base > 0 ? strip_weight(0u, (uint32_t)base, false) : 0.0;
+            }
+            if (b1 == kBins) part = 0.0;                           // (nothing learnt; `above` stays 0)
+        }
+        int shift = shift_for(end - base + 1);
+        for (int rounds = 0; rounds < kMaxRounds; ++rounds) {
+            uint32_t bins[2];
+            const double sum = count_level(base, shift, part, bins);
+            if (rounds == 0 && !even) target = (double)top_p * (sum + cut_part); else above += sum;
+            double lo[2], hi[2];                                   // bounds of the weight in this thread's two bins
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint64_t from = base + ((uint64_t)(2 * tid + e) << shift), to = from + ((uint64_t)1 << shift) - 1;
+                int c = (int)bins[e];
+                if (from > cut) c = 0;
+                else if (quota != 0x7fffffff && cut <= to) c -= ties_at_cut - quota;   // of the equal ones only some are left
+                // (a bin that holds the cut may hold distances behind it as well: its bounds are too high then, but the
+                // threshold does not lie behind it, whatever they say)
+                bins[e] = (uint32_t)max(c, 0);
+                lo[e] = c > 0 ? c * weight(top - (uint32_t)min(to, (uint64_t)furthest)) : 0.0;
+                hi[e] = c > 0 ? (shift == 0 ? lo[e] : c * weight(top - (uint32_t)from)) : 0.0;
+            }
+            find(bins, lo, hi, shift == 0 ? 0.0 : 1e-12 * target); // at single distances the sums are exact
             uint64_t next;
             if (b1 == kBins) {                                     // not within this window: on to the next one
                 next = base + ((uint64_t)kBins << shift);
@@ -402,9 +448,9 @@ kap_sample_rows_kernel(const SampleParams p)
                 break;
             } else {
                 next = base + ((uint64_t)b1 << shift);
-                const uint64_t end = next + ((uint64_t)1 << shift) - 1;
-                if (b1 == b2 && in_bin == 1 && end < cut) {        // the one logit in it belongs to the prefix
-                    cut = (uint32_t)end;
+                const uint64_t bin_end = next + ((uint64_t)1 << shift) - 1;
+                if (b1 == b2 && in_bin == 1 && bin_end < cut) {    // the one logit in it belongs to the prefix
+                    cut = (uint32_t)bin_end;
                     quota = 0x7fffffff;
                     break;
                 }
