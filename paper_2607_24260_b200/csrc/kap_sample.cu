@@ -30,6 +30,7 @@ namespace {
 constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 1024;
+constexpr int kFew = kSampleThreads;               // logits that one CTA finishes alone: one a thread
 constexpr uint32_t kImageMinusInf = 0x007fffffu;   // image of -inf; nothing at or below it has weight
 constexpr uint32_t kImagePlusInf = 0xff800000u;
 constexpr int kMaxRounds = 96;                     // of a search: at most 11 widths of interval, four windows each
@@ -85,6 +86,11 @@ struct SampleShared {
     int32_t warp_i[kSampleWarps];
     int32_t bin[2];
     int32_t before[2];
+    // first CTA: the logits that can still be drawn, when they are few
+    int32_t few;
+    uint32_t few_image[kFew];
+    int32_t few_index[kFew];
+    double few_weight[kFew];
     uint32_t bin_count;
     double edge;
 };
@@ -158,6 +164,7 @@ kap_sample_rows_kernel(const SampleParams p)
     for (int i = head + n_vec * kVec + tid; i < n; i += kSampleThreads) img[i] = image_of(as_float(x[i]));
     for (int i = n + tid; i < room; i += kSampleThreads) img[i] = 0u;
     for (int i = tid; i < 2 * kBins; i += kSampleThreads) (&sh.hist[0][0])[i] = 0u;
+    if (tid == 0) sh.few = 0;
     best = __reduce_max_sync(0xffffffffu, best);
     finite = __reduce_add_sync(0xffffffffu, finite);
     if (lane == 0) { sh.warp_u[warp] = best; sh.warp_i[warp] = finite; }
@@ -207,28 +214,53 @@ kap_sample_rows_kernel(const SampleParams p)
         const double e = log2_weight(u);
         return vanishes(e) ? 0.0 : exp2_f64(e);
     };
-    // Weights of the distances from .. from + span - 1 in this thread's strip.  Without a branch where most of them are wanted: three
-    // chains of products side by side; one logit at a time where few are.
-    auto strip_weight = [&](uint32_t from, uint32_t span, bool most) {
+    // Weights of the distances below `span` (and, of those equal to it, of the ones whose rank among the equal ones, from `tie_rank` on, is
+    // below `quota`) in this thread's strip: which ones, 32 at a time, then three chains of products side by side for as long as a
+    // lane of the warp has one left.
+    auto strip_weight = [&](uint32_t from, uint32_t span, int tie_rank, int quota) {
         const uint32_t high = top - from;
         double s = 0.0;
-        if (most) {
-            for (int i = 0; i < p.strip; i += 3) {
-                uint32_t u[3];
+        for (int i0 = 0; i0 < p.strip; i0 += 32) {
+            const int n_here = min(32, p.strip - i0);
+            uint32_t wanted = 0u;
+#pragma unroll 4
+            for (int i = 0; i < n_here; ++i) {
+                const uint32_t d = high - mine[i0 + i];
+                bool in = d < span;
+                if (quota > 0 && d == span) in = tie_rank++ < quota;
+                wanted |= (uint32_t)in << i;
+            }
+            while (__any_sync(0xffffffffu, wanted != 0u)) {
                 double e[3], w[3];
+                bool have[3];
 #pragma unroll
-                for (int j = 0; j < 3; ++j) u[j] = i + j < p.strip ? mine[i + j] : 0u;
+                for (int j = 0; j < 3; ++j) {
+                    have[j] = wanted != 0u;
+                    e[j] = log2_weight(mine[i0 + (have[j] ? __ffs(wanted) - 1 : 0)]);
+                    wanted &= wanted - 1u;
+                }
 #pragma unroll
-                for (int j = 0; j < 3; ++j) { e[j] = log2_weight(u[j]); w[j] = exp2_f64(e[j]); }
+                for (int j = 0; j < 3; ++j) w[j] = exp2_f64(e[j]);
 #pragma unroll
                 for (int j = 0; j < 3; ++j)
-                    if (high - u[j] < span && !vanishes(e[j])) s += w[j];
+                    if (have[j] && !vanishes(e[j])) s += w[j];
             }
-        } else {
-            for (int i = 0; i < p.strip; ++i) {
-                const uint32_t u = mine[i];
-                if (high - u < span) s += weight(u);
-            }
+        }
+        return s;
+    };
+    // the same for everything that has weight, without the search
+    auto strip_weight_all = [&](uint32_t span) {
+        double s = 0.0;
+        for (int i = 0; i < p.strip; i += 3) {
+            uint32_t u[3];
+            double e[3], w[3];
+#pragma unroll
+            for (int j = 0; j < 3; ++j) u[j] = i + j < p.strip ? mine[i + j] : 0u;
+#pragma unroll
+            for (int j = 0; j < 3; ++j) { e[j] = log2_weight(u[j]); w[j] = exp2_f64(e[j]); }
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (top - u[j] < span && !vanishes(e[j])) s += w[j];
         }
         return s;
     };
@@ -282,6 +314,91 @@ kap_sample_rows_kernel(const SampleParams p)
         return gather_level(partial, bins);
     };
 
+    const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? fminf(p.min_p[r], 1.f) : 0.f;
+    uint32_t min_p_cut = 0xffffffffu;                              // min-p as a cut: logits from the least float with weight enough on
+    if (min_p > 0.f) {
+        const uint32_t least = logit_image(__double2float_ru(x_max + (double)t * log((double)min_p)));
+        min_p_cut = least < top ? top - least : 0u;
+    }
+    const double u01 = (double)p.uniform[r];
+    auto draw_at = [&](double total) { return u01 >= 0.0 ? fmin(u01 * total, total * 0.99999999999999978) : 0.0; };
+
+    // When the logits up to a distance are at most kFew and hold whatever can be drawn, the first CTA gets them all and finishes alone, one
+    // logit a thread: ranks by counting, then running sums by rank for top-p and by index for the draw.  Running sums of the block
+    // are taken one after the other inside a warp, as in the draw below.
+    auto block_run = [&](double v, double& before) {               // returns the total
+        double run = 0.0;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const double s = __shfl_sync(0xffffffffu, v, j);
+            if (lane > j) run += s;
+        }
+        __syncthreads();
+        if (lane == 31) sh.warp_d[warp][0] = run + v;
+        __syncthreads();
+        double all = 0.0, offset = 0.0;
+        for (int w = 0; w < kSampleWarps; ++w) { if (w == warp) offset = all; all += sh.warp_d[w][0]; }
+        before = offset + run;
+        return all;
+    };
+    auto finish_few = [&](uint32_t up_to, int most, double whole) {    // the first `most` ranks; weight that top-p refers to, or -1: theirs
+        const uint32_t few_at = map_to_cta(smem_u32(&sh.few), 0), image_at = map_to_cta(smem_u32(sh.few_image), 0), index_at = map_to_cta(smem_u32(sh.few_index), 0);
+        for (int i = 0; i < p.strip; ++i) {
+            if (top - mine[i] > up_to) continue;
+            int32_t slot;
+            asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(slot) : "r"(few_at) : "memory");
+            if (slot >= kFew) continue;                            // (cannot be: they were counted)
+            put_remote(image_at + 4 * slot, (int32_t)mine[i]);
+            put_remote(index_at + 4 * slot, first + tid * p.strip + i);
+        }
+        meet();
+        if (rank != 0) return;
+        const int m = min(sh.few, kFew);
+        const bool mine_too = tid < m;
+        const uint32_t u = mine_too ? sh.few_image[tid] : 0u;
+        const int index = mine_too ? sh.few_index[tid] : 0x7fffffff;
+        int by_value = 0, by_index = 0;
+        for (int j = 0; j < m; ++j) {
+            const uint32_t uj = sh.few_image[j];
+            const int ij = sh.few_index[j];
+            by_value += uj > u || (uj == u && ij < index);
+            by_index += ij < index;
+        }
+        double w = mine_too && by_value < most ? weight(u) : 0.0;
+        bool keep = mine_too && by_value < most && top - u <= min_p_cut;
+        if (top_p < 1.f) {
+            sh.few_weight[tid] = 0.0;
+            __syncthreads();
+            if (mine_too) sh.few_weight[by_value] = w;
+            __syncthreads();
+            double before;
+            const double all = block_run(sh.few_weight[tid], before);
+            const bool stays = tid == 0 || before < (double)top_p * (whole < 0.0 ? all : whole);
+            __syncthreads();
+            sh.few_weight[tid] = stays ? 1.0 : 0.0;
+            __syncthreads();
+            keep = keep && sh.few_weight[by_value] > 0.0;
+            __syncthreads();
+        }
+        if (!keep) w = 0.0;
+        sh.few_weight[tid] = 0.0;
+        __syncthreads();
+        if (mine_too) sh.few_weight[by_index] = w;
+        __syncthreads();
+        double before;
+        const double v = sh.few_weight[tid], total = block_run(v, before), target = draw_at(total);
+        // (the place in index order whose weight holds the target; block_run's sums end where the next begins only up to a rounding,
+        // so the last place that begins at or before the target is taken)
+        if (tid == 0) sh.bin[0] = -1;
+        __syncthreads();
+        if (v > 0.0 && before <= target) atomicMax(&sh.bin[0], tid);
+        __syncthreads();
+        if (mine_too && by_index == sh.bin[0]) {
+            p.token[r] = index;
+            if (p.logprob) p.logprob[r] = (float)((log2_weight(u) - log2(total)) * 0.69314718055994531);
+        }
+    };
+
     // The cut: distances below it are kept, and `quota` of those equal to it (lowest index first).  At first all that have weight:
     // behind +inf nothing has.
     uint32_t cut = furthest;
@@ -323,13 +440,16 @@ kap_sample_rows_kernel(const SampleParams p)
             const int in_bin = (int)sh.bin_count;
             base += (uint64_t)b << shift;
             __syncthreads();
+            if (above + in_bin <= kFew) {
+                finish_few((uint32_t)min(base + ((uint64_t)1 << shift) - 1, (uint64_t)furthest), k, -1.0);
+                return;
+            }
             if (above + in_bin == k) { cut = (uint32_t)min(base + ((uint64_t)1 << shift) - 1, (uint64_t)furthest); break; }     // the whole bin
             if (shift == 0) { cut = (uint32_t)base; quota = k - above; ties_at_cut = in_bin; break; }
             shift = max(0, shift - 10);
         }
     }
 
-    const float top_p = p.top_p ? p.top_p[r] : 1.f;
     if (top_p < 1.f) {
         // the threshold lies where weights still matter: N exp(-R / T) < 1 - p leaves less than 1 - p of the whole behind R
         const double reach = (double)t * (log((double)p.vocab) - log(1.0 - fmax((double)top_p, 0.0))) * (1.0 + 1e-9) + 1e-30;
@@ -370,7 +490,7 @@ kap_sample_rows_kernel(const SampleParams p)
             in_bin = (int)sh.bin_count;
             edge = sh.edge;
         };
-        double part = strip_weight(0u, quota == 0x7fffffff ? cut + 1u : cut, cut == furthest);   // the whole: everything kept so far
+        double part = cut == furthest && quota == 0x7fffffff ? strip_weight_all(cut + 1u) : strip_weight(0u, quota == 0x7fffffff ? cut + 1u : cut, 0, 0);   // the whole: everything kept so far
         const double cut_part = quota == 0x7fffffff ? 0.0 : (double)quota * weight(top - cut);
         uint64_t base = 0, end = last;                             // distances between which the threshold lies
         const bool even = top != kImagePlusInf && last >= kBins;   // (few distances: their own intervals at once)
@@ -399,6 +519,37 @@ kap_sample_rows_kernel(const SampleParams p)
                 lo[e] = bins[e] ? (vanishes(b) ? 0.0 : bins[e] * exp2_f64(b)) : 0.0;
             }
             find(bins, lo, hi, 1e-12 * target);
+            if (b2 < kBins && quota == 0x7fffffff) {               // few enough up to the end of the last bin in question?
+                int upto = (2 * tid <= b2 ? (int)bins[0] : 0) + (2 * tid + 1 <= b2 ? (int)bins[1] : 0);
+                upto = __reduce_add_sync(0xffffffffu, upto);
+                if (lane == 0) sh.warp_i[warp] = upto;
+                __syncthreads();
+                upto = 0;
+                for (int w = 0; w < kSampleWarps; ++w) upto += sh.warp_i[w];
+                const uint32_t to = logit_image(__double2float_rd(x_max - (double)(b2 + 1) * bin_value * (1.0 + 1e-5)));
+                // (the bins' ends are not exact: what lies up to `to` are these and perhaps some of the next bin, counted below)
+                int exact = 0;
+                if (upto <= kFew) {
+                    for (int i = 0; i < p.strip; ++i) exact += top - mine[i] <= min(top - to, cut);
+                }
+                exact = __reduce_add_sync(0xffffffffu, exact);
+                __syncthreads();
+                if (lane == 0) sh.warp_i[warp] = exact;
+                __syncthreads();
+                if (upto <= kFew) {
+                    exact = 0;
+                    for (int w = 0; w < kSampleWarps; ++w) exact += sh.warp_i[w];
+                    if (tid < C) to_all(sh.ties, exact);
+                    meet();
+                    exact = 0;
+                    for (int c = 0; c < C; ++c) exact += sh.ties[c];
+                    if (exact <= kFew) {
+                        finish_few(min(top - to, cut), 0x7fffffff, target / (double)top_p);
+                        return;
+                    }
+                    meet();                                        // sh.ties is used again
+                }
+            }
             if (b1 < kBins) {
                 const uint32_t from = logit_image(__double2float_ru(x_max - (double)b1 * bin_value * (1.0 - 1e-5)));
                 base = from < top ? top - from : 0u;
@@ -407,7 +558,7 @@ kap_sample_rows_kernel(const SampleParams p)
                     end = min(end, (uint64_t)(top - to));
                 }
                 base = min(base, end);
-                part = base > 0 ? strip_weight(0u, (uint32_t)base, false) : 0.0;
+                part = base > 0 ? strip_weight(0u, (uint32_t)base, 0, 0) : 0.0;
             }
             if (b1 == kBins) part = 0.0;                           // (nothing learnt; `above` stays 0)
         }
@@ -456,7 +607,7 @@ kap_sample_rows_kernel(const SampleParams p)
                 }
             }
             // what lies between the old base and the new one is above the range from now on
-            part = strip_weight((uint32_t)base, (uint32_t)(next - base), false);
+            part = strip_weight((uint32_t)base, (uint32_t)(next - base), 0, 0);
             base = next;
             // finer by at least two bits, so that the search ends; windows that do not cover the range follow one another
             if (b1 < kBins) shift = max(0, min(shift - 2, b2 < kBins ? shift_for((uint64_t)(b2 - b1 + 1) << shift) : shift));
@@ -464,12 +615,7 @@ kap_sample_rows_kernel(const SampleParams p)
     }
 
     // ---- the draw: running sums in index order over threads, CTAs, and then inside one thread's strip
-    const float min_p = p.min_p ? fminf(p.min_p[r], 1.f) : 0.f;
-    if (min_p > 0.f) {                                             // a cut of its own: logits from the least float with weight enough on
-        const uint32_t least = logit_image(__double2float_ru(x_max + (double)t * log((double)min_p)));
-        const uint32_t d = least < top ? top - least : 0u;
-        if (d < cut) { cut = d; quota = 0x7fffffff; }
-    }
+    if (min_p_cut < cut) { cut = min_p_cut; quota = 0x7fffffff; }
     int tie_rank = 0;                                              // equal ones before this thread's strip
     if (quota != 0x7fffffff) {
         int ties = 0;
@@ -488,17 +634,7 @@ kap_sample_rows_kernel(const SampleParams p)
         for (int c = 0; c < rank; ++c) tie_rank += sh.ties[c];
     }
     // (images below top - cut, the padding's 0 among them, are cut)
-    double sum;
-    if (quota == 0x7fffffff) {
-        sum = strip_weight(0u, cut + 1u, cut == furthest);
-    } else {
-        sum = 0.0;
-        int tr = tie_rank;
-        for (int i = 0; i < p.strip; ++i) {
-            const uint32_t d = top - mine[i];
-            if (d < cut || (d == cut && tr++ < quota)) sum += weight(mine[i]);
-        }
-    }
+    const double sum = quota != 0x7fffffff ? strip_weight(0u, cut, tie_rank, quota) : cut == furthest ? strip_weight_all(cut + 1u) : strip_weight(0u, cut + 1u, 0, 0);
     // Running sums one after the other, so that a thread without weight ends exactly where the one before it does, and the end of a
     // warp or a CTA is the same number as the start of the next: one thread, with weight, holds the target.
     double run = 0.0;
@@ -516,8 +652,7 @@ kap_sample_rows_kernel(const SampleParams p)
     meet();
     double total = 0.0, before = 0.0, cta_end = 0.0;
     for (int c = 0; c < C; ++c) { if (c == rank) before = total; total += sh.kept_sum[c]; if (c == rank) cta_end = total; }
-    const double u01 = (double)p.uniform[r];
-    const double target = u01 >= 0.0 ? fmin(u01 * total, total * 0.99999999999999978) : 0.0;
+    const double target = draw_at(total);
     if (!(before <= target && target < cta_end)) return;           // another CTA's (no remote access from here on)
     const double inner = offset + run, prev = __shfl_up_sync(0xffffffffu, inner, 1);
     const double start = before + (lane == 0 ? offset : prev), end = before + inner;
