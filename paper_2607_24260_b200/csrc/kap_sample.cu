@@ -50,19 +50,25 @@ __device__ __forceinline__ double wide_logit(uint32_t u) {
     const uint32_t mag = (u ^ flip) & 0x7fffffffu;
     return __hiloint2double((int)(((mag >> 3) + 0x38000000u) | (flip & 0x80000000u)), (int)(mag << 29));
 }
+// the same from the logit itself (-0 = +0); any number for NaN
+__device__ __forceinline__ double wide_float(float v) {
+    const uint32_t u = __float_as_uint(v + 0.0f), mag = u & 0x7fffffffu;
+    return __hiloint2double((int)(((mag >> 3) + 0x38000000u) | (u & 0x80000000u)), (int)(mag << 29));
+}
 // 2^t for t <= 0 in 64 bits, to be discarded below the smallest normal number (`vanishes`).  t = n + f with |f| <= 1/2 (a sum with
 // 1.5 2^52 holds n in its low word), 2^f by the polynomial of degree 9 of least largest relative error there (1.3e-14; Remez
 // exchange), its coefficients in constant memory, from where the products take them without a register.
 __constant__ double kExp2[10] = {1.0150336270671598e-07, 1.3259405604554393e-06, 1.5252984841153802e-05, 0.00015403434948094166, 0.0013333557617599588,
                                  0.009618129192067212, 0.055504108668685645, 0.24022650695649653, 0.693147180559871, 1.0000000000000127};
 __device__ __forceinline__ bool vanishes(double t) { return (uint32_t)__double2hiint(t) > 0xc08ff000u; }       // t < -1022
-__device__ __forceinline__ double exp2_f64(double t) {
-    const double s = t + 6755399441055744.0, f = t - (s - 6755399441055744.0);
+__device__ __forceinline__ double exp2_f64(double d, double scale) {           // 2^(d scale)
+    const double s = fma(d, scale, 6755399441055744.0), f = fma(d, scale, 6755399441055744.0 - s);
     double y = kExp2[0];
 #pragma unroll
     for (int i = 1; i < 10; ++i) y = fma(y, f, kExp2[i]);
     return __hiloint2double(__double2hiint(y) + (__double2loint(s) << 20), __double2loint(y));
 }
+__device__ __forceinline__ double exp2_f64(double t) { return exp2_f64(t, 1.0); }
 
 struct SampleParams {
     const void* logits;
@@ -687,6 +693,230 @@ kap_sample_rows_kernel(const SampleParams p)
     }
 }
 
+// ------------------------------------------------------------------ many rows without a filter
+// The draw alone: one pass over a row.  A warp reads 512 consecutive logits at a time into registers, 16 a lane, keeps their largest
+// and the sum of their weights relative to it (64 bits).  The cluster agrees on the row's largest logit, puts the sums on it and adds
+// them up in index order; the warp whose sums hold the target reads that block once more and walks through it.
+constexpr int kDrawThreads = 256, kDrawWarps = kDrawThreads / 32;
+constexpr int kDrawBlock = 512, kDrawPer = kDrawBlock / 32;
+constexpr int kDrawBlocks = kMaxCluster * kSampleThreads * kMaxStrip / kDrawBlock + 1;      // of a row at most; one more for an unaligned start
+constexpr int kDrawRounds = (kDrawBlocks + kDrawThreads - 1) / kDrawThreads;
+
+struct DrawShared {
+    double sum[kDrawBlocks];
+    float top[kDrawBlocks];
+    uint32_t best[kMaxCluster];                    // filled by all CTAs of the cluster, one entry each
+    double total[kMaxCluster];
+    double warp_sum[kDrawWarps];
+    uint32_t warp_top[kDrawWarps];
+    int32_t first_block;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kDrawThreads, 4)
+kap_sample_draw_kernel(const SampleParams p)
+{
+    __shared__ __align__(16) DrawShared sh;
+    constexpr int kVec = 16 / (int)sizeof(T), kLoads = kDrawPer / kVec;
+    const int C = p.cluster, r = blockIdx.x / C, rank = blockIdx.x % C, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (C > 1) cluster_arrive();                                   // (its wait: every peer runs before anybody writes to it)
+    const T* row = reinterpret_cast<const T*>(p.logits) + (long long)r * p.row_stride;
+    // places are counted from the 16-byte boundary at or before the row's first logit; `skip` of them are not the row's
+    const int skip = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)), end = skip + p.vocab;
+    const int all_blocks = (end + kDrawBlock - 1) / kDrawBlock, per_cta = (all_blocks + C - 1) / C;
+    const int block0 = min(all_blocks, rank * per_cta), n_blocks = min(all_blocks, block0 + per_cta) - block0;
+    const float t = p.temperature ? p.temperature[r] : 1.f;
+    const double u01 = (double)p.uniform[r], per_bit = 1.4426950408889634 / (double)t;
+    // logit e of load l of this lane has the place place_of(b, l) + e
+    auto place_of = [&](int b, int l) { return (block0 + b) * kDrawBlock + l * (32 * kVec) + lane * kVec; };
+    auto load = [&](int b, uint4 (&raw)[kLoads]) {                 // places that are not the row's: all bits set, which is NaN
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const int i = place_of(b, l);
+            if (i >= skip && i + kVec <= end) {
+                raw[l] = __ldcs(reinterpret_cast<const uint4*>(row + (i - skip)));
+            } else {
+                raw[l] = make_uint4(0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu);
+                T* e = reinterpret_cast<T*>(&raw[l]);
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+                    if (i + j >= skip && i + j < end) e[j] = row[i + j - skip];
+            }
+        }
+    };
+    auto logit = [](const uint4 (&raw)[kLoads], int q) { return as_float(reinterpret_cast<const T*>(&raw[q / kVec])[q % kVec]); };
+    // 2^((v - top) / T / ln 2); nothing for -inf and NaN, nor below the smallest normal number; beside +inf only +inf has weight
+    auto bar_of = [](float top) { return top == INFINITY ? 3.402823466e38f : -INFINITY; };
+    const uint32_t far = (uint32_t)__double2hiint(-1021.0 / per_bit);      // (-inf for an endless T)
+    auto weight = [&](float v, double from, float bar) {
+        const double d = wide_float(v) - from, w = exp2_f64(d, per_bit);
+        return v > bar && (uint32_t)__double2hiint(d) < far ? w : 0.0;
+    };
+
+    uint32_t best = 0u;
+    uint4 raw[kLoads];
+    if (warp < n_blocks) load(warp, raw);
+    for (int b = warp; b < n_blocks; b += kDrawWarps) {
+        float top = -INFINITY;                                     // (fmaxf passes over NaN)
+        uint4 now[kLoads];
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) now[l] = raw[l];
+        if (b + kDrawWarps < n_blocks) load(b + kDrawWarps, raw);
+#pragma unroll
+        for (int q = 0; q < kDrawPer; ++q) top = fmaxf(top, logit(now, q));
+        const uint32_t image = __reduce_max_sync(0xffffffffu, logit_image(top));
+        best = max(best, image);
+        const double from = wide_logit(image);
+        const float bar = bar_of(image_logit(image));
+        double s0 = 0.0, s1 = 0.0;
+#pragma unroll
+        for (int q = 0; q < kDrawPer; q += 2) {
+            s0 += weight(logit(now, q), from, bar);
+            s1 += weight(logit(now, q + 1), from, bar);
+        }
+        s0 += s1;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) s0 += __shfl_xor_sync(0xffffffffu, s0, d);
+        if (lane == 0) { sh.top[b] = image_logit(image); sh.sum[b] = s0; }
+    }
+    if (lane == 0) sh.warp_top[warp] = best;
+    if (tid == 0) sh.first_block = n_blocks;
+    __syncthreads();
+    if (C > 1) cluster_wait();
+    auto to_all = [&](auto* slot, auto v) { put_remote(map_to_cta(smem_u32(slot + rank), tid), v); };
+    auto meet = [&] { if (C > 1) cluster_sync(); else __syncthreads(); };
+    if (tid < C) {
+        best = 0u;
+        for (int w = 0; w < kDrawWarps; ++w) best = max(best, sh.warp_top[w]);
+        to_all(reinterpret_cast<int32_t*>(sh.best), (int32_t)best);
+    }
+    meet();
+    uint32_t top = 0u;
+    for (int c = 0; c < C; ++c) top = max(top, sh.best[c]);
+    if (top <= kImageMinusInf) {                                   // no token at all
+        if (rank == 0 && tid == 0) {
+            p.token[r] = -1;
+            if (p.logprob) p.logprob[r] = -INFINITY;
+        }
+        return;
+    }
+    const float top_logit = image_logit(top);
+    if (!(t > 0.f)) {                                              // greedy: the first CTA that has the largest logit
+        int c = 0;
+        while (sh.best[c] != top) ++c;
+        if (c != rank) return;
+        for (int b = tid; b < n_blocks; b += kDrawThreads)
+            if (sh.top[b] == top_logit) atomicMin(&sh.first_block, b);
+        __syncthreads();
+        if (warp == 0) {
+            load(sh.first_block, raw);
+            int at = 0x7fffffff;
+#pragma unroll
+            for (int q = kDrawPer - 1; q >= 0; --q)
+                if (logit(raw, q) == top_logit) at = place_of(sh.first_block, q / kVec) + q % kVec;
+            at = __reduce_min_sync(0xffffffffu, at);
+            if (lane == 0) {
+                p.token[r] = at - skip;
+                if (p.logprob) p.logprob[r] = 0.f;
+            }
+        }
+        return;
+    }
+    const double x_max = wide_logit(top);
+    const float bar = bar_of(top_logit);
+    // Running sums one after the other: consecutive blocks to a thread, then threads, warps and CTAs, so that a thread without weight
+    // ends exactly where the one before it does, and the end of a warp or a CTA is the same number as the start of the next.
+    const int per_thread = (n_blocks + kDrawThreads - 1) / kDrawThreads, own0 = min(n_blocks, tid * per_thread), own1 = min(n_blocks, own0 + per_thread);
+    double mine = 0.0;
+    for (int b = own0; b < own1; ++b) {
+        const double e = (wide_float(sh.top[b]) - x_max) * per_bit;
+        const double s = sh.top[b] > bar && !vanishes(e) ? exp2_f64(e) * sh.sum[b] : 0.0;
+        sh.sum[b] = s;                                             // (this thread's alone, until the walk below)
+        mine += s;
+    }
+    double run = 0.0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const double s = __shfl_sync(0xffffffffu, mine, j);
+        if (lane >= j) run += s;
+    }
+    if (lane == 31) sh.warp_sum[warp] = run;
+    __syncthreads();
+    double cta = 0.0, offset = 0.0;
+    for (int w = 0; w < kDrawWarps; ++w) { if (w == warp) offset = cta; cta += sh.warp_sum[w]; }
+    if (tid < C) to_all(sh.total, cta);
+    meet();                                                        // (no remote access from here on)
+    double total = 0.0, before = 0.0, cta_end = 0.0;
+    for (int c = 0; c < C; ++c) {
+        if (c == rank) before = total;
+        total += sh.total[c];
+        if (c == rank) cta_end = total;
+    }
+    const double target = u01 >= 0.0 ? fmin(u01 * total, total * 0.99999999999999978) : 0.0;
+    if (!(before <= target && target < cta_end)) return;
+    const double inner = offset + run, prev = __shfl_up_sync(0xffffffffu, inner, 1);
+    const double start = before + (lane == 0 ? offset : prev);
+    const uint32_t holder = __ballot_sync(0xffffffffu, start <= target && target < before + inner);
+    if (!holder) return;
+    const int who = __ffs(holder) - 1;
+    double at = __shfl_sync(0xffffffffu, start, who), upto = at;
+    const int b0 = __shfl_sync(0xffffffffu, own0, who), b1 = __shfl_sync(0xffffffffu, own1, who);
+    int block = -1;                                                // the last one with weight when a rounding falls short
+    for (int b = b0; b < b1; ++b) {
+        const double s = sh.sum[b];
+        if (!(s > 0.0)) continue;
+        if (block >= 0 && upto > target) break;
+        block = b;
+        at = upto;
+        upto += s;
+    }
+    load(block, raw);
+    int found = -1;                                                // likewise
+    float chosen = 0.f;
+    for (int l = 0; l < kLoads; ++l) {
+        // this load's logits in index order: a lane's one after the other, lane by lane
+        uint4 part = raw[0];
+#pragma unroll
+        for (int j = 1; j < kLoads; ++j) if (l == j) part = raw[j];
+        float v[kVec];
+        double w[kVec], lane_sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+            v[j] = as_float(reinterpret_cast<const T*>(&part)[j]);
+            w[j] = weight(v[j], x_max, bar);
+            lane_sum += w[j];
+        }
+        double to = at;
+        for (int j = 0; j < 32; ++j) {
+            const double s = __shfl_sync(0xffffffffu, lane_sum, j);
+            if (lane > j) to += s;
+        }
+        int place = -1;
+        float v_place = 0.f;
+        bool past = false;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j)
+            if (w[j] > 0.0 && !past) {
+                to += w[j];
+                place = place_of(block, l) + j;
+                v_place = v[j];
+                past = to > target;
+            }
+        const uint32_t over = __ballot_sync(0xffffffffu, past), weighed = __ballot_sync(0xffffffffu, place >= 0);
+        if (weighed) {
+            const int pick = over ? __ffs(over) - 1 : 31 - __clz(weighed);
+            found = __shfl_sync(0xffffffffu, place, pick);
+            chosen = __shfl_sync(0xffffffffu, v_place, pick);
+        }
+        if (over) break;
+        at = __shfl_sync(0xffffffffu, to, 31);
+    }
+    if (lane == 0) {
+        p.token[r] = found - skip;
+        if (p.logprob) p.logprob[r] = (float)(((wide_float(chosen) - x_max) * per_bit - log2(total)) * 0.69314718055994531);
+    }
+}
+
 }  // namespace
 }  // namespace kap
 
@@ -706,33 +936,44 @@ extern "C" kap_status kap_sample_tokens(
     if (!logits || !uniform || !token) return fail(KAP_ERR_INVALID_ARG, "NULL pointer");
     if (reinterpret_cast<uintptr_t>(logits) & (logits_type == KAP_LOGITS_F32 ? 3 : 1))
         return fail(KAP_ERR_INVALID_ARG, "logits are not aligned to their type");
-    // CTAs of a row: as many as keep two CTAs on an SM (33 logits a thread), and more while there are SMs to spare
-    auto strip_of = [&](int c) { const int s = ((vocab + c - 1) / c + kSampleThreads - 1) / kSampleThreads; return s | 1; };
-    int C = 1;
-    while (C < kMaxCluster && strip_of(C) > 33) C *= 2;
-    while (C < kMaxCluster && strip_of(C) > 5 && (int64_t)rows * C * 2 <= 148) C *= 2;
-    SampleParams p{logits, row_stride, vocab, 0, strip_of(C), C, temperature, top_p, min_p, uniform, top_k, token, logprob};
-    p.slice = p.strip * kSampleThreads;
+    SampleParams p{logits, row_stride, vocab, 0, 0, 1, temperature, top_p, min_p, uniform, top_k, token, logprob};
+    int& C = p.cluster;                                            // CTAs of a row
+    const bool f32 = logits_type == KAP_LOGITS_F32;
+    void (*kernel)(SampleParams);
+    cudaLaunchConfig_t cfg{};
+    const int draw_blocks = (vocab + kDrawBlock - 1) / kDrawBlock;
+    cudaError_t e = cudaSuccess;
+    if (!top_k && !top_p && !min_p && (draw_blocks > 32 || rows > 148)) {
+        // (three CTAs on an SM and a block for each of their warps; two CTAs of long rows, whose tail one CTA would stretch)
+        kernel = f32 ? kap_sample_draw_kernel<float> : kap_sample_draw_kernel<__nv_bfloat16>;
+        while (C < 8 && C * 2 * kDrawWarps <= draw_blocks && (int64_t)rows * C * 2 <= 3 * 148) C *= 2;
+        if (C == 1 && draw_blocks >= 128) C = 2;
+        cfg.blockDim = dim3(kDrawThreads);
+    } else {
+        // as many CTAs as keep two of them on an SM (33 logits a thread), and more while there are SMs to spare
+        kernel = f32 ? kap_sample_rows_kernel<float> : kap_sample_rows_kernel<__nv_bfloat16>;
+        auto strip_of = [&](int c) { const int s = ((vocab + c - 1) / c + kSampleThreads - 1) / kSampleThreads; return s | 1; };
+        while (C < kMaxCluster && strip_of(C) > 33) C *= 2;
+        while (C < kMaxCluster && strip_of(C) > 5 && (int64_t)rows * C * 2 <= 148) C *= 2;
+        p.strip = strip_of(C);
+        p.slice = p.strip * kSampleThreads;
+        auto smem_for = [](int slice) { return (sizeof(SampleShared) + 15) / 16 * 16 + ((size_t)slice + 4) * sizeof(uint32_t); };
+        static_assert((sizeof(SampleShared) + 15) / 16 * 16 + ((size_t)kSampleThreads * kMaxStrip + 4) * 4 <= 232448, "more than 227 KiB of shared memory");
+        cfg.blockDim = dim3(kSampleThreads);
+        cfg.dynamicSmemBytes = smem_for(p.slice);
+        // (attributes belong to the current device; setting them again costs less than a microsecond)
+        e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_for(kSampleThreads * kMaxStrip));
+        if (e == cudaSuccess && C > 8) e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    }
     if (rows > 0x7fffffff / C) return fail(KAP_ERR_UNSUPPORTED, "%d rows", rows);
-    auto smem_for = [](int slice) { return (sizeof(SampleShared) + 15) / 16 * 16 + ((size_t)slice + 4) * sizeof(uint32_t); };
-    static_assert((sizeof(SampleShared) + 15) / 16 * 16 + ((size_t)kSampleThreads * kMaxStrip + 4) * 4 <= 232448, "more than 227 KiB of shared memory");
-    const void* fn = logits_type == KAP_LOGITS_F32 ? (const void*)kap_sample_rows_kernel<float> : (const void*)kap_sample_rows_kernel<__nv_bfloat16>;
-    // (attributes belong to the current device; setting them again costs less than a microsecond)
-    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_for(kSampleThreads * kMaxStrip));
-    if (e == cudaSuccess && C > 8) e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)rows * (unsigned)C);
-    cfg.blockDim = dim3(kSampleThreads);
-    cfg.dynamicSmemBytes = smem_for(p.slice);
     cfg.stream = (cudaStream_t)cuda_stream;
     cfg.attrs = attr;
     cfg.numAttrs = C > 1 ? 1 : 0;
-    if (e == cudaSuccess)
-        e = logits_type == KAP_LOGITS_F32 ? cudaLaunchKernelEx(&cfg, kap_sample_rows_kernel<float>, p)
-                                          : cudaLaunchKernelEx(&cfg, kap_sample_rows_kernel<__nv_bfloat16>, p);
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, p);
     if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "kap_sample_tokens launch failed: %s", cudaGetErrorString(e));
     count_launch();
     return KAP_OK;

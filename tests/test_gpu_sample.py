@@ -186,6 +186,36 @@ def test_large_vocabularies(vocab):
         check(f32(x), rng.random(3), **settings(rng, 3))
 
 
+@pytest.mark.parametrize("vocab,dtype", [(1, torch.float32), (5, torch.bfloat16), (129, torch.float32), (4099, torch.bfloat16), (50257, torch.float32),
+                                         (128256, torch.float32), (128256, torch.bfloat16), (262144, torch.float32)])
+def test_many_rows_without_filters(vocab, dtype):
+    rng = np.random.default_rng(vocab)
+    rows = 70 if vocab < 60000 else 52
+    x = rng.normal(0, 1, (rows, vocab)) * rng.choice([0.0, 0.01, 1.0, 3.0, 50.0], (rows, 1))
+    x[0, rng.integers(0, vocab, 3)] = np.inf
+    x[1] = -np.inf
+    x[2, rng.permutation(vocab)[:vocab - 1]] = np.nan
+    x[3, rng.permutation(vocab)[:max(0, vocab - 40)]] = -np.inf
+    x[4, rng.permutation(vocab)[:max(0, vocab - 7)]] = LOWEST
+    t, u = rng.uniform(0.2, 2.0, rows), rng.random(rows)
+    t[5:9] = [0.0, -1.0, 1e-6, 1e30]
+    t[0] = 3e38 if vocab > 3 else 1.0
+    x[12, ::2], t[12] = -0.0, 1e-37
+    u[9:12] = [0.0, 1.0 - 2.0 ** -24, 2.0 ** -24]
+    store = torch.full((rows, vocab + 9), 60.0, device=gu.DEV, dtype=dtype)
+    for offset in (0, 1, 3):
+        view = store[:, offset:offset + vocab]
+        view.copy_(torch.from_numpy(x))
+        check(view, u, t=t)
+        store.fill_(60.0)
+    # the same rows, few at a time, go another way and draw the same tokens
+    logits = torch.from_numpy(x).to(gu.DEV).to(dtype)
+    many = run(logits, u, t)
+    for r0 in range(0, rows, 20):
+        some = run(logits[r0:r0 + 20].contiguous(), u[r0:r0 + 20], t[r0:r0 + 20])
+        np.testing.assert_array_equal(some[0], many[0][r0:r0 + 20])
+
+
 def test_frequencies_follow_the_distribution():
     # 2^14 evenly spread numbers: every token comes within one of its share of them
     x = np.array([[0.0, 1.0, 2.0, -1.0, 0.5]])
