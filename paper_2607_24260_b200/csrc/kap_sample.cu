@@ -50,11 +50,6 @@ __device__ __forceinline__ double wide_logit(uint32_t u) {
     const uint32_t mag = (u ^ flip) & 0x7fffffffu;
     return __hiloint2double((int)(((mag >> 3) + 0x38000000u) | (flip & 0x80000000u)), (int)(mag << 29));
 }
-// the same from the logit itself (-0 = +0); any number for NaN
-__device__ __forceinline__ double wide_float(float v) {
-    const uint32_t u = __float_as_uint(v + 0.0f), mag = u & 0x7fffffffu;
-    return __hiloint2double((int)(((mag >> 3) + 0x38000000u) | (u & 0x80000000u)), (int)(mag << 29));
-}
 // 2^t for t <= 0 in 64 bits, to be discarded below the smallest normal number (`vanishes`).  t = n + f with |f| <= 1/2 (a sum with
 // 1.5 2^52 holds n in its low word), 2^f by the polynomial of degree 9 of least largest relative error there (1.3e-14; Remez
 // exchange), its coefficients in constant memory, from where the products take them without a register.
@@ -745,12 +740,15 @@ kap_sample_draw_kernel(const SampleParams p)
         }
     };
     auto logit = [](const uint4 (&raw)[kLoads], int q) { return as_float(reinterpret_cast<const T*>(&raw[q / kVec])[q % kVec]); };
-    // 2^((v - top) / T / ln 2); nothing for -inf and NaN, nor below the smallest normal number; beside +inf only +inf has weight
-    auto bar_of = [](float top) { return top == INFINITY ? 3.402823466e38f : -INFINITY; };
+    // s += 2^((v - from) / T / ln 2), `from` the largest logit; nothing for -inf and NaN, nor far below the smallest normal number; beside
+    // +inf, which stands for the largest finite number, only +inf has weight.  (The conversion runs beside the sums, on its own pipe.)
+    constexpr float kLargest = 3.402823466e38f;
+    auto widen = [](float v) { return (double)fminf(v, kLargest); };
+    auto bar_of = [](float top) { return top == INFINITY ? kLargest : -INFINITY; };
     const uint32_t far = (uint32_t)__double2hiint(-1021.0 / per_bit);      // (-inf for an endless T)
-    auto weight = [&](float v, double from, float bar) {
-        const double d = wide_float(v) - from, w = exp2_f64(d, per_bit);
-        return v > bar && (uint32_t)__double2hiint(d) < far ? w : 0.0;
+    auto add_weight = [&](double& s, float v, double from, float bar) {
+        const double d = widen(v) - from, w = exp2_f64(d, per_bit);
+        if (v > bar && (uint32_t)__double2hiint(d) < far) s += w;
     };
 
     uint32_t best = 0u;
@@ -766,18 +764,18 @@ kap_sample_draw_kernel(const SampleParams p)
         for (int q = 0; q < kDrawPer; ++q) top = fmaxf(top, logit(now, q));
         const uint32_t image = __reduce_max_sync(0xffffffffu, logit_image(top));
         best = max(best, image);
-        const double from = wide_logit(image);
-        const float bar = bar_of(image_logit(image));
+        const float block_top = image_logit(image), bar = bar_of(block_top);
+        const double from = widen(block_top);
         double s0 = 0.0, s1 = 0.0;
 #pragma unroll
         for (int q = 0; q < kDrawPer; q += 2) {
-            s0 += weight(logit(now, q), from, bar);
-            s1 += weight(logit(now, q + 1), from, bar);
+            add_weight(s0, logit(now, q), from, bar);
+            add_weight(s1, logit(now, q + 1), from, bar);
         }
         s0 += s1;
 #pragma unroll
         for (int d = 16; d; d >>= 1) s0 += __shfl_xor_sync(0xffffffffu, s0, d);
-        if (lane == 0) { sh.top[b] = image_logit(image); sh.sum[b] = s0; }
+        if (lane == 0) { sh.top[b] = block_top; sh.sum[b] = s0; }
     }
     if (lane == 0) sh.warp_top[warp] = best;
     if (tid == 0) sh.first_block = n_blocks;
@@ -822,15 +820,16 @@ kap_sample_draw_kernel(const SampleParams p)
         }
         return;
     }
-    const double x_max = wide_logit(top);
+    const double x_max = widen(top_logit);
     const float bar = bar_of(top_logit);
     // Running sums one after the other: consecutive blocks to a thread, then threads, warps and CTAs, so that a thread without weight
     // ends exactly where the one before it does, and the end of a warp or a CTA is the same number as the start of the next.
     const int per_thread = (n_blocks + kDrawThreads - 1) / kDrawThreads, own0 = min(n_blocks, tid * per_thread), own1 = min(n_blocks, own0 + per_thread);
     double mine = 0.0;
     for (int b = own0; b < own1; ++b) {
-        const double e = (wide_float(sh.top[b]) - x_max) * per_bit;
-        const double s = sh.top[b] > bar && !vanishes(e) ? exp2_f64(e) * sh.sum[b] : 0.0;
+        double s = 0.0;
+        add_weight(s, sh.top[b], x_max, bar);
+        s *= sh.sum[b];
         sh.sum[b] = s;                                             // (this thread's alone, until the walk below)
         mine += s;
     }
@@ -883,7 +882,8 @@ kap_sample_draw_kernel(const SampleParams p)
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
             v[j] = as_float(reinterpret_cast<const T*>(&part)[j]);
-            w[j] = weight(v[j], x_max, bar);
+            w[j] = 0.0;
+            add_weight(w[j], v[j], x_max, bar);
             lane_sum += w[j];
         }
         double to = at;
@@ -913,7 +913,7 @@ kap_sample_draw_kernel(const SampleParams p)
     }
     if (lane == 0) {
         p.token[r] = found - skip;
-        if (p.logprob) p.logprob[r] = (float)(((wide_float(chosen) - x_max) * per_bit - log2(total)) * 0.69314718055994531);
+        if (p.logprob) p.logprob[r] = (float)(((widen(chosen) - x_max) * per_bit - log2(total)) * 0.69314718055994531);
     }
 }
 
