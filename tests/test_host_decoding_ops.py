@@ -93,3 +93,10 @@ def test_shared_prefix_refusals(change, code):
 def test_shared_prefix_items_of_good_groups():
     assert _items() >= 1
     assert kap.shared_prefix_items(np.array([1]), np.array([1]), np.array([0, 1]), np.array([0])) >= 1
+
+
+def test_sample_tokens_refuses_rows_that_do_not_fit():
+    most = 16 * 512 * 99
+    assert _sample(vocab=most + 1, stride=most + 1) == kap.ERR_UNSUPPORTED
+    assert b"vocab" in kap.lib().kap_last_error()
+    assert _sample(vocab=100000, stride=100000, rows=0x7fffffff, k=A) == kap.ERR_UNSUPPORTED          # more CTAs than a grid has
