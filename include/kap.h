@@ -582,6 +582,10 @@ kap_status kap_append_kv_rope(
  * context of a group may hold anything.  A context shorter than its group's shared prefix is allowed (the rows
  * see what lies below their own position) as long as the shared pages hold finite values.
  * A row that sees no token gets out = 0, lse = -inf.  out rows beyond q_indptr[batch] are left alone.
+ * Reported through kap_workspace_check: KAP_ERR_DEVICE_INDEX for a page outside the pool, a context beyond 16 list_len[b], a
+ * q_indptr that differs from the schedule's row counts (the results of such a call are not defined; nothing outside the
+ * arrays is touched).  One workspace serves one call at a time: calls, and graphs that hold them, which may run at the
+ * same time on two streams need a workspace each.
  * Errors: as kap_schedule and kap_verify_attn, plus KAP_ERR_INVALID_ARG for groups that do not
  * cover the batch in order, a prefix longer than a sequence's list, or an sm_scale that is not a positive number.
  */
@@ -632,13 +636,16 @@ enum {
  *   token[r]          the lowest index i such that the kept weights of tokens 0 .. i sum to more
  *                     than u times the sum of all kept weights (u in [0, 1))
  *   logprob[r]        ln(w_token / sum of kept weights)
- * Sums and comparisons are in 64 bits.  T <= 0 (or NaN): the lowest index of the largest logit,
- * logprob 0.  NaN and -inf logits have no weight; if +inf occurs only the +inf tokens do.  A row
- * without any token of weight (all -inf or NaN) gives token -1, logprob -inf.  A parameter array
- * that is NULL switches its filter off for all rows (temperature: 1).  Results do not depend on
- * timing or on the other rows.
+ * Sums and comparisons are in 64 bits (weights to about 1e-14 of themselves; weights below 2^-1021 of the largest count
+ * as none).  T <= 0 (or NaN): the lowest index of the largest logit, logprob 0.  NaN and -inf logits have no weight; if
+ * +inf occurs only the +inf tokens do.  A row without any token of weight (all -inf or NaN) gives token -1, logprob -inf.
+ * min_p above 1 counts as 1, u outside [0, 1) as its nearer end, NaN as 0.  A parameter array that is NULL switches its
+ * filter off for all rows (temperature: 1).  Results do not depend on timing or on the other rows' contents; the number
+ * of rows chooses the order in which a row is summed, so that a u within about 1e-13 of a border between two tokens may fall
+ * on either side of it.  logits may be a view with padding behind its rows; nothing of the padding is used.
  * Errors: KAP_ERR_INVALID_ARG (NULL or misaligned pointer, vocab < 1, row_stride < vocab, negative rows),
- * KAP_ERR_UNSUPPORTED (logits_type), KAP_ERR_CUDA.  Asynchronous on cuda_stream.
+ * KAP_ERR_UNSUPPORTED (logits_type, vocab above 811008, more rows than a grid can hold), KAP_ERR_CUDA.  Asynchronous on
+ * cuda_stream, without a workspace; can be captured into a CUDA graph.
  */
 kap_status kap_sample_tokens(
     const void* logits,                /* DEVICE, row r starts at element r * row_stride */

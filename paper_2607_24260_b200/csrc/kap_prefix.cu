@@ -52,7 +52,7 @@ kap_status upload_schedule(kap_workspace* ws, const PrefixSchedule& s, int32_t b
     if (ws->schedule_key) ws->schedule_key->clear();
     ws->batch = batch; ws->num_q_heads = hq; ws->num_kv_heads = hkv; ws->total_rows = s.total_rows;
     ws->n_items = (int32_t)s.items.size(); ws->n_groups = (int32_t)s.units.size(); ws->prefix_segments = (int32_t)s.segments.size();
-    ws->ring_slots = s.ring_slots;
+    ws->ring_slots = kPrefixRingSlots;
     ws->max_splits = 1;
     for (const PrefixUnit& u : s.units) ws->max_splits = std::max(ws->max_splits, u.n_states);
     return KAP_OK;
@@ -153,12 +153,15 @@ extern "C" kap_status kap_shared_prefix_attn(
         else KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<false>, kv, q_map, p));
         count_launch();
     }
-    // Few cells: one a warp, and four warps a cell when its states are more than one batch of loads.  Many: four heads a warp (one
-    // metadata chain for all of them), four warps a set while the sets are one wave of CTAs.
+    // Few cells: one a warp.  Many: four heads a warp, one metadata chain for all of them.  (64 sequences with 32K shared tokens: 61.3 us
+    // for the call, one head a warp 63.7; 16 sequences of two rows with 64K 71.3 against 74.6.  4 sequences with 512 / 8K tokens: one head a
+    // warp 9.7 / 18.9, four 10.7 / 23.7.)  More than four states: four warps a set, while the sets are one wave of CTAs (64 sequences with
+    // 32K, 20 states: 61.3 against 71.7 with one warp; 4 sequences with 512, eight states 8.4 against 8.8; 256 sequences in two groups,
+    // five states, several waves: 56.1 with one warp, 60.1 with four).
     const int64_t cells = ws->total_rows * num_q_heads, one_wave = (int64_t)ws->sm_count * 6;
     const int H = cells <= one_wave ? 1 : G >= 4 ? 4 : G;
     const int64_t sets = cells / H;
-    const bool wide = ws->max_splits > (H == 1 ? 8 : 4) && sets <= one_wave;
+    const bool wide = ws->max_splits > 4 && sets <= one_wave;
     cfg.gridDim = dim3((unsigned)(wide ? sets : (sets + 3) / 4));
     cfg.blockDim = dim3(128);
     cfg.dynamicSmemBytes = 0;

@@ -8,6 +8,9 @@ constexpr int kPrefixStepPages = 5;                    // a step of the tcgen05 
 constexpr int kPrefixStepTokens = kPrefixStepPages * kPageSize;
 constexpr int kPrefixTileRows = 128;                   // query rows of one tile (TMEM lanes)
 constexpr int kPrefixUnitRows = 2 * kPrefixTileRows;
+// Ring of the split kernel, 8 KiB a slot.  More for grids that leave SMs room only cost start-up (4 sequences with 512 shared tokens, 96
+// CTAs: 8.8 us with 8 slots, 9.7 with 24).
+constexpr int kPrefixRingSlots = 8;
 
 enum { kSegPair = 1, kSegTwoStates = 2 };
 
@@ -40,7 +43,6 @@ struct PrefixSchedule {
     std::vector<PrefixSeq> seqs;
     std::vector<PrefixRow> rows;
     int32_t n_cta = 0, total_rows = 0;
-    int32_t ring_slots = 8;                            // of the split kernel
     int64_t state_rows = 0;
 };
 // Places of the arrays inside the workspace's metadata: items and segments in the first array, units in the second, sequences,

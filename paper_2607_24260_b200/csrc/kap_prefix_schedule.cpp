@@ -21,7 +21,8 @@ constexpr int32_t kSplitCtasPerSm = 3;
 constexpr int32_t kMinSplitPages = 4;                          // a page for each of a CTA's warps
 constexpr int32_t kMaxSplitPages = 1024;                       // page ids a CTA holds: 1600
 // Short parts of at most 16 rows may go four KV heads to a CTA, one per warp, instead of a CTA each: for many short lists a CTA is
-// mostly start-up.  A warp alone takes about a microsecond a page, so long lists do not belong there.
+// mostly start-up (256 sequences with 19 own pages: the call takes 56 us, with a CTA for each head 67).  A warp alone takes about a
+// microsecond a page, so long lists do not belong there.
 constexpr int32_t kByHeadPages = 48;
 // What a CTA of the split kernel takes, in pages that one warp group streams (about a microsecond each): its start and its end as much
 // as five.  Measured on B200: 384 slices of 16 pages of 32 rows (two groups, one wave) 14.5 us, 768 of 8 pages 21.5; 384 of 16 pages
@@ -194,8 +195,6 @@ kap_status build_prefix_schedule(int32_t batch, const int32_t* list_len, const i
     }
     std::stable_sort(timed.begin(), timed.end(), [](const Timed& a, const Timed& b) { return a.pages > b.pages; });
     for (const Timed& t : timed) out.items.push_back(t.item);
-    // fewer CTAs than fit: deeper rings
-    out.ring_slots = (int64_t)timed.size() <= sm_count ? 24 : (int64_t)timed.size() <= 2 * (int64_t)sm_count ? 12 : 8;
 
     // ---- tcgen05 kernel: the tapes of all (group, KV head, bundle of row blocks) end to end, cut into equal pieces; bundle b of
     // `width` CTAs takes piece b, CTA p of it row block p

@@ -11,13 +11,16 @@
 // order of the atomics does not matter): two or three levels instead of 32 bisections.  For top-p the counts give bounds of
 // the weight in every interval; the weight above the remaining range is summed exactly.
 //
-// All sums are held in 64 bits and added in an order that the row's length alone fixes: the token is decided by comparing long
+// All sums are held in 64 bits and added in an order that the shape of the call alone fixes: the token is decided by comparing long
 // sums, and 32-bit ones over 128 256 weights would move a border in every few hundred rows.  exp is a
 // 64-bit polynomial after reduction to a power of two (exp2_f64 below).
 //
-// Layout: one cluster of up to 16 CTAs per row, 512 threads each; the row is read once, into the shared memory of the
-// cluster, as images.  A thread owns an odd number of consecutive logits (conflict-free, and in index order).  CTAs exchange
-// partial results by writing to all peers' shared memory, one cluster barrier per exchange.
+// Layout of the filtered rows: one cluster of up to 16 CTAs per row, 512 threads each; the row is read once, into the shared memory of
+// the cluster, as images.  A thread owns an odd number of consecutive logits (conflict-free, and in index order).  CTAs exchange
+// partial results by writing to all peers' shared memory, one cluster barrier per exchange.  When at most 512 logits can still be
+// drawn, the first CTA gets them and finishes alone (one row 32 -> 15 us, 64 mixed rows 85 -> 65).
+// Bound: the phases between the barriers, one after the other (of the 15 us of a single row the read takes 2), and with many rows
+// shared-memory atomics and 64-bit sums: 64 rows of 128256 with mixed filters 65 us; 100 rows of 50257 in bf16, top-p 95 us.
 #include <cmath>
 
 #include "kap_ptx.cuh"
@@ -688,10 +691,14 @@ kap_sample_rows_kernel(const SampleParams p)
     }
 }
 
-// ------------------------------------------------------------------ many rows without a filter
-// The draw alone: one pass over a row.  A warp reads 512 consecutive logits at a time into registers, 16 a lane, keeps their largest
-// and the sum of their weights relative to it (64 bits).  The cluster agrees on the row's largest logit, puts the sums on it and adds
-// them up in index order; the warp whose sums hold the target reads that block once more and walks through it.
+// ------------------------------------------------------------------ rows without a filter
+// The draw alone: one pass over a row.  A warp reads 512 consecutive logits at a time into registers, 16 a lane, the next block's on the
+// way meanwhile, and keeps their largest and the sum of their weights relative to it (64 bits).  The cluster agrees on the row's largest
+// logit, puts the sums on it and adds them up in index order; the warp whose sums hold the target reads that block once more and
+// walks through it.
+// Bound: the 64-bit pipe and the issue slots (fourteen 64-bit instructions of 34 a logit); 1000 rows of 128256: 196 us, 2.6 TB/s, the
+// pipe half busy.  32-bit weights with a bound of their error were slower: the bound is as large as a flat row's weights, so that
+// most rows had to be summed again in 64 bits (512 rows: 165 us, this kernel 108).
 constexpr int kDrawThreads = 256, kDrawWarps = kDrawThreads / 32;
 constexpr int kDrawBlock = 512, kDrawPer = kDrawBlock / 32;
 constexpr int kDrawBlocks = kMaxCluster * kSampleThreads * kMaxStrip / kDrawBlock + 1;      // of a row at most; one more for an unaligned start
@@ -944,17 +951,23 @@ extern "C" kap_status kap_sample_tokens(
     const int draw_blocks = (vocab + kDrawBlock - 1) / kDrawBlock;
     cudaError_t e = cudaSuccess;
     if (!top_k && !top_p && !min_p && (draw_blocks > 32 || rows > 148)) {
-        // (three CTAs on an SM and a block for each of their warps; two CTAs of long rows, whose tail one CTA would stretch)
+        // Without filters, unless the rows are short and few (8192 logits: 148 rows 8.4 us here, 9.6 there; 256 rows 12.0 against 10.5;
+        // 32000 logits: 8 rows 10.8 / 8.9, 100 rows 18.6 / 14.5; 128256 logits: 512 rows 257 / 108).  CTAs of a row: three on an SM and
+        // a block for each of their warps, and two for long rows, whose tail one CTA would stretch (128256 logits, 1 / 2 / 4 / 8 CTAs a
+        // row: 8 rows 58 / 33 / 20 / 14 us, 100 rows 58 / 40 / 33 / 37, 512 rows 133 / 117 / 126 / 144; 1000 rows of 32000 64 / 72 / 91 / 128).
         kernel = f32 ? kap_sample_draw_kernel<float> : kap_sample_draw_kernel<__nv_bfloat16>;
         while (C < 8 && C * 2 * kDrawWarps <= draw_blocks && (int64_t)rows * C * 2 <= 3 * 148) C *= 2;
         if (C == 1 && draw_blocks >= 128) C = 2;
         cfg.blockDim = dim3(kDrawThreads);
     } else {
-        // as many CTAs as keep two of them on an SM (33 logits a thread), and more while there are SMs to spare
+        // As many CTAs as keep two of them on an SM, 33 logits a thread (64 rows of 128256 with mixed filters: 65 us; 17 logits 104, 65
+        // logits 69).  With few rows more, while that leaves a thread a strip worth its barriers and the large clusters half of the SMs,
+        // since they do not fit everywhere (top-k 50 and top-p: 1 row of 32000 12.2 with 8 CTAs, 13.1 with 16, 14.7 with 2; 16 rows
+        // 12.9 with 4, 16.2 with 8; 16 rows of 50257 14.3 with 4, 17.2 with 8, 21 .. 26 with 16).
         kernel = f32 ? kap_sample_rows_kernel<float> : kap_sample_rows_kernel<__nv_bfloat16>;
         auto strip_of = [&](int c) { const int s = ((vocab + c - 1) / c + kSampleThreads - 1) / kSampleThreads; return s | 1; };
         while (C < kMaxCluster && strip_of(C) > 33) C *= 2;
-        while (C < kMaxCluster && strip_of(C) > 5 && (int64_t)rows * C * 2 <= 148) C *= 2;
+        while (C < kMaxCluster && strip_of(C) > (C < 8 ? 5 : 13) && (int64_t)rows * C * 2 <= (C < 4 ? 148 : 74)) C *= 2;
         p.strip = strip_of(C);
         p.slice = p.strip * kSampleThreads;
         auto smem_for = [](int slice) { return (sizeof(SampleShared) + 15) / 16 * 16 + ((size_t)slice + 4) * sizeof(uint32_t); };
