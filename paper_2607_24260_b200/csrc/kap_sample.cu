@@ -702,7 +702,6 @@ kap_sample_rows_kernel(const SampleParams p)
 constexpr int kDrawThreads = 256, kDrawWarps = kDrawThreads / 32;
 constexpr int kDrawBlock = 512, kDrawPer = kDrawBlock / 32;
 constexpr int kDrawBlocks = kMaxCluster * kSampleThreads * kMaxStrip / kDrawBlock + 1;      // of a row at most; one more for an unaligned start
-constexpr int kDrawRounds = (kDrawBlocks + kDrawThreads - 1) / kDrawThreads;
 
 struct DrawShared {
     double sum[kDrawBlocks];
