@@ -10,10 +10,10 @@
 // Every value is rounded to bf16 once, when it is stored.
 //
 // Bound: memory; a token row moves 2 (Hq + 2 Hkv) 256 bytes and its angles are shared by all heads.  2 x 8192 rows of 32 / 8 heads
-// take 68 us, 5.9 TB/s (90 % of a plain copy's rate); a batch's single step is a launch, 3.3 us for 4 rows, 3.5 for 64.
+// take 66 us, 6.1 TB/s (93 % of a plain copy's rate); a batch's single step is a launch, 3.3 us for 4 rows, 3.5 for 64.
 // Layout: one CTA per token row, 128 threads; a thread task is two 16-byte pieces of one head that hold
 // both partners of eight pairs, so a rotation never crosses threads and q may be rotated in place.  What hides the look-ups is other
-// CTAs on the SM: reading a thread's values before them costs registers and was slower (4800 rows 20 us with 12 CTAs on an SM, 17 with 16).
+// CTAs on the SM: reading a thread's values before them costs registers and was slower (2 x 8192 rows: 72 us with the 10 CTAs that then fit on an SM, 68 with 12, 66 with 16).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -56,13 +56,13 @@ __device__ __forceinline__ uint32_t rotate_neighbours(uint32_t v, const float2 t
     return *reinterpret_cast<const uint32_t*>(&x);
 }
 
-__global__ void __launch_bounds__(kRopeThreads)
+__global__ void __launch_bounds__(kRopeThreads, 16)
 kap_append_kv_rope_kernel(const RopeParams p)
 {
     __shared__ float2 turn[kHeadDim / 2];           // (cos, sin) of this row's pairs
     const int row = blockIdx.x, tid = threadIdx.x;
     // the sequence that owns the row, the last one that begins at or before it: 32 probes at a time (a bisection waits for one
-    // probe after the other; 4800 rows of 24 sequences 17.6 us with it, 17.0 so)
+    // probe after the other; 4800 rows of 24 sequences 17.6 us with it, 17.1 so)
     int b = row, place = 0;
     if (p.new_indptr) {
         const int first = p.new_indptr[0], end = p.new_indptr[p.batch];

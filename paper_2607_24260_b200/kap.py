@@ -264,7 +264,11 @@ def _torch_module():
 
 
 def _stream_ptr(stream=None):
-    return (_torch_module().cuda.current_stream() if stream is None else stream).cuda_stream
+    """the handle of a torch stream, or of the current one (read without building a Stream object for it)"""
+    if stream is not None:
+        return stream.cuda_stream
+    torch = _torch_module()
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dptr(t):
