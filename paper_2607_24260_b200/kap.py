@@ -435,6 +435,8 @@ def _head_rows(name, t, rows, heads):
         raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(shape)}, expected bfloat16 [{rows}, {heads}, d]")
     if stride[2] != 1 or (heads > 1 and stride[1] != shape[2]):
         raise KapError(ERR_INVALID_ARG, f"{name} has strides {stride}: the heads of a row must be contiguous")
+    if not t.is_cuda:
+        raise KapError(ERR_INVALID_ARG, f"{name} is not on a GPU")
     return heads * shape[2] if rows <= 1 else stride[0]
 
 
@@ -467,11 +469,13 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
     if positions is not None:
         if positions.dim() == 1:
             positions = positions.view(1, -1)
-        if positions.dtype is not torch.int32 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
-            raise KapError(ERR_INVALID_ARG, f"positions {positions.dtype} {tuple(positions.shape)} for {rows} rows")
+        if positions.dtype is not torch.int32 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1) or not positions.is_cuda:
+            raise KapError(ERR_INVALID_ARG, f"positions {positions.dtype} {tuple(positions.shape)} on {positions.device} for {rows} rows")
         axes, pos_stride = positions.shape[0], positions.stride(0)
         if axes == 1:
             pos_stride = max(pos_stride, rows)
+    if inv_freq.dtype is not torch.float32 or not inv_freq.is_contiguous() or not inv_freq.is_cuda:
+        raise KapError(ERR_INVALID_ARG, f"inv_freq must be a contiguous float32 tensor on a GPU, not {inv_freq.dtype}")
     rot = 2 * inv_freq.shape[0]
     axis = None
     if freq_axis is not None:
@@ -493,15 +497,15 @@ def sample_tokens(logits, uniform, token, logprob=None, temperature=None, top_k=
     min_p (fp32 [rows]) and top_k (int32 [rows]) are optional; None switches a filter off."""
     torch = _torch_module()
     kind = LOGITS_F32 if logits.dtype is torch.float32 else LOGITS_BF16 if logits.dtype is torch.bfloat16 else None
-    if kind is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise KapError(ERR_INVALID_ARG, f"logits are {logits.dtype} {tuple(logits.shape)} with strides {logits.stride()}")
+    if kind is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1) or not logits.is_cuda:
+        raise KapError(ERR_INVALID_ARG, f"logits are {logits.dtype} {tuple(logits.shape)} with strides {logits.stride()} on {logits.device}")
     rows, vocab = logits.shape
 
     def ptr(name, t, dt):
         if t is None:
             return None
-        if t.dtype is not dt or t.numel() != rows or not t.is_contiguous():
-            raise KapError(ERR_INVALID_ARG, f"{name} must be a contiguous {dt} tensor of {rows}")
+        if t.dtype is not dt or t.numel() != rows or not t.is_contiguous() or not t.is_cuda:
+            raise KapError(ERR_INVALID_ARG, f"{name} must be a contiguous {dt} tensor of {rows} on a GPU")
         return t.data_ptr()
 
     f32, i32 = torch.float32, torch.int32

@@ -162,3 +162,37 @@ def test_steps_without_shared_pages_match_the_verification_call():
     # kap_verify_attn's small-row kernel sums the weights after their rounding to bf16: every term, and so the sum, is within 2^-8 of itself, and
     # the sum's logarithm within -ln(1 - 2^-8) < 2^-8 + 2^-16; the scores' errors add 2e-5 on either side
     assert (lse - lse2).abs().max().item() <= 2.0 ** -8 + 2.0 ** -16 + 4e-5
+
+
+@pytest.mark.parametrize("layout", [kap.KV_HND, kap.KV_NHD])
+def test_offsets_past_32_bits(layout):
+    # the pages at the end of a pool of 4.6 G elements, and logits rows 2.2 G elements apart, give what the same data does at the front
+    c = Case(77, [(6, [(1, 40), (2, 9)]), (40, [(2, 50)] * 20)], 32, 8, layout, spare=1, poison=0.0)
+    n, pages = c.pool.shape[0], 140000
+    first = pages - n
+    far = torch.empty((pages,) + tuple(c.pool.shape[1:]), dtype=torch.bfloat16, device=gu.DEV)
+    far[first:] = c.pool
+    table = gu.i32(c.bt), gu.i32(c.bt + first)
+    rows, qi, bti, inv = int(c.n_q.sum()), gu.i32(c.q_indptr), gu.i32(c.bt_indptr), torch.full((64,), 0.01, device=gu.DEV)
+    k, v = (torch.randn(rows, 8, D, device=gu.DEV).to(torch.bfloat16) for _ in range(2))
+    ws, got = c.workspace(), []
+    for pool, bt in zip((c.pool, far), table):
+        ctx, out, q = gu.i32(c.ctx), torch.empty_like(c.q), torch.empty_like(c.q)
+        status = torch.zeros(1, dtype=torch.int32, device=gu.DEV)
+        kap.append_kv_rope(c.q, k, v, pool, bti, bt, ctx, inv, q_out=q, new_indptr=qi, device_status=status, kv_layout=layout)
+        kap.shared_prefix_attn(q, qi, pool, bti, bt, ctx, out, ws)
+        ws.check()
+        assert int(status.item()) == 0
+        got.append(out)
+    assert torch.equal(*got) and torch.equal(far[first:], c.pool) and torch.isfinite(got[0].float()).all()
+    del far
+    stride, vocab = 2_200_000_003, 50257
+    store = torch.empty(stride + vocab, dtype=torch.bfloat16, device=gu.DEV)
+    logits = store.as_strided((2, vocab), (stride, 1))
+    logits.copy_(torch.randn(2, vocab, device=gu.DEV))
+    u, near, lp = torch.tensor([0.3, 0.8], device=gu.DEV), logits.contiguous(), torch.empty(2, device=gu.DEV)
+    for filters in ({}, dict(top_p=torch.full((2,), 0.9, device=gu.DEV))):
+        a, b = (torch.empty(2, dtype=torch.int32, device=gu.DEV) for _ in range(2))
+        kap.sample_tokens(logits, u, a, lp, **filters)
+        kap.sample_tokens(near, u, b, lp, **filters)
+        assert torch.equal(a, b) and (a >= 0).all()

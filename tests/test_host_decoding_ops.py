@@ -100,3 +100,14 @@ def test_sample_tokens_refuses_rows_that_do_not_fit():
     assert _sample(vocab=most + 1, stride=most + 1) == kap.ERR_UNSUPPORTED
     assert b"vocab" in kap.lib().kap_last_error()
     assert _sample(vocab=100000, stride=100000, rows=0x7fffffff, k=A) == kap.ERR_UNSUPPORTED          # more CTAs than a grid has
+
+
+def test_the_binding_refuses_host_tensors():
+    import torch
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    rows = torch.zeros(2, 8, 128, dtype=bf)
+    pool, idx, freq = torch.zeros(3, 2, 8, 16, 128, dtype=bf), torch.zeros(3, dtype=i32), torch.ones(64)
+    with pytest.raises(kap.KapError, match="not on a GPU"):
+        kap.append_kv_rope(None, rows, rows, pool, idx, idx, idx[:2], freq)
+    with pytest.raises(kap.KapError, match="on cpu"):
+        kap.sample_tokens(torch.zeros(2, 10), torch.zeros(2, dtype=f32), torch.zeros(2, dtype=i32))
