@@ -18,9 +18,10 @@
 // Layout of the filtered rows: one cluster of up to 16 CTAs per row, 512 threads each; the row is read once, into the shared memory of
 // the cluster, as images.  A thread owns an odd number of consecutive logits (conflict-free, and in index order).  CTAs exchange
 // partial results by writing to all peers' shared memory, one cluster barrier per exchange.  When at most 512 logits can still be
-// drawn, the first CTA gets them and finishes alone (one row 32 -> 15 us, 64 mixed rows 85 -> 65).
+// drawn, the first CTA gets them and finishes alone (one row 32 -> 15 us, 64 mixed rows 85 -> 65).  A thread carries its weight of what
+// the top-p search has passed, all of it kept, into the draw (64 mixed rows 65 -> 62, 100 flat rows 95 -> 87).
 // Bound: the phases between the barriers, one after the other (of the 15 us of a single row the read takes 2), and with many rows
-// shared-memory atomics and 64-bit sums: 64 rows of 128256 with mixed filters 65 us; 100 rows of 50257 in bf16, top-p 95 us.
+// shared-memory atomics and 64-bit sums: 64 rows of 128256 with mixed filters 62 us; 100 rows of 50257 in bf16, top-p 87 us.
 #include <cmath>
 
 #include "kap_ptx.cuh"
@@ -211,12 +212,15 @@ kap_sample_rows_kernel(const SampleParams p)
         }
         return;
     }
-    const double x_max = wide_logit(top), per_bit = 1.4426950408889634 / (double)t;
-    // logarithm of a weight and the weight: 2^((x - max) / T / ln 2)
-    auto log2_weight = [&](uint32_t u) { return (wide_logit(u) - x_max) * per_bit; };
+    // the weight 2^((x - max) / T / ln 2); +inf stands for the largest finite number (the conversion runs beside the sums, on its own pipe)
+    auto widen = [](uint32_t u) { return (double)fminf(image_logit(u), 3.402823466e38f); };
+    const double x_max = widen(top), per_bit = 1.4426950408889634 / (double)t;
+    const uint32_t far_off = (uint32_t)__double2hiint(-1021.0 / per_bit);      // (-inf for an endless T)
+    auto behind = [&](uint32_t u) { return widen(u) - x_max; };
+    auto gone = [&](double d) { return (uint32_t)__double2hiint(d) >= far_off; };
     auto weight = [&](uint32_t u) {
-        const double e = log2_weight(u);
-        return vanishes(e) ? 0.0 : exp2_f64(e);
+        const double d = behind(u);
+        return gone(d) ? 0.0 : exp2_f64(d, per_bit);
     };
     // Weights of the distances below `span` (and, of those equal to it, of the ones whose rank among the equal ones, from `tie_rank` on, is
     // below `quota`) in this thread's strip: which ones, 32 at a time, then three chains of products side by side for as long as a
@@ -240,14 +244,14 @@ kap_sample_rows_kernel(const SampleParams p)
 #pragma unroll
                 for (int j = 0; j < 3; ++j) {
                     have[j] = wanted != 0u;
-                    e[j] = log2_weight(mine[i0 + (have[j] ? __ffs(wanted) - 1 : 0)]);
+                    e[j] = behind(mine[i0 + (have[j] ? __ffs(wanted) - 1 : 0)]);
                     wanted &= wanted - 1u;
                 }
 #pragma unroll
-                for (int j = 0; j < 3; ++j) w[j] = exp2_f64(e[j]);
+                for (int j = 0; j < 3; ++j) w[j] = exp2_f64(e[j], per_bit);
 #pragma unroll
                 for (int j = 0; j < 3; ++j)
-                    if (have[j] && !vanishes(e[j])) s += w[j];
+                    if (have[j] && !gone(e[j])) s += w[j];
             }
         }
         return s;
@@ -261,10 +265,10 @@ kap_sample_rows_kernel(const SampleParams p)
 #pragma unroll
             for (int j = 0; j < 3; ++j) u[j] = i + j < p.strip ? mine[i + j] : 0u;
 #pragma unroll
-            for (int j = 0; j < 3; ++j) { e[j] = log2_weight(u[j]); w[j] = exp2_f64(e[j]); }
+            for (int j = 0; j < 3; ++j) { e[j] = behind(u[j]); w[j] = exp2_f64(e[j], per_bit); }
 #pragma unroll
             for (int j = 0; j < 3; ++j)
-                if (top - u[j] < span && !vanishes(e[j])) s += w[j];
+                if (top - u[j] < span && !gone(e[j])) s += w[j];
         }
         return s;
     };
@@ -281,6 +285,8 @@ kap_sample_rows_kernel(const SampleParams p)
         for (int w = 0; w < kSampleWarps; ++w) v += sh.warp_d[w][0];
         return v;
     };
+    double kept_near = 0.0;                                        // this thread's weight of distances below kept_from, all of them kept
+    uint32_t kept_from = 0u;
     int level = 0;                                                 // of all searches of the row: parity selects the buffers
     // One level: the CTAs' histograms (of the distances base + [b << shift, (b + 1) << shift), by count_level) summed over the row, two
     // bins a thread; `partial` is summed over the row along the way.
@@ -399,7 +405,7 @@ kap_sample_rows_kernel(const SampleParams p)
         __syncthreads();
         if (mine_too && by_index == sh.bin[0]) {
             p.token[r] = index;
-            if (p.logprob) p.logprob[r] = (float)((log2_weight(u) - log2(total)) * 0.69314718055994531);
+            if (p.logprob) p.logprob[r] = (float)((per_bit * behind(u) - log2(total)) * 0.69314718055994531);
         }
     };
 
@@ -494,7 +500,7 @@ kap_sample_rows_kernel(const SampleParams p)
             in_bin = (int)sh.bin_count;
             edge = sh.edge;
         };
-        double part = cut == furthest && quota == 0x7fffffff ? strip_weight_all(cut + 1u) : strip_weight(0u, quota == 0x7fffffff ? cut + 1u : cut, 0, 0);   // the whole: everything kept so far
+        double part = cut == furthest && quota == 0x7fffffff ? strip_weight_all(cut + 1u) : strip_weight(0u, quota == 0x7fffffff ? cut + 1u : cut, 0, 0);   // everything kept so far
         const double cut_part = quota == 0x7fffffff ? 0.0 : (double)quota * weight(top - cut);
         uint64_t base = 0, end = last;                             // distances between which the threshold lies
         const bool even = top != kImagePlusInf && last >= kBins;   // (few distances: their own intervals at once)
@@ -563,6 +569,8 @@ kap_sample_rows_kernel(const SampleParams p)
                 }
                 base = min(base, end);
                 part = base > 0 ? strip_weight(0u, (uint32_t)base, 0, 0) : 0.0;
+                kept_near = part;
+                kept_from = (uint32_t)base;
             }
             if (b1 == kBins) part = 0.0;                           // (nothing learnt; `above` stays 0)
         }
@@ -613,6 +621,8 @@ kap_sample_rows_kernel(const SampleParams p)
             // what lies between the old base and the new one is above the range from now on
             part = strip_weight((uint32_t)base, (uint32_t)(next - base), 0, 0);
             base = next;
+            kept_near += part;
+            kept_from = (uint32_t)base;
             // finer by at least two bits, so that the search ends; windows that do not cover the range follow one another
             if (b1 < kBins) shift = max(0, min(shift - 2, b2 < kBins ? shift_for((uint64_t)(b2 - b1 + 1) << shift) : shift));
         }
@@ -638,7 +648,10 @@ kap_sample_rows_kernel(const SampleParams p)
         for (int c = 0; c < rank; ++c) tie_rank += sh.ties[c];
     }
     // (images below top - cut, the padding's 0 among them, are cut)
-    const double sum = quota != 0x7fffffff ? strip_weight(0u, cut, tie_rank, quota) : cut == furthest ? strip_weight_all(cut + 1u) : strip_weight(0u, cut + 1u, 0, 0);
+    if (kept_from > cut) { kept_near = 0.0; kept_from = 0u; }      // (min-p cuts deeper)
+    const double sum = quota != 0x7fffffff ? kept_near + strip_weight(kept_from, cut - kept_from, tie_rank, quota)
+                       : cut == furthest   ? strip_weight_all(cut + 1u)
+                                           : kept_near + strip_weight(kept_from, cut - kept_from + 1u, 0, 0);
     // Running sums one after the other, so that a thread without weight ends exactly where the one before it does, and the end of a
     // warp or a CTA is the same number as the start of the next: one thread, with weight, holds the target.
     double run = 0.0;
@@ -687,7 +700,7 @@ kap_sample_rows_kernel(const SampleParams p)
     }
     if (lane == 0) {
         p.token[r] = first + (warp * 32 + who) * p.strip + found;
-        if (p.logprob) p.logprob[r] = (float)((log2_weight(strip[found]) - log2(total)) * 0.69314718055994531);
+        if (p.logprob) p.logprob[r] = (float)((per_bit * behind(strip[found]) - log2(total)) * 0.69314718055994531);
     }
 }
 
