@@ -24,6 +24,7 @@ struct alignas(16) PrefixSegment {                     // what one CTA of the tc
     int32_t pad[3];
 };
 static_assert(sizeof(PrefixSegment) == 48, "segments are read as three 16-byte pieces");
+static_assert(sizeof(MergeGroup) == sizeof(WorkItem), "the workspace's three metadata arrays have max_items entries of one size");
 
 struct alignas(16) PrefixUnit { int32_t state_row0, rows, n_states, pad; };
 struct alignas(16) PrefixSeq {                         // where the merge pass finds a sequence's states

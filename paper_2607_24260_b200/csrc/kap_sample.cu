@@ -709,9 +709,9 @@ kap_sample_rows_kernel(const SampleParams p)
 // way meanwhile, and keeps their largest and the sum of their weights relative to it (64 bits).  The cluster agrees on the row's largest
 // logit, puts the sums on it and adds them up in index order; the warp whose sums hold the target reads that block once more and
 // walks through it.
-// Bound: the 64-bit pipe and the issue slots (fourteen 64-bit instructions of 34 a logit); 1000 rows of 128256: 196 us, 2.6 TB/s, the
-// pipe half busy.  32-bit weights with a bound of their error were slower: the bound is as large as a flat row's weights, so that
-// most rows had to be summed again in 64 bits (512 rows: 165 us, this kernel 108).
+// Bound: the 64-bit pipe and the issue slots (fourteen 64-bit instructions of about thirty a logit); 1000 rows of 128256: 184 us,
+// 2.8 TB/s, the pipe half busy.  (Two blocks a pass, without the copy from the block on the way, spilled: 223 us.)  32-bit weights with a bound of their error were slower: the bound is as large as a flat row's weights, so that
+// most rows had to be summed again in 64 bits (512 rows: 165 us, this kernel 97).
 constexpr int kDrawThreads = 256, kDrawWarps = kDrawThreads / 32;
 constexpr int kDrawBlock = 512, kDrawPer = kDrawBlock / 32;
 constexpr int kDrawBlocks = kMaxCluster * kSampleThreads * kMaxStrip / kDrawBlock + 1;      // of a row at most; one more for an unaligned start
@@ -744,30 +744,39 @@ kap_sample_draw_kernel(const SampleParams p)
     // logit e of load l of this lane has the place place_of(b, l) + e
     auto place_of = [&](int b, int l) { return (block0 + b) * kDrawBlock + l * (32 * kVec) + lane * kVec; };
     auto load = [&](int b, uint4 (&raw)[kLoads]) {                 // places that are not the row's: all bits set, which is NaN
+        const int from = (block0 + b) * kDrawBlock;
+        const T* const at = row + (place_of(b, 0) - skip);
+        if (from >= skip && from + kDrawBlock <= end) {
 #pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
-            const int i = place_of(b, l);
-            if (i >= skip && i + kVec <= end) {
-                raw[l] = __ldcs(reinterpret_cast<const uint4*>(row + (i - skip)));
-            } else {
+            for (int l = 0; l < kLoads; ++l) raw[l] = __ldcs(reinterpret_cast<const uint4*>(at) + 32 * l);
+        } else {                                                   // an end of the row
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
                 raw[l] = make_uint4(0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu);
                 T* e = reinterpret_cast<T*>(&raw[l]);
 #pragma unroll
-                for (int j = 0; j < kVec; ++j)
-                    if (i + j >= skip && i + j < end) e[j] = row[i + j - skip];
+                for (int j = 0; j < kVec; ++j) {
+                    const int i = place_of(b, l) + j;
+                    if (i >= skip && i < end) e[j] = row[i - skip];
+                }
             }
         }
     };
     auto logit = [](const uint4 (&raw)[kLoads], int q) { return as_float(reinterpret_cast<const T*>(&raw[q / kVec])[q % kVec]); };
-    // s += 2^((v - from) / T / ln 2), `from` the largest logit; nothing for -inf and NaN, nor far below the smallest normal number; beside
-    // +inf, which stands for the largest finite number, only +inf has weight.  (The conversion runs beside the sums, on its own pipe.)
+    // s += 2^((v - from) / T / ln 2), `from` the largest logit, for logits above `bar`: none for -inf and NaN, nor more than 2^-1021 below the
+    // largest one, which is counted whatever T; beside +inf, which stands for the largest finite number, only +inf.  (The
+    // conversion runs beside the sums, on its own pipe.)
     constexpr float kLargest = 3.402823466e38f;
     auto widen = [](float v) { return (double)fminf(v, kLargest); };
-    auto bar_of = [](float top) { return top == INFINITY ? kLargest : -INFINITY; };
-    const uint32_t far = (uint32_t)__double2hiint(-1021.0 / per_bit);      // (-inf for an endless T)
+    const double reach = 1021.0 / per_bit;                         // (+inf for an endless T)
+    auto bar_of = [&](uint32_t image) {
+        const float before = image_logit(image - 1u);              // of +inf: the largest finite number
+        const double bar = widen(image_logit(image)) - reach;
+        return image == kImagePlusInf ? before : bar < -(double)kLargest ? -INFINITY : fminf(__double2float_ru(bar), before);
+    };
     auto add_weight = [&](double& s, float v, double from, float bar) {
-        const double d = widen(v) - from, w = exp2_f64(d, per_bit);
-        if (v > bar && (uint32_t)__double2hiint(d) < far) s += w;
+        const double w = exp2_f64(widen(v) - from, per_bit);
+        if (v > bar) s += w;
     };
 
     uint32_t best = 0u;
@@ -783,7 +792,7 @@ kap_sample_draw_kernel(const SampleParams p)
         for (int q = 0; q < kDrawPer; ++q) top = fmaxf(top, logit(now, q));
         const uint32_t image = __reduce_max_sync(0xffffffffu, logit_image(top));
         best = max(best, image);
-        const float block_top = image_logit(image), bar = bar_of(block_top);
+        const float block_top = image_logit(image), bar = bar_of(image);
         const double from = widen(block_top);
         double s0 = 0.0, s1 = 0.0;
 #pragma unroll
@@ -840,7 +849,7 @@ kap_sample_draw_kernel(const SampleParams p)
         return;
     }
     const double x_max = widen(top_logit);
-    const float bar = bar_of(top_logit);
+    const float bar = bar_of(top);
     // Running sums one after the other: consecutive blocks to a thread, then threads, warps and CTAs, so that a thread without weight
     // ends exactly where the one before it does, and the end of a warp or a CTA is the same number as the start of the next.
     const int per_thread = (n_blocks + kDrawThreads - 1) / kDrawThreads, own0 = min(n_blocks, tid * per_thread), own1 = min(n_blocks, own0 + per_thread);
@@ -964,7 +973,7 @@ extern "C" kap_status kap_sample_tokens(
     cudaError_t e = cudaSuccess;
     if (!top_k && !top_p && !min_p && (draw_blocks > 32 || rows > 148)) {
         // Without filters, unless the rows are short and few (8192 logits: 148 rows 8.4 us here, 9.6 there; 256 rows 12.0 against 10.5;
-        // 32000 logits: 8 rows 10.8 / 8.9, 100 rows 18.6 / 14.5; 128256 logits: 512 rows 257 / 108).  CTAs of a row: three on an SM and
+        // 32000 logits: 8 rows 10.8 / 8.9, 100 rows 18.6 / 14.5; 128256 logits: 512 rows 257 / 97).  CTAs of a row: three on an SM and
         // a block for each of their warps, and two for long rows, whose tail one CTA would stretch (128256 logits, 1 / 2 / 4 / 8 CTAs a
         // row: 8 rows 58 / 33 / 20 / 14 us, 100 rows 58 / 40 / 33 / 37, 512 rows 133 / 117 / 126 / 144; 1000 rows of 32000 64 / 72 / 91 / 128).
         kernel = f32 ? kap_sample_draw_kernel<float> : kap_sample_draw_kernel<__nv_bfloat16>;
