@@ -55,10 +55,11 @@ __device__ __forceinline__ double wide_logit(uint32_t u) {
     return __hiloint2double((int)(((mag >> 3) + 0x38000000u) | (flip & 0x80000000u)), (int)(mag << 29));
 }
 // 2^t for t <= 0 in 64 bits, to be discarded below the smallest normal number (`vanishes`).  t = n + f with |f| <= 1/2 (a sum with
-// 1.5 2^52 holds n in its low word), 2^f by the polynomial of degree 9 of least largest relative error there (1.3e-14; Remez
-// exchange), its coefficients in constant memory, from where the products take them without a register.
-__constant__ double kExp2[10] = {1.0150336270671598e-07, 1.3259405604554393e-06, 1.5252984841153802e-05, 0.00015403434948094166, 0.0013333557617599588,
-                                 0.009618129192067212, 0.055504108668685645, 0.24022650695649653, 0.693147180559871, 1.0000000000000127};
+// 1.5 2^52 holds n in its low word), 2^f by the polynomial of degree 9 of least largest relative error there among those that are 1
+// at 0 (1.5e-14; Lawson's iteration), so that logits equal to the largest have the weight 1 and sums of them are exact.  Its
+// coefficients are in constant memory, from where the products take them without a register.
+__constant__ double kExp2[10] = {1.0148340385735375e-07, 1.3258335410465268e-06, 1.5252990017215676e-05, 0.0001540344088444558, 0.0013333557625466606,
+                                 0.009618129181163905, 0.05550410866841578, 0.2402265069572282, 0.6931471805598851, 1.0};
 __device__ __forceinline__ bool vanishes(double t) { return (uint32_t)__double2hiint(t) > 0xc08ff000u; }       // t < -1022
 __device__ __forceinline__ double exp2_f64(double d, double scale) {           // 2^(d scale)
     const double s = fma(d, scale, 6755399441055744.0), f = fma(d, scale, 6755399441055744.0 - s);

@@ -109,6 +109,19 @@ def test_equal_logits_rank_by_index(filters, step):
     check(f32(x), rng.random(rows), **s)
 
 
+@pytest.mark.parametrize("vocab", [2, 12, 30, 716, 2048, 40000])
+@pytest.mark.parametrize("value", [0.0, -9984.0, np.inf, 1e-42])
+def test_equal_logits_split_by_top_p_exactly(vocab, value):
+    # n equal logits have n equal weights: p = 1/2, 1/4 and 3/4 of them end on a token when 4 divides n, and the next one stays out
+    n = vocab // 4 * 4 if vocab > 2 else 2
+    x = np.full((9, vocab), -np.inf)
+    x[:, np.random.default_rng(vocab).permutation(vocab)[:n]] = value
+    p = np.repeat([0.5, 0.25, 0.75], 3) if vocab > 2 else np.full(9, 0.5)
+    got = check(f32(x), np.tile([0.0, 0.6, 1.0 - 2.0 ** -24], 3), t=np.tile([1.0, 0.3, 1e30], 3), p=p)
+    at = np.nonzero(np.isfinite(x[0]) | (x[0] == np.inf))[0]
+    assert (got[2::3] == at[(p[2::3] * n).astype(int) - 1]).all()
+
+
 def test_ends_of_the_parameter_ranges():
     rng = np.random.default_rng(3)
     vocab = 1111
