@@ -23,7 +23,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 RATIO_FILE = os.path.join(ROOT, "profiles", "traffic_ratio.txt")
-KERNEL_SOURCES = ("kap_attn_kernel.cuh", "kap_attn.cu", "kap_schedule.cpp", "kap_internal.h")
+KERNEL_SOURCES = ("kap_ptx.cuh", "kap_attn_kernel.cuh", "kap_attn.cu", "kap_schedule.cpp", "kap_internal.h")
 
 
 def kernel_digest() -> str:
