@@ -21,7 +21,7 @@ constexpr int32_t kSplitCtasPerSm = 3;
 constexpr int32_t kMinSplitPages = 4;                          // a page for each of a CTA's warps
 constexpr int32_t kMaxSplitPages = 1024;                       // page ids a CTA holds: 1600
 // Short parts of at most 16 rows may go four KV heads to a CTA, one per warp, instead of a CTA each: for many short lists a CTA is
-// mostly start-up (256 sequences with 19 own pages: the call takes 56 us, with a CTA for each head 67).  A warp alone takes about a
+// mostly start-up (256 sequences with up to 19 own pages: the call takes 56 us, with a CTA for each head 67).  A warp alone takes about a
 // microsecond a page, so long lists do not belong there.
 constexpr int32_t kByHeadPages = 48;
 // What a CTA of the split kernel takes, in pages that one warp group streams (about a microsecond each): its start and its end as much
