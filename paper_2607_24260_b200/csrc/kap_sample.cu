@@ -37,7 +37,7 @@ constexpr int kBins = 1024;
 constexpr int kFew = kSampleThreads;               // logits that one CTA finishes alone: one a thread
 constexpr uint32_t kImageMinusInf = 0x007fffffu;   // image of -inf; nothing at or below it has weight
 constexpr uint32_t kImagePlusInf = 0xff800000u;
-constexpr int kMaxRounds = 96;                     // of a search: at most 11 widths of interval, four windows each
+constexpr int kMaxRounds = 48;                     // of a search, more than either can take
 constexpr int kMaxStrip = 99;                      // logits a thread owns at most: 512 x 99 x 4 bytes of shared memory
 
 __device__ __forceinline__ uint32_t logit_image(float v) {          // NaN like -inf, -0 = +0
@@ -417,7 +417,7 @@ kap_sample_rows_kernel(const SampleParams p)
     if (counted && k < finite) {
         uint64_t base = 0;
         int shift = 14, above = 0;                                 // two octaves below the largest logit at first
-        for (int rounds = 0; rounds < kMaxRounds; ++rounds) {      // (ends by itself; the bound is for a mistake in this argument)
+        for (int rounds = 0; rounds < kMaxRounds; ++rounds) {      // (at most four windows, then widths of 2^22, 2^12, 2^2 and 1)
             uint32_t bins[2];
             count_level(base, shift, 0.0, bins);
             // inclusive running count; the bin in which the k-th falls
@@ -575,10 +575,29 @@ kap_sample_rows_kernel(const SampleParams p)
             }
             if (b1 == kBins) part = 0.0;                           // (nothing learnt; `above` stays 0)
         }
-        int shift = shift_for(end - base + 1);
+        // A window of 1024 intervals over all distances in question.  What it leaves between the two bins found is at most half of them,
+        // or (bounds too wide, as beside a gap in the values) their middle is tried: the weight in front of it, summed exactly, says on
+        // which side of it the threshold lies.  So two rounds halve a range that begins below 2^32 and ends in single intervals
+        // at 2^10: at most 45 rounds.  One to three are usual, ten the most seen (three values, p just past the weight of one of them).
+        bool trial = false;                                        // `part` is the weight between base and `middle`
+        uint64_t middle = 0;
         for (int rounds = 0; rounds < kMaxRounds; ++rounds) {
+            const int shift = shift_for(end - base + 1);
             uint32_t bins[2];
             const double sum = count_level(base, shift, part, bins);
+            if (trial) {
+                trial = false;
+                if (above + sum < target) {
+                    above += sum;
+                    kept_near += part;
+                    base = middle;
+                    kept_from = (uint32_t)base;
+                } else {
+                    end = middle - 1;
+                }
+                part = 0.0;
+                continue;
+            }
             if (rounds == 0 && !even) target = (double)top_p * (sum + cut_part); else above += sum;
             double lo[2], hi[2];                                   // bounds of the weight in this thread's two bins
 #pragma unroll
@@ -594,15 +613,13 @@ kap_sample_rows_kernel(const SampleParams p)
                 hi[e] = c > 0 ? (shift == 0 ? lo[e] : c * weight(top - (uint32_t)from)) : 0.0;
             }
             find(bins, lo, hi, shift == 0 ? 0.0 : 1e-12 * target); // at single distances the sums are exact
-            uint64_t next;
-            if (b1 == kBins) {                                     // not within this window: on to the next one
-                next = base + ((uint64_t)kBins << shift);
-                if (next > last) {                                 // (a rounding short of the end: all that there is)
-                    if (last < cut) { cut = last; quota = 0x7fffffff; }
-                    break;
-                }
-            } else if (shift == 0) {
-                const uint32_t d = (uint32_t)(base + (uint64_t)b1);
+            if (b1 == kBins) {                                     // (a rounding short of the end: all that there is)
+                if (end < cut) { cut = (uint32_t)end; quota = 0x7fffffff; }
+                break;
+            }
+            const uint64_t next = base + ((uint64_t)b1 << shift), bin_end = next + ((uint64_t)1 << shift) - 1;
+            if (shift == 0) {
+                const uint32_t d = (uint32_t)next;
                 const double w = weight(top - d), m = w > 0.0 ? ceil((target - edge) / w) : 1.0;
                 const int keep = m < 1.0 ? 1 : m < (double)in_bin ? (int)m : in_bin;
                 const bool all = keep == in_bin && !(d == cut && quota != 0x7fffffff);
@@ -610,22 +627,32 @@ kap_sample_rows_kernel(const SampleParams p)
                 quota = all ? 0x7fffffff : keep;
                 cut = d;
                 break;
-            } else {
-                next = base + ((uint64_t)b1 << shift);
-                const uint64_t bin_end = next + ((uint64_t)1 << shift) - 1;
-                if (b1 == b2 && in_bin == 1 && bin_end < cut) {    // the one logit in it belongs to the prefix
-                    cut = (uint32_t)bin_end;
-                    quota = 0x7fffffff;
-                    break;
-                }
             }
+            if (b1 == b2 && in_bin == 1 && bin_end < cut) {        // the one logit in it belongs to the prefix
+                cut = (uint32_t)bin_end;
+                quota = 0x7fffffff;
+                break;
+            }
+            const uint64_t half = (end - base + 1) / 2;
+            if (b2 == kBins) {                                     // the last bin that has any must
+                int filled = bins[1] ? 2 * tid + 1 : bins[0] ? 2 * tid : 0;
+                filled = __reduce_max_sync(0xffffffffu, filled);
+                if (lane == 0) sh.warp_i[warp] = filled;
+                __syncthreads();
+                b2 = b1;
+                for (int w = 0; w < kSampleWarps; ++w) b2 = max(b2, sh.warp_i[w]);
+            }
+            end = min(end, base + ((uint64_t)(b2 + 1) << shift) - 1);
+            end = max(end, next);                                  // (a rounding past the end)
+            trial = end - next >= half;
+            middle = trial ? base + half : next;
             // what lies between the old base and the new one is above the range from now on
-            part = strip_weight((uint32_t)base, (uint32_t)(next - base), 0, 0);
-            base = next;
-            kept_near += part;
-            kept_from = (uint32_t)base;
-            // finer by at least two bits, so that the search ends; windows that do not cover the range follow one another
-            if (b1 < kBins) shift = max(0, min(shift - 2, b2 < kBins ? shift_for((uint64_t)(b2 - b1 + 1) << shift) : shift));
+            part = strip_weight((uint32_t)base, (uint32_t)(middle - base), 0, 0);
+            if (!trial) {
+                base = next;
+                kept_near += part;
+                kept_from = (uint32_t)base;
+            }
         }
     }
 
