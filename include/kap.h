@@ -639,10 +639,11 @@ enum {
  * Sums and comparisons are in 64 bits (weights to about 1e-14 of themselves; weights below 2^-1021 of the largest count
  * as none).  T <= 0 (or NaN): the lowest index of the largest logit, logprob 0.  NaN and -inf logits have no weight; if
  * +inf occurs only the +inf tokens do.  A row without any token of weight (all -inf or NaN) gives token -1, logprob -inf.
- * min_p above 1 counts as 1, u outside [0, 1) as its nearer end, NaN as 0.  A parameter array that is NULL switches its
- * filter off for all rows (temperature: 1).  Results do not depend on timing or on the other rows' contents; the number
- * of rows chooses the order in which a row is summed, so that a u within about 1e-13 of a border between two tokens may fall
- * on either side of it.  logits may be a view with padding behind its rows; nothing of the padding is used.
+ * min_p above 1 counts as 1, u outside [0, 1) as its nearer end and u = NaN as 0; a NaN top_p or min_p switches its filter
+ * off for the row.  A parameter array that is NULL does so for all rows (temperature: 1).  Results do not depend on
+ * timing or on the other rows' contents; the number of rows chooses the order in which a row is summed, so that a u within
+ * about 1e-13 of a border between two tokens may fall on either side of it.  logits may be a view with padding behind its
+ * rows; nothing of the padding is used.
  * Errors: KAP_ERR_INVALID_ARG (NULL or misaligned pointer, vocab < 1, row_stride < vocab, negative rows),
  * KAP_ERR_UNSUPPORTED (logits_type, vocab above 811008, more rows than a grid can hold), KAP_ERR_CUDA.  Asynchronous on
  * cuda_stream, without a workspace; can be captured into a CUDA graph.

@@ -325,10 +325,10 @@ kap_sample_rows_kernel(const SampleParams p)
         return gather_level(partial, bins);
     };
 
-    const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? fminf(p.min_p[r], 1.f) : 0.f;
+    const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;     // NaN: no filter
     uint32_t min_p_cut = 0xffffffffu;                              // min-p as a cut: logits from the least float with weight enough on
     if (min_p > 0.f) {
-        const uint32_t least = logit_image(__double2float_ru(x_max + (double)t * log((double)min_p)));
+        const uint32_t least = logit_image(__double2float_ru(x_max + (double)t * log(fmin((double)min_p, 1.0))));
         min_p_cut = least < top ? top - least : 0u;
     }
     const double u01 = (double)p.uniform[r];
