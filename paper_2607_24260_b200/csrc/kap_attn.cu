@@ -317,13 +317,13 @@ bool launch_programmatically() { return g_use_pdl.load() != 0; }
 // The split kernel on the parts that kap_shared_prefix_attn gives it (mode 3): every item leaves a partial state.
 kap_status launch_prefix_parts(kap_workspace* ws, const void* kv_map, const void* q, const int32_t* bt_indptr, const int32_t* bt_pages,
                                const int32_t* ctx_len, const WorkItem* items, int32_t n_items, const void* row_map,
-                               int64_t num_pool_pages, int32_t batch, int32_t hq, int32_t hkv, float scale_log2, cudaStream_t stream) {
+                               const int32_t* q_end, int64_t num_pool_pages, int32_t batch, int32_t hq, int32_t hkv, float scale_log2, cudaStream_t stream) {
     AttnParams p{};
     p.q = (const __nv_bfloat16*)q; p.list_indptr = bt_indptr; p.phys_pages = bt_pages; p.ctx_len = ctx_len;
     p.items = items; p.part_o = ws->d_part_o; p.part_ml = ws->d_part_ml; p.status = ws->d_status;
     p.num_pool_pages = num_pool_pages; p.Hq = hq; p.Hkv = hkv; p.G = hq / hkv; p.rows_cap = 1; p.batch = batch;
     p.cluster = 1; p.early_kv = 0; p.ring_slots = ws->ring_slots; p.scale_log2 = scale_log2;
-    p.row_map = (const int2*)row_map;
+    p.row_map = (const int2*)row_map; p.q_end = q_end;
     const bool nhd = ws->kv_layout == KAP_KV_NHD;
     KAP_CUDA(cudaFuncSetAttribute(nhd ? kap_attn_split_kernel<3, true> : kap_attn_split_kernel<3, false>,
                                   cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes_for(kMaxSlots)));

@@ -87,6 +87,7 @@ struct AttnParams {
     int32_t ring_slots;              // page slots in the shared-memory ring (8, 12, 16 or 24)
     float scale_log2;                // sm_scale * log2(e)
     const int2* row_map;             // mode 3: a token row's (sequence, place in it minus n_q - 1)
+    const int32_t* q_end;            // mode 3: the caller's row count, q_indptr[batch]
 #ifdef KAP_TRACE
     unsigned long long* trace;       // [8192 records][8] timestamps of this launch (debug builds)
 #endif
@@ -312,14 +313,16 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     const int gid = lane >> 2, tid4 = lane & 3;
     const uint32_t* q_src[2];
     int q_tok[2];
+    const int64_t q_end = kParts ? *p.q_end : 0;             // (mode 3: rows that the caller does not have are not read)
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         const int R = rt * kRowTile + gid + half * 8;
         const bool valid = R < rows;
         q_tok[half] = valid ? R / p.G : item.n_q - 1;
-        q_src[half] = valid ? reinterpret_cast<const uint32_t*>(
+        const bool there = valid && (!kParts || q_row0 + q_tok[half] < q_end);
+        q_src[half] = there ? reinterpret_cast<const uint32_t*>(
             p.q + ((q_row0 + q_tok[half]) * p.Hq + kv_head * p.G + R % p.G) * kHeadDim) : nullptr;
-        if (valid && tid4 < 2)
+        if (there && tid4 < 2)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(q_src[half] + tid4 * 32) : "memory");
     }
     // ---- nothing else produced by earlier kernels (Q, fresh KV, partial buffers) is touched above

@@ -14,7 +14,7 @@ kap_status encode_query_map(void* map, const void* q, int64_t rows, int32_t hq, 
 bool launch_programmatically();
 kap_status launch_prefix_parts(kap_workspace* ws, const void* kv_map, const void* q, const int32_t* bt_indptr, const int32_t* bt_pages,
                                const int32_t* ctx_len, const WorkItem* items, int32_t n_items, const void* row_map,
-                               int64_t num_pool_pages, int32_t batch, int32_t hq, int32_t hkv, float scale_log2, cudaStream_t stream);
+                               const int32_t* q_end, int64_t num_pool_pages, int32_t batch, int32_t hq, int32_t hkv, float scale_log2, cudaStream_t stream);
 
 namespace {
 
@@ -128,12 +128,12 @@ extern "C" kap_status kap_shared_prefix_attn(
     p.cta_begin = reinterpret_cast<const int32_t*>(third + at.ctas);
     p.q_indptr = q_indptr; p.bt_indptr = bt_indptr; p.bt_pages = bt_pages; p.ctx_len = ctx_len;
     p.part_o = ws->d_part_o; p.part_ml = ws->d_part_ml; p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ws->d_status;
-    p.num_pool_pages = num_pool_pages; p.total_rows = (int32_t)ws->total_rows;
+    p.num_pool_pages = num_pool_pages; p.total_rows = (int32_t)ws->total_rows; p.q_end = q_indptr + batch;
     p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G; p.behind_parts = ws->n_items > 0;
     p.scale_log2 = sm_scale * 1.4426950408889634f;
     // the sequences' own pages and small prefixes, then the large prefixes, then the join of their states
     if (ws->n_items > 0) {
-        st = launch_prefix_parts(ws, kv_map, q, bt_indptr, bt_pages, ctx_len, ws->d_items, ws->n_items, p.row_map, num_pool_pages, batch,
+        st = launch_prefix_parts(ws, kv_map, q, bt_indptr, bt_pages, ctx_len, ws->d_items, ws->n_items, p.row_map, p.q_end, num_pool_pages, batch,
                                  num_q_heads, num_kv_heads, p.scale_log2, (cudaStream_t)cuda_stream);
         if (st != KAP_OK) return st;
     }

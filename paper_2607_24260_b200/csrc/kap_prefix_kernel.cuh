@@ -63,6 +63,7 @@ struct PfxParams {
     const PrefixRow* row_map;
     const PrefixUnit* units;
     const int32_t *q_indptr, *bt_indptr, *bt_pages, *ctx_len;
+    const int32_t* q_end;                                              // the caller's row count, q_indptr[batch]
     float *part_o, *part_ml;
     __nv_bfloat16* out;
     float* lse;
@@ -180,6 +181,7 @@ kap_prefix_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_const
         int slot = 0, loads = 0, q_use[2] = {0, 0}, q_slot = 0;
         uint32_t parity = 1;                                           // of the slots' free barriers: the first round does not wait
         bool ok = true;
+        const int q_end = *p.q_end;
         for (int k = seg0; k < seg1 && ok; ++k) {
             const PrefixSegment s = p.segments[k];
             const int list_at = p.bt_indptr[s.seq], listed = p.bt_indptr[s.seq + 1] - list_at;
@@ -199,9 +201,13 @@ kap_prefix_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_const
                 if (elect_one()) {
                     const uint32_t bar = smem_u32(&c->q_full[to]), dst = smem_u32(q_tiles) + to * kPfxQBytes;
                     const int tok = tok_row0 + t * (kPrefixTileRows / p.G);
-                    mbar_expect_tx(bar, kPfxQBytes);
-                    tma_load_3d(dst, &q_map, 0, kv_head * p.G, tok, bar, keep);
-                    tma_load_3d(dst + kPfxQHalfBytes, &q_map, 64, kv_head * p.G, tok, bar, keep);
+                    if (min(tok + kPrefixTileRows / p.G, p.total_rows) <= q_end) {
+                        mbar_expect_tx(bar, kPfxQBytes);
+                        tma_load_3d(dst, &q_map, 0, kv_head * p.G, tok, bar, keep);
+                        tma_load_3d(dst + kPfxQHalfBytes, &q_map, 64, kv_head * p.G, tok, bar, keep);
+                    } else {                                           // fewer rows than scheduled (reported by the merge pass): none are read
+                        mbar_arrive(bar);
+                    }
                 }
                 __syncwarp();
                 ++q_use[to];
@@ -473,10 +479,11 @@ kap_prefix_merge_kernel(const PfxParams p)
         n[1] = u.n_states; stride[1] = u.rows; at[1] = u.state_row0 + (row - s.row0) * p.G + h;
     }
     pdl_wait();
+    const int q_end = *p.q_end;                                        // rows behind it are not the caller's
     // not the scheduled rows, or a context that outgrew the schedule or its block table
     if (lane == 0 && (!kWide || warp == 0)) {
         const int most = min(s.list_pages, p.bt_indptr[where.seq + 1] - p.bt_indptr[where.seq]);
-        if (p.q_indptr[where.seq] != s.row0 || p.ctx_len[where.seq] > (long long)most * kPageSize) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
+        if (p.q_indptr[where.seq] != s.row0 || q_end != p.total_rows || p.ctx_len[where.seq] > (long long)most * kPageSize) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
     }
     Merged acc[H];
 #pragma unroll
@@ -520,6 +527,7 @@ kap_prefix_merge_kernel(const PfxParams p)
             for (int e = 0; e < H; ++e)
                 if (other_ml[w][e].y > 0.f) merge_into(acc[e], other_ml[w][e].x, other_ml[w][e].y, other_o[w][e][lane]);
     }
+    if (row >= q_end) return;
 #pragma unroll
     for (int e = 0; e < H; ++e) {
         const long long cell = (long long)row * p.hq + head + e;

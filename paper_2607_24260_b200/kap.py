@@ -287,6 +287,7 @@ class Workspace:
     def __init__(self, device=0, max_items=8192, max_rows_per_item=16, max_batch=256):
         self._h = C.c_void_p()
         self.device = int(device)
+        self.shared_prefix_rows = 0          # of the last schedule_shared_prefix
         self._destroy = lib().kap_workspace_destroy
         _check(lib().kap_workspace_create(C.byref(self._h), self.device, max_items,
                                           max_rows_per_item, max_batch))
@@ -323,6 +324,7 @@ class Workspace:
             self._h, int(list_len.shape[0]), _ptr(list_len, C.c_int32), _ptr(n_q, C.c_int32),
             int(prefix_pages.shape[0]), _ptr(group_indptr, C.c_int32), _ptr(prefix_pages, C.c_int32),
             num_q_heads, num_kv_heads, _stream_ptr(stream)))
+        self.shared_prefix_rows = int(n_q.sum())
 
     def info(self):
         v = [C.c_int32(0) for _ in range(5)]
@@ -386,8 +388,12 @@ def shared_prefix_items(list_len, n_q, group_indptr, prefix_pages, num_q_heads=3
 def shared_prefix_attn(q, q_indptr, kv_pool, bt_indptr, bt_pages, ctx_len, out, ws: Workspace, lse=None,
                        sm_scale=None, stream=None):
     """kap_shared_prefix_attn on torch CUDA tensors: the arguments and the result of verify_attn, for a
-    workspace scheduled with schedule_shared_prefix."""
-    _, Hq, d = q.shape
+    workspace scheduled with schedule_shared_prefix.  q, out and lse have at least the scheduled rows."""
+    (rows, Hq, d), (out_rows, out_heads, out_d), need = q.shape, out.shape, ws.shared_prefix_rows
+    lse_rows, lse_heads = (need, Hq) if lse is None else lse.shape
+    if rows < need or out_rows < need or lse_rows < need or out_heads != Hq or lse_heads != Hq or out_d != d:
+        raise KapError(ERR_INVALID_ARG, f"q {tuple(q.shape)}, out {tuple(out.shape)}, lse {None if lse is None else tuple(lse.shape)}: "
+                       f"expected at least {need} scheduled rows of {Hq} heads")
     pages, Hkv, P = _pool_shape(kv_pool, ws)
     sm_scale = float(d) ** -0.5 if sm_scale is None else float(sm_scale)
     _check(lib().kap_shared_prefix_attn(
