@@ -434,16 +434,16 @@ def append_kv(k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, new_indptr=No
                                _stream_ptr(stream)))
 
 
-def _head_rows(name, t, rows, heads):
+def _head_rows(name, t, rows, heads, d):
     """the row stride of a bf16 [rows, heads, d] tensor whose heads are contiguous within a row"""
     shape, stride = t.shape, t.stride()
-    if t.dtype is not _torch.bfloat16 or len(shape) != 3 or shape[0] != rows or shape[1] != heads:
-        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(shape)}, expected bfloat16 [{rows}, {heads}, d]")
-    if stride[2] != 1 or (heads > 1 and stride[1] != shape[2]):
+    if t.dtype is not _torch.bfloat16 or shape != (rows, heads, d):
+        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(shape)}, expected bfloat16 [{rows}, {heads}, {d}]")
+    if stride[2] != 1 or (heads > 1 and stride[1] != d):
         raise KapError(ERR_INVALID_ARG, f"{name} has strides {stride}: the heads of a row must be contiguous")
     if not t.is_cuda:
         raise KapError(ERR_INVALID_ARG, f"{name} is not on a GPU")
-    return heads * shape[2] if rows <= 1 else stride[0]
+    return heads * d if rows <= 1 else stride[0]
 
 
 def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_freq, q_out=None,
@@ -460,17 +460,17 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
     else:
         pages, _, Hkv, P, d = kv_pool.shape
     rows, Hq = k_new.shape[0], 0
-    ks, vs = _head_rows("k_new", k_new, rows, Hkv), _head_rows("v_new", v_new, rows, Hkv)
+    ks, vs = _head_rows("k_new", k_new, rows, Hkv, d), _head_rows("v_new", v_new, rows, Hkv, d)
     qs = os_ = 0
     if q is None:
         q_out = None
     else:
         Hq = q.shape[1]
-        qs = _head_rows("q", q, rows, Hq)
+        qs = _head_rows("q", q, rows, Hq, d)
         if q_out is None:
             q_out, os_ = q, qs
         else:
-            os_ = _head_rows("q_out", q_out, rows, Hq)
+            os_ = _head_rows("q_out", q_out, rows, Hq, d)
     axes, pos_stride = 0, 0
     if positions is not None:
         if positions.dim() == 1:

@@ -1,5 +1,5 @@
 """What the Python binding refuses before it hands pointers on: tensors whose shapes, types, strides or devices the kernels would
-misread.  Nothing is launched: the tensors here only say that they are on a GPU and have addresses that nobody follows."""
+misread.  The C entry points are replaced by ones that only note their arguments, and the tensors here only say that they are on a GPU."""
 import pytest
 import torch
 
@@ -40,6 +40,19 @@ def gpu(*shape, dtype=BF, index=0):
     return OnGpu(torch.empty(shape, dtype=dtype, device="meta"), index)
 
 
+@pytest.fixture(autouse=True)
+def noted(monkeypatch):
+    """the arguments of the C calls that the binding makes"""
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: calls.append((name, args)) or kap.OK
+
+    monkeypatch.setattr(kap, "_lib", Library())
+    return calls
+
+
 class Scheduled:
     """a workspace that holds a shared-prefix schedule of so many rows"""
 
@@ -59,24 +72,49 @@ def attend(rows=8, hq=8, hkv=2, batch=2, **change):
     kap.shared_prefix_attn(**a)
 
 
-def passes_the_binding(call):
-    """the C entry point answers: here with an error of its own, since there is neither a workspace nor a GPU"""
-    with pytest.raises(kap.KapError) as e:
-        call()
-    return "NULL workspace" in str(e.value)
+def refused(noted, match, call, **change):
+    with pytest.raises(kap.KapError, match=match) as e:
+        call(**change)
+    assert e.value.code == kap.ERR_INVALID_ARG and not noted
 
 
-def test_shared_prefix_attn_takes_the_scheduled_rows_and_more():
-    assert passes_the_binding(attend)
-    assert passes_the_binding(lambda: attend(rows=11))
-    assert passes_the_binding(lambda: attend(q=gpu(11, 8, 128), lse=None))
+def test_shared_prefix_attn_takes_the_scheduled_rows_and_more(noted):
+    attend()
+    attend(rows=11)
+    attend(q=gpu(11, 8, 128), lse=None)
+    assert [name for name, _ in noted] == ["kap_shared_prefix_attn"] * 3
 
 
 @pytest.mark.parametrize("change", [
     dict(rows=2), dict(rows=7), dict(q=gpu(7, 8, 128)), dict(out=gpu(7, 8, 128)), dict(lse=gpu(7, 8, dtype=F32)), dict(lse=gpu(8, 7, dtype=F32)),
     dict(out=gpu(8, 4, 128)), dict(out=gpu(8, 8, 64)), dict(ws=Scheduled(9)),
 ])
-def test_shared_prefix_attn_refuses_arrays_with_fewer_rows_than_scheduled(change):
-    with pytest.raises(kap.KapError, match="scheduled rows") as e:
-        attend(**change)
-    assert e.value.code == kap.ERR_INVALID_ARG
+def test_shared_prefix_attn_refuses_arrays_with_fewer_rows_than_scheduled(noted, change):
+    refused(noted, "scheduled rows", attend, **change)
+
+
+def append(rows=4, hq=8, hkv=2, batch=4, d=128, **change):
+    a = dict(q=gpu(rows, hq, d), k_new=gpu(rows, hkv, d), v_new=gpu(rows, hkv, d), kv_pool=gpu(9, 2, hkv, 16, 128), bt_indptr=gpu(batch + 1, dtype=I32),
+             bt_pages=gpu(12, dtype=I32), ctx_len=gpu(batch, dtype=I32), inv_freq=gpu(64, dtype=F32), q_out=gpu(rows, hq, d), stream=STREAM)
+    assert set(change) <= set(a) | {"new_indptr", "positions", "freq_axis", "position_offset", "device_status", "kv_layout"}
+    a.update(change)
+    kap.append_kv_rope(**a)
+
+
+def test_append_kv_rope_passes_views_of_a_fused_projection_on(noted):
+    fused = gpu(4, 12, 128)
+    append(q=fused[:, :8], k_new=fused[:, 8:10], v_new=fused[:, 10:], q_out=None)
+    append(q=None)
+    append(kv_pool=gpu(9, 2, 16, 2, 128), kv_layout=kap.KV_NHD)
+    strides = noted[0][1]
+    assert (strides[1], strides[3], strides[5], strides[7]) == (12 * 128,) * 4 and strides[6] == strides[0]
+    assert len(noted) == 3
+
+
+@pytest.mark.parametrize("change", [
+    # heads of 64 columns whose rows are far enough apart for two heads of 128
+    dict(k_new=gpu(4, 32, 64)[:, 16:18], v_new=gpu(4, 32, 64)[:, 18:20]), dict(k_new=gpu(4, 32, 64)[:, 16:18]), dict(v_new=gpu(4, 32, 64)[:, 16:18]),
+    dict(q=gpu(4, 32, 64)[:, :8]), dict(q=gpu(4, 32, 64)[:, :8], q_out=None), dict(q_out=gpu(4, 32, 64)[:, :8]), dict(d=64), dict(d=256),
+])
+def test_append_kv_rope_refuses_heads_of_another_width_than_the_pools(noted, change):
+    refused(noted, "expected bfloat16", append, **change)
