@@ -446,6 +446,18 @@ def _head_rows(name, t, rows, heads, d):
     return heads * d if rows <= 1 else stride[0]
 
 
+def _check_pool(kv_pool):
+    if kv_pool.dtype is not _torch.bfloat16 or kv_pool.shape[1] != 2 or not kv_pool.is_contiguous():
+        raise KapError(ERR_INVALID_ARG, f"kv_pool is {kv_pool.dtype} {tuple(kv_pool.shape)} with strides {kv_pool.stride()}, "
+                       f"expected a contiguous bfloat16 tensor of K and V")
+
+
+def _check_index(name, t, least):
+    if t.dtype is not _torch.int32 or t.numel() < least or not t.is_contiguous():
+        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)} with strides {t.stride()}, expected a contiguous int32 tensor "
+                       f"of at least {least}")
+
+
 def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_freq, q_out=None,
                    new_indptr=None, positions=None, freq_axis=None, position_offset=None,
                    interleaved=False, advance=True, device_status=None, stream=None, kv_layout=KV_HND):
@@ -488,11 +500,22 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
         axis = bytes(freq_axis) if type(freq_axis) in (list, tuple, bytes) else _np(freq_axis, np.uint8).tobytes()
         if len(axis) != rot // 2:
             raise KapError(ERR_INVALID_ARG, f"freq_axis names {len(axis)} pairs, inv_freq {rot // 2}")
+    batch = ctx_len.shape[0]
+    _check_pool(kv_pool)
+    _check_index("bt_indptr", bt_indptr, batch + 1)
+    _check_index("bt_pages", bt_pages, 0)
+    _check_index("ctx_len", ctx_len, batch)
+    if new_indptr is not None:
+        _check_index("new_indptr", new_indptr, batch + 1)
+    if position_offset is not None:
+        _check_index("position_offset", position_offset, batch)
+    if device_status is not None:
+        _check_index("device_status", device_status, 1)
     _check(lib().kap_append_kv_rope(
         _dptr(q), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, _dptr(q_out), os_, _dptr(new_indptr), rows,
         inv_freq.data_ptr(), rot, 1 if interleaved else 0, _dptr(positions), pos_stride, axes, axis,
         _dptr(position_offset), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
-        ctx_len.data_ptr(), 1 if advance else 0, ctx_len.shape[0], Hq, Hkv, d, P, kv_layout,
+        ctx_len.data_ptr(), 1 if advance else 0, batch, Hq, Hkv, d, P, kv_layout,
         _dptr(device_status), _stream_ptr(stream)))
 
 

@@ -118,3 +118,29 @@ def test_append_kv_rope_passes_views_of_a_fused_projection_on(noted):
 ])
 def test_append_kv_rope_refuses_heads_of_another_width_than_the_pools(noted, change):
     refused(noted, "expected bfloat16", append, **change)
+
+
+@pytest.mark.parametrize("change", [
+    dict(bt_indptr=gpu(5, dtype=I64)), dict(bt_pages=gpu(12, dtype=I64)), dict(ctx_len=gpu(4, dtype=I64)), dict(ctx_len=gpu(4, dtype=F32)),
+    dict(bt_pages=gpu(24, dtype=I32)[::2]), dict(bt_indptr=gpu(10, dtype=I32)[::2]), dict(ctx_len=gpu(4, 2, dtype=I32)[:, 0]),
+    dict(bt_indptr=gpu(4, dtype=I32)), dict(new_indptr=gpu(5, dtype=I64)), dict(new_indptr=gpu(4, dtype=I32)), dict(new_indptr=gpu(10, dtype=I32)[::2]),
+    dict(position_offset=gpu(4, dtype=I64)), dict(position_offset=gpu(3, dtype=I32)), dict(position_offset=gpu(4, dtype=F32)),
+    dict(device_status=gpu(1, dtype=I64)), dict(device_status=gpu(0, dtype=I32)),
+])
+def test_append_kv_rope_refuses_index_arrays_that_it_would_misread(noted, change):
+    refused(noted, "contiguous int32", append, **change)
+
+
+def test_append_kv_rope_takes_longer_index_arrays(noted):
+    append(bt_indptr=gpu(9, dtype=I32), new_indptr=gpu(9, dtype=I32), position_offset=gpu(9, dtype=I32), device_status=gpu(2, dtype=I32))
+    append(new_indptr=gpu(5, dtype=I32), position_offset=gpu(4, dtype=I32), device_status=gpu(1, dtype=I32))
+    assert len(noted) == 2
+
+
+@pytest.mark.parametrize("change", [
+    dict(kv_pool=gpu(9, 2, 2, 16, 128, dtype=torch.float16)), dict(kv_pool=gpu(9, 2, 2, 16, 128, dtype=F32)),
+    dict(kv_pool=gpu(9, 2, 16, 2, 128).transpose(2, 3)), dict(kv_pool=gpu(18, 2, 2, 16, 128)[::2]), dict(kv_pool=gpu(9, 3, 2, 16, 128)[:, :2]),
+    dict(kv_pool=gpu(9, 1, 2, 16, 128)), dict(kv_pool=gpu(9, 3, 2, 16, 128)),
+])
+def test_append_kv_rope_refuses_pools_that_are_not_dense_bf16(noted, change):
+    refused(noted, "kv_pool", append, **change)
