@@ -281,6 +281,19 @@ def _pool_shape(kv_pool, ws):
     return (pages, b, a) if getattr(ws, "kv_layout", KV_HND) == KV_NHD else (pages, a, b)
 
 
+def _check_pool(kv_pool, d):
+    shape = kv_pool.shape
+    if kv_pool.dtype is not _torch.bfloat16 or shape[1] != 2 or shape[4] != d or not kv_pool.is_contiguous():
+        raise KapError(ERR_INVALID_ARG, f"kv_pool is {kv_pool.dtype} {tuple(shape)} with strides {kv_pool.stride()}, "
+                       f"expected a contiguous bfloat16 tensor of K and V with {d} columns")
+
+
+def _check_index(name, t, least):
+    if t.dtype is not _torch.int32 or t.numel() < least or not t.is_contiguous():
+        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)} with strides {t.stride()}, expected a contiguous int32 tensor "
+                       f"of at least {least}")
+
+
 class Workspace:
     """kap_workspace: split-K schedule + partial-result buffers for one launch shape."""
 
@@ -394,11 +407,24 @@ def shared_prefix_attn(q, q_indptr, kv_pool, bt_indptr, bt_pages, ctx_len, out, 
     if rows < need or out_rows < need or lse_rows < need or out_heads != Hq or lse_heads != Hq or out_d != d:
         raise KapError(ERR_INVALID_ARG, f"q {tuple(q.shape)}, out {tuple(out.shape)}, lse {None if lse is None else tuple(lse.shape)}: "
                        f"expected at least {need} scheduled rows of {Hq} heads")
+    torch = _torch_module()
+    bf16 = torch.bfloat16
+    if q.dtype is not bf16 or out.dtype is not bf16 or not q.is_contiguous() or not out.is_contiguous():
+        raise KapError(ERR_INVALID_ARG, f"q is {q.dtype} with strides {q.stride()}, out {out.dtype} with strides {out.stride()}: "
+                       f"expected contiguous bfloat16 tensors")
+    if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous()):
+        raise KapError(ERR_INVALID_ARG, f"lse is {lse.dtype} with strides {lse.stride()}, expected a contiguous float32 tensor")
+    _check_pool(kv_pool, d)
+    batch = ctx_len.shape[0]
+    _check_index("q_indptr", q_indptr, batch + 1)
+    _check_index("bt_indptr", bt_indptr, batch + 1)
+    _check_index("bt_pages", bt_pages, 0)
+    _check_index("ctx_len", ctx_len, batch)
     pages, Hkv, P = _pool_shape(kv_pool, ws)
-    sm_scale = float(d) ** -0.5 if sm_scale is None else float(sm_scale)
+    sm_scale = d ** -0.5 if sm_scale is None else float(sm_scale)
     _check(lib().kap_shared_prefix_attn(
-        _dptr(q), _dptr(q_indptr), _dptr(kv_pool), int(pages), _dptr(bt_indptr), _dptr(bt_pages),
-        _dptr(ctx_len), int(ctx_len.shape[0]), Hq, Hkv, d, P, sm_scale, _dptr(out), _dptr(lse),
+        q.data_ptr(), q_indptr.data_ptr(), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
+        ctx_len.data_ptr(), batch, Hq, Hkv, d, P, sm_scale, out.data_ptr(), _dptr(lse),
         ws._h, _stream_ptr(stream)))
     return out
 
@@ -446,18 +472,6 @@ def _head_rows(name, t, rows, heads, d):
     return heads * d if rows <= 1 else stride[0]
 
 
-def _check_pool(kv_pool):
-    if kv_pool.dtype is not _torch.bfloat16 or kv_pool.shape[1] != 2 or not kv_pool.is_contiguous():
-        raise KapError(ERR_INVALID_ARG, f"kv_pool is {kv_pool.dtype} {tuple(kv_pool.shape)} with strides {kv_pool.stride()}, "
-                       f"expected a contiguous bfloat16 tensor of K and V")
-
-
-def _check_index(name, t, least):
-    if t.dtype is not _torch.int32 or t.numel() < least or not t.is_contiguous():
-        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)} with strides {t.stride()}, expected a contiguous int32 tensor "
-                       f"of at least {least}")
-
-
 def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_freq, q_out=None,
                    new_indptr=None, positions=None, freq_axis=None, position_offset=None,
                    interleaved=False, advance=True, device_status=None, stream=None, kv_layout=KV_HND):
@@ -501,7 +515,7 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
         if len(axis) != rot // 2:
             raise KapError(ERR_INVALID_ARG, f"freq_axis names {len(axis)} pairs, inv_freq {rot // 2}")
     batch = ctx_len.shape[0]
-    _check_pool(kv_pool)
+    _check_pool(kv_pool, d)
     _check_index("bt_indptr", bt_indptr, batch + 1)
     _check_index("bt_pages", bt_pages, 0)
     _check_index("ctx_len", ctx_len, batch)

@@ -144,3 +144,23 @@ def test_append_kv_rope_takes_longer_index_arrays(noted):
 ])
 def test_append_kv_rope_refuses_pools_that_are_not_dense_bf16(noted, change):
     refused(noted, "kv_pool", append, **change)
+
+
+@pytest.mark.parametrize("change,match", [
+    (dict(q=gpu(8, 8, 128, dtype=torch.float16)), "bfloat16"), (dict(q=gpu(8, 8, 128, dtype=F32)), "bfloat16"), (dict(out=gpu(8, 8, 128, dtype=F32)), "bfloat16"),
+    (dict(q=gpu(8, 12, 128)[:, :8]), "contiguous"), (dict(q=gpu(16, 8, 128)[::2]), "contiguous"), (dict(out=gpu(8, 8, 256)[..., :128]), "contiguous"),
+    (dict(q=gpu(8, 8, 128).transpose(0, 1)), "contiguous"), (dict(lse=gpu(8, 8)), "lse"), (dict(lse=gpu(8, 8, dtype=F32).transpose(0, 1)), "lse"),
+    (dict(kv_pool=gpu(9, 2, 2, 16, 128, dtype=torch.float16)), "kv_pool"), (dict(kv_pool=gpu(9, 2, 16, 2, 128).transpose(2, 3)), "kv_pool"),
+    (dict(kv_pool=gpu(18, 2, 2, 16, 128)[::2]), "kv_pool"), (dict(kv_pool=gpu(9, 2, 2, 16, 64)), "kv_pool"),
+    (dict(q_indptr=gpu(3, dtype=I64)), "q_indptr"), (dict(q_indptr=gpu(2, dtype=I32)), "q_indptr"), (dict(bt_indptr=gpu(3, dtype=I64)), "bt_indptr"),
+    (dict(bt_indptr=gpu(2, dtype=I32)), "bt_indptr"), (dict(bt_pages=gpu(12, dtype=I64)), "bt_pages"), (dict(bt_pages=gpu(24, dtype=I32)[::2]), "bt_pages"),
+    (dict(ctx_len=gpu(2, dtype=I64)), "ctx_len"), (dict(ctx_len=gpu(4, dtype=I32)[::2]), "ctx_len"),
+])
+def test_shared_prefix_attn_refuses_arrays_that_it_would_misread(noted, change, match):
+    refused(noted, match, attend, **change)
+
+
+def test_shared_prefix_attn_takes_pools_of_either_layout(noted):
+    attend(kv_pool=gpu(9, 2, 16, 2, 128), ws=Scheduled(8, kap.KV_NHD))
+    attend(q_indptr=gpu(9, dtype=I32), bt_indptr=gpu(9, dtype=I32))
+    assert len(noted) == 2
