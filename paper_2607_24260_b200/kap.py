@@ -252,14 +252,14 @@ def schedule_host(list_len, n_q, num_q_heads, num_kv_heads, cta_slots, max_chunk
 
 
 # ------------------------------------------------------------------------- workspace + attention
-_torch = None
+_torch = _BF16 = _F32 = _I32 = None
 
 
 def _torch_module():
-    global _torch
+    global _torch, _BF16, _F32, _I32
     if _torch is None:
         import torch
-        _torch = torch
+        _torch, _BF16, _F32, _I32 = torch, torch.bfloat16, torch.float32, torch.int32
     return _torch
 
 
@@ -269,6 +269,14 @@ def _stream_ptr(stream=None):
         return stream.cuda_stream
     torch = _torch_module()
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _stream_on(dev, stream):
+    """_stream_ptr for tensors on device dev: kernels are launched on the current device, so they have to be there"""
+    current = _torch.cuda.current_device()
+    if dev != current:
+        raise KapError(ERR_INVALID_ARG, f"the tensors are on device {dev}, but device {current} is current")
+    return _torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _dptr(t):
@@ -281,17 +289,17 @@ def _pool_shape(kv_pool, ws):
     return (pages, b, a) if getattr(ws, "kv_layout", KV_HND) == KV_NHD else (pages, a, b)
 
 
-def _check_pool(kv_pool, d):
+def _check_pool(kv_pool, d, dev):
     shape = kv_pool.shape
-    if kv_pool.dtype is not _torch.bfloat16 or shape[1] != 2 or shape[4] != d or not kv_pool.is_contiguous():
-        raise KapError(ERR_INVALID_ARG, f"kv_pool is {kv_pool.dtype} {tuple(shape)} with strides {kv_pool.stride()}, "
-                       f"expected a contiguous bfloat16 tensor of K and V with {d} columns")
+    if kv_pool.dtype is not _BF16 or shape[1] != 2 or shape[4] != d or not kv_pool.is_contiguous() or kv_pool.get_device() != dev:
+        raise KapError(ERR_INVALID_ARG, f"kv_pool is {kv_pool.dtype} {tuple(shape)} with strides {kv_pool.stride()} on {kv_pool.device}, "
+                       f"expected a contiguous bfloat16 tensor of K and V with {d} columns on GPU {dev}")
 
 
-def _check_index(name, t, least):
-    if t.dtype is not _torch.int32 or t.numel() < least or not t.is_contiguous():
-        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)} with strides {t.stride()}, expected a contiguous int32 tensor "
-                       f"of at least {least}")
+def _check_index(name, t, least, dev):
+    if t.dtype is not _I32 or t.get_device() != dev or not t.is_contiguous() or t.numel() < least:
+        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}, expected a "
+                       f"contiguous int32 tensor of at least {least} on GPU {dev}")
 
 
 class Workspace:
@@ -407,25 +415,25 @@ def shared_prefix_attn(q, q_indptr, kv_pool, bt_indptr, bt_pages, ctx_len, out, 
     if rows < need or out_rows < need or lse_rows < need or out_heads != Hq or lse_heads != Hq or out_d != d:
         raise KapError(ERR_INVALID_ARG, f"q {tuple(q.shape)}, out {tuple(out.shape)}, lse {None if lse is None else tuple(lse.shape)}: "
                        f"expected at least {need} scheduled rows of {Hq} heads")
-    torch = _torch_module()
-    bf16 = torch.bfloat16
-    if q.dtype is not bf16 or out.dtype is not bf16 or not q.is_contiguous() or not out.is_contiguous():
-        raise KapError(ERR_INVALID_ARG, f"q is {q.dtype} with strides {q.stride()}, out {out.dtype} with strides {out.stride()}: "
-                       f"expected contiguous bfloat16 tensors")
-    if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous()):
-        raise KapError(ERR_INVALID_ARG, f"lse is {lse.dtype} with strides {lse.stride()}, expected a contiguous float32 tensor")
-    _check_pool(kv_pool, d)
+    _torch_module()
+    dev = ws.device
+    if q.dtype is not _BF16 or out.dtype is not _BF16 or not q.is_contiguous() or not out.is_contiguous() or q.get_device() != dev or out.get_device() != dev:
+        raise KapError(ERR_INVALID_ARG, f"q is {q.dtype} with strides {q.stride()} on {q.device}, out {out.dtype} with strides {out.stride()} on "
+                       f"{out.device}: expected contiguous bfloat16 tensors on GPU {dev}, the workspace's device")
+    if lse is not None and (lse.dtype is not _F32 or not lse.is_contiguous() or lse.get_device() != dev):
+        raise KapError(ERR_INVALID_ARG, f"lse is {lse.dtype} with strides {lse.stride()} on {lse.device}, expected a contiguous float32 tensor on GPU {dev}")
+    _check_pool(kv_pool, d, dev)
     batch = ctx_len.shape[0]
-    _check_index("q_indptr", q_indptr, batch + 1)
-    _check_index("bt_indptr", bt_indptr, batch + 1)
-    _check_index("bt_pages", bt_pages, 0)
-    _check_index("ctx_len", ctx_len, batch)
+    _check_index("q_indptr", q_indptr, batch + 1, dev)
+    _check_index("bt_indptr", bt_indptr, batch + 1, dev)
+    _check_index("bt_pages", bt_pages, 0, dev)
+    _check_index("ctx_len", ctx_len, batch, dev)
     pages, Hkv, P = _pool_shape(kv_pool, ws)
     sm_scale = d ** -0.5 if sm_scale is None else float(sm_scale)
     _check(lib().kap_shared_prefix_attn(
         q.data_ptr(), q_indptr.data_ptr(), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
         ctx_len.data_ptr(), batch, Hq, Hkv, d, P, sm_scale, out.data_ptr(), _dptr(lse),
-        ws._h, _stream_ptr(stream)))
+        ws._h, _stream_on(dev, stream)))
     return out
 
 
@@ -460,15 +468,15 @@ def append_kv(k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, new_indptr=No
                                _stream_ptr(stream)))
 
 
-def _head_rows(name, t, rows, heads, d):
+def _head_rows(name, t, rows, heads, d, dev):
     """the row stride of a bf16 [rows, heads, d] tensor whose heads are contiguous within a row"""
-    shape, stride = t.shape, t.stride()
-    if t.dtype is not _torch.bfloat16 or shape != (rows, heads, d):
-        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(shape)}, expected bfloat16 [{rows}, {heads}, {d}]")
+    if t.dtype is not _BF16 or t.shape != (rows, heads, d) or t.get_device() != dev:
+        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}, expected bfloat16 [{rows}, {heads}, {d}] on GPU {dev}")
+    if t.is_contiguous():
+        return heads * d
+    stride = t.stride()
     if stride[2] != 1 or (heads > 1 and stride[1] != d):
         raise KapError(ERR_INVALID_ARG, f"{name} has strides {stride}: the heads of a row must be contiguous")
-    if not t.is_cuda:
-        raise KapError(ERR_INVALID_ARG, f"{name} is not on a GPU")
     return heads * d if rows <= 1 else stride[0]
 
 
@@ -480,34 +488,36 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
     append_kv.  q_out None rotates q in place; q None handles k and v only.  positions None: the
     logical index (+ position_offset[b]); else int32 [rows] or [axes, rows], freq_axis naming the axis
     of each pair (host sequence)."""
-    torch = _torch_module()
+    _torch_module()
     if kv_layout == KV_NHD:
         pages, _, P, Hkv, d = kv_pool.shape
     else:
         pages, _, Hkv, P, d = kv_pool.shape
-    rows, Hq = k_new.shape[0], 0
-    ks, vs = _head_rows("k_new", k_new, rows, Hkv, d), _head_rows("v_new", v_new, rows, Hkv, d)
+    rows, Hq, dev = k_new.shape[0], 0, k_new.get_device()
+    if dev < 0:
+        raise KapError(ERR_INVALID_ARG, "k_new is not on a GPU")
+    ks, vs = _head_rows("k_new", k_new, rows, Hkv, d, dev), _head_rows("v_new", v_new, rows, Hkv, d, dev)
     qs = os_ = 0
     if q is None:
         q_out = None
     else:
         Hq = q.shape[1]
-        qs = _head_rows("q", q, rows, Hq, d)
+        qs = _head_rows("q", q, rows, Hq, d, dev)
         if q_out is None:
             q_out, os_ = q, qs
         else:
-            os_ = _head_rows("q_out", q_out, rows, Hq, d)
+            os_ = _head_rows("q_out", q_out, rows, Hq, d, dev)
     axes, pos_stride = 0, 0
     if positions is not None:
         if positions.dim() == 1:
             positions = positions.view(1, -1)
-        if positions.dtype is not torch.int32 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1) or not positions.is_cuda:
-            raise KapError(ERR_INVALID_ARG, f"positions {positions.dtype} {tuple(positions.shape)} on {positions.device} for {rows} rows")
+        if positions.dtype is not _I32 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1) or positions.get_device() != dev:
+            raise KapError(ERR_INVALID_ARG, f"positions {positions.dtype} {tuple(positions.shape)} on {positions.device} for {rows} rows on GPU {dev}")
         axes, pos_stride = positions.shape[0], positions.stride(0)
         if axes == 1:
             pos_stride = max(pos_stride, rows)
-    if inv_freq.dtype is not torch.float32 or not inv_freq.is_contiguous() or not inv_freq.is_cuda:
-        raise KapError(ERR_INVALID_ARG, f"inv_freq must be a contiguous float32 tensor on a GPU, not {inv_freq.dtype}")
+    if inv_freq.dtype is not _F32 or not inv_freq.is_contiguous() or inv_freq.get_device() != dev:
+        raise KapError(ERR_INVALID_ARG, f"inv_freq must be a contiguous float32 tensor on GPU {dev}, not {inv_freq.dtype} on {inv_freq.device}")
     rot = 2 * inv_freq.shape[0]
     axis = None
     if freq_axis is not None:
@@ -515,22 +525,22 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
         if len(axis) != rot // 2:
             raise KapError(ERR_INVALID_ARG, f"freq_axis names {len(axis)} pairs, inv_freq {rot // 2}")
     batch = ctx_len.shape[0]
-    _check_pool(kv_pool, d)
-    _check_index("bt_indptr", bt_indptr, batch + 1)
-    _check_index("bt_pages", bt_pages, 0)
-    _check_index("ctx_len", ctx_len, batch)
+    _check_pool(kv_pool, d, dev)
+    _check_index("bt_indptr", bt_indptr, batch + 1, dev)
+    _check_index("bt_pages", bt_pages, 0, dev)
+    _check_index("ctx_len", ctx_len, batch, dev)
     if new_indptr is not None:
-        _check_index("new_indptr", new_indptr, batch + 1)
+        _check_index("new_indptr", new_indptr, batch + 1, dev)
     if position_offset is not None:
-        _check_index("position_offset", position_offset, batch)
+        _check_index("position_offset", position_offset, batch, dev)
     if device_status is not None:
-        _check_index("device_status", device_status, 1)
+        _check_index("device_status", device_status, 1, dev)
     _check(lib().kap_append_kv_rope(
         _dptr(q), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, _dptr(q_out), os_, _dptr(new_indptr), rows,
         inv_freq.data_ptr(), rot, 1 if interleaved else 0, _dptr(positions), pos_stride, axes, axis,
         _dptr(position_offset), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
         ctx_len.data_ptr(), 1 if advance else 0, batch, Hq, Hkv, d, P, kv_layout,
-        _dptr(device_status), _stream_ptr(stream)))
+        _dptr(device_status), _stream_on(dev, stream)))
 
 
 def sample_tokens(logits, uniform, token, logprob=None, temperature=None, top_k=None, top_p=None,
@@ -538,24 +548,24 @@ def sample_tokens(logits, uniform, token, logprob=None, temperature=None, top_k=
     """kap_sample_tokens on torch CUDA tensors: logits fp32 or bf16 [rows, vocab] (any row stride), uniform
     fp32 [rows]; outputs int32 token [rows] and optional fp32 logprob [rows].  temperature, top_p,
     min_p (fp32 [rows]) and top_k (int32 [rows]) are optional; None switches a filter off."""
-    torch = _torch_module()
-    kind = LOGITS_F32 if logits.dtype is torch.float32 else LOGITS_BF16 if logits.dtype is torch.bfloat16 else None
+    _torch_module()
+    kind = LOGITS_F32 if logits.dtype is _F32 else LOGITS_BF16 if logits.dtype is _BF16 else None
     if kind is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1) or not logits.is_cuda:
         raise KapError(ERR_INVALID_ARG, f"logits are {logits.dtype} {tuple(logits.shape)} with strides {logits.stride()} on {logits.device}")
-    rows, vocab = logits.shape
+    (rows, vocab), dev = logits.shape, logits.get_device()
 
     def ptr(name, t, dt):
         if t is None:
             return None
-        if t.dtype is not dt or t.numel() != rows or not t.is_contiguous() or not t.is_cuda:
-            raise KapError(ERR_INVALID_ARG, f"{name} must be a contiguous {dt} tensor of {rows} on a GPU")
+        if t.dtype is not dt or t.numel() != rows or not t.is_contiguous() or t.get_device() != dev:
+            raise KapError(ERR_INVALID_ARG, f"{name} must be a contiguous {dt} tensor of {rows} on GPU {dev}")
         return t.data_ptr()
 
-    f32, i32 = torch.float32, torch.int32
+    f32, i32 = _F32, _I32
     _check(lib().kap_sample_tokens(
         logits.data_ptr(), kind, vocab if rows <= 1 else logits.stride(0), rows, vocab,
         ptr("temperature", temperature, f32), ptr("top_k", top_k, i32), ptr("top_p", top_p, f32), ptr("min_p", min_p, f32),
-        ptr("uniform", uniform, f32), ptr("token", token, i32), ptr("logprob", logprob, f32), _stream_ptr(stream)))
+        ptr("uniform", uniform, f32), ptr("token", token, i32), ptr("logprob", logprob, f32), _stream_on(dev, stream)))
 
 
 def top3_accept(logits, row_indptr, proposed, top3, accepted, next_token, stream=None, ctx_len=None):

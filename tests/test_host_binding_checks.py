@@ -50,6 +50,7 @@ def noted(monkeypatch):
             return lambda *args: calls.append((name, args)) or kap.OK
 
     monkeypatch.setattr(kap, "_lib", Library())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     return calls
 
 
@@ -164,3 +165,48 @@ def test_shared_prefix_attn_takes_pools_of_either_layout(noted):
     attend(kv_pool=gpu(9, 2, 16, 2, 128), ws=Scheduled(8, kap.KV_NHD))
     attend(q_indptr=gpu(9, dtype=I32), bt_indptr=gpu(9, dtype=I32))
     assert len(noted) == 2
+
+
+def sample(rows=4, vocab=50, **change):
+    f = lambda dtype=F32: gpu(rows, dtype=dtype)                                  # noqa: E731
+    a = dict(logits=gpu(rows, vocab, dtype=F32), uniform=f(), token=f(I32), logprob=f(), temperature=f(), top_k=f(I32), top_p=f(), min_p=f(), stream=STREAM)
+    assert set(change) <= set(a)
+    a.update(change)
+    kap.sample_tokens(**a)
+
+
+APPEND = dict(q=(4, 8, 128), k_new=(4, 2, 128), v_new=(4, 2, 128), kv_pool=(9, 2, 2, 16, 128), bt_indptr=(5, I32), bt_pages=(12, I32), ctx_len=(4, I32),
+              inv_freq=(64, F32), q_out=(4, 8, 128), new_indptr=(5, I32), positions=(4, I32), device_status=(1, I32))
+OFFSET = dict(position_offset=(4, I32))
+ATTEND = dict(q=(8, 8, 128), q_indptr=(3, I32), kv_pool=(9, 2, 2, 16, 128), bt_indptr=(3, I32), bt_pages=(12, I32), ctx_len=(2, I32), out=(8, 8, 128), lse=(8, 8, F32))
+SAMPLE = dict(logits=(4, 50, F32), uniform=(4, F32), token=(4, I32), logprob=(4, F32), temperature=(4, F32), top_k=(4, I32), top_p=(4, F32), min_p=(4, F32))
+
+
+def shape_type(s):
+    return (s[:-1], s[-1]) if isinstance(s[-1], torch.dtype) else (s, BF)
+
+
+EACH = [(call, name, shape) for call, arrays in ((append, APPEND), (append, OFFSET), (attend, ATTEND), (sample, SAMPLE)) for name, shape in arrays.items()]
+
+
+@pytest.mark.parametrize("call,name,shape", EACH, ids=lambda x: x if isinstance(x, str) else getattr(x, "__name__", ""))
+def test_an_array_on_another_device_than_the_others_is_refused(noted, call, name, shape):
+    size, dtype = shape_type(shape)
+    refused(noted, "GPU|device", call, **{name: gpu(*size, dtype=dtype, index=1)})
+    refused(noted, "GPU|on cpu", call, **{name: torch.empty(size, dtype=dtype)})  # in host memory
+
+
+@pytest.mark.parametrize("call,arrays", [(append, APPEND), (attend, ATTEND), (sample, SAMPLE)], ids=["append", "attend", "sample"])
+def test_arrays_on_another_device_than_the_current_one_are_refused(noted, monkeypatch, call, arrays):
+    there = {}
+    for name, shape in arrays.items():
+        size, dtype = shape_type(shape)
+        there[name] = gpu(*size, dtype=dtype, index=1)
+    refused(noted, "device", call, **there)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    if call is attend:                                                            # the workspace is on device 0
+        refused(noted, "device", call, **there)
+        there["ws"] = Scheduled(8)
+        there["ws"].device = 1
+    call(**there)
+    assert len(noted) == 1
