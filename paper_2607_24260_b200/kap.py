@@ -289,11 +289,14 @@ def _pool_shape(kv_pool, ws):
     return (pages, b, a) if getattr(ws, "kv_layout", KV_HND) == KV_NHD else (pages, a, b)
 
 
-def _check_pool(kv_pool, d, dev):
+def _dense_pool(kv_pool, nhd, dev):
+    """(pages, Hkv, P, d) of a pool tensor that the kernels can address"""
     shape = kv_pool.shape
-    if kv_pool.dtype is not _BF16 or shape[1] != 2 or shape[4] != d or not kv_pool.is_contiguous() or kv_pool.get_device() != dev:
+    if kv_pool.dtype is not _BF16 or shape[1] != 2 or not kv_pool.is_contiguous() or kv_pool.get_device() != dev:
         raise KapError(ERR_INVALID_ARG, f"kv_pool is {kv_pool.dtype} {tuple(shape)} with strides {kv_pool.stride()} on {kv_pool.device}, "
-                       f"expected a contiguous bfloat16 tensor of K and V with {d} columns on GPU {dev}")
+                       f"expected a contiguous bfloat16 tensor of K and V on GPU {dev}")
+    pages, _, a, b, d = shape
+    return (pages, b, a, d) if nhd else (pages, a, b, d)
 
 
 def _check_index(name, t, least, dev):
@@ -302,12 +305,22 @@ def _check_index(name, t, least, dev):
                        f"contiguous int32 tensor of at least {least} on GPU {dev}")
 
 
+def _check_block_table(bt_indptr, bt_pages, ctx_len, batch, dev):
+    if bt_indptr.dtype is not _I32 or bt_pages.dtype is not _I32 or ctx_len.dtype is not _I32 or bt_indptr.numel() <= batch or \
+            bt_indptr.get_device() != dev or bt_pages.get_device() != dev or ctx_len.get_device() != dev or \
+            not bt_indptr.is_contiguous() or not bt_pages.is_contiguous() or not ctx_len.is_contiguous():
+        _check_index("bt_indptr", bt_indptr, batch + 1, dev)
+        _check_index("bt_pages", bt_pages, 0, dev)
+        _check_index("ctx_len", ctx_len, batch, dev)
+
+
 class Workspace:
     """kap_workspace: split-K schedule + partial-result buffers for one launch shape."""
 
     def __init__(self, device=0, max_items=8192, max_rows_per_item=16, max_batch=256):
         self._h = C.c_void_p()
         self.device = int(device)
+        self.kv_layout = KV_HND
         self.shared_prefix_rows = 0          # of the last schedule_shared_prefix
         self._destroy = lib().kap_workspace_destroy
         _check(lib().kap_workspace_create(C.byref(self._h), self.device, max_items,
@@ -422,13 +435,12 @@ def shared_prefix_attn(q, q_indptr, kv_pool, bt_indptr, bt_pages, ctx_len, out, 
                        f"{out.device}: expected contiguous bfloat16 tensors on GPU {dev}, the workspace's device")
     if lse is not None and (lse.dtype is not _F32 or not lse.is_contiguous() or lse.get_device() != dev):
         raise KapError(ERR_INVALID_ARG, f"lse is {lse.dtype} with strides {lse.stride()} on {lse.device}, expected a contiguous float32 tensor on GPU {dev}")
-    _check_pool(kv_pool, d, dev)
     batch = ctx_len.shape[0]
     _check_index("q_indptr", q_indptr, batch + 1, dev)
-    _check_index("bt_indptr", bt_indptr, batch + 1, dev)
-    _check_index("bt_pages", bt_pages, 0, dev)
-    _check_index("ctx_len", ctx_len, batch, dev)
-    pages, Hkv, P = _pool_shape(kv_pool, ws)
+    _check_block_table(bt_indptr, bt_pages, ctx_len, batch, dev)
+    pages, Hkv, P, pool_d = _dense_pool(kv_pool, ws.kv_layout == KV_NHD, dev)
+    if pool_d != d:
+        raise KapError(ERR_INVALID_ARG, f"q has heads of {d} columns, kv_pool of {pool_d}")
     sm_scale = d ** -0.5 if sm_scale is None else float(sm_scale)
     _check(lib().kap_shared_prefix_attn(
         q.data_ptr(), q_indptr.data_ptr(), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
@@ -489,13 +501,10 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
     logical index (+ position_offset[b]); else int32 [rows] or [axes, rows], freq_axis naming the axis
     of each pair (host sequence)."""
     _torch_module()
-    if kv_layout == KV_NHD:
-        pages, _, P, Hkv, d = kv_pool.shape
-    else:
-        pages, _, Hkv, P, d = kv_pool.shape
     rows, Hq, dev = k_new.shape[0], 0, k_new.get_device()
     if dev < 0:
         raise KapError(ERR_INVALID_ARG, "k_new is not on a GPU")
+    pages, Hkv, P, d = _dense_pool(kv_pool, kv_layout == KV_NHD, dev)
     ks, vs = _head_rows("k_new", k_new, rows, Hkv, d, dev), _head_rows("v_new", v_new, rows, Hkv, d, dev)
     qs = os_ = 0
     if q is None:
@@ -525,10 +534,7 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
         if len(axis) != rot // 2:
             raise KapError(ERR_INVALID_ARG, f"freq_axis names {len(axis)} pairs, inv_freq {rot // 2}")
     batch = ctx_len.shape[0]
-    _check_pool(kv_pool, d, dev)
-    _check_index("bt_indptr", bt_indptr, batch + 1, dev)
-    _check_index("bt_pages", bt_pages, 0, dev)
-    _check_index("ctx_len", ctx_len, batch, dev)
+    _check_block_table(bt_indptr, bt_pages, ctx_len, batch, dev)
     if new_indptr is not None:
         _check_index("new_indptr", new_indptr, batch + 1, dev)
     if position_offset is not None:
