@@ -327,7 +327,7 @@ kap_attn_split_kernel(const __grid_constant__ CUtensorMap kv_map, const AttnPara
     }
     // ---- nothing else produced by earlier kernels (Q, fresh KV, partial buffers) is touched above
     pdl_wait();
-    // mode 3: the kernel behind may start once every CTA here knows that the kernels in front are complete: it does not wait itself
+    // mode 3: the kernel behind takes whole SMs, which it is not to hold while the kernels in front of this one still run
     if constexpr (kParts) pdl_launch_dependents();
     KAP_TRACE_POINT(blockIdx.x, 2);
     if (producer)

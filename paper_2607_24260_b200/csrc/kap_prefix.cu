@@ -129,7 +129,7 @@ extern "C" kap_status kap_shared_prefix_attn(
     p.q_indptr = q_indptr; p.bt_indptr = bt_indptr; p.bt_pages = bt_pages; p.ctx_len = ctx_len;
     p.part_o = ws->d_part_o; p.part_ml = ws->d_part_ml; p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ws->d_status;
     p.num_pool_pages = num_pool_pages; p.total_rows = (int32_t)ws->total_rows; p.q_end = q_indptr + batch;
-    p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G; p.behind_parts = ws->n_items > 0;
+    p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G;
     p.scale_log2 = sm_scale * 1.4426950408889634f;
     // the sequences' own pages and small prefixes, then the large prefixes, then the join of their states
     if (ws->n_items > 0) {
