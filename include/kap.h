@@ -587,7 +587,8 @@ kap_status kap_append_kv_rope(
  * from q_indptr[batch] or the schedule's row count on, whichever comes first, are neither read nor written).  One workspace serves one call at a time: calls, and graphs that hold them, which may run at the
  * same time on two streams need a workspace each.
  * Errors: as kap_schedule and kap_verify_attn, plus KAP_ERR_INVALID_ARG for groups that do not
- * cover the batch in order, a prefix longer than a sequence's list, or an sm_scale that is not a positive number.
+ * cover the batch in order, a prefix longer than a sequence's list, an index array or lse that is not 4-byte aligned, or
+ * an sm_scale that is not a positive number.
  */
 kap_status kap_shared_prefix_items(
     int32_t batch, const int32_t* list_len, const int32_t* n_q,       /* HOST [batch] */

@@ -181,6 +181,11 @@ extern "C" kap_status kap_append_kv_rope(
     if (q) bits |= reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(q_out) | (uintptr_t)(q_stride * 2) | (uintptr_t)(q_out_stride * 2);
     if (bits & 15) return fail(KAP_ERR_INVALID_ARG, "q, k_new, v_new, q_out, kv_pool and their row strides must be 16-byte aligned");
 
+    if ((reinterpret_cast<uintptr_t>(new_indptr) | reinterpret_cast<uintptr_t>(inv_freq) | reinterpret_cast<uintptr_t>(positions) |
+         reinterpret_cast<uintptr_t>(position_offset) | reinterpret_cast<uintptr_t>(bt_indptr) | reinterpret_cast<uintptr_t>(bt_pages) |
+         reinterpret_cast<uintptr_t>(ctx_len) | reinterpret_cast<uintptr_t>(device_status)) & 3)
+        return fail(KAP_ERR_INVALID_ARG, "an index or frequency array is not 4-byte aligned");
+
     RopeParams p{};
     p.q = (const __nv_bfloat16*)q; p.k = (const __nv_bfloat16*)k_new; p.v = (const __nv_bfloat16*)v_new;
     p.q_out = (__nv_bfloat16*)q_out; p.pool = (__nv_bfloat16*)kv_pool;

@@ -102,6 +102,9 @@ extern "C" kap_status kap_shared_prefix_attn(
         return fail(KAP_ERR_INVALID_ARG, "NULL pointer or empty pool");
     if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(kv_pool) | reinterpret_cast<uintptr_t>(out)) & 15)
         return fail(KAP_ERR_INVALID_ARG, "q, kv_pool and out must be 16-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(q_indptr) | reinterpret_cast<uintptr_t>(bt_indptr) | reinterpret_cast<uintptr_t>(bt_pages) |
+         reinterpret_cast<uintptr_t>(ctx_len) | reinterpret_cast<uintptr_t>(lse)) & 3)
+        return fail(KAP_ERR_INVALID_ARG, "an index array or lse is not 4-byte aligned");
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev != ws->device)
         return fail(KAP_ERR_INVALID_ARG, "the workspace belongs to device %d but device %d is current", ws->device, dev);

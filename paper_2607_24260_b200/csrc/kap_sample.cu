@@ -993,6 +993,10 @@ extern "C" kap_status kap_sample_tokens(
     if (!logits || !uniform || !token) return fail(KAP_ERR_INVALID_ARG, "NULL pointer");
     if (reinterpret_cast<uintptr_t>(logits) & (logits_type == KAP_LOGITS_F32 ? 3 : 1))
         return fail(KAP_ERR_INVALID_ARG, "logits are not aligned to their type");
+    if ((reinterpret_cast<uintptr_t>(temperature) | reinterpret_cast<uintptr_t>(top_k) | reinterpret_cast<uintptr_t>(top_p) |
+         reinterpret_cast<uintptr_t>(min_p) | reinterpret_cast<uintptr_t>(uniform) | reinterpret_cast<uintptr_t>(token) |
+         reinterpret_cast<uintptr_t>(logprob)) & 3)
+        return fail(KAP_ERR_INVALID_ARG, "a parameter or result array is not 4-byte aligned");
     SampleParams p{logits, row_stride, vocab, 0, 0, 1, temperature, top_p, min_p, uniform, top_k, token, logprob};
     int& C = p.cluster;                                            // CTAs of a row
     const bool f32 = logits_type == KAP_LOGITS_F32;

@@ -6,7 +6,7 @@ import torch
 
 import gpu_util as gu
 from paper_2607_24260_b200 import kap
-from test_gpu_shared_prefix import Case
+from test_gpu_shared_prefix import Case, PAGE
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,19 @@ def test_more_rows_than_scheduled_are_reported():
     indptr[-1] += 2
     call(c, indptr)
     c.check()
+
+
+@pytest.mark.parametrize("place", ["q_indptr", "bt_indptr", "bt_pages", "ctx_len", "lse", "q", "out", "pool"])
+def test_misaligned_arrays_are_refused(place):
+    c = Case(52, GROUPS[0], poison=0.0)
+    c.ws = c.workspace()
+    q, qi, pool, bti, btp, ctx = c.arrays()
+    out, lse = torch.full_like(q, 3.0), torch.zeros(q.shape[:2], device=gu.DEV)
+    at = dict(q=q.data_ptr(), q_indptr=qi.data_ptr(), pool=pool.data_ptr(), bt_indptr=bti.data_ptr(), bt_pages=btp.data_ptr(), ctx_len=ctx.data_ptr(),
+              out=out.data_ptr(), lse=lse.data_ptr())
+    at[place] += 2
+    code = kap.lib().kap_shared_prefix_attn(at["q"], at["q_indptr"], at["pool"], pool.shape[0], at["bt_indptr"], at["bt_pages"], at["ctx_len"], 2, c.hq, c.hkv,
+                                            128, PAGE, c.scale, at["out"], at["lse"], c.ws._h, torch.cuda.current_stream().cuda_stream)
+    assert code == kap.ERR_INVALID_ARG and b"aligned" in kap.lib().kap_last_error()
+    torch.cuda.synchronize()
+    assert (out == 3.0).all()
