@@ -575,8 +575,8 @@ kap_status kap_append_kv_rope(
  * every step whose counts are unchanged; ctx_len may grow up to 16 list_len[b].
  * The workspace's partial buffer of max_items * max_rows_per_item rows is used as a whole:
  * kap_shared_prefix_items (HOST only) gives the max_items that a workspace with this
- * max_rows_per_item needs for such a schedule on a device of cta_slots SMs.  A workspace holds one schedule of
- * either kind at a time.
+ * max_rows_per_item needs for such a schedule on a device of cta_slots SMs (at most 4096).  A workspace holds one schedule
+ * of either kind at a time.
  *
  * Every token below a sequence's ctx_len must hold finite K and V; what lies behind the longest
  * context of a group may hold anything.  A context shorter than its group's shared prefix is allowed (the rows

@@ -30,6 +30,8 @@ constexpr int32_t kByHeadPages = 48;
 constexpr int32_t kSliceTime = 5;
 // A segment of the tcgen05 kernel pays for its query tiles, the pipeline's fill and its states about as much as for two steps.
 constexpr int64_t kSegmentSteps = 2;
+constexpr int32_t kMaxLists = 1 << 23;
+constexpr int32_t kMaxCtaSlots = 4096;
 
 struct Unit {                                                  // of the tcgen05 kernel
     int32_t seq, kv_head, n_pages, tok_row0, rows, unit;
@@ -70,6 +72,8 @@ kap_status build_prefix_schedule(int32_t batch, const int32_t* list_len, const i
     if (kRowTile % G) return fail(KAP_ERR_UNSUPPORTED, "group size %d must divide %d", G, kRowTile);
     if (batch > 0 && (n_groups < 1 || group_indptr[0] != 0 || group_indptr[n_groups] != batch))
         return fail(KAP_ERR_INVALID_ARG, "group_indptr must run from 0 to the batch size %d", batch);
+    // (a list is a sequence's pages for one KV head; the counts below stay within 32 bits with room to spare)
+    if ((int64_t)batch * hkv > kMaxLists) return fail(KAP_ERR_CAPACITY, "%d sequences x %d KV heads exceed %d lists", batch, hkv, kMaxLists);
     for (int32_t b = 0; b < batch; ++b) {
         if (list_len[b] <= 0 || n_q[b] < 1 || list_len[b] > 0x7fffffff / kPageSize) return fail(KAP_ERR_INVALID_ARG, "sequence %d: list_len %d, n_q %d", b, list_len[b], n_q[b]);
         if ((int64_t)n_q[b] * G > kRowTile * kMaxRowTiles)
@@ -277,7 +281,8 @@ extern "C" kap_status kap_shared_prefix_items(
     int32_t* max_items)
 {
     using namespace kap;
-    if (!max_items || max_rows_per_item <= 0 || cta_slots <= 0) return fail(KAP_ERR_INVALID_ARG, "NULL pointer or sizes below 1");
+    if (!max_items || max_rows_per_item <= 0 || cta_slots <= 0 || cta_slots > kMaxCtaSlots)
+        return fail(KAP_ERR_INVALID_ARG, "NULL pointer, sizes below 1 or more than %d cta_slots", kMaxCtaSlots);
     try {
         PrefixSchedule s;
         kap_status st = build_prefix_schedule(batch, list_len, n_q, n_groups, group_indptr, prefix_pages, num_q_heads, num_kv_heads, cta_slots, s);
