@@ -210,3 +210,15 @@ def test_arrays_on_another_device_than_the_current_one_are_refused(noted, monkey
         there["ws"].device = 1
     call(**there)
     assert len(noted) == 1
+
+
+def test_the_current_stream_is_found_without_the_short_way_too(monkeypatch):
+    class Torch:
+        _C = object()
+
+        class cuda:
+            @staticmethod
+            def current_stream(dev):
+                return type("Stream", (), dict(cuda_stream=1000 + dev))()
+
+    assert kap._stream_reader(Torch)(3) == 1003
