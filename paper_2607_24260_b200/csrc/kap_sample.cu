@@ -596,6 +596,7 @@ kap_sample_rows_kernel(const SampleParams p)
                     end = middle - 1;
                 }
                 part = 0.0;
+                __syncthreads();                                   // the histogram that the next level counts into has been cleared
                 continue;
             }
             if (rounds == 0 && !even) target = (double)top_p * (sum + cut_part); else above += sum;

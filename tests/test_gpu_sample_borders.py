@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import gpu_util as gu
-from test_gpu_sample import check, definition, f32
+from test_gpu_sample import check, definition, f32, run
 
 pytestmark = pytest.mark.gpu
 
@@ -119,3 +119,48 @@ def test_the_definition_of_a_known_row():
         token, logprob = definition(x, 1.0 - 2.0 ** -24, p=float(np.float32(p)))
         assert token == kept - 1
         check(f32(x[None]), [1.0 - 2.0 ** -24], p=[p])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_equal_rows_beside_gaps_get_equal_tokens(dtype):
+    # every row 150 times: whichever way its CTAs come through the search, the result is one
+    rng = np.random.default_rng(24)
+    x, ps = [], []
+    for _ in range(20):
+        values = np.sort(rng.normal(0, 2.0, int(rng.integers(2, 6))))[::-1]
+        x.append(rng.choice(values, 17000))
+        v, n = np.unique(x[-1], return_counts=True)
+        share = rng.choice(np.cumsum(n[::-1] * np.exp(v[::-1] - v[-1]))[:-1]) / (n * np.exp(v - v[-1])).sum()
+        ps.append(min(share * (1 + 10.0 ** rng.uniform(-6, -2)), 1 - 1e-6))
+    x.append(np.sign(rng.normal(0, 1, 17000)) * 10.0 ** rng.uniform(-38, 1, 17000))
+    ps.append(0.9999)
+    copies, u = 150, rng.random(len(ps))
+    logits = torch.from_numpy(np.stack(x)).to(gu.DEV).to(dtype)
+    check(logits, u, p=ps)
+    token, logprob = run(logits.repeat(copies, 1), np.tile(u, copies), p=np.tile(ps, copies))
+    token, logprob = token.reshape(copies, -1), logprob.reshape(copies, -1)
+    assert (token == token[0]).all() and (logprob == logprob[0]).all()
+
+
+def test_rows_of_every_kind_and_shares_next_to_their_borders():
+    rng = np.random.default_rng(25)
+    for _ in range(40):
+        rows, vocab = 24, int(np.exp(rng.uniform(np.log(600), np.log(20000))))
+        x, p, t = np.empty((rows, vocab), dtype=np.float32), rng.uniform(0, 1, rows), 10.0 ** rng.uniform(-1.5, 1.5, rows)
+        for r in range(rows):
+            scale = 10.0 ** rng.uniform(-3, 2)
+            x[r] = [lambda: rng.normal(0, scale, vocab), lambda: rng.choice(rng.normal(0, scale, 3), vocab),
+                    lambda: np.round(rng.normal(0, 4, vocab)) * scale / 4, lambda: np.sign(rng.normal(0, 1, vocab)) * 10.0 ** rng.uniform(-38, 2, vocab),
+                    lambda: rng.normal(0, 1e-3 * scale, vocab) + rng.choice([-3.0, 0.0, 3.0], vocab, p=[0.6, 0.3, 0.1]),
+                    lambda: -np.log(2) * np.floor(rng.uniform(0, 40, vocab)) * scale][r % 6]()
+            z = np.sort(x[r].astype(np.float64))[::-1]
+            border = np.nonzero(np.diff(z) < 0)[0][:8]
+            if border.size and r % 4:
+                w = np.cumsum(np.exp((z - z[0]) / np.float64(np.float32(t[r]))))
+                p[r] = min(w[rng.choice(border)] / w[-1] * (1 + 10.0 ** rng.uniform(-6, -2)), 1 - 1e-7)
+        s = dict(t=t, p=p)
+        if rng.random() < 0.3:
+            s["k"] = rng.integers(1, vocab, rows)
+        if rng.random() < 0.3:
+            s["m"] = 10.0 ** rng.uniform(-6, 0, rows)
+        check(f32(x), np.where(rng.random(rows) < 0.3, 1 - 2.0 ** -24, rng.random(rows)), **s)
