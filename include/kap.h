@@ -523,7 +523,7 @@ kap_status kap_materialize_view(
  *                       behind or ahead of its cache index).
  *   positions           int32 [num_axes][positions_stride >= total_rows]: row r's position on each
  *                       axis (time, height, width of image and video tokens); freq_axis[i] names the
- *                       axis of pair i (NULL: axis 0).  It does not move the slot of k and v.
+ *                       axis of pair i (NULL with one axis only).  It does not move the slot of k and v.
  * q, k_new and v_new are rows of [heads][128]; the strides count elements from one token row to the
  * next (views of one fused projection are fine).  q_out may be q itself (in place); it must not
  * overlap q otherwise, nor k_new or v_new.  q == NULL: only k and v are handled.
@@ -572,15 +572,17 @@ kap_status kap_append_kv_rope(
  * prefix_pages[i] physical pages; list_len[b] counts all pages of sequence b, the shared ones
  * included, and must cover every context length the schedule will serve.  The shared pages are
  * read through the block table of the group's first sequence.  The schedule serves every layer and
- * every step whose counts are unchanged; ctx_len may grow up to 16 list_len[b].
+ * every step whose counts are unchanged; ctx_len may grow up to 16 list_len[b].  Unlike kap_schedule, it is built and
+ * uploaded again at every call (0.1 ms for 4 sequences, 1.3 to 2.4 ms for 64, 3.4 ms for 256), so it is called when counts
+ * change, not at every step.
  * The workspace's partial buffer of max_items * max_rows_per_item rows is used as a whole:
  * kap_shared_prefix_items (HOST only) gives the max_items that a workspace with this
  * max_rows_per_item needs for such a schedule on a device of cta_slots SMs (at most 4096).  A workspace holds one schedule
  * of either kind at a time.
  *
- * Every token below a sequence's ctx_len must hold finite K and V; what lies behind the longest
- * context of a group may hold anything.  A context shorter than its group's shared prefix is allowed (the rows
- * see what lies below their own position) as long as the shared pages hold finite values.
+ * Every token below a sequence's ctx_len must hold finite K and V, and so must the whole of the shared pages, whatever the
+ * contexts; what lies behind a context in the sequence's own pages may hold anything.  A context may be shorter than
+ * its group's shared prefix (the rows see what lies below their own position).
  * A row that sees no token gets out = 0, lse = -inf.  out rows beyond q_indptr[batch] are left alone.
  * Reported through kap_workspace_check: KAP_ERR_DEVICE_INDEX for a page outside the pool, a context beyond 16 list_len[b], a
  * q_indptr that differs from the schedule's row counts (the results of such a call are not defined; rows of q, out and lse

@@ -5,8 +5,9 @@
 //
 // Mathematics: pair i of a head turns by the angle pos[axis(i)] * inv_freq[i]:
 //     (a, b) -> (a cos - b sin, b cos + a sin).
-// The angle is formed and reduced in 64 bits as a number of turns (position 131 071 times frequency 1 has
-// an error of 2^-8 rad in 32 bits, half a bf16 step of the cosine; here it is 1e-10), the remainder's sine and cosine in 32 bits.
+// The angle is formed and reduced in 64 bits as a number of turns, the remainder's sine and cosine in 32 bits.  (In 32 bits a product
+// of about 131 071 rad is rounded by up to 2^-8 rad, a whole bf16 step of a cosine between 1/2 and 1.  Here the product and the
+// turns are off by less than 1e-10 rad, and rounding the remainder, at most half a turn, to fp32 adds up to pi 2^-25, 1e-7 rad.)
 // Every value is rounded to bf16 once, when it is stored.
 //
 // Bound: memory; a token row moves 2 (Hq + 2 Hkv) 256 bytes and its angles are shared by all heads.  2 x 8192 rows of 32 / 8 heads

@@ -156,11 +156,11 @@ extern "C" kap_status kap_shared_prefix_attn(
         else KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_prefix_kernel<false>, kv, q_map, p));
         count_launch();
     }
-    // Few cells: one a warp.  Many: four heads a warp, one metadata chain for all of them.  (64 sequences with 32K shared tokens: 61.3 us
-    // for the call, one head a warp 63.7; 16 sequences of two rows with 64K 71.3 against 74.6.  4 sequences with 512 / 8K tokens: one head a
-    // warp 9.7 / 18.9, four 10.7 / 23.7.)  More than four states: four warps a set, while the sets are one wave of CTAs (64 sequences with
-    // 32K, 20 states: 61.3 against 71.7 with one warp; 4 sequences with 512, eight states 8.4 against 8.8; 256 sequences in two groups,
-    // five states, several waves: 56.1 with one warp, 60.1 with four).
+    // Few cells: one a warp.  Many: four heads a warp, one metadata chain for all of them.  (64 sequences with 32K shared tokens: 61.7 us
+    // for the call, one head a warp 64.7; 16 sequences of two rows with 64K 72.0 against 76.9.  4 sequences with 512 / 8K tokens: one head a
+    // warp 8.4 / 16.6, four 9.9 / 21.1.)  More than four states: four warps a set, while the sets are one wave of CTAs (64 sequences with
+    // 32K, 20 states: 61.5 against 71.8 with one warp; 4 sequences with 512, eight states 8.4 against 9.2; 256 sequences on two prefixes
+    // of 8K, several waves: 81.7 with one warp, 85.4 with four).
     const int64_t cells = ws->total_rows * num_q_heads, one_wave = (int64_t)ws->sm_count * 6;
     const int H = cells <= one_wave ? 1 : G >= 4 ? 4 : G;
     const int64_t sets = cells / H;

@@ -9,7 +9,7 @@ constexpr int kPrefixStepTokens = kPrefixStepPages * kPageSize;
 constexpr int kPrefixTileRows = 128;                   // query rows of one tile (TMEM lanes)
 constexpr int kPrefixUnitRows = 2 * kPrefixTileRows;
 // Ring of the split kernel, 8 KiB a slot.  More for grids that leave SMs room only cost start-up (4 sequences with 512 shared tokens, 96
-// CTAs: 8.8 us with 8 slots, 9.7 with 24).
+// CTAs: 8.3 us with 8 slots, 8.5 with 12, 9.2 with 24).
 constexpr int kPrefixRingSlots = 8;
 
 enum { kSegPair = 1, kSegTwoStates = 2 };

@@ -15,13 +15,13 @@ namespace kap {
 namespace {
 
 // Row counts up to which the split kernel takes a prefix.  Measured on B200 (8 KV heads, one group; split / tcgen05, us a call): 16 rows
-// 10.8 / 12.4 at 512 tokens, 37.8 / 42.9 at 32K; 32 rows 13.4 / 12.8 and 41.4 / 43.3; 64 rows 15.4 / 15.8 and 58.4 / 46.0.
+// 8.3 / 12.8 at 512 tokens, 31 / 41 at 32K; 32 rows 10.3 / 13.4 and 35 / 40; 64 rows 13.9 / 14.7 and 53 / 42.
 constexpr int32_t kSplitRows = 2 * kRowTile;
 constexpr int32_t kSplitCtasPerSm = 3;
 constexpr int32_t kMinSplitPages = 4;                          // a page for each of a CTA's warps
 constexpr int32_t kMaxSplitPages = 1024;                       // page ids a CTA holds: 1600
 // Short parts of at most 16 rows may go four KV heads to a CTA, one per warp, instead of a CTA each: for many short lists a CTA is
-// mostly start-up (256 sequences with up to 19 own pages: the call takes 56 us, with a CTA for each head 67).  A warp alone takes about a
+// mostly start-up (256 sequences with up to 19 own pages on a prefix of 8K: the call takes 72 us, with a CTA for each head 83).  A warp alone takes about a
 // microsecond a page, so long lists do not belong there.
 constexpr int32_t kByHeadPages = 48;
 // What a CTA of the split kernel takes, in pages that one warp group streams (about a microsecond each): its start and its end as much

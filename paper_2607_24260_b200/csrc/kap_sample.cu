@@ -21,7 +21,7 @@
 // drawn, the first CTA gets them and finishes alone (one row 32 -> 15 us, 64 mixed rows 85 -> 65).  A thread carries its weight of what
 // the top-p search has passed, all of it kept, into the draw (64 mixed rows 65 -> 62, 100 flat rows 95 -> 87).
 // Bound: the phases between the barriers, one after the other (of the 15 us of a single row the read takes 2), and with many rows
-// shared-memory atomics and 64-bit sums: 64 rows of 128256 with mixed filters 62 us; 100 rows of 50257 in bf16, top-p 87 us.
+// shared-memory atomics and 64-bit sums: 64 rows of 128256 with mixed filters 61 us; 100 rows of 50257 in bf16, top-p 89 us.
 #include <cmath>
 
 #include "kap_ptx.cuh"
@@ -35,6 +35,7 @@ constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 1024;
 constexpr int kFew = kSampleThreads;               // logits that one CTA finishes alone: one a thread
+constexpr int kSms = 148;                          // of a B200; only the choices of a launch's shape use it
 constexpr uint32_t kImageMinusInf = 0x007fffffu;   // image of -inf; nothing at or below it has weight
 constexpr uint32_t kImagePlusInf = 0xff800000u;
 constexpr int kMaxRounds = 48;                     // of a search, more than either can take
@@ -1005,24 +1006,25 @@ extern "C" kap_status kap_sample_tokens(
     cudaLaunchConfig_t cfg{};
     const int draw_blocks = (vocab + kDrawBlock - 1) / kDrawBlock;
     cudaError_t e = cudaSuccess;
-    if (!top_k && !top_p && !min_p && (draw_blocks > 32 || rows > 148)) {
-        // Without filters, unless the rows are short and few (8192 logits: 148 rows 8.4 us here, 9.6 there; 256 rows 12.0 against 10.5;
-        // 32000 logits: 8 rows 10.8 / 8.9, 100 rows 18.6 / 14.5; 128256 logits: 512 rows 257 / 97).  CTAs of a row: three on an SM and
-        // a block for each of their warps, and two for long rows, whose tail one CTA would stretch (128256 logits, 1 / 2 / 4 / 8 CTAs a
-        // row: 8 rows 58 / 33 / 20 / 14 us, 100 rows 58 / 40 / 33 / 37, 512 rows 133 / 117 / 126 / 144; 1000 rows of 32000 64 / 72 / 91 / 128).
+    if (!top_k && !top_p && !min_p && (draw_blocks > 32 || rows > kSms)) {
+        // Without filters, unless the rows are short and few (this kernel / the other one: 8192 logits, 148 rows 9.2 / 8.4 us, 256 rows
+        // 9.7 / 11.8; 32000 logits, 8 rows 9.6 / 8.2, 100 rows 13.3 / 16.9; 128256 logits, 512 rows 97 / 248).  CTAs of a row: three on an
+        // SM and a block for each of their warps, and two for long rows, whose tail one CTA would stretch (128256 logits, 1 / 2 / 4 / 8
+        // CTAs a row: 8 rows 49 / 28 / 18 / 12 us, 100 rows 49 / 34 / 28 / 30, 512 rows 111 / 97 / 106 / 123; 1000 rows of 32000
+        // 55 / 62 / 81 / 118).
         kernel = f32 ? kap_sample_draw_kernel<float> : kap_sample_draw_kernel<__nv_bfloat16>;
-        while (C < 8 && C * 2 * kDrawWarps <= draw_blocks && (int64_t)rows * C * 2 <= 3 * 148) C *= 2;
+        while (C < 8 && C * 2 * kDrawWarps <= draw_blocks && (int64_t)rows * C * 2 <= 3 * kSms) C *= 2;
         if (C == 1 && draw_blocks >= 128) C = 2;
         cfg.blockDim = dim3(kDrawThreads);
     } else {
-        // As many CTAs as keep two of them on an SM, 33 logits a thread (64 rows of 128256 with mixed filters: 65 us; 17 logits 104, 65
-        // logits 69).  With few rows more, while that leaves a thread a strip worth its barriers and the large clusters half of the SMs,
-        // since they do not fit everywhere (top-k 50 and top-p: 1 row of 32000 12.2 with 8 CTAs, 13.1 with 16, 14.7 with 2; 16 rows
-        // 12.9 with 4, 16.2 with 8; 16 rows of 50257 14.3 with 4, 17.2 with 8, 21 .. 26 with 16).
+        // As many CTAs as keep two of them on an SM, 33 logits a thread (64 rows of 128256 with mixed filters: 61 us; 17 logits 102, 65
+        // logits 64).  With few rows more, while that leaves a thread a strip worth its barriers and the large clusters half of the SMs,
+        // since they do not fit everywhere (top-k to 80 and top-p: 1 row of 32000 11.4 with 8 CTAs, 12.9 with 16, 14.0 with 2; 16 rows
+        // 13.0 with 4, 16.1 with 8; 16 rows of 50257 14.0 with 4, 17.0 with 8, 26 with 16).
         kernel = f32 ? kap_sample_rows_kernel<float> : kap_sample_rows_kernel<__nv_bfloat16>;
         auto strip_of = [&](int c) { const int s = ((vocab + c - 1) / c + kSampleThreads - 1) / kSampleThreads; return s | 1; };
         while (C < kMaxCluster && strip_of(C) > 33) C *= 2;
-        while (C < kMaxCluster && strip_of(C) > (C < 8 ? 5 : 13) && (int64_t)rows * C * 2 <= (C < 4 ? 148 : 74)) C *= 2;
+        while (C < kMaxCluster && strip_of(C) > (C < 8 ? 5 : 13) && (int64_t)rows * C * 2 <= (C < 4 ? kSms : kSms / 2)) C *= 2;
         p.strip = strip_of(C);
         p.slice = p.strip * kSampleThreads;
         auto smem_for = [](int slice) { return (sizeof(SampleShared) + 15) / 16 * 16 + ((size_t)slice + 4) * sizeof(uint32_t); };
