@@ -586,8 +586,9 @@ kap_status kap_append_kv_rope(
  * A row that sees no token gets out = 0, lse = -inf.  out rows beyond q_indptr[batch] are left alone.
  * Reported through kap_workspace_check: KAP_ERR_DEVICE_INDEX for a page outside the pool, a context beyond 16 list_len[b], a
  * q_indptr that differs from the schedule's row counts (the results of such a call are not defined; rows of q, out and lse
- * from q_indptr[batch] or the schedule's row count on, whichever comes first, are neither read nor written).  One workspace serves one call at a time: calls, and graphs that hold them, which may run at the
- * same time on two streams need a workspace each.
+ * from q_indptr[batch] or the schedule's row count on, whichever comes first, are neither read nor written).  One workspace
+ * serves one call at a time: calls, and graphs that hold them, which may run at the same time on two streams need a
+ * workspace each.
  * Errors: as kap_schedule and kap_verify_attn, plus KAP_ERR_INVALID_ARG for groups that do not
  * cover the batch in order, a prefix longer than a sequence's list, an index array or lse that is not 4-byte aligned, or
  * an sm_scale that is not a positive number.

@@ -44,3 +44,18 @@ def test_nan_temperature_is_greedy_and_nan_top_p_no_filter():
     got = run(f32(x), u, p=[NAN] * 4, m=[NAN] * 4)[0]
     want = [definition(x[r].astype(np.float64), float(np.float32(u[r])))[0] for r in range(4)]
     np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("rows", [3, 400])
+def test_an_endless_temperature_draws_evenly(rows):
+    # every weight is 1: token and log-probability follow from the counts alone, whichever way the rows go
+    rng = np.random.default_rng(6)
+    vocab = 9000
+    x, u = f32(rng.normal(0, 3.0, (rows, vocab))), rng.random(rows)
+    t = [np.inf] * rows
+    for s, n in ((dict(), 9000), (dict(k=[700] * rows), 700), (dict(p=[0.25] * rows), 2250), (dict(k=[4000] * rows, p=[0.25] * rows), 1000), (dict(m=[0.5] * rows), 9000)):
+        token, logprob = run(x, u, t=t, **s)
+        assert (np.abs(logprob + np.log(n)) <= 2.0 ** -24 * np.log(n) + 1e-9).all()
+        for r in range(3):
+            kept = np.sort(np.argsort(-x[r].cpu().numpy(), kind="stable")[:n])
+            assert token[r] == kept[int(np.float64(np.float32(u[r])) * n)]
