@@ -740,9 +740,9 @@ kap_sample_rows_kernel(const SampleParams p)
 // logit, puts the sums on it and adds them up in index order; the warp whose sums hold the target reads that block once more and
 // walks through it.
 // Bound: the 64-bit pipe and the issue slots (fourteen 64-bit instructions of about thirty a logit); 1000 rows of 128256: 184 us,
-// 2.8 TB/s, the pipe half busy.  (Two blocks a pass, without the copy from the block on the way, spilled: 223 us.)  32-bit weights with
-// a bound of their error were slower: the bound is as large as a flat row's weights, so that most rows had to be summed again in
-// 64 bits (512 rows: 165 us, this kernel 97).
+// 2.8 TB/s, the pipe half busy.  (Two blocks a pass, without the copy from the block on the way, spilled: 223 us.)  32-bit weights
+// were slower with the bound of their error that was tried: as large as a flat row's weights, so that most rows had to be summed
+// again in 64 bits (512 rows: 165 us, this kernel 97).
 constexpr int kDrawThreads = 256, kDrawWarps = kDrawThreads / 32;
 constexpr int kDrawBlock = 512, kDrawPer = kDrawBlock / 32;
 constexpr int kDrawBlocks = kMaxCluster * kSampleThreads * kMaxStrip / kDrawBlock + 1;      // of a row at most; one more for an unaligned start
