@@ -622,6 +622,45 @@ kap_status kap_shared_prefix_attn(
     float* lse,                        /* DEVICE fp32 [sum n_q, Hq] or NULL */
     kap_workspace* ws, void* cuda_stream);
 
+/*
+ * kap_chunk_attn - attention of the new tokens of a step over the paged cache, for a batch that mixes chunks of prompts with single
+ * tokens (kap_verify_attn's rows and rule, without its limit on the rows; the paper has no counterpart: its prompts are in the cache).
+ * Sequence b has n_q = q_indptr[b+1] - q_indptr[b] rows, from none to all of its tokens; row j sits at logical position
+ * p = ctx_len[b] - n_q + j (ctx_len counts the rows' own tokens, whose K/V are already in the pool) and sees token t <= p iff
+ *     window == 0  or  t > p - window  or  t < n_sink
+ * (a sliding window of `window` tokens, the row's own included, and the first n_sink tokens of the sequence; n_sink counts only
+ * with a window).  out and lse as kap_selected_decode_attn; a row that sees no token (p < 0) gets out = 0, lse = -inf.  Rows outside
+ * q_indptr[0] .. q_indptr[batch] - 1 are left alone.  Pages that no row of a sequence sees are not read: their entries in bt_pages may
+ * hold anything.  Every token below ctx_len in the pages that are read must hold finite K and V; what lies behind ctx_len may hold anything.
+ *
+ * No schedule: the work is divided on the device, from q_indptr and ctx_len as they are when the kernel runs, so a captured call serves
+ * steps of any lengths within total_rows.  Of the workspace the partial buffer of max_items * max_rows_per_item rows is used (a
+ * schedule that the workspace holds stays); kap_chunk_attn_items gives the max_items that it needs on a device of cta_slots SMs.
+ * One workspace serves one call at a time: calls, and graphs that hold them, which may run at the same time on two streams need a workspace
+ * each.  Results do not depend on timing; a row's sums run in an order that depends on the whole batch's lengths.
+ * Reported through kap_workspace_check (KAP_ERR_DEVICE_INDEX; results of that sequence are not defined): a page outside the pool, a
+ * q_indptr that falls or leaves 0 .. total_rows, a negative ctx_len or one beyond the block table.
+ * Errors: as kap_verify_attn (the workspace needs no schedule), plus KAP_ERR_CAPACITY for a workspace that is too small and
+ * KAP_ERR_INVALID_ARG for a negative window or n_sink, a misaligned array, or an sm_scale that is not a positive number.
+ */
+kap_status kap_chunk_attn_items(int32_t max_rows_per_item, int32_t cta_slots, int32_t* max_items);
+
+kap_status kap_chunk_attn(
+    const void* q,                     /* DEVICE bf16 [total_rows, Hq, d], a sequence's rows contiguous */
+    const int32_t* q_indptr,           /* DEVICE [batch+1] */
+    int32_t total_rows,                /* rows that q, out and lse have */
+    const void* kv_pool, int64_t num_pool_pages,
+    const int32_t* bt_indptr,          /* DEVICE [batch+1] CSR full block table */
+    const int32_t* bt_pages,           /* DEVICE */
+    const int32_t* ctx_len,            /* DEVICE [batch] */
+    int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+    float sm_scale,
+    int32_t window,                    /* 0: every earlier token is visible */
+    int32_t n_sink,
+    void* out,                         /* DEVICE bf16 [total_rows, Hq, d] */
+    float* lse,                        /* DEVICE fp32 [total_rows, Hq] or NULL */
+    kap_workspace* ws, void* cuda_stream);
+
 /* element type of kap_sample_tokens' logits */
 enum {
     KAP_LOGITS_F32 = 0,

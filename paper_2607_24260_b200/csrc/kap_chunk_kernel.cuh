@@ -1,0 +1,779 @@
+// Attention of many new tokens over the paged cache on the tensor cores (tcgen05.mma, accumulators in tensor memory): prompt chunks and
+// single tokens of one batch in one launch, causal, with an optional sliding window and first tokens that stay visible.
+#pragma once
+
+#include "kap_ptx.cuh"
+
+namespace kap {
+
+constexpr int kChunkThreads = 384;
+constexpr int kChunkTileRows = 128;                                    // query rows of one tile (TMEM lanes)
+constexpr int kChunkUnitRows = 2 * kChunkTileRows;
+constexpr int kChunkStepPages = 5;
+constexpr int kChunkStepTokens = kChunkStepPages * kPageSize;          // 80
+constexpr int kChunkSlots = 8;                                         // step n: K in slot 2 n, V in slot 2 n + 1 (mod 8)
+constexpr int kChunkPlaneBytes = kChunkStepTokens * 128;               // 80 tokens x 64 columns: 10 KiB
+constexpr int kChunkSlotBytes = 2 * kChunkPlaneBytes;                  // columns 0-63 | 64-127
+constexpr int kChunkQHalfBytes = kChunkTileRows * 128;                 // 128 rows x 64 columns: 16 KiB
+constexpr int kChunkQBytes = 2 * kChunkQHalfBytes;
+constexpr int kChunkTmemP = 80, kChunkTmemO = 128;                     // columns of a stream's 256; S from 0
+constexpr int kChunkMaxSegments = 72;                                  // planned at a time
+// Cost of a unit beyond its tokens (query load, first products, epilogue), in tokens; it places the cuts, nothing else.
+constexpr int kChunkUnitCost = 160;
+constexpr int kChunkLeastCost = 640;                                   // of a CTA's share: fewer CTAs work when there is little to do
+
+struct alignas(16) ChunkSegment {                                      // what one CTA does of one unit (query tile pair, KV head)
+    int32_t list_at;                                                   // the sequence's first entry in bt_pages
+    int32_t tok0, lo;                                                  // first token row of q, its logical position (negative: sees nothing)
+    int32_t rows_head;                                                 // query rows | KV head << 16
+    int32_t step_begin, step_end;
+    int32_t length;                                                    // tokens of the sequence
+    int32_t slot;                                                      // of its partial state; -1: the whole unit, writes the output
+};
+struct ChunkCut { long long unit; int32_t inside, tok0, rows_head, pad; };   // where a CTA begins; inside: in the middle of this unit
+
+struct ChunkControl {
+    unsigned long long full[kChunkSlots], free[kChunkSlots];
+    unsigned long long q_full[2], q_free[2];
+    unsigned long long s_ready[2], s_free[2], p_ready[2], pv_done[2];  // [stream]
+    unsigned long long drained;
+    uint32_t tmem_base;
+    int32_t timed_out;
+    int32_t n_segments, more;                                          // of this round; another round follows
+    // plan: this CTA's range of the tape
+    int32_t seq, unit, step, end_seq, end_unit, end_step, first_done;
+    long long warp_sum[kChunkThreads / 32];
+    int32_t cut_seq[2];
+    long long cut_rest[2];
+};
+struct ChunkShared {
+    ChunkControl c;
+    alignas(16) ChunkSegment segments[kChunkMaxSegments];
+};
+constexpr int kChunkSmemBytes = 2 * kChunkQBytes + kChunkSlots * kChunkSlotBytes + 3072;
+static_assert(sizeof(ChunkShared) <= 3072 && kChunkSmemBytes <= 232448, "shared memory");
+
+struct ChunkParams {
+    const int32_t *q_indptr, *bt_indptr, *bt_pages, *ctx_len;
+    float *part_o, *part_ml;
+    ChunkCut* cuts;                                                    // [gridDim.x + 1]
+    __nv_bfloat16* out;
+    float* lse;
+    int32_t* status;
+    long long num_pool_pages;
+    int32_t batch, total_rows, hq, hkv, G, window, n_sink;
+    float scale_log2;
+};
+
+// ------------------------------------------------------------------------------------------------------------------ plan
+// All units of the batch, ordered by sequence, KV head and tile, lie on a tape whose length is their cost; CTA i of n takes the tape from
+// i / n to (i + 1) / n of it.  Every CTA finds its two ends by itself, from closed forms, so that lengths may live on the device.
+struct ChunkSeq { int32_t row0, n, length, list_at; };                 // first row of q, rows, tokens, block table
+
+__device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams& p, int b, bool& bad) {
+    const int r0 = p.q_indptr[b], r1 = p.q_indptr[b + 1], L = p.ctx_len[b], l0 = p.bt_indptr[b], l1 = p.bt_indptr[b + 1];
+    const long long listed = max(0ll, (long long)l1 - l0) * kPageSize;
+    ChunkSeq s;
+    s.row0 = min(max(r0, 0), p.total_rows);
+    s.n = max(min(r1, p.total_rows) - s.row0, 0);
+    s.length = (int)min((long long)max(L, 0), listed);
+    s.list_at = l0;
+    bad = r0 != s.row0 || r1 != s.row0 + s.n || L != s.length;
+    return s;
+}
+__device__ __forceinline__ int chunk_tiles(const ChunkParams& p, int n) {
+    const int R = kChunkUnitRows / p.G;
+    return (n + R - 1) / R;
+}
+// cost of the first k tiles of a sequence, for one KV head
+__device__ __forceinline__ long long chunk_cost(const ChunkParams& p, const ChunkSeq& s, int k) {
+    if (k <= 0) return 0;
+    const int R = kChunkUnitRows / p.G, t = chunk_tiles(p, s.n), whole = min(k, t - 1);
+    const long long lo = max(0, s.length - s.n), knee = (long long)p.window + p.n_sink;   // where the window begins to leave tokens out
+    const long long m = p.window ? min((long long)whole, max(0ll, (knee - lo + R - 1) / R)) : whole;
+    long long c = 2 * (whole * (long long)kChunkUnitCost + m * lo + R * (m * (m + 1) / 2) + (whole - m) * (knee + R));
+    if (k == t) {
+        const int rest = s.n - (t - 1) * R;
+        const long long at = lo + (long long)(t - 1) * R, seen = p.window && at >= knee ? knee + rest : at + rest;
+        c += (rest * p.G > kChunkTileRows ? 2 : 1) * (kChunkUnitCost + seen);
+    }
+    return c;
+}
+struct ChunkPages { int32_t head, first, n; };                         // logical pages 0 .. head-1 and first .. first + n - head - 1
+__device__ __forceinline__ ChunkPages chunk_pages(const ChunkParams& p, int lo, int hi) {
+    ChunkPages g;
+    const int end = hi < 0 ? 0 : hi / kPageSize + 1;
+    g.first = p.window ? (int)(max(0ll, (long long)lo - p.window + 1) / kPageSize) : 0;
+    g.first = min(g.first, end);
+    g.head = min(g.first, (int)(((long long)p.n_sink + kPageSize - 1) / kPageSize));
+    g.n = g.head + end - g.first;
+    return g;
+}
+__device__ __forceinline__ int chunk_steps(const ChunkParams& p, const ChunkSeq& s, int tile) {
+    const int R = kChunkUnitRows / p.G, lo = s.length - s.n + tile * R, hi = min(lo + R, s.length) - 1;
+    return (chunk_pages(p, lo, hi).n + kChunkStepPages - 1) / kChunkStepPages;
+}
+
+// this CTA's ends; called by all threads
+__device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = (p.batch + kChunkThreads - 1) / kChunkThreads;
+    long long mine = 0;
+    for (int i = 0; i < per; ++i) {
+        const int b = tid * per + i;
+        if (b >= p.batch) break;
+        bool bad;
+        const ChunkSeq s = chunk_seq(p, b, bad);
+        if (bad && blockIdx.x == 0) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
+        mine += chunk_cost(p, s, chunk_tiles(p, s.n)) * p.hkv;
+    }
+    long long upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const long long o = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 31) c.warp_sum[warp] = upto;
+    if (tid < 2) c.cut_seq[tid] = p.batch;                             // the tape's end
+    __syncthreads();
+    long long total = 0, before = 0;
+#pragma unroll
+    for (int w = 0; w < kChunkThreads / 32; ++w) {
+        if (w == warp) before = total;
+        total += c.warp_sum[w];
+    }
+    before += upto - mine;
+    const long long parts = max(1ll, min((long long)gridDim.x, total / kChunkLeastCost));
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const long long i = min((long long)blockIdx.x + e, parts), x = total / parts * i + total % parts * i / parts;
+        if (x < before || x >= before + mine) continue;
+        long long rest = x - before;
+        for (int k = 0; k < per; ++k) {
+            const int b = tid * per + k;
+            bool bad;
+            const ChunkSeq s = chunk_seq(p, b, bad);
+            const long long cost = chunk_cost(p, s, chunk_tiles(p, s.n)) * p.hkv;
+            if (rest < cost || k == per - 1 || b == p.batch - 1) {
+                c.cut_seq[e] = b;
+                c.cut_rest[e] = rest;
+                break;
+            }
+            rest -= cost;
+        }
+    }
+    __syncthreads();
+    if (warp < 2) {                                                    // unit and step of each end
+        const int b = c.cut_seq[warp];
+        int unit = 0, step = 0, tok0 = 0, rows_head = 0, inside = 0;
+        if (b < p.batch) {
+            bool bad;
+            const ChunkSeq s = chunk_seq(p, b, bad);
+            const int t = chunk_tiles(p, s.n), R = kChunkUnitRows / p.G;
+            const long long one = chunk_cost(p, s, t);
+            const int head = min((int)(c.cut_rest[warp] / one), p.hkv - 1);
+            const long long y = c.cut_rest[warp] - head * one;
+            int k = 0, hi = t;                                         // cost(k) <= y < cost(hi)
+            while (hi - k > 1) {
+                const int stride = (hi - k + 31) / 32, probe = k + lane * stride;
+                const uint32_t below = __ballot_sync(0xffffffffu, probe < hi && chunk_cost(p, s, probe) <= y);
+                const int at = k + max(31 - __clz(below), 0) * stride;
+                hi = min(hi, at + stride);
+                k = at;
+            }
+            const int steps = chunk_steps(p, s, k), rows = min(R, s.n - k * R) * p.G;
+            const long long z = (y - chunk_cost(p, s, k)) / (rows > kChunkTileRows ? 2 : 1) - kChunkUnitCost;
+            step = (int)min((long long)steps, max(0ll, (z + kChunkStepTokens / 2) / kChunkStepTokens));
+            unit = head * t + k;
+            inside = step > 0 && step < steps;
+            tok0 = s.row0 + k * R;
+            rows_head = rows | head << 16;
+            if (step == steps && steps > 0) { ++unit; step = 0; }      // (unit = t hkv: the next sequence's first)
+        }
+        if (lane == 0) {
+            if (warp == 0) { c.seq = b; c.unit = unit; c.step = step; c.first_done = 0; }
+            else { c.end_seq = b; c.end_unit = unit; c.end_step = step; }
+            if (warp == 0 || blockIdx.x == gridDim.x - 1) {
+                ChunkCut cut;
+                cut.unit = (long long)b << 32 | (unsigned)unit;
+                cut.inside = inside ? step : 0; cut.tok0 = tok0; cut.rows_head = rows_head; cut.pad = 0;
+                p.cuts[blockIdx.x + warp] = cut;
+            }
+        }
+    }
+    __syncthreads();
+}
+
+// the next segments of this CTA; called by one warp
+__device__ __forceinline__ void chunk_segments(const ChunkParams& p, ChunkShared& sh) {
+    ChunkControl& c = sh.c;
+    const int lane = threadIdx.x & 31, R = kChunkUnitRows / p.G;
+    int seq = c.seq, unit = c.unit, step = c.step, first_done = c.first_done, n = 0;
+    const int end_seq = c.end_seq, end_unit = c.end_unit, end_step = c.end_step;
+    const int last_seq = end_unit > 0 || end_step > 0 ? end_seq : end_seq - 1;
+    while (n < kChunkMaxSegments && seq <= last_seq) {
+        const int b = seq + lane;
+        ChunkSeq s{0, 0, 0, 0};
+        bool bad;
+        if (b <= last_seq) s = chunk_seq(p, b, bad);
+        const int t = chunk_tiles(p, s.n), skip = lane == 0 ? unit : 0;
+        const int units = (b == end_seq ? end_unit + (end_step > 0 ? 1 : 0) : t * p.hkv) - skip;
+        int upto = max(units, 0);
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int o = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += o;
+        }
+        const int all = __shfl_sync(0xffffffffu, upto, 31), take = min(all, kChunkMaxSegments - n);
+        int next_seq = seq + 32, next_unit = 0;
+        for (int k0 = 0; k0 < take; k0 += 32) {
+            const int k = min(k0 + lane, take - 1);
+            int owner = 0;                                             // lanes whose units all come before k
+#pragma unroll
+            for (int d = 16; d > 0; d /= 2)
+                if (__shfl_sync(0xffffffffu, upto, owner + d - 1) <= k) owner += d;
+            ChunkSeq o;
+            o.row0 = __shfl_sync(0xffffffffu, s.row0, owner); o.n = __shfl_sync(0xffffffffu, s.n, owner);
+            o.length = __shfl_sync(0xffffffffu, s.length, owner); o.list_at = __shfl_sync(0xffffffffu, s.list_at, owner);
+            const int prior = __shfl_sync(0xffffffffu, upto, max(owner - 1, 0)), before = owner ? prior : 0;
+            const int ot = chunk_tiles(p, o.n), u = k - before + (owner == 0 ? unit : 0), head = u / ot, tile = u % ot;
+            const int steps = chunk_steps(p, o, tile);
+            ChunkSegment g;
+            g.list_at = o.list_at; g.tok0 = o.row0 + tile * R; g.lo = o.length - o.n + tile * R;
+            g.rows_head = min(R, o.n - tile * R) * p.G | head << 16;
+            const bool cta_first = !first_done && n + k == 0, cta_last = seq + owner == end_seq && u == end_unit;
+            g.step_begin = cta_first ? step : 0;
+            g.step_end = cta_last ? end_step : steps;
+            g.length = o.length;
+            g.slot = g.step_begin == 0 && g.step_end == steps ? -1 : (int)blockIdx.x * 2 + (g.step_end < steps ? 1 : 0);
+            if (k0 + lane < take) sh.segments[n + k] = g;
+            if (k0 + 32 >= take) {                                     // where the next round goes on, if these were not all
+                const int src = take - 1 - k0;
+                const int nu = __shfl_sync(0xffffffffu, u + 1, src), no = __shfl_sync(0xffffffffu, owner, src), nt = __shfl_sync(0xffffffffu, ot * p.hkv, src);
+                if (take < all) { next_seq = seq + no + (nu == nt); next_unit = nu == nt ? 0 : nu; }
+            }
+        }
+        n += take;
+        if (take == all) { next_seq = seq + 32; next_unit = 0; }
+        seq = next_seq; unit = next_unit;
+    }
+    if (lane == 0) {
+        c.n_segments = n;
+        c.more = seq < last_seq || (seq == last_seq && (seq != end_seq || unit < end_unit + (end_step > 0 ? 1 : 0)));
+        c.seq = seq; c.unit = unit; c.first_done = first_done || n > 0;
+    }
+}
+
+// --------------------------------------------------------------------------------------------------------------- softmax
+__device__ __forceinline__ void chunk_load_scores(uint32_t at, float (&s)[kChunkStepTokens]) {
+    uint32_t u[kChunkStepPages][16];
+#pragma unroll
+    for (int i = 0; i < kChunkStepPages; ++i) tmem_ld16_nowait(at + i * 16, u[i]);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < kChunkStepTokens; ++i) s[i] = __uint_as_float(u[i >> 4][i & 15]);
+}
+__device__ __forceinline__ float chunk_row_max(const float (&s)[kChunkStepTokens]) {
+    float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+    for (int i = 4; i + 8 <= kChunkStepTokens; i += 8)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx[e] = max3(mx[e], s[i + e], s[i + 4 + e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], s[kChunkStepTokens - 4 + e]);
+    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+}
+// The weights 2^(s scale - mu) as packed bf16; returns their fp32 sum.  With kPoly one pair in four is computed on the FMA pipe, which
+// gives at least 2^-126 where 2^-inf = 0 is wanted, so steps with masked scores do without it.
+template <bool kPoly>
+__device__ __forceinline__ float chunk_weights(const float (&s)[kChunkStepTokens], float scale, float mu, uint32_t (&w)[kChunkStepTokens / 2]) {
+    const uint64_t sc2 = pack_f32x2(scale, scale), mu2 = pack_f32x2(-mu, -mu);
+    uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+    for (int e = 0; e < kChunkStepTokens / 2; ++e) {
+        const uint64_t x = fma_f32x2(pack_f32x2(s[2 * e], s[2 * e + 1]), sc2, mu2);
+        float a, b;
+        if (kPoly && e % 4 == 3) {
+            exp2_poly(x, a, b);
+        } else {
+            unpack_f32x2(x, a, b);
+            a = ex2(a);
+            b = ex2(b);
+        }
+        sum[e & 1] = add_f32x2(sum[e & 1], pack_f32x2(a, b));
+        w[e] = pack_bf16(a, b);
+    }
+    float a, b;
+    unpack_f32x2(add_f32x2(sum[0], sum[1]), a, b);
+    return a + b;
+}
+__device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+
+template <bool kNhd>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_constant__ CUtensorMap q_map, const ChunkParams p)
+{
+    extern __shared__ unsigned char smem_raw[];
+    if (smem_u32(smem_raw) & 1023u) {                                  // the tiles need it; no static shared memory, so it holds
+        if (threadIdx.x == 0) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
+        pdl_wait();
+        return;
+    }
+    unsigned char* const q_tiles = smem_raw;
+    unsigned char* const slots = smem_raw + 2 * kChunkQBytes;
+    ChunkShared& sh = *reinterpret_cast<ChunkShared*>(slots + kChunkSlots * kChunkSlotBytes);
+    ChunkControl* const c = &sh.c;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        for (int i = 0; i < kChunkSlots; ++i) { mbar_init(smem_u32(&c->full[i]), 1); mbar_init(smem_u32(&c->free[i]), 1); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&c->q_full[i]), 1);
+            mbar_init(smem_u32(&c->q_free[i]), 1);
+            mbar_init(smem_u32(&c->s_ready[i]), 1);
+            mbar_init(smem_u32(&c->s_free[i]), 4);                     // the stream's four softmax warps
+            mbar_init(smem_u32(&c->p_ready[i]), 4);
+            mbar_init(smem_u32(&c->pv_done[i]), 1);
+        }
+        mbar_init(smem_u32(&c->drained), 1);
+        c->timed_out = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&kv_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+    }
+    __syncwarp();
+    if (warp == 0) {                                                   // one CTA per SM: never waits
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&c->tmem_base)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = c->tmem_base;
+    pdl_wait();                                                        // nothing of the caller's is read above
+    pdl_launch_dependents();
+    chunk_plan(p, *c);
+    uint64_t deadline = global_ns() + kWaitBudgetNs;                   // of a segment's waits; every role sets it anew
+    volatile int32_t* const late = &c->timed_out;
+    auto wait = [&](unsigned long long& bar, uint32_t parity) { return mbar_wait(smem_u32(&bar), parity, deadline, late); };
+
+    // state of the roles, kept over the rounds
+    int slot = 0, loads = 0, q_use[2] = {0, 0}, q_slot = 0, step0 = 0, count0 = 0, count1 = 0, count = 0;
+    uint32_t parity = 1, q_parity = 0;
+    bool ok = true;
+    uint64_t keep;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(keep));
+
+    for (;;) {
+    if (warp == 11) chunk_segments(p, sh);
+    __syncthreads();
+    const int n_segments = c->n_segments, more_rounds = c->more;
+    if (warp == 8) {
+        // ---- TMA: up to 20 copies a step (five pages, K and V, two halves of 64 columns), issued by one elected lane with
+        // warp-uniform coordinates
+        for (int k = 0; k < n_segments && ok; ++k) {
+            const ChunkSegment s = sh.segments[k];
+            deadline = global_ns() + kWaitBudgetNs;
+            const int rows = s.rows_head & 0xffff, kv_head = s.rows_head >> 16;
+            const ChunkPages g = chunk_pages(p, s.lo, s.lo + rows / p.G - 1);
+            const int n_steps = s.step_end - s.step_begin, page0 = s.step_begin * kChunkStepPages;
+            const int n_pages = min(g.n - page0, n_steps * kChunkStepPages);
+            const bool pair = rows > kChunkTileRows;
+            if (n_steps <= 0) continue;
+            auto fetch = [&](int i) {                                  // physical page of the segment's i-th
+                if (i >= n_pages) return 0;
+                const int v = page0 + i;
+                return p.bt_pages[s.list_at + (v < g.head ? v : v - g.head + g.first)];
+            };
+            constexpr int kBatch = 30 / kChunkStepPages;               // page ids, 30 at a time and one batch ahead
+            int32_t ids = 0, next_ids = lane < 30 ? fetch(lane) : 0;
+            for (int t = 0; t < (pair ? 2 : 1) && ok; ++t) {
+                const int to = pair ? t : q_slot;
+                ok = q_use[to] == 0 || wait(c->q_free[to], (uint32_t)(q_use[to] - 1) & 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t bar = smem_u32(&c->q_full[to]), dst = smem_u32(q_tiles) + to * kChunkQBytes;
+                    const int tok = s.tok0 + t * (kChunkTileRows / p.G);
+                    mbar_expect_tx(bar, kChunkQBytes);
+                    tma_load_3d(dst, &q_map, 0, kv_head * p.G, tok, bar, keep);
+                    tma_load_3d(dst + kChunkQHalfBytes, &q_map, 64, kv_head * p.G, tok, bar, keep);
+                }
+                __syncwarp();
+                ++q_use[to];
+            }
+            if (!pair) q_slot ^= 1;
+            int in_batch = 0;
+            for (int j = 0; j < n_steps && ok; ++j) {
+                if (in_batch == 0) {
+                    ids = next_ids;
+                    next_ids = lane < 30 ? fetch((j + kBatch) * kChunkStepPages + lane) : 0;
+                    if (ids < 0 || ids >= p.num_pool_pages) { ids = 0; atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX); }
+                }
+                const int n = min(kChunkStepPages, n_pages - j * kChunkStepPages);
+                int32_t page[kChunkStepPages];
+#pragma unroll
+                for (int i = 0; i < kChunkStepPages; ++i) page[i] = __shfl_sync(0xffffffffu, ids, in_batch * kChunkStepPages + i);
+                if (++in_batch == kBatch) in_batch = 0;
+#pragma unroll 1
+                for (int v = 0; v < 2 && ok; ++v) {
+                    ok = wait(c->free[slot], parity);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        const uint32_t bar = smem_u32(&c->full[slot]), dst = smem_u32(slots) + slot * kChunkSlotBytes;
+                        mbar_expect_tx(bar, (uint32_t)n * kTileBytes);
+#pragma unroll
+                        for (int i = 0; i < kChunkStepPages; ++i) {
+                            if (i >= n) break;
+                            if (kNhd) {
+                                const int z = (page[i] * 2 + v) * kPageSize;
+                                tma_load_3d(dst + i * kHalfTileBytes, &kv_map, 0, kv_head, z, bar, keep);
+                                tma_load_3d(dst + kChunkPlaneBytes + i * kHalfTileBytes, &kv_map, 64, kv_head, z, bar, keep);
+                            } else {
+                                const int y = ((page[i] * 2 + v) * p.hkv + kv_head) * kPageSize;
+                                tma_load_2d(dst + i * kHalfTileBytes, &kv_map, 0, y, bar, keep);
+                                tma_load_2d(dst + kChunkPlaneBytes + i * kHalfTileBytes, &kv_map, 64, y, bar, keep);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    ++loads;
+                    if (++slot == kChunkSlots) { slot = 0; parity ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 9) {
+        // ---- tensor core: one elected lane runs through a whole segment, waits included, with warp-uniform operands
+        constexpr uint32_t idesc_o = umma_idesc(kChunkTileRows, kHeadDim, true);
+        const uint64_t q_desc = umma_smem_desc(smem_u32(q_tiles), 16, 1024), k_desc = umma_smem_desc(smem_u32(slots), 16, 1024);
+        // V: 16 tokens (K) x 128 columns (N), N contiguous; columns 64-127 one plane further, 8 tokens = 1 KiB
+        const uint64_t v_desc = umma_smem_desc(smem_u32(slots), kChunkPlaneBytes, 1024);
+        for (int k = 0; k < n_segments; ++k) {
+            const ChunkSegment seg = sh.segments[k];
+            deadline = global_ns() + kWaitBudgetNs;
+            const int rows = __shfl_sync(0xffffffffu, seg.rows_head & 0xffff, 0);
+            const ChunkPages g = chunk_pages(p, seg.lo, seg.lo + rows / p.G - 1);
+            const int n_steps = __shfl_sync(0xffffffffu, seg.step_end - seg.step_begin, 0);
+            const int n_pages = __shfl_sync(0xffffffffu, g.n - seg.step_begin * kChunkStepPages, 0);
+            const int pair = rows > kChunkTileRows ? 1 : 0;
+            if (n_steps <= 0) continue;
+            const int base0 = count0, base1 = count1, base = step0, q_at = q_slot;
+            if (elect_one()) {
+                // S of step j for stream t (its work n)
+                auto issue_s = [&](int t, int n, int j, bool last_user) {
+                    const int slot = (2 * (base + j)) % kChunkSlots;
+                    wait(c->full[slot], (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u);
+                    if (n > 0) wait(c->s_free[t], (uint32_t)(n - 1) & 1u);     // the softmax warps have read the scores before
+                    tc_fence_after();
+                    const uint64_t q = q_desc + (uint32_t)(pair ? t : q_at) * (kChunkQBytes / 16), kd = k_desc + (uint32_t)slot * (kChunkSlotBytes / 16);
+                    const int pages = min(kChunkStepPages, n_pages - j * kChunkStepPages);
+                    const uint32_t idesc_s = umma_idesc(kChunkTileRows, kPageSize, false) + ((uint32_t)(pages - 1) * (kPageSize >> 3) << 17);
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)
+                        umma_ss(tmem + t * 256, q + ((ks >> 2) * kChunkQHalfBytes + (ks & 3) * 32) / 16,
+                                kd + ((ks >> 2) * kChunkPlaneBytes + (ks & 3) * 32) / 16, idesc_s, ks > 0);
+                    umma_commit(smem_u32(&c->s_ready[t]));
+                    if (last_user) umma_commit(smem_u32(&c->free[slot]));
+                };
+                auto issue_pv = [&](int t, int n, int j, bool first, bool last_user) {
+                    const int slot = (2 * (base + j)) % kChunkSlots + 1;
+                    wait(c->full[slot], (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u);
+                    wait(c->p_ready[t], (uint32_t)n & 1u);
+                    tc_fence_after();
+                    const uint64_t v = v_desc + (uint32_t)slot * (kChunkSlotBytes / 16);
+                    const uint32_t o = tmem + t * 256 + kChunkTmemO, w = tmem + t * 256 + kChunkTmemP;
+                    const int pages = min(kChunkStepPages, n_pages - j * kChunkStepPages);
+#pragma unroll
+                    for (int pg = 0; pg < kChunkStepPages; ++pg)
+                        if (pg < pages) umma_ts(o, w + pg * 8, v + pg * (kHalfTileBytes / 16), idesc_o, !first || pg > 0);
+                    umma_commit(smem_u32(&c->pv_done[t]));
+                    if (last_user) umma_commit(smem_u32(&c->free[slot]));
+                };
+                wait(c->q_full[pair ? 0 : q_at], (q_parity >> (pair ? 0 : q_at)) & 1u);
+                if (pair) {
+                    wait(c->q_full[1], q_parity >> 1);
+                    for (int j = 0; j < n_steps; ++j) {
+                        issue_s(0, base0 + j, j, false);
+                        if (j > 0) issue_pv(0, base0 + j - 1, j - 1, j == 1, false);
+                        issue_s(1, base1 + j, j, true);
+                        if (j > 0) issue_pv(1, base1 + j - 1, j - 1, j == 1, true);
+                    }
+                    issue_pv(0, base0 + n_steps - 1, n_steps - 1, n_steps == 1, false);
+                    issue_pv(1, base1 + n_steps - 1, n_steps - 1, n_steps == 1, true);
+                    umma_commit(smem_u32(&c->q_free[0]));              // (all products of the segment are among those waited for)
+                    umma_commit(smem_u32(&c->q_free[1]));
+                } else {                                               // step j: work j / 2 of stream j mod 2
+                    for (int j = 0; j < n_steps; ++j) {
+                        issue_s(j & 1, (j & 1 ? base1 : base0) + (j >> 1), j, true);
+                        if (j > 1) issue_pv(j & 1, (j & 1 ? base1 : base0) + (j >> 1) - 1, j - 2, j < 4, true);
+                    }
+                    for (int j = max(0, n_steps - 2); j < n_steps; ++j)
+                        issue_pv(j & 1, (j & 1 ? base1 : base0) + (j >> 1), j, j < 2, true);
+                    umma_commit(smem_u32(&c->q_free[q_at]));
+                }
+            }
+            __syncwarp();
+            step0 += n_steps;
+            count0 += pair ? n_steps : (n_steps + 1) >> 1;
+            count1 += pair ? n_steps : n_steps >> 1;
+            q_parity ^= pair ? 3u : 1u << q_slot;
+            if (!pair) q_slot ^= 1;
+        }
+    } else if (warp < 8) {
+        // ---- softmax: stream = warp group, one query row per thread
+        const int stream = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + stream * 256, t_p = t_s + kChunkTmemP, t_o = t_s + kChunkTmemO;
+        const float sc = p.scale_log2;
+        for (int k = 0; k < n_segments; ++k) {
+            const ChunkSegment seg = sh.segments[k];
+            deadline = global_ns() + kWaitBudgetNs;
+            const int rows = seg.rows_head & 0xffff, kv_head = seg.rows_head >> 16;
+            const bool pair = rows > kChunkTileRows;
+            const int n_steps = seg.step_end - seg.step_begin;
+            const int tile = pair ? stream : 0, R = tile * kChunkTileRows + r;
+            const bool valid = R < rows, any_valid = tile * kChunkTileRows + (warp & 3) * 32 < rows;
+            // The row sees tokens [0, sink_end) and [from, to), counted along the segment's pages
+            int sink_end = 0, from = 0, to = 0;
+            const int hi = seg.lo + rows / p.G - 1;
+            const ChunkPages g = chunk_pages(p, seg.lo, hi);
+            // the last step holds the page in which the sequence ends
+            const bool tail = g.n - seg.step_begin * kChunkStepPages <= n_steps * kChunkStepPages && seg.length % kPageSize != 0 && hi / kPageSize == (seg.length - 1) / kPageSize;
+            if (valid) {
+                const int pos = seg.lo + R / p.G, shift = (g.first - g.head) * kPageSize;
+                to = pos + 1 - shift;
+                if (p.window) {
+                    from = (int)max((long long)pos - p.window + 1, 0ll) - shift;
+                    sink_end = min(p.n_sink, to);
+                    if (from <= sink_end) from = 0;
+                }
+            }
+            float m_ref = -INFINITY, l = 0.f;
+            int mine = 0;                                              // works of this stream in the segment
+            for (int j = pair ? 0 : stream; j < n_steps; j += pair ? 1 : 2) {
+                const int at = (seg.step_begin + j) * kChunkStepTokens;
+                wait(c->s_ready[stream], (uint32_t)count & 1u);
+                __syncwarp();
+                tc_fence_after();
+                if (any_valid) {
+                    float s[kChunkStepTokens];
+                    chunk_load_scores(t_s, s);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&c->s_free[stream]));
+                    const bool masked = __any_sync(0xffffffffu, valid && (to - at < kChunkStepTokens || (from > at && sink_end - at < kChunkStepTokens)));
+                    if (masked) {
+                        const int n_to = to - at, n_from = from - at, n_sink = sink_end - at;
+#pragma unroll
+                        for (int i = 0; i < kChunkStepTokens; ++i) s[i] = i < n_to && (i >= n_from || i < n_sink) ? s[i] : -INFINITY;
+                    }
+                    const float m_step = chunk_row_max(s) * sc;        // -inf: the row sees nothing here
+                    const bool lift = m_step > m_ref + kLazyMax;       // always so for the first visible step
+                    if (__any_sync(0xffffffffu, lift)) {
+                        const float m_new = lift ? m_step : m_ref;
+                        const float factor = m_new == -INFINITY ? 1.f : ex2(m_ref - m_new);
+                        if (mine > 0) {                                // O follows, once the products issued so far are in it
+                            wait(c->pv_done[stream], (uint32_t)(count - 1) & 1u);
+                            __syncwarp();
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int i = 0; i < kHeadDim; i += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(t_o + i, o);
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                                tmem_st16(t_o + i, o);
+                            }
+                        }
+                        l *= factor;
+                        m_ref = m_new;
+                    }
+                    const float mu = m_ref == -INFINITY ? 0.f : m_ref;
+                    uint32_t w[kChunkStepTokens / 2];
+                    l += masked ? chunk_weights<false>(s, sc, mu, w) : chunk_weights<true>(s, sc, mu, w);
+                    if (count > 0) {                                   // the weights before have been multiplied
+                        wait(c->pv_done[stream], (uint32_t)(count - 1) & 1u);
+                        __syncwarp();
+                        tc_fence_after();
+                    }
+                    tmem_st16(t_p, *reinterpret_cast<uint32_t(*)[16]>(&w[0]));
+                    tmem_st16(t_p + 16, *reinterpret_cast<uint32_t(*)[16]>(&w[16]));
+                    tmem_st8(t_p + 32, *reinterpret_cast<uint32_t(*)[8]>(&w[32]));
+                    tmem_wait_st();
+                } else {
+                    if (lane == 0) mbar_arrive(smem_u32(&c->s_free[stream]));
+                    // a warp without rows must not run ahead either: its p_ready arrival would count for the step before
+                    if (count > 0) wait(c->pv_done[stream], (uint32_t)(count - 1) & 1u);
+                }
+                if (tail && j == n_steps - 1 && (warp & 3) == 0) {
+                    // Rows of V behind the sequence's end may hold anything, and 0 x NaN is NaN: they are set to zero in shared memory before
+                    // the product (in a pair by both streams, each before its own).
+                    const int v_step = step0 + j, v_slot = (2 * v_step) % kChunkSlots + 1;
+                    wait(c->full[v_slot], (uint32_t)(v_step / (kChunkSlots / 2)) & 1u);
+                    __syncwarp();
+                    unsigned char* v = slots + v_slot * kChunkSlotBytes + (g.n - 1) % kChunkStepPages * kHalfTileBytes;
+                    for (int i = lane; i < 2 * kPageSize * 8; i += 32) {       // (plane, token, 16 bytes)
+                        const int tok = i >> 3 & (kPageSize - 1);
+                        if (tok >= seg.length % kPageSize)
+                            *reinterpret_cast<uint4*>(v + (i >> 7) * kChunkPlaneBytes + tok * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&c->p_ready[stream]));
+                ++count; ++mine;
+            }
+            // ---- the segment's result: the output of a whole unit, a state of a part of one
+            if (mine > 0) {
+                wait(c->pv_done[stream], (uint32_t)(count - 1) & 1u);
+                __syncwarp();
+                tc_fence_after();
+            }
+            float factor0 = 1.f, factor1 = 0.f;                        // of this stream's O and, in solo segments, of the other's
+            int col0 = 0, col1 = kHeadDim;
+            if (!pair) {
+                // both streams hold a part of the rows' state: each warp takes half of the columns of its 32 rows
+                tmem_st2(t_p, __float_as_uint(m_ref), __float_as_uint(l));
+                tmem_wait_st();
+                tc_fence_before();
+                pair_barrier(1 + (warp & 3));
+                tc_fence_after();
+                float2 other;
+                tmem_ld2(t_lane + (stream ^ 1) * 256 + kChunkTmemP, other.x, other.y);
+                const float m = fmaxf(m_ref, other.x), mu = m == -INFINITY ? 0.f : m;
+                factor0 = ex2(m_ref - mu); factor1 = ex2(other.x - mu);
+                const float l0 = l * factor0, l1 = other.y * factor1;
+                l = stream ? l1 + l0 : l0 + l1;
+                m_ref = m;
+                col0 = stream * (kHeadDim / 2); col1 = col0 + kHeadDim / 2;
+            }
+            if (any_valid) {
+                const bool own = mine > 0, both = !pair && n_steps > 1, have = pair ? own : n_steps > 0;
+                const uint32_t t_first = pair ? t_o : t_lane + kChunkTmemO, t_second = t_lane + 256 + kChunkTmemO;
+                const float f0 = pair || stream == 0 ? factor0 : factor1, f1 = stream == 0 ? factor1 : factor0;
+                const float inv = seg.slot >= 0 ? 1.f : l > 0.f ? 1.f / l : 0.f;
+                const int tok = seg.tok0 + R / p.G, h = kv_head * p.G + R % p.G;
+                const long long cell = (long long)tok * p.hq + h, state = (long long)seg.slot * kChunkUnitRows + R;
+#pragma unroll 1
+                for (int i = col0; i < col1; i += 32) {
+                    float o[32];
+                    if (have) {
+                        uint32_t u[2][16];
+                        tmem_ld16_nowait(t_first + i, u[0]);
+                        tmem_ld16_nowait(t_first + i + 16, u[1]);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(u[e >> 4][e & 15]) * (pair ? 1.f : f0);
+                        if (both) {
+                            tmem_ld16_nowait(t_second + i, u[0]);
+                            tmem_ld16_nowait(t_second + i + 16, u[1]);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] += __uint_as_float(u[e >> 4][e & 15]) * f1;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                    }
+                    if (valid && seg.slot < 0) {
+                        uint32_t v[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] = l > 0.f ? pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv) : 0u;
+                        uint4* dst = reinterpret_cast<uint4*>(p.out + cell * kHeadDim + i);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) dst[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                    } else if (valid) {
+                        // 32-byte stores: each lane has a row of its own, so an instruction touches 32 lines whatever its width
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) store_32b(p.part_o + state * kHeadDim + i + 8 * e, reinterpret_cast<const uint32_t*>(&o[8 * e]));
+                    }
+                }
+                if (valid && (pair || stream == 0)) {
+                    if (seg.slot >= 0) *reinterpret_cast<float2*>(p.part_ml + state * 2) = make_float2(m_ref, l);
+                    else if (p.lse) p.lse[cell] = l > 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                }
+            }
+            tc_fence_before();                                         // O has been read: the next segment's products may replace it
+            if (!pair) pair_barrier(1 + (warp & 3));
+            __syncwarp();
+            step0 += n_steps;
+        }
+    }
+    if (!more_rounds) break;
+    __syncthreads();                                                   // everybody has read this round's segments
+    }
+
+    if (warp == 8 && *late) {                                          // copies in flight must land before the CTA ends
+        const uint64_t last = global_ns() + kWaitBudgetNs;
+        int32_t more = 0;
+        for (int s = max(0, loads - kChunkSlots); s < loads; ++s) mbar_wait(smem_u32(&c->full[s % kChunkSlots]), (uint32_t)(s / kChunkSlots) & 1u, last, &more);
+        for (int s = 0; s < 2; ++s)
+            if (q_use[s]) mbar_wait(smem_u32(&c->q_full[s]), (uint32_t)(q_use[s] - 1) & 1u, last, &more);
+    }
+    if (warp == 9) {
+        if (elect_one()) umma_commit(smem_u32(&c->drained));           // everything issued, whatever happened
+        int32_t more = 0;
+        mbar_wait(smem_u32(&c->drained), 0, global_ns() + kWaitBudgetNs, &more);
+        __syncwarp();
+    }
+    if (lane == 0 && *late) atomicOr(p.status, 1 << KAP_ERR_TIMEOUT);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+}
+
+// ---- joins the states of the units that were cut.  Block (c, part): the unit in which CTA c begins, if no CTA before it begins in its middle;
+// CTA c - 1 began it, the CTAs that follow as long as their cuts lie in it hold the rest.  A warp takes a row at a time, a lane
+// four columns.
+constexpr int kChunkMergeThreads = 256;
+constexpr int kChunkMergeParts = kChunkUnitRows / 32;
+__global__ void __launch_bounds__(kChunkMergeThreads)
+kap_chunk_merge_kernel(const ChunkParams p, const int n_cta)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = 1 + blockIdx.x / kChunkMergeParts, part = blockIdx.x % kChunkMergeParts;
+    pdl_wait();
+    const ChunkCut cut = p.cuts[c];
+    if (!cut.inside) return;
+    const ChunkCut prior = p.cuts[c - 1];
+    if (prior.inside && prior.unit == cut.unit) return;
+    const int rows = cut.rows_head & 0xffff, head = cut.rows_head >> 16;
+    if (part * 32 >= rows) return;
+    int n = 1;                                                         // cuts inside the unit
+    for (;;) {
+        const int i = c + n + lane;
+        const bool same = i < n_cta && p.cuts[i].inside && p.cuts[i].unit == cut.unit;
+        const uint32_t m = __ballot_sync(0xffffffffu, same);
+        const int more = m == 0xffffffffu ? 32 : __ffs(~m) - 1;
+        n += more;
+        if (more < 32) break;
+    }
+    const int total = n + 1;
+    for (int R = part * 32 + warp; R < min(rows, part * 32 + 32); R += kChunkMergeThreads / 32) {
+        Merged acc;
+        acc.m = -INFINITY; acc.l = 0.f; acc.o = make_float4(0.f, 0.f, 0.f, 0.f);
+        constexpr int kBatch = 8;
+        for (int i0 = 0; i0 < total; i0 += kBatch) {
+            float2 ml[kBatch];
+            float4 o[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const int i = min(i0 + j, total - 1);
+                const long long row = ((long long)(c - 1 + i) * 2 + (i < total - 1 ? 1 : 0)) * kChunkUnitRows + R;
+                ml[j] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + row * 2));
+                o[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + row * kHeadDim) + lane);
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)
+                if (i0 + j < total && ml[j].y > 0.f) merge_into(acc, ml[j].x, ml[j].y, o[j]);
+        }
+        const long long cell = (long long)(cut.tok0 + R / p.G) * p.hq + head * p.G + R % p.G;
+        const float inv = acc.l > 0.f ? 1.f / acc.l : 0.f;
+        uint2 v;
+        v.x = pack_bf16(acc.o.x * inv, acc.o.y * inv);
+        v.y = pack_bf16(acc.o.z * inv, acc.o.w * inv);
+        *reinterpret_cast<uint2*>(p.out + cell * kHeadDim + lane * 4) = v;
+        if (p.lse && lane == 0) p.lse[cell] = acc.l > 0.f ? (acc.m + log2f(acc.l)) * 0.6931471805599453f : -INFINITY;
+    }
+}
+
+}  // namespace kap

@@ -58,6 +58,7 @@ struct kap_workspace {
                                    // next attention kernel as an ordinary (fully ordered) one
     int32_t shared_prefix = 0;     // the schedule was made by kap_schedule_shared_prefix (its arrays: kap_prefix.h)
     int32_t prefix_attrs_set = 0, prefix_ctas = 0, prefix_segments = 0;
+    int32_t chunk_attrs_set = 0;   // kap_chunk_attn's kernels may use their shared memory on this device
     int64_t total_rows = 0;        // sum over sequences of n_q
     unsigned long long bulk_overflows_seen = 0;   // see kv_written_in_bulk() in kap_attn.cu
     // host (pinned) staging and device copies

@@ -71,6 +71,9 @@ SIGNATURES = {
                                              C.c_int32, _vp]),
     "kap_shared_prefix_attn": (C.c_int, [_vp, _vp, _vp, C.c_int64, _vp, _vp, _vp, C.c_int32, C.c_int32,
                                          C.c_int32, C.c_int32, C.c_int32, C.c_float, _vp, _vp, _vp, _vp]),
+    "kap_chunk_attn_items": (C.c_int, [C.c_int32, C.c_int32, _i32p]),
+    "kap_chunk_attn": (C.c_int, [_vp, _vp, C.c_int32, _vp, C.c_int64, _vp, _vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                 C.c_int32, C.c_float, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp]),
     "kap_sample_tokens": (C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp, _vp,
                                     _vp, _vp, _vp]),
     "kap_device_sm_rates": (C.c_int, [C.c_int32, C.c_int32, _f32p, _i32p]),
@@ -452,6 +455,43 @@ def shared_prefix_attn(q, q_indptr, kv_pool, bt_indptr, bt_pages, ctx_len, out, 
     _check(lib().kap_shared_prefix_attn(
         q.data_ptr(), q_indptr.data_ptr(), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
         ctx_len.data_ptr(), batch, Hq, Hkv, d, P, sm_scale, out.data_ptr(), _dptr(lse),
+        ws._h, _stream_on(dev, stream)))
+    return out
+
+
+def chunk_attn_items(max_rows_per_item=64, cta_slots=148):
+    """kap_chunk_attn_items: the max_items of a Workspace (with this max_rows_per_item) that can hold the
+    partial results of chunk_attn on a device of cta_slots SMs."""
+    n = C.c_int32(0)
+    _check(lib().kap_chunk_attn_items(int(max_rows_per_item), int(cta_slots), C.byref(n)))
+    return n.value
+
+
+def chunk_attn(q, q_indptr, kv_pool, bt_indptr, bt_pages, ctx_len, out, ws: Workspace, lse=None, window=0,
+               n_sink=0, sm_scale=None, stream=None):
+    """kap_chunk_attn on torch CUDA tensors: q/out bf16 [rows, Hq, d], the rows of sequence b at
+    q_indptr[b] .. q_indptr[b+1]-1; window 0 sees the whole context, otherwise the last `window` tokens and
+    the first n_sink.  The workspace needs no schedule, only the size that chunk_attn_items gives."""
+    _torch_module()
+    dev = ws.device
+    if q.dtype is not _BF16 or out.dtype is not _BF16 or q.dim() != 3 or out.shape != q.shape or not q.is_contiguous() or \
+            not out.is_contiguous() or q.get_device() != dev or out.get_device() != dev:
+        raise KapError(ERR_INVALID_ARG, f"q is {q.dtype} {tuple(q.shape)} with strides {q.stride()} on {q.device}, out {out.dtype} {tuple(out.shape)} with "
+                       f"strides {out.stride()} on {out.device}: expected contiguous bfloat16 tensors of one shape on GPU {dev}, the workspace's device")
+    rows, Hq, d = q.shape
+    if lse is not None and (lse.dtype is not _F32 or lse.shape != (rows, Hq) or not lse.is_contiguous() or lse.get_device() != dev):
+        raise KapError(ERR_INVALID_ARG, f"lse is {lse.dtype} {tuple(lse.shape)} with strides {lse.stride()} on {lse.device}, expected a contiguous "
+                       f"float32 [{rows}, {Hq}] tensor on GPU {dev}")
+    batch = ctx_len.shape[0]
+    _check_index("q_indptr", q_indptr, batch + 1, dev)
+    _check_block_table(bt_indptr, bt_pages, ctx_len, batch, dev)
+    pages, Hkv, P, pool_d = _dense_pool(kv_pool, ws.kv_layout == KV_NHD, dev)
+    if pool_d != d:
+        raise KapError(ERR_INVALID_ARG, f"q has heads of {d} columns, kv_pool of {pool_d}")
+    sm_scale = d ** -0.5 if sm_scale is None else float(sm_scale)
+    _check(lib().kap_chunk_attn(
+        q.data_ptr(), q_indptr.data_ptr(), rows, kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
+        ctx_len.data_ptr(), batch, Hq, Hkv, d, P, sm_scale, window, n_sink, out.data_ptr(), _dptr(lse),
         ws._h, _stream_on(dev, stream)))
     return out
 
