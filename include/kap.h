@@ -560,6 +560,100 @@ kap_status kap_append_kv_rope(
     void* cuda_stream);
 
 /*
+ * kap_build_block_tables / kap_release_pages - the block tables, slots and positions of a step, built on the device from the requests'
+ * lengths, with the pages they need taken from a stack of free pages (the KAP paper takes block tables and slot mappings, Section 3.1,
+ * from its host runtime).  State, all DEVICE arrays of the caller's:
+ *   page_table [num_requests][table_stride]  physical page of each logical page of a request
+ *   pages_held [num_requests]                logical pages of a request that have one: its first entries in page_table
+ *   free_pages [free_capacity]               a stack; free_count[0] entries of it, the last one on top
+ * kap_build_block_tables: sequence b of the step is request request[b] (NULL: request b) with ctx_len[b] tokens cached and n_new[b] new ones
+ * (NULL: one each), ceil((ctx_len + n_new) / page_size) pages.  Those beyond pages_held are taken: the i-th page taken in the step,
+ * sequences in order, logical pages ascending, is free_pages[free_count - 1 - i].  A request that holds more keeps it (after rejected
+ * proposals, say).  Written: page_table, pages_held, free_count, and
+ *   bt_indptr [batch+1], bt_pages            the step's CSR block table (bt_capacity entries)
+ *   new_indptr [batch+1]                     first new row of each sequence (kap_append_kv_rope's new_indptr, kap_chunk_attn's q_indptr), or NULL
+ *   slot, position [new_indptr[batch]]       page * page_size + place in it, and logical index, of each new row; each may be NULL
+ * Entries behind the last one are left as they were.  All or nothing: a step that cannot be built (stack, table row, bt_capacity or
+ * row_capacity too small: KAP_ERR_CAPACITY; a request out of range or named twice, a negative length, a pages_held or free_count out of
+ * range: KAP_ERR_DEVICE_INDEX; as 1 << code in *device_status) changes no state and leaves bt_indptr and new_indptr all 0, which the
+ * append and attention calls take as a step without rows.
+ * kap_release_pages: of each request in request[0 .. n-1] (NULL: requests 0 .. n-1) the pages beyond ceil(keep_tokens / page_size) (NULL: all)
+ * go back, the i-th to free_pages[free_count + all - 1 - i]: released at once, the pages of a step lie where it took them from.  A request
+ * that holds fewer keeps them.  All or nothing as above (KAP_ERR_CAPACITY: free_capacity).
+ * The pages of a sliding window's past are not tracked: entries of page_table that no row sees may be overwritten by the caller, but count as held.
+ * Two calls that share state must be ordered.  Asynchronous on cuda_stream, without a workspace; can be captured into a CUDA graph.
+ * Errors: KAP_ERR_INVALID_ARG (NULL or misaligned pointer, negative size, batch > num_requests, slot or position without new_indptr),
+ * KAP_ERR_UNSUPPORTED (num_requests above 1048576), KAP_ERR_CUDA.
+ */
+kap_status kap_build_block_tables(
+    const int32_t* request,            /* DEVICE [batch] or NULL */
+    const int32_t* ctx_len,            /* DEVICE [batch] tokens cached before the step */
+    const int32_t* n_new,              /* DEVICE [batch] or NULL */
+    int32_t batch, int32_t page_size,
+    int32_t* page_table, int32_t num_requests, int64_t table_stride, int32_t* pages_held,
+    int32_t* free_pages, int32_t free_capacity, int32_t* free_count,
+    int32_t* bt_indptr,                /* DEVICE out [batch+1] */
+    int32_t* bt_pages, int64_t bt_capacity,
+    int32_t* new_indptr,               /* DEVICE out [batch+1] or NULL */
+    int64_t* slot,                     /* DEVICE out [row_capacity] or NULL */
+    int32_t* position,                 /* DEVICE out [row_capacity] or NULL */
+    int64_t row_capacity,
+    int32_t* device_status,            /* DEVICE int32 or NULL */
+    void* cuda_stream);
+
+kap_status kap_release_pages(
+    const int32_t* request, int32_t n, /* DEVICE [n] or NULL */
+    const int32_t* keep_tokens,        /* DEVICE [n] or NULL */
+    int32_t page_size,
+    int32_t* page_table, int32_t num_requests, int64_t table_stride, int32_t* pages_held,
+    int32_t* free_pages, int32_t free_capacity, int32_t* free_count,
+    int32_t* device_status,            /* DEVICE int32 or NULL */
+    void* cuda_stream);
+
+/* element type of kap_append_kv_norm_rope's weights */
+enum {
+    KAP_NORM_F32 = 0,
+    KAP_NORM_BF16 = 1
+};
+
+/*
+ * kap_append_kv_norm_rope - kap_append_kv_rope for models that normalise the heads of q and k before the rotation: each head x of q
+ * and k becomes
+ *     y = x / sqrt(mean(x^2) + eps) * w        (w: the weights, or 1 + the weights with unit_offset != 0)
+ * and y is rotated; v is copied as it is.  Sums, norms and rotation run in fp32 (a head whose squares sum to more than fp32 holds
+ * becomes 0), each result is rounded to bf16 once.  q_weight / k_weight: 128 values for all heads, or with weight_per_head != 0
+ * [Hq][128] and [Hkv][128]; NULL means w = 1.
+ * All other arguments, rules, reports and errors are kap_append_kv_rope's, plus KAP_ERR_UNSUPPORTED for the weights' type and
+ * KAP_ERR_INVALID_ARG for weights that are not 16-byte aligned or an eps that is negative or not a number.
+ */
+kap_status kap_append_kv_norm_rope(
+    const void* q, int64_t q_stride,          /* DEVICE bf16 [total_rows][Hq][d] or NULL */
+    const void* k_new, int64_t k_stride,      /* DEVICE bf16 [total_rows][Hkv][d] */
+    const void* v_new, int64_t v_stride,      /* DEVICE bf16 [total_rows][Hkv][d] */
+    void* q_out, int64_t q_out_stride,        /* DEVICE bf16 [total_rows][Hq][d] */
+    const int32_t* new_indptr,                /* DEVICE [batch+1], or NULL: one new token per sequence */
+    int32_t total_rows,
+    const void* q_weight,                     /* DEVICE [d], [Hq][d] or NULL */
+    const void* k_weight,                     /* DEVICE [d], [Hkv][d] or NULL */
+    int32_t weight_type,                      /* KAP_NORM_F32 or KAP_NORM_BF16 */
+    int32_t weight_per_head, int32_t unit_offset, float eps,
+    const float* inv_freq,                    /* DEVICE [rotary_dim / 2] */
+    int32_t rotary_dim, int32_t interleaved,
+    const int32_t* positions,                 /* DEVICE [num_axes][positions_stride] or NULL */
+    int64_t positions_stride, int32_t num_axes,
+    const uint8_t* freq_axis,                 /* HOST [rotary_dim / 2] or NULL */
+    const int32_t* position_offset,           /* DEVICE [batch] or NULL */
+    void* kv_pool, int64_t num_pool_pages,
+    const int32_t* bt_indptr,                 /* DEVICE [batch+1] CSR block table */
+    const int32_t* bt_pages,                  /* DEVICE */
+    int32_t* ctx_len,                         /* DEVICE [batch], read; updated when advance != 0 */
+    int32_t advance,
+    int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+    int32_t kv_layout,                        /* KAP_KV_HND or KAP_KV_NHD */
+    int32_t* device_status,                   /* DEVICE int32 or NULL */
+    void* cuda_stream);
+
+/*
  * kap_shared_prefix_attn - kap_verify_attn for a batch whose sequences come in groups that share
  * the first pages of their block tables (one document or instruction, many requests on it).  Same
  * arguments, same rows, same visibility rule (row j of sequence b sees t <= ctx_len[b] - n_q + j),
@@ -666,6 +760,49 @@ enum {
     KAP_LOGITS_F32 = 0,
     KAP_LOGITS_BF16 = 1
 };
+
+/*
+ * kap_adjust_logits - penalties for repeated tokens, biases and grammar masks on logits rows, in front of kap_sample_tokens or
+ * kap_top3_accept (the paper fixes no such rule).  For token t of row r with logit x:
+ *   c = how often t occurs in the answer so far, s = whether t occurs in the prompt or the answer
+ *   x1 = s ? (x > 0 ? x / repetition[r] : x * repetition[r]) : x
+ *   x2 = c > 0 ? x1 - frequency[r] c - presence[r] : x1
+ *   x3 = x2 + the sum of the row's biases of t
+ *   out = t is allowed ? x3 : -inf
+ * in fp32, rounded to the logits' type once.  out may be logits (in place: only logits that change are written); it must not overlap
+ * them otherwise.
+ *   history_at[r] = {b, a, e}: the prompt is history[b .. a-1], the answer history[a .. e-1]; rows may share tokens (the rows of a verification
+ *                   window, each one longer than the one before).  Tokens outside 0 .. vocab-1 are passed over.
+ *   bias_indptr     biases bias_indptr[r] .. bias_indptr[r+1]-1 belong to row r, ascending by token; of equal tokens all are added, in order.
+ *                   Tokens outside 0 .. vocab-1 are passed over.
+ *   allowed         bit t % 32 of word t / 32 of mask allowed_row[r] (NULL: mask r; -1: every token is allowed) says whether t is allowed
+ * A NULL array switches its rule off; so do, for a row, a repetition that is not above 0 and a NaN presence or frequency.
+ * Reported in *device_status (1 << KAP_ERR_DEVICE_INDEX): a history_at that is out of order or leaves 0 .. history_len (or spans 2^30 tokens and
+ * more; the row then has no history), a bias_indptr that falls or leaves 0 .. bias_len (the row
+ * then has no biases), an allowed_row below -1 or beyond the masks (the row is not masked), biases out of order (the results of such
+ * tokens are not defined).
+ * Results do not depend on timing.  Asynchronous on cuda_stream, without a workspace; can be captured into a CUDA graph.
+ * Errors: KAP_ERR_INVALID_ARG (NULL or misaligned pointer, vocab < 1, a row stride < vocab, penalties without a history, incomplete
+ * biases, masks that are too short or too few, in place with two strides), KAP_ERR_UNSUPPORTED (logits_type, vocab above 811008, more than
+ * 65535 rows), KAP_ERR_CUDA.
+ */
+kap_status kap_adjust_logits(
+    const void* logits,                /* DEVICE, row r starts at element r * row_stride */
+    int32_t logits_type,               /* KAP_LOGITS_F32 or KAP_LOGITS_BF16 */
+    int64_t row_stride, int32_t rows, int32_t vocab,
+    void* out, int64_t out_stride,     /* DEVICE out, the logits' type */
+    const int32_t* history, int64_t history_len,   /* DEVICE [history_len] or NULL */
+    const int64_t* history_at,         /* DEVICE [rows][3] */
+    const float* repetition,           /* DEVICE [rows] or NULL */
+    const float* presence,             /* DEVICE [rows] or NULL */
+    const float* frequency,            /* DEVICE [rows] or NULL */
+    const int32_t* bias_indptr,        /* DEVICE [rows+1] or NULL */
+    const int32_t* bias_token, const float* bias_value, int64_t bias_len,   /* DEVICE [bias_len] */
+    const uint32_t* allowed,           /* DEVICE [num_masks][allowed_stride] or NULL */
+    int32_t num_masks, int64_t allowed_stride,
+    const int32_t* allowed_row,        /* DEVICE [rows] or NULL */
+    int32_t* device_status,            /* DEVICE int32 or NULL */
+    void* cuda_stream);
 
 /*
  * kap_sample_tokens - draw one token per logits row with given random numbers (the proposal steps'

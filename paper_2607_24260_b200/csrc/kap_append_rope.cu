@@ -41,6 +41,11 @@ struct RopeParams {
     int32_t batch, hq, hkv, half, interleaved, nhd;            // half = rotated pairs of a head
     uint8_t axis[kHeadDim / 2];
 };
+struct NormParams {                                // of kap_append_kv_norm_rope
+    const void *q_weight, *k_weight;               // [128], or [heads][128] with a head stride of 128; NULL: ones
+    int32_t q_head_stride, k_head_stride, f32, unit_offset;
+    float eps;
+};
 
 __device__ __forceinline__ void rotate(uint32_t& a, uint32_t& b, const float2 t0, const float2 t1) {
     // a holds the first partners of two pairs, b the second ones
@@ -57,8 +62,44 @@ __device__ __forceinline__ uint32_t rotate_neighbours(uint32_t v, const float2 t
     return *reinterpret_cast<const uint32_t*>(&x);
 }
 
-__global__ void __launch_bounds__(kRopeThreads, 16)
-kap_append_kv_rope_kernel(const RopeParams p)
+// Weights of a norm for the eight columns of one 16-byte piece.
+__device__ __forceinline__ void load_weights(const NormParams& n, const void* w, int at, float (&f)[8]) {
+    if (!w) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = 1.f;
+        return;
+    }
+    if (n.f32) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>((const float*)w + at)), b = __ldg(reinterpret_cast<const float4*>((const float*)w + at) + 1);
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    } else {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)w + at));
+        const uint32_t v[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(v[e] << 16); f[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u); }
+    }
+    if (n.unit_offset)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] += 1.f;
+}
+__device__ __forceinline__ void widen(const uint4 a, float (&f)[8]) {
+    const uint32_t v[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(v[e] << 16); f[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u); }
+}
+__device__ __forceinline__ uint4 narrow(const float (&f)[8]) {
+    uint32_t v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const __nv_bfloat162 x = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+        v[e] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+template <bool kNorm>
+__global__ void __launch_bounds__(kRopeThreads, kNorm ? 10 : 16)
+kap_append_kv_rope_kernel(const RopeParams p, const NormParams n)
 {
     __shared__ float2 turn[kHeadDim / 2];           // (cos, sin) of this row's pairs
     const int row = blockIdx.x, tid = threadIdx.x;
@@ -110,7 +151,41 @@ kap_append_kv_rope_kernel(const RopeParams p)
         const uint4* s4 = reinterpret_cast<const uint4*>(src + head * kHeadDim);
         if (!is_q && !stored) continue;
         uint4 x = s4[c0], y = s4[c1];
-        if (apart) {
+        if (kNorm && !is_v) {
+            // a head's eight threads are neighbours: its sum of squares takes three exchanges
+            float a[8], b[8], w[8];
+            widen(x, a); widen(y, b);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += a[e] * a[e] + b[e] * b[e];
+            const uint32_t group = 0xffu << (tid & 24);
+#pragma unroll
+            for (int d = 1; d < kTasks; d *= 2) sum += __shfl_xor_sync(group, sum, d);
+            const float r = rsqrtf(sum * (1.f / kHeadDim) + n.eps);
+            const void* weight = is_q ? n.q_weight : n.k_weight;
+            const int at = head * (is_q ? n.q_head_stride : n.k_head_stride);
+            load_weights(n, weight, at + c0 * 8, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] *= r * w[e];
+            load_weights(n, weight, at + c1 * 8, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) b[e] *= r * w[e];
+            if (t < rotated) {
+                const float2* f = turn + t * 8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (apart) {
+                        const float u = a[e] * f[e].x - b[e] * f[e].y, v = b[e] * f[e].x + a[e] * f[e].y;
+                        a[e] = u; b[e] = v;
+                    } else {                         // pairs 0 to 3 in the first piece, 4 to 7 in the second
+                        float* z = e < 4 ? a + 2 * e : b + 2 * (e - 4);
+                        const float u = z[0] * f[e].x - z[1] * f[e].y, v = z[1] * f[e].x + z[0] * f[e].y;
+                        z[0] = u; z[1] = v;
+                    }
+                }
+            }
+            x = narrow(a); y = narrow(b);
+        } else if (apart) {
             const float2* f = turn + t * 8;
             rotate(x.x, y.x, f[0], f[1]); rotate(x.y, y.y, f[2], f[3]);
             rotate(x.z, y.z, f[4], f[5]); rotate(x.w, y.w, f[6], f[7]);
@@ -143,8 +218,11 @@ __global__ void kap_advance_ctx_kernel(const int32_t* __restrict__ new_indptr, i
 }  // namespace
 }  // namespace kap
 
-extern "C" kap_status kap_append_kv_rope(
-    const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+namespace kap {
+namespace {
+
+kap_status append_rope(
+    const NormParams* norm, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
     void* q_out, int64_t q_out_stride, const int32_t* new_indptr, int32_t total_rows, const float* inv_freq,
     int32_t rotary_dim, int32_t interleaved, const int32_t* positions, int64_t positions_stride, int32_t num_axes,
     const uint8_t* freq_axis, const int32_t* position_offset, void* kv_pool, int64_t num_pool_pages,
@@ -152,7 +230,6 @@ extern "C" kap_status kap_append_kv_rope(
     int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t kv_layout,
     int32_t* device_status, void* cuda_stream)
 {
-    using namespace kap;
     if (head_dim != kHeadDim || page_size != kPageSize)
         return fail(KAP_ERR_UNSUPPORTED, "head_dim %d / page_size %d (supported: 128 / 16)", head_dim, page_size);
     if (rotary_dim < 16 || rotary_dim > kHeadDim || rotary_dim % 16)
@@ -199,18 +276,63 @@ extern "C" kap_status kap_append_kv_rope(
     p.interleaved = interleaved != 0; p.nhd = kv_layout == KAP_KV_NHD;
     if (freq_axis)
         for (int i = 0; i < p.half; ++i) p.axis[i] = freq_axis[i];
-    kap_append_kv_rope_kernel<<<(unsigned)total_rows, kRopeThreads, 0, (cudaStream_t)cuda_stream>>>(p);
+    if (norm) kap_append_kv_rope_kernel<true><<<(unsigned)total_rows, kRopeThreads, 0, (cudaStream_t)cuda_stream>>>(p, *norm);
+    else kap_append_kv_rope_kernel<false><<<(unsigned)total_rows, kRopeThreads, 0, (cudaStream_t)cuda_stream>>>(p, NormParams{});
     cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "kap_append_kv_rope launch failed: %s", cudaGetErrorString(e));
+    if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
     count_launch();
     if (new_indptr) {
         if (advance) {                              // several CTAs read a ctx_len[b]: it moves when they are done
             kap_advance_ctx_kernel<<<(unsigned)((batch + 127) / 128), 128, 0, (cudaStream_t)cuda_stream>>>(new_indptr, ctx_len, batch);
             e = cudaGetLastError();
-            if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "kap_append_kv_rope launch failed: %s", cudaGetErrorString(e));
+            if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
             count_launch();
         }
         kv_written_in_bulk(cuda_stream);            // see kap_append_kv
     }
     return KAP_OK;
+}
+
+}  // namespace
+}  // namespace kap
+
+extern "C" kap_status kap_append_kv_rope(
+    const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+    void* q_out, int64_t q_out_stride, const int32_t* new_indptr, int32_t total_rows, const float* inv_freq,
+    int32_t rotary_dim, int32_t interleaved, const int32_t* positions, int64_t positions_stride, int32_t num_axes,
+    const uint8_t* freq_axis, const int32_t* position_offset, void* kv_pool, int64_t num_pool_pages,
+    const int32_t* bt_indptr, const int32_t* bt_pages, int32_t* ctx_len, int32_t advance, int32_t batch,
+    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t kv_layout,
+    int32_t* device_status, void* cuda_stream)
+{
+    return kap::append_rope(nullptr, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, q_out_stride, new_indptr, total_rows, inv_freq,
+                            rotary_dim, interleaved, positions, positions_stride, num_axes, freq_axis, position_offset, kv_pool,
+                            num_pool_pages, bt_indptr, bt_pages, ctx_len, advance, batch, num_q_heads, num_kv_heads, head_dim, page_size,
+                            kv_layout, device_status, cuda_stream);
+}
+
+extern "C" kap_status kap_append_kv_norm_rope(
+    const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+    void* q_out, int64_t q_out_stride, const int32_t* new_indptr, int32_t total_rows,
+    const void* q_weight, const void* k_weight, int32_t weight_type, int32_t weight_per_head, int32_t unit_offset, float eps,
+    const float* inv_freq, int32_t rotary_dim, int32_t interleaved, const int32_t* positions, int64_t positions_stride, int32_t num_axes,
+    const uint8_t* freq_axis, const int32_t* position_offset, void* kv_pool, int64_t num_pool_pages,
+    const int32_t* bt_indptr, const int32_t* bt_pages, int32_t* ctx_len, int32_t advance, int32_t batch,
+    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t kv_layout,
+    int32_t* device_status, void* cuda_stream)
+{
+    using namespace kap;
+    if (weight_type != KAP_NORM_F32 && weight_type != KAP_NORM_BF16)
+        return fail(KAP_ERR_UNSUPPORTED, "weight_type %d (KAP_NORM_F32 = 0, KAP_NORM_BF16 = 1)", weight_type);
+    if (!(eps >= 0.f) || eps > 3e38f) return fail(KAP_ERR_INVALID_ARG, "eps %g", (double)eps);
+    if ((reinterpret_cast<uintptr_t>(q_weight) | reinterpret_cast<uintptr_t>(k_weight)) & 15)
+        return fail(KAP_ERR_INVALID_ARG, "q_weight and k_weight must be 16-byte aligned");
+    NormParams n{};
+    n.q_weight = q_weight; n.k_weight = k_weight;
+    n.q_head_stride = n.k_head_stride = weight_per_head ? kHeadDim : 0;
+    n.f32 = weight_type == KAP_NORM_F32; n.unit_offset = unit_offset != 0; n.eps = eps;
+    return append_rope(&n, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, q_out_stride, new_indptr, total_rows, inv_freq,
+                       rotary_dim, interleaved, positions, positions_stride, num_axes, freq_axis, position_offset, kv_pool,
+                       num_pool_pages, bt_indptr, bt_pages, ctx_len, advance, batch, num_q_heads, num_kv_heads, head_dim, page_size,
+                       kv_layout, device_status, cuda_stream);
 }

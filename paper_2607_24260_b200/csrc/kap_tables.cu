@@ -1,0 +1,280 @@
+// kap_build_block_tables / kap_release_pages: the step's block tables and slots from the requests' lengths, on the device (the KAP paper's
+// block tables and slot mappings, Section 3.1, are taken as given by its host runtime).
+//
+// Mathematics: with L tokens cached, n new ones and held pages, sequence b lists ceil((L + n) / P) pages and takes those it does not hold from the
+// top of a stack of free pages; where a sequence's list, new rows and taken pages begin are three prefix sums over the batch.
+// Layout: one CTA does the sums, the checks and the state (page table, held pages, stack), all or nothing; a second kernel, started while
+// the first runs, copies the lists and writes the slots, a CTA for each 2048 entries, whose owners it finds by bisection.
+#include <cuda_runtime.h>
+
+#include "kap_internal.h"
+
+namespace kap {
+void count_launch();
+bool launch_programmatically();
+
+namespace {
+
+constexpr int kTableThreads = 1024, kTableWarps = kTableThreads / 32;
+constexpr int kFillThreads = 256, kFillEntries = 2048;
+constexpr int32_t kMaxRequests = 1 << 20;                     // a bit each in the first kernel's shared memory
+
+struct TableParams {
+    const int32_t *request, *ctx_len, *n_new;                 // release: ctx_len = tokens to keep
+    int32_t *page_table, *pages_held, *free_pages, *free_count, *bt_indptr, *bt_pages, *new_indptr, *position, *status;
+    long long* slot;
+    long long table_stride, bt_capacity, row_capacity;
+    int32_t batch, page_size, num_requests, free_capacity;
+};
+
+struct Entry { int32_t request, held, pages, moved, n; bool bad, full; };   // pages: listed (build) or kept (release); moved: taken or given back
+
+template <bool kRelease>
+__device__ __forceinline__ Entry load_entry(const TableParams& p, int b, uint32_t* seen) {
+    Entry e{0, 0, 0, 0, 0, false, false};
+    if (b >= p.batch) return e;
+    e.request = p.request ? p.request[b] : b;
+    const int L = p.ctx_len ? p.ctx_len[b] : 0;
+    e.n = kRelease ? 0 : p.n_new ? p.n_new[b] : 1;
+    if (e.request < 0 || e.request >= p.num_requests || L < 0 || e.n < 0) { e.bad = true; e.n = 0; return e; }
+    e.held = p.pages_held[e.request];
+    if (seen) e.bad = atomicOr(&seen[e.request >> 5], 1u << (e.request & 31)) >> (e.request & 31) & 1u;   // named twice
+    if (e.held < 0 || e.held > p.table_stride) { e.bad = true; e.held = 0; }
+    const long long pages = ((long long)L + e.n + p.page_size - 1) / p.page_size;
+    if (kRelease) {
+        e.pages = (int32_t)min(pages, (long long)e.held);
+        e.moved = e.held - e.pages;
+    } else {
+        if (pages > p.table_stride) { e.full = true; return e; }
+        e.pages = (int32_t)pages;
+        e.moved = max(0, e.pages - e.held);
+    }
+    return e;
+}
+
+// inclusive sums over the block; `carry` comes before, and is moved on
+struct Sums { long long pages, moved, rows; };
+__device__ __forceinline__ Sums block_scan(Sums v, Sums& carry, Sums* warp_sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const long long a = __shfl_up_sync(0xffffffffu, v.pages, d), b = __shfl_up_sync(0xffffffffu, v.moved, d), c = __shfl_up_sync(0xffffffffu, v.rows, d);
+        if (lane >= d) { v.pages += a; v.moved += b; v.rows += c; }
+    }
+    __syncthreads();
+    if (lane == 31) warp_sums[warp] = v;
+    __syncthreads();
+    Sums total = carry;
+#pragma unroll 4
+    for (int w = 0; w < kTableWarps; ++w) {
+        if (w == warp) { v.pages += total.pages; v.moved += total.moved; v.rows += total.rows; }
+        total.pages += warp_sums[w].pages; total.moved += warp_sums[w].moved; total.rows += warp_sums[w].rows;
+    }
+    carry = total;
+    return v;
+}
+
+template <bool kRelease>
+__global__ void __launch_bounds__(kTableThreads)
+kap_tables_kernel(const TableParams p)
+{
+    extern __shared__ uint32_t seen[];
+    __shared__ Sums warp_sums[kTableWarps];
+    __shared__ int32_t upto[kTableThreads], first[kTableThreads], request[kTableThreads];
+    const int tid = threadIdx.x;
+    for (int i = tid; i < (p.num_requests + 31) / 32; i += kTableThreads) seen[i] = 0u;
+    if (!kRelease) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the second kernel, which waits
+    __syncthreads();
+    const int count = *p.free_count;
+    // ---- what the step needs, and whether that can be had
+    Sums total{0, 0, 0};
+    bool bad = false, full = false;
+    const Entry e0 = load_entry<kRelease>(p, tid, seen);
+    for (int b0 = 0; b0 < p.batch; b0 += kTableThreads) {
+        const Entry e = b0 == 0 ? e0 : load_entry<kRelease>(p, b0 + tid, seen);
+        bad |= e.bad;
+        full |= e.full;
+        total.pages += e.pages; total.moved += e.moved; total.rows += e.n;
+    }
+    Sums all{0, 0, 0};
+    const Sums mine0 = block_scan(total, all, warp_sums);     // (sums of the first 1024 sequences, when there are no more)
+    bad |= count < 0 || count > p.free_capacity;
+    bad = __syncthreads_or(bad);
+    if (kRelease) full = all.moved > (long long)p.free_capacity - count;
+    else full = __syncthreads_or(full) || all.moved > count || all.pages > p.bt_capacity || all.rows > p.row_capacity;
+    if (bad || full) {                                        // nothing is taken: a step without pages and rows
+        if (!kRelease)
+            for (int b = tid; b <= p.batch; b += kTableThreads) {
+                p.bt_indptr[b] = 0;
+                if (p.new_indptr) p.new_indptr[b] = 0;
+            }
+        if (tid == 0 && p.status) atomicOr(p.status, (bad ? 1 << KAP_ERR_DEVICE_INDEX : 0) | (full ? 1 << KAP_ERR_CAPACITY : 0));
+        return;
+    }
+    // ---- the state and the prefix sums
+    Sums carry{0, 0, 0};
+    if (!kRelease && tid == 0) {
+        p.bt_indptr[0] = 0;
+        if (p.new_indptr) p.new_indptr[0] = 0;
+    }
+    for (int b0 = 0; b0 < p.batch; b0 += kTableThreads) {
+        const int b = b0 + tid;
+        const Entry e = b0 == 0 ? e0 : load_entry<kRelease>(p, b, nullptr);
+        const long long moved0 = carry.moved;
+        Sums v{e.pages, e.moved, e.n};
+        if (p.batch <= kTableThreads) { v = mine0; carry = all; }
+        else v = block_scan(v, carry, warp_sums);
+        if (b < p.batch) {
+            if (!kRelease) {
+                p.bt_indptr[b + 1] = (int32_t)v.pages;
+                if (p.new_indptr) p.new_indptr[b + 1] = (int32_t)v.rows;
+            }
+            if (e.moved > 0) p.pages_held[e.request] = e.pages;
+        }
+        upto[tid] = (int32_t)(v.moved - moved0);
+        first[tid] = kRelease ? e.pages : e.held;
+        request[tid] = e.request;
+        __syncthreads();
+        const int moved = (int)(carry.moved - moved0);
+        for (int i = tid; i < moved; i += kTableThreads) {
+            int lo = 0;                                       // the owner: sequences whose pages all come before i
+#pragma unroll
+            for (int d = kTableThreads / 2; d > 0; d /= 2)
+                if (upto[lo + d - 1] <= i) lo += d;
+            const int before = lo ? upto[lo - 1] : 0;
+            int32_t* entry = p.page_table + request[lo] * p.table_stride + first[lo] + (i - before);
+            // the i-th page moved, in the batch's order, is the i-th from the larger of the two tops
+            if (kRelease) p.free_pages[count + all.moved - 1 - (moved0 + i)] = *entry;
+            else *entry = p.free_pages[count - 1 - (moved0 + i)];
+        }
+        __syncthreads();
+    }
+    if (tid == 0 && all.moved > 0) *p.free_count = (int32_t)(kRelease ? count + all.moved : count - all.moved);
+}
+
+// the last sequence whose entries begin at or before i
+__device__ __forceinline__ int owner_of(const int32_t* __restrict__ indptr, int lo, int hi, int i) {
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (indptr[mid] <= i) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__global__ void __launch_bounds__(kFillThreads)
+kap_fill_tables_kernel(const TableParams p, const int list_blocks)
+{
+    // (It lets nothing start before it ends: attention kernels read block tables ahead of their dependency wait.)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const bool lists = (int)blockIdx.x < list_blocks;
+    const int32_t* const indptr = lists ? p.bt_indptr : p.new_indptr;
+    const int total = indptr[p.batch], at = (lists ? blockIdx.x : blockIdx.x - list_blocks) * kFillEntries, end = min(at + kFillEntries, total);
+    if (at >= total) return;
+    const int b0 = owner_of(indptr, 0, p.batch, at), b1 = owner_of(indptr, b0, p.batch, end - 1) + 1;
+#pragma unroll 4
+    for (int i = at + threadIdx.x; i < end; i += kFillThreads) {
+        const int b = owner_of(indptr, b0, b1, i), place = i - indptr[b];
+        const long long row = (p.request ? p.request[b] : b) * p.table_stride;
+        if (lists) {
+            p.bt_pages[i] = p.page_table[row + place];
+        } else {
+            const int pos = p.ctx_len[b] + place;
+            if (p.position) p.position[i] = pos;
+            if (p.slot) p.slot[i] = (long long)p.page_table[row + pos / p.page_size] * p.page_size + pos % p.page_size;
+        }
+    }
+}
+
+bool misaligned(const void* a, uintptr_t bits) { return (reinterpret_cast<uintptr_t>(a) & bits) != 0; }
+
+kap_status check_state(int32_t batch, int32_t page_size, const void* page_table, int32_t num_requests, int64_t table_stride, const void* pages_held,
+                       const void* free_pages, int32_t free_capacity, const void* free_count, const int32_t* request, const int32_t* device_status) {
+    if (batch < 0 || page_size <= 0 || num_requests < 0 || table_stride < 0 || free_capacity < 0)
+        return fail(KAP_ERR_INVALID_ARG, "batch %d, page_size %d, %d requests of %lld pages, %d free pages", batch, page_size, num_requests, (long long)table_stride, free_capacity);
+    if (num_requests > kMaxRequests || table_stride > INT32_MAX) return fail(KAP_ERR_UNSUPPORTED, "%d requests of %lld pages (at most %d)", num_requests, (long long)table_stride, kMaxRequests);
+    if (batch > num_requests) return fail(KAP_ERR_INVALID_ARG, "%d sequences of %d requests", batch, num_requests);
+    if (batch > 0 && (!page_table || !pages_held || !free_pages || !free_count)) return fail(KAP_ERR_INVALID_ARG, "NULL pointer");
+    for (const void* a : {page_table, pages_held, free_pages, free_count, (const void*)request, (const void*)device_status})
+        if (misaligned(a, 3)) return fail(KAP_ERR_INVALID_ARG, "an index array is not 4-byte aligned");
+    return KAP_OK;
+}
+
+template <typename K>
+kap_status launch(K kernel, dim3 grid, int threads, size_t smem, cudaStream_t stream, const TableParams& p) {
+    if (smem > 32 * 1024) {                                   // with the kernel's own arrays more than the default 48 KiB
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "cudaFuncSetAttribute failed: %s", cudaGetErrorString(e));
+    }
+    kernel<<<grid, threads, smem, stream>>>(p);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "block table kernel launch failed: %s", cudaGetErrorString(e));
+    count_launch();
+    return KAP_OK;
+}
+
+}  // namespace
+}  // namespace kap
+
+using namespace kap;
+
+extern "C" kap_status kap_build_block_tables(
+    const int32_t* request, const int32_t* ctx_len, const int32_t* n_new, int32_t batch, int32_t page_size, int32_t* page_table,
+    int32_t num_requests, int64_t table_stride, int32_t* pages_held, int32_t* free_pages, int32_t free_capacity, int32_t* free_count,
+    int32_t* bt_indptr, int32_t* bt_pages, int64_t bt_capacity, int32_t* new_indptr, int64_t* slot, int32_t* position, int64_t row_capacity,
+    int32_t* device_status, void* cuda_stream)
+{
+    kap_status st = check_state(batch, page_size, page_table, num_requests, table_stride, pages_held, free_pages, free_capacity, free_count, request, device_status);
+    if (st != KAP_OK) return st;
+    if (bt_capacity < 0 || row_capacity < 0) return fail(KAP_ERR_INVALID_ARG, "bt_capacity %lld, row_capacity %lld", (long long)bt_capacity, (long long)row_capacity);
+    if (!bt_indptr || (batch > 0 && (!ctx_len || !bt_pages))) return fail(KAP_ERR_INVALID_ARG, "NULL pointer");
+    if ((slot || position) && !new_indptr) return fail(KAP_ERR_INVALID_ARG, "slot and position need new_indptr");
+    for (const void* a : {(const void*)ctx_len, (const void*)n_new, (const void*)bt_indptr, (const void*)bt_pages, (const void*)new_indptr, (const void*)position})
+        if (misaligned(a, 3)) return fail(KAP_ERR_INVALID_ARG, "an index array is not 4-byte aligned");
+    if (misaligned(slot, 7)) return fail(KAP_ERR_INVALID_ARG, "slot is not 8-byte aligned");
+    TableParams p{};
+    p.request = request; p.ctx_len = ctx_len; p.n_new = n_new; p.page_table = page_table; p.pages_held = pages_held;
+    p.free_pages = free_pages; p.free_count = free_count; p.bt_indptr = bt_indptr; p.bt_pages = bt_pages; p.new_indptr = new_indptr;
+    p.slot = reinterpret_cast<long long*>(slot); p.position = position; p.status = device_status;
+    p.table_stride = table_stride; p.bt_capacity = bt_capacity < INT32_MAX ? bt_capacity : INT32_MAX;
+    p.row_capacity = (slot || position) && row_capacity < INT32_MAX ? row_capacity : INT32_MAX;
+    p.batch = batch; p.page_size = page_size; p.num_requests = num_requests; p.free_capacity = free_capacity;
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    if (batch == 0) {                                         // an empty table
+        cudaError_t e = cudaMemsetAsync(bt_indptr, 0, sizeof(int32_t), stream);
+        if (e == cudaSuccess && new_indptr) e = cudaMemsetAsync(new_indptr, 0, sizeof(int32_t), stream);
+        return e == cudaSuccess ? KAP_OK : fail(KAP_ERR_CUDA, "cudaMemsetAsync failed: %s", cudaGetErrorString(e));
+    }
+    st = launch(kap_tables_kernel<false>, dim3(1), kTableThreads, (size_t)(num_requests + 31) / 32 * 4, stream, p);
+    if (st != KAP_OK) return st;
+    const int64_t list_blocks = (p.bt_capacity + kFillEntries - 1) / kFillEntries;
+    const int64_t row_blocks = slot || position ? (p.row_capacity + kFillEntries - 1) / kFillEntries : 0;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(list_blocks + row_blocks > 0 ? list_blocks + row_blocks : 1));
+    cfg.blockDim = dim3(kFillThreads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = launch_programmatically() ? 1 : 0;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kap_fill_tables_kernel, p, (int)list_blocks);
+    if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "block table kernel launch failed: %s", cudaGetErrorString(e));
+    count_launch();
+    return KAP_OK;
+}
+
+extern "C" kap_status kap_release_pages(
+    const int32_t* request, int32_t n, const int32_t* keep_tokens, int32_t page_size, int32_t* page_table, int32_t num_requests, int64_t table_stride,
+    int32_t* pages_held, int32_t* free_pages, int32_t free_capacity, int32_t* free_count, int32_t* device_status, void* cuda_stream)
+{
+    kap_status st = check_state(n, page_size, page_table, num_requests, table_stride, pages_held, free_pages, free_capacity, free_count, request, device_status);
+    if (st != KAP_OK) return st;
+    if (misaligned(keep_tokens, 3)) return fail(KAP_ERR_INVALID_ARG, "an index array is not 4-byte aligned");
+    if (n == 0) return KAP_OK;
+    TableParams p{};
+    p.request = request; p.ctx_len = keep_tokens; p.page_table = page_table; p.pages_held = pages_held;
+    p.free_pages = free_pages; p.free_count = free_count; p.status = device_status; p.table_stride = table_stride;
+    p.batch = n; p.page_size = page_size; p.num_requests = num_requests; p.free_capacity = free_capacity;
+    return launch(kap_tables_kernel<true>, dim3(1), kTableThreads, (size_t)(num_requests + 31) / 32 * 4, (cudaStream_t)cuda_stream, p);
+}

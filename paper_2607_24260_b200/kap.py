@@ -18,6 +18,7 @@ OK, ERR_INVALID_ARG, ERR_CAPACITY, ERR_UNSUPPORTED, ERR_CUDA, ERR_TIMEOUT, ERR_D
 PLAN_FULL, PLAN_OVER_BUDGET, PLAN_S_HIGH, PLAN_MOVES_WITH_LENGTH = 1, 2, 4, 8
 KV_HND, KV_NHD = 0, 1
 LOGITS_F32, LOGITS_BF16 = 0, 1
+NORM_F32, NORM_BF16 = 0, 1
 
 _i32p, _f32p, _u8p, _vp = C.POINTER(C.c_int32), C.POINTER(C.c_float), C.POINTER(C.c_uint8), C.c_void_p
 
@@ -65,6 +66,16 @@ SIGNATURES = {
                                      _vp, C.c_int32, C.c_int32, _vp, C.c_int64, C.c_int32, _vp, _vp, _vp,
                                      C.c_int64, _vp, _vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                      C.c_int32, C.c_int32, C.c_int32, _vp, _vp]),
+    "kap_build_block_tables": (C.c_int, [_vp, _vp, _vp, C.c_int32, C.c_int32, _vp, C.c_int32, C.c_int64, _vp, _vp, C.c_int32, _vp,
+                                         _vp, _vp, C.c_int64, _vp, _vp, _vp, C.c_int64, _vp, _vp]),
+    "kap_release_pages": (C.c_int, [_vp, C.c_int32, _vp, C.c_int32, _vp, C.c_int32, C.c_int64, _vp, _vp, C.c_int32, _vp, _vp, _vp]),
+    "kap_adjust_logits": (C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp, _vp, _vp,
+                                    _vp, _vp, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, _vp, _vp, _vp]),
+    "kap_append_kv_norm_rope": (C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int32,
+                                          _vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_float,
+                                          _vp, C.c_int32, C.c_int32, _vp, C.c_int64, C.c_int32, _vp, _vp, _vp,
+                                          C.c_int64, _vp, _vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                          C.c_int32, C.c_int32, C.c_int32, _vp, _vp]),
     "kap_shared_prefix_items": (C.c_int, [C.c_int32, _i32p, _i32p, C.c_int32, _i32p, _i32p, C.c_int32,
                                           C.c_int32, C.c_int32, C.c_int32, _i32p]),
     "kap_schedule_shared_prefix": (C.c_int, [_vp, C.c_int32, _i32p, _i32p, C.c_int32, _i32p, _i32p, C.c_int32,
@@ -527,6 +538,60 @@ def append_kv(k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, new_indptr=No
                                _stream_ptr(stream)))
 
 
+def _page_state(page_table, pages_held, free_pages, free_count):
+    """(requests, table_stride, device) of the arrays that build_block_tables and release_pages keep"""
+    _torch_module()
+    dev = page_table.get_device()
+    if page_table.dtype is not _I32 or page_table.dim() != 2 or dev < 0 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise KapError(ERR_INVALID_ARG, f"page_table is {page_table.dtype} {tuple(page_table.shape)} with strides {page_table.stride()} on "
+                       f"{page_table.device}, expected an int32 [requests, pages] tensor on a GPU")
+    requests, wide = page_table.shape
+    if requests > 1 and page_table.stride(0) != wide:
+        raise KapError(ERR_INVALID_ARG, f"page_table has strides {page_table.stride()}: its rows must lie one behind the other")
+    _check_index("pages_held", pages_held, requests, dev)
+    _check_index("free_pages", free_pages, 0, dev)
+    _check_index("free_count", free_count, 1, dev)
+    return requests, wide, dev
+
+
+def build_block_tables(ctx_len, page_table, pages_held, free_pages, free_count, bt_indptr, bt_pages, n_new=None, request=None,
+                       new_indptr=None, slot=None, position=None, page_size=16, device_status=None, stream=None):
+    """kap_build_block_tables on torch CUDA tensors (int32; slot int64): the CSR block table of the step's sequences
+    (request[b], ctx_len[b] tokens cached, n_new[b] new ones; None: row b of page_table, one new token), with the pages it lacks taken
+    from free_pages[:free_count].  page_table [requests, pages], pages_held [requests], free_pages and free_count [1] are kept up to
+    date; new_indptr [batch + 1], slot and position [rows] are optional."""
+    requests, wide, dev = _page_state(page_table, pages_held, free_pages, free_count)
+    batch = ctx_len.shape[0]
+    _check_index("ctx_len", ctx_len, batch, dev)
+    _check_index("bt_indptr", bt_indptr, batch + 1, dev)
+    _check_index("bt_pages", bt_pages, 0, dev)
+    for name, t, least in (("n_new", n_new, batch), ("request", request, batch), ("new_indptr", new_indptr, batch + 1),
+                           ("position", position, 0), ("device_status", device_status, 1)):
+        if t is not None:
+            _check_index(name, t, least, dev)
+    if slot is not None and (slot.dtype is not _torch.int64 or slot.get_device() != dev or not slot.is_contiguous()):
+        raise KapError(ERR_INVALID_ARG, f"slot is {slot.dtype} with strides {slot.stride()} on {slot.device}, expected a contiguous int64 tensor on GPU {dev}")
+    rows = [t.numel() for t in (slot, position) if t is not None]
+    _check(lib().kap_build_block_tables(
+        _dptr(request), ctx_len.data_ptr(), _dptr(n_new), batch, page_size, page_table.data_ptr(), requests, wide, pages_held.data_ptr(),
+        free_pages.data_ptr(), free_pages.numel(), free_count.data_ptr(), bt_indptr.data_ptr(), bt_pages.data_ptr(), bt_pages.numel(),
+        _dptr(new_indptr), _dptr(slot), _dptr(position), min(rows) if rows else 0, _dptr(device_status), _stream_on(dev, stream)))
+
+
+def release_pages(request, page_table, pages_held, free_pages, free_count, keep_tokens=None, page_size=16, device_status=None,
+                  stream=None):
+    """kap_release_pages on torch CUDA tensors: the pages of the requests beyond keep_tokens (None: all) go back to the
+    stack; request None names every row of page_table."""
+    requests, wide, dev = _page_state(page_table, pages_held, free_pages, free_count)
+    n = requests if request is None else request.numel()
+    for name, t, least in (("request", request, n), ("keep_tokens", keep_tokens, n), ("device_status", device_status, 1)):
+        if t is not None:
+            _check_index(name, t, least, dev)
+    _check(lib().kap_release_pages(
+        _dptr(request), n, _dptr(keep_tokens), page_size, page_table.data_ptr(), requests, wide, pages_held.data_ptr(), free_pages.data_ptr(),
+        free_pages.numel(), free_count.data_ptr(), _dptr(device_status), _stream_on(dev, stream)))
+
+
 def _head_rows(name, t, rows, heads, d, dev):
     """the row stride of a bf16 [rows, heads, d] tensor whose heads are contiguous within a row"""
     if t.dtype is not _BF16 or t.shape != (rows, heads, d) or t.get_device() != dev:
@@ -547,6 +612,41 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
     append_kv.  q_out None rotates q in place; q None handles k and v only.  positions None: the
     logical index (+ position_offset[b]); else int32 [rows] or [axes, rows], freq_axis naming the axis
     of each pair (host sequence)."""
+    _append_rope(None, q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_freq, q_out, new_indptr, positions,
+                 freq_axis, position_offset, interleaved, advance, device_status, stream, kv_layout)
+
+
+def append_kv_norm_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_freq, q_weight=None, k_weight=None,
+                        eps=1e-6, unit_offset=False, q_out=None, new_indptr=None, positions=None, freq_axis=None,
+                        position_offset=None, interleaved=False, advance=True, device_status=None, stream=None,
+                        kv_layout=KV_HND):
+    """kap_append_kv_norm_rope: append_kv_rope with the heads of q and k_new normalised before the rotation,
+    x / sqrt(mean(x^2) + eps) * weight (1 + weight with unit_offset).  Weights: fp32 or bf16, both of one
+    type and form, [d] for all heads or [heads, d]; None means 1."""
+    _append_rope((q_weight, k_weight, eps, unit_offset), q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_freq, q_out,
+                 new_indptr, positions, freq_axis, position_offset, interleaved, advance, device_status, stream, kv_layout)
+
+
+def _norm_arguments(norm, Hq, Hkv, d, dev):
+    """(q_weight, k_weight, type, per head, unit offset, eps) of kap_append_kv_norm_rope"""
+    q_weight, k_weight, eps, unit_offset = norm
+    kinds = set()
+    for name, w, heads in (("q_weight", q_weight, Hq), ("k_weight", k_weight, Hkv)):
+        if w is None or (name == "q_weight" and Hq == 0):
+            continue
+        if w.dtype is not _F32 and w.dtype is not _BF16 or w.shape != (d,) and w.shape != (heads, d) or not w.is_contiguous() or w.get_device() != dev:
+            raise KapError(ERR_INVALID_ARG, f"{name} is {w.dtype} {tuple(w.shape)} with strides {w.stride()} on {w.device}, expected a contiguous "
+                           f"float32 or bfloat16 tensor [{d}] or [{heads}, {d}] on GPU {dev}")
+        kinds.add((w.dtype, w.dim()))
+    if len(kinds) > 1:
+        raise KapError(ERR_INVALID_ARG, f"q_weight and k_weight differ in type or form: {kinds}")
+    dtype, dims = kinds.pop() if kinds else (_F32, 1)
+    return (_dptr(q_weight) if Hq else None, _dptr(k_weight), NORM_F32 if dtype is _F32 else NORM_BF16, 1 if dims == 2 else 0,
+            1 if unit_offset else 0, eps)
+
+
+def _append_rope(norm, q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_freq, q_out, new_indptr, positions, freq_axis,
+                 position_offset, interleaved, advance, device_status, stream, kv_layout):
     _torch_module()
     rows, Hq, dev = k_new.shape[0], 0, k_new.get_device()
     if dev < 0:
@@ -588,12 +688,58 @@ def append_kv_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, inv_f
         _check_index("position_offset", position_offset, batch, dev)
     if device_status is not None:
         _check_index("device_status", device_status, 1, dev)
-    _check(lib().kap_append_kv_rope(
-        _dptr(q), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, _dptr(q_out), os_, _dptr(new_indptr), rows,
-        inv_freq.data_ptr(), rot, 1 if interleaved else 0, _dptr(positions), pos_stride, axes, axis,
-        _dptr(position_offset), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
-        ctx_len.data_ptr(), 1 if advance else 0, batch, Hq, Hkv, d, P, kv_layout,
-        _dptr(device_status), _stream_on(dev, stream)))
+    first = (_dptr(q), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, _dptr(q_out), os_, _dptr(new_indptr), rows)
+    rest = (inv_freq.data_ptr(), rot, 1 if interleaved else 0, _dptr(positions), pos_stride, axes, axis,
+            _dptr(position_offset), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
+            ctx_len.data_ptr(), 1 if advance else 0, batch, Hq, Hkv, d, P, kv_layout,
+            _dptr(device_status), _stream_on(dev, stream))
+    if norm is None:
+        _check(lib().kap_append_kv_rope(*first, *rest))
+    else:
+        _check(lib().kap_append_kv_norm_rope(*first, *_norm_arguments(norm, Hq, Hkv, d, dev), *rest))
+
+
+def adjust_logits(logits, out=None, history=None, history_at=None, repetition=None, presence=None, frequency=None, bias_indptr=None,
+                  bias_token=None, bias_value=None, allowed=None, allowed_row=None, device_status=None, stream=None):
+    """kap_adjust_logits on torch CUDA tensors: logits and out fp32 or bf16 [rows, vocab] (any row stride; out None: in place);
+    history int32, history_at int64 [rows, 3] (prompt from, answer from, end); repetition, presence, frequency fp32 [rows]; biases as
+    int32 bias_indptr [rows + 1], int32 bias_token, fp32 bias_value; allowed int32 bit masks [masks, words], allowed_row int32 [rows]."""
+    _torch_module()
+    kind = LOGITS_F32 if logits.dtype is _F32 else LOGITS_BF16 if logits.dtype is _BF16 else None
+    if kind is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1) or not logits.is_cuda:
+        raise KapError(ERR_INVALID_ARG, f"logits are {logits.dtype} {tuple(logits.shape)} with strides {logits.stride()} on {logits.device}")
+    (rows, vocab), dev = logits.shape, logits.get_device()
+    if out is None:
+        out = logits
+    elif out.dtype is not logits.dtype or out.shape != logits.shape or (vocab > 1 and out.stride(1) != 1) or out.get_device() != dev:
+        raise KapError(ERR_INVALID_ARG, f"out is {out.dtype} {tuple(out.shape)} with strides {out.stride()} on {out.device}, logits {logits.dtype} {tuple(logits.shape)} on GPU {dev}")
+
+    def ptr(name, t, dt, n):
+        if t is None:
+            return None
+        if t.dtype is not dt or (t.numel() != n and n >= 0) or not t.is_contiguous() or t.get_device() != dev:
+            raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}, expected a contiguous {dt} "
+                           f"tensor{f' of {n}' if n >= 0 else ''} on GPU {dev}")
+        return t.data_ptr()
+
+    f32, i32 = _F32, _I32
+    masks = words = 0
+    if allowed is not None:
+        if allowed.dim() != 2 or allowed.dtype is not i32 or (allowed.shape[1] > 1 and allowed.stride(1) != 1) or allowed.get_device() != dev:
+            raise KapError(ERR_INVALID_ARG, f"allowed is {allowed.dtype} {tuple(allowed.shape)} with strides {allowed.stride()} on {allowed.device}, expected int32 [masks, words]")
+        masks, words = allowed.shape[0], allowed.stride(0) if allowed.shape[0] > 1 else allowed.shape[1]
+        if allowed.shape[1] * 32 < vocab:
+            raise KapError(ERR_INVALID_ARG, f"allowed has {allowed.shape[1]} words for {vocab} logits")
+    if bias_token is not None and bias_value is not None and bias_token.numel() != bias_value.numel():
+        raise KapError(ERR_INVALID_ARG, f"{bias_token.numel()} bias tokens, {bias_value.numel()} values")
+    _check(lib().kap_adjust_logits(
+        logits.data_ptr(), kind, vocab if rows <= 1 else logits.stride(0), rows, vocab, out.data_ptr(), vocab if rows <= 1 else out.stride(0),
+        ptr("history", history, i32, -1), 0 if history is None else history.numel(), ptr("history_at", history_at, _torch.int64, 3 * rows),
+        ptr("repetition", repetition, f32, rows), ptr("presence", presence, f32, rows), ptr("frequency", frequency, f32, rows),
+        ptr("bias_indptr", bias_indptr, i32, rows + 1), ptr("bias_token", bias_token, i32, -1), ptr("bias_value", bias_value, f32, -1),
+        0 if bias_token is None else bias_token.numel(),
+        _dptr(allowed), masks, words, ptr("allowed_row", allowed_row, i32, rows), ptr("device_status", device_status, i32, 1), _stream_on(dev, stream)))
+    return out
 
 
 def sample_tokens(logits, uniform, token, logprob=None, temperature=None, top_k=None, top_p=None,
