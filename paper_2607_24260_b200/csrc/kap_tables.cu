@@ -108,7 +108,7 @@ kap_tables_kernel(const TableParams p)
                 p.bt_indptr[b] = 0;
                 if (p.new_indptr) p.new_indptr[b] = 0;
             }
-        if (tid == 0 && p.status) atomicOr(p.status, (bad ? 1 << KAP_ERR_DEVICE_INDEX : 0) | (full ? 1 << KAP_ERR_CAPACITY : 0));
+        if (tid == 0 && p.status) atomicOr(p.status, 1 << (bad ? KAP_ERR_DEVICE_INDEX : KAP_ERR_CAPACITY));
         return;
     }
     // ---- the state and the prefix sums
