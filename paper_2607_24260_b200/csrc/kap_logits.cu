@@ -4,12 +4,10 @@
 // Mathematics, for token t of a row with logit x: c = times t occurs in the answer so far, s = t occurs in the prompt or the answer,
 //     x1 = s ? (x > 0 ? x / r : x r) : x,   x2 = x1 - f c - p [c > 0],   x3 = x2 + bias_t,   out = allowed_t ? x3 : -inf,
 // in fp32, rounded to the logits' type once.
-// Layout: a cluster of CTAs per row; CTA i owns the i-th slice of the vocabulary, copies it under the mask, and keeps a 32-bit word for each
-// of its tokens in shared memory (times in the answer; whether in the prompt).  The history is dealt out over the cluster: each
-// CTA clears, then counts its share's tokens in their owners' words through distributed shared memory, so no word is touched that no
-// token names, and the history is read from memory once (its second and third pass hit L1 / L2).  Whoever then takes a token's word out
-// (an atomic exchange) corrects that token's logit; which thread it is does not change the value.  Tokens with a bias are left to the
-// owner of the bias.
+// Layout: a cluster of CTAs per row; CTA i owns the i-th slice of the vocabulary and keeps a 32-bit word for each of its tokens in shared
+// memory (times in the answer; whether in the prompt; whether it has a bias).  The history is dealt out over the cluster and counted in the
+// owners' words through distributed shared memory, read once; the owner then passes over its slice once, logits and words together.
+// Its first logits are loaded before the history is counted.  Tokens with a bias are left to the biases' pass.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -38,15 +36,6 @@ struct LogitParams {
     int32_t rows, vocab, num_masks, slice;                    // slice: tokens of a CTA, a multiple of 32
 };
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void cluster_arrive_release() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait_acquire() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 template <typename T> __device__ __forceinline__ float to_float(T x);
 template <> __device__ __forceinline__ float to_float(float x) { return x; }
 template <> __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -65,171 +54,186 @@ __device__ __forceinline__ float penalised(float x, uint32_t word, const Rules& 
     return x;
 }
 
+// The values of a row that decide what has to be done, the same for its whole cluster.
+struct LogitRow {
+    Rules r;
+    long long h0, h1, h2;
+    int b0, b1;
+    const uint32_t* mask;
+    bool counted;
+};
+__device__ __forceinline__ LogitRow load_row(const LogitParams& p, int row, bool reports) {
+    LogitRow v;
+    const float rep = p.repetition ? p.repetition[row] : 1.f, pres = p.presence ? p.presence[row] : 0.f, freq = p.frequency ? p.frequency[row] : 0.f;
+    v.h0 = v.h1 = v.h2 = 0;
+    if (p.history) { v.h0 = p.history_at[row * 3ll]; v.h1 = p.history_at[row * 3ll + 1]; v.h2 = p.history_at[row * 3ll + 2]; }
+    v.b0 = p.bias_token ? p.bias_indptr[row] : 0;
+    v.b1 = p.bias_token ? p.bias_indptr[row + 1] : 0;
+    const int m = !p.allowed ? -1 : p.allowed_row ? p.allowed_row[row] : row;
+    bool bad = false;
+    v.r.repetition = rep > 0.f ? rep : 1.f;
+    v.r.presence = pres == pres ? pres : 0.f;
+    v.r.frequency = freq == freq ? freq : 0.f;
+    if (v.r.repetition == 1.f && v.r.presence == 0.f && v.r.frequency == 0.f) v.h0 = v.h1 = v.h2 = 0;
+    if (v.h0 < 0 || v.h1 < v.h0 || v.h2 < v.h1 || v.h2 > p.history_len || v.h2 - v.h0 > (long long)kCountMask) { bad = true; v.h0 = v.h1 = v.h2 = 0; }
+    if (v.b0 < 0 || v.b1 < v.b0 || v.b1 > p.bias_len) { bad = true; v.b0 = v.b1 = 0; }
+    v.mask = m >= 0 && m < p.num_masks ? p.allowed + m * p.allowed_stride : nullptr;
+    if (m < -1 || m >= p.num_masks) bad = bad || p.allowed;
+    if (bad && reports && p.status) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
+    v.counted = v.h2 > v.h0;
+    return v;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(kLogitThreads)
+__global__ void __launch_bounds__(kLogitThreads, 3)
 kap_adjust_logits_kernel(const LogitParams p)
 {
-    extern __shared__ uint32_t words[];                       // [slice], used when the row has a history or biases
-    cluster_arrive_release();                                 // (peers' words may be written once they run: waited for below)
-    const int tid = threadIdx.x, n_cta = gridDim.x, rank = blockIdx.x, row = blockIdx.y;     // (the cluster spans x)
+    extern __shared__ uint4 word_space[];                     // [slice] words, used when the row has a history
+    constexpr int kVec = 16 / sizeof(T), kAhead = 2;
+    const int tid = threadIdx.x, rank = blockIdx.x, row = blockIdx.y;
     const T* const in = reinterpret_cast<const T*>(p.logits) + row * p.row_stride;
     T* const out = reinterpret_cast<T*>(p.out) + row * p.out_stride;
     const bool in_place = p.logits == p.out;
-    Rules r{1.f, 0.f, 0.f};
-    if (p.repetition) { const float v = p.repetition[row]; if (v > 0.f) r.repetition = v; }
-    if (p.presence) { const float v = p.presence[row]; if (v == v) r.presence = v; }
-    if (p.frequency) { const float v = p.frequency[row]; if (v == v) r.frequency = v; }
-    long long h0 = 0, h1 = 0, h2 = 0;
-    if (p.history && (r.repetition != 1.f || r.presence != 0.f || r.frequency != 0.f)) {
-        h0 = p.history_at[row * 3ll]; h1 = p.history_at[row * 3ll + 1]; h2 = p.history_at[row * 3ll + 2];
-        if (h0 < 0 || h1 < h0 || h2 < h1 || h2 > p.history_len || h2 - h0 > (long long)kCountMask) {
-            if (tid == 0 && rank == 0 && p.status) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
-            h0 = h1 = h2 = 0;
-        }
-    }
-    const bool counted = h2 > h0;                             // the same for the whole cluster
-    int b0 = 0, b1 = 0;
-    if (p.bias_token) {
-        b0 = p.bias_indptr[row]; b1 = p.bias_indptr[row + 1];
-        if (b0 < 0 || b1 < b0 || b1 > p.bias_len) {
-            if (tid == 0 && rank == 0 && p.status) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
-            b0 = b1 = 0;
-        }
-    }
-    const uint32_t* mask = nullptr;
-    if (p.allowed) {
-        const int m = p.allowed_row ? p.allowed_row[row] : row;
-        if (m >= 0 && m < p.num_masks) mask = p.allowed + m * p.allowed_stride;
-        else if (m != -1 && tid == 0 && rank == 0 && p.status) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
-    }
     const int v0 = min(rank * p.slice, p.vocab), v1 = min(v0 + p.slice, p.vocab);
-    const uint32_t base = smem_addr(words);
-    // this CTA's share of the history
-    const long long share = (h2 - h0 + n_cta - 1) / n_cta, s0 = min(h0 + rank * share, h2), s1 = min(s0 + share, h2);
-    auto word_of = [&](int t) { return peer_addr(base + (uint32_t)(t % p.slice) * 4u, (uint32_t)(t / p.slice)); };
-
-    cluster_wait_acquire();
-    if (counted) {
-        for (long long i = s0 + tid; i < s1; i += kLogitThreads) {
-            const int t = p.history[i];
-            if (t >= 0 && t < p.vocab) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(word_of(t)), "r"(0u) : "memory");
-        }
-        for (int i = b0 + tid; i < b1; i += kLogitThreads) {
-            const int t = p.bias_token[i];
-            if (t >= v0 && t < v1) words[t - v0] = 0u;
-        }
-        cluster_arrive_release();
-    }
-    // ---- the slice, under the mask
-    if (!in_place || mask) {
-        constexpr int kVec = 16 / sizeof(T);
-        const uintptr_t from = reinterpret_cast<uintptr_t>(in + v0), to = reinterpret_cast<uintptr_t>(out + v0);
-        if (((from ^ to) & 15) == 0) {
-            const int head = min((int)((16 - (to & 15)) & 15) / (int)sizeof(T), v1 - v0), n_vec = (v1 - v0 - head) / kVec;
-            auto single = [&](int t) {
-                const bool open = !mask || (__ldg(mask + (t >> 5)) >> (t & 31) & 1u);
-                if (!open) out[t] = from_float<T>(-INFINITY);
-                else if (!in_place) out[t] = in[t];
-            };
-            for (int i = tid; i < head; i += kLogitThreads) single(v0 + i);
-            for (int i = v0 + head + n_vec * kVec + tid; i < v1; i += kLogitThreads) single(i);
-            const uint4* src = reinterpret_cast<const uint4*>(in + v0 + head);
-            uint4* dst = reinterpret_cast<uint4*>(out + v0 + head);
-#pragma unroll 4
-            for (int i = tid; i < n_vec; i += kLogitThreads) {
-                uint32_t open = (1u << kVec) - 1u;
-                if (mask) {
-                    const int t = v0 + head + i * kVec, w = t >> 5, k = t & 31;
-                    open = __ldg(mask + w) >> k;
-                    if (k + kVec > 32) open |= __ldg(mask + w + 1) << (32 - k);
-                    open &= (1u << kVec) - 1u;
-                }
-                if (open == 0u) { dst[i] = minus_inf_vector<T>(); continue; }
-                if (open == (1u << kVec) - 1u) {
-                    if (!in_place) dst[i] = __ldcs(src + i);
-                    continue;
-                }
-                uint4 x = src[i];
-                T* e = reinterpret_cast<T*>(&x);
+    // the slice in 16-byte vectors of logits and results, where both lie alike; head and rest singly
+    const uintptr_t from = reinterpret_cast<uintptr_t>(in + v0), to = reinterpret_cast<uintptr_t>(out + v0);
+    const bool alike = ((from ^ to) & 15) == 0;
+    const int row_head = alike ? (int)((16 - (reinterpret_cast<uintptr_t>(out) & 15)) & 15) / (int)sizeof(T) : 0;      // (slices begin at multiples of 32 tokens)
+    const int head = alike ? min(row_head, v1 - v0) : v1 - v0, n_vec = (v1 - v0 - head) / kVec;
+    const uint4* const src = reinterpret_cast<const uint4*>(in + v0 + head);
+    uint4* const dst = reinterpret_cast<uint4*>(out + v0 + head);
+    // the word of token v0 + i is words[i], placed so that a vector's words are aligned
+    uint32_t* const words = reinterpret_cast<uint32_t*>(word_space) + (kVec - row_head) % kVec;
+    uint4 ahead[kAhead];
+    if (!in_place) {
 #pragma unroll
-                for (int j = 0; j < kVec; ++j)
-                    if (!(open >> j & 1u)) e[j] = from_float<T>(-INFINITY);
-                dst[i] = x;
-            }
-        } else {
-#pragma unroll 4
-            for (int t = v0 + tid; t < v1; t += kLogitThreads) {
-                const bool open = !mask || (__ldg(mask + (t >> 5)) >> (t & 31) & 1u);
-                out[t] = open ? in[t] : from_float<T>(-INFINITY);
-            }
-        }
+        for (int k = 0; k < kAhead; ++k)
+            if (tid + k * kLogitThreads < n_vec) ahead[k] = __ldcs(src + tid + k * kLogitThreads);
     }
+    const LogitRow q = load_row(p, row, tid == 0 && rank == 0);
+    const bool counted = q.counted;
+
+    // ---- the words: every CTA of the row reads the whole history and counts the tokens of its slice
     if (counted) {
-        cluster_wait_acquire();
-        for (long long i = s0 + tid; i < s1; i += kLogitThreads) {
-            const int t = p.history[i];
-            if (t < 0 || t >= p.vocab) continue;
-            if (i < h1) asm volatile("red.shared::cluster.or.b32 [%0], %1;" ::"r"(word_of(t)), "r"(kInPrompt) : "memory");
-            else asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(word_of(t)), "r"(1u) : "memory");
+        for (int i = tid; i < (p.slice + kVec) / 4; i += kLogitThreads) word_space[i] = make_uint4(0u, 0u, 0u, 0u);
+        __syncthreads();
+        const int n_prompt = (int)(q.h1 - q.h0), n_all = (int)(q.h2 - q.h0);              // (below 2^30)
+        const int32_t* const h = p.history + q.h0;
+        auto count = [&](int i, int t) {
+            const uint32_t at = (uint32_t)(t - v0);
+            if (at >= (uint32_t)(v1 - v0)) return;
+            if (i < n_prompt) atomicOr(&words[at], kInPrompt);
+            else atomicAdd(&words[at], 1u);
+        };
+        // in fours, from the first 16-byte boundary on
+        const int before = min((int)((16 - (reinterpret_cast<uintptr_t>(h) & 15)) & 15) / 4, n_all), n4 = (n_all - before) / 4;
+        const int4* const fours = reinterpret_cast<const int4*>(h + before);
+        if (tid < before) count(tid, h[tid]);
+        if (tid < n_all - before - 4 * n4) count(before + 4 * n4 + tid, h[before + 4 * n4 + tid]);
+#pragma unroll 4
+        for (int k = tid; k < n4; k += kLogitThreads) {
+            const int4 t = __ldg(fours + k);
+            const int i = before + 4 * k;
+            count(i, t.x); count(i + 1, t.y); count(i + 2, t.z); count(i + 3, t.w);
         }
-        for (int i = b0 + tid; i < b1; i += kLogitThreads) {
+        for (int i = q.b0 + tid; i < q.b1; i += kLogitThreads) {
             const int t = p.bias_token[i];
             if (t >= v0 && t < v1) atomicOr(&words[t - v0], kHasBias);
         }
-        cluster_arrive_release();
-        cluster_wait_acquire();
-    } else {
         __syncthreads();
     }
-    auto closed = [&](int t) { return mask && !(__ldg(mask + (t >> 5)) >> (t & 31) & 1u); };
-    // ---- biases, ascending by token, by the owner of the slice; of equal tokens the first entry adds up all
-    for (int i = b0 + tid; i < b1; i += kLogitThreads) {
-        const int t = p.bias_token[i];
-        const int prior = i > b0 ? p.bias_token[i - 1] : INT32_MIN;
-        if (prior > t && rank == 0 && p.status) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
-        if (prior == t || t < v0 || t >= v1 || closed(t)) continue;
-        float add = p.bias_value[i];
-        for (int j = i + 1; j < b1 && p.bias_token[j] == t; ++j) add += p.bias_value[j];
-        float x = to_float(in[t]);
-        if (counted) x = penalised(x, words[t - v0], r);
-        out[t] = from_float<T>(x + add);
-    }
-    if (counted) {
-        for (long long i = s0 + tid; i < s1; i += kLogitThreads) {
-            const int t = p.history[i];
-            if (t < 0 || t >= p.vocab) continue;
-            const uint32_t at = word_of(t);
-            uint32_t word;
-            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(word) : "r"(at) : "memory");
-            if (word == 0u || (word & kHasBias)) continue;
-            asm volatile("atom.shared::cluster.exch.b32 %0, [%1], %2;" : "=r"(word) : "r"(at), "r"(0u) : "memory");
-            if (word == 0u || closed(t)) continue;
-            out[t] = from_float<T>(penalised(to_float(in[t]), word, r));
+    // ---- the slice: logits, words and mask
+    auto closed = [&](int t) { return q.mask && !(__ldg(q.mask + (t >> 5)) >> (t & 31) & 1u); };
+    if (!in_place || q.mask || counted) {
+        auto single = [&](int t) {
+            const uint32_t w = counted ? words[t - v0] : 0u;
+            if (closed(t)) out[t] = from_float<T>(-INFINITY);
+            else if (w & kHasBias) return;
+            else if (w) out[t] = from_float<T>(penalised(to_float(in[t]), w, q.r));
+            else if (!in_place) out[t] = in[t];
+        };
+#pragma unroll 4
+        for (int i = tid; i < head; i += kLogitThreads) single(v0 + i);
+        for (int i = v0 + head + n_vec * kVec + tid; i < v1; i += kLogitThreads) single(i);
+        auto vector = [&](int i, uint4 x, bool loaded) {
+            const int t = v0 + head + i * kVec;
+            uint32_t open = (1u << kVec) - 1u;
+            if (q.mask) {
+                const int w = t >> 5, k = t & 31;
+                open = __ldg(q.mask + w) >> k;
+                if (k + kVec > 32) open |= __ldg(q.mask + w + 1) << (32 - k);
+                open &= (1u << kVec) - 1u;
+            }
+            if (open == 0u) { dst[i] = minus_inf_vector<T>(); return; }
+            uint32_t w[kVec], any = 0u;
+            if (counted) {
+#pragma unroll
+                for (int j = 0; j < kVec; j += 4) {
+                    const uint4 z = *reinterpret_cast<const uint4*>(words + (t - v0) + j);
+                    w[j] = z.x; w[j + 1] = z.y; w[j + 2] = z.z; w[j + 3] = z.w;
+                    any |= z.x | z.y | z.z | z.w;
+                }
+            }
+            if (any == 0u && open == (1u << kVec) - 1u) {
+                if (!in_place) __stcs(dst + i, x);
+                return;
+            }
+            if (!loaded) x = src[i];
+            T* e = reinterpret_cast<T*>(&x);
+            bool leave = false;
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) {
+                if (!(open >> j & 1u)) e[j] = from_float<T>(-INFINITY);
+                else if (any && (w[j] & kHasBias)) leave = true;
+                else if (any && w[j]) e[j] = from_float<T>(penalised(to_float(e[j]), w[j], q.r));
+            }
+            if (!leave) { dst[i] = x; return; }
+#pragma unroll
+            for (int j = 0; j < kVec; ++j)
+                if (!(open >> j & 1u) || !(w[j] & kHasBias)) out[t + j] = e[j];
+        };
+        if (!in_place) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (tid + k * kLogitThreads < n_vec) vector(tid + k * kLogitThreads, ahead[k], true);
+            int i = tid + kAhead * kLogitThreads;
+            for (; i + (kAhead - 1) * kLogitThreads < n_vec; i += kAhead * kLogitThreads) {
+                uint4 x[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) x[k] = __ldcs(src + i + k * kLogitThreads);
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) vector(i + k * kLogitThreads, x[k], true);
+            }
+            for (; i < n_vec; i += kLogitThreads) vector(i, __ldcs(src + i), true);
+        } else {
+            for (int i = tid; i < n_vec; i += kLogitThreads) vector(i, make_uint4(0u, 0u, 0u, 0u), false);
         }
-        cluster_arrive_release();                             // nobody leaves while a peer may still read its words
-        cluster_wait_acquire();
+    }
+    if (q.b1 > q.b0) {
+        // biases, ascending by token, by the owner of the slice; of equal tokens the first entry adds up all
+        if (!counted) __syncthreads();                        // their logits have been copied above
+        for (int i = q.b0 + tid; i < q.b1; i += kLogitThreads) {
+            const int t = p.bias_token[i];
+            const int prior = i > q.b0 ? p.bias_token[i - 1] : INT32_MIN;
+            if (prior > t && rank == 0 && p.status) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
+            if (prior == t || t < v0 || t >= v1 || closed(t)) continue;
+            float add = p.bias_value[i];
+            for (int j = i + 1; j < q.b1 && p.bias_token[j] == t; ++j) add += p.bias_value[j];
+            float x = to_float(in[t]);
+            if (counted) x = penalised(x, words[t - v0], q.r);
+            out[t] = from_float<T>(x + add);
+        }
     }
 }
 
 template <typename T>
-kap_status launch_logits(const LogitParams& p, int cluster, size_t smem, cudaStream_t stream) {
+kap_status launch_logits(const LogitParams& p, int slices, size_t smem, cudaStream_t stream) {
     auto* kernel = kap_adjust_logits_kernel<T>;
     cudaError_t e = cudaSuccess;
     if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "cudaFuncSetAttribute failed: %s", cudaGetErrorString(e));
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)cluster, (unsigned)p.rows);
-    cfg.blockDim = dim3(kLogitThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, p);
+    kernel<<<dim3((unsigned)slices, (unsigned)p.rows), kLogitThreads, smem, stream>>>(p);
+    e = cudaGetLastError();
     if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "kap_adjust_logits launch failed: %s", cudaGetErrorString(e));
     count_launch();
     return KAP_OK;
@@ -279,10 +283,15 @@ extern "C" kap_status kap_adjust_logits(
     p.rows = rows; p.vocab = vocab; p.num_masks = num_masks;
     const bool needs_words = history && (repetition || presence || frequency);
     if (!needs_words) p.history = nullptr;
-    int cluster = 8;
-    while (cluster < 16 && (int64_t)(vocab + cluster - 1) / cluster * 4 > 200 * 1024) cluster *= 2;
-    p.slice = ((vocab + cluster - 1) / cluster + 31) / 32 * 32;
-    const size_t smem = needs_words ? (size_t)p.slice * 4 : 0;
-    return logits_type == KAP_LOGITS_F32 ? launch_logits<float>(p, cluster, smem, (cudaStream_t)cuda_stream)
-                                         : launch_logits<__nv_bfloat16>(p, cluster, smem, (cudaStream_t)cuda_stream);
+    // Slices of at most 16384 tokens (64 KiB of words: three CTAs on an SM), and of fewer where there are rows too few to fill the device: every CTA of a
+    // row reads its whole history, so no more than that (512 rows of 128256, histories of 2000 to 4000: 8 slices 135 us, 16 167; one row
+    // with 20000: 8 slices 14 us, 64 7.6).
+    constexpr int kOneWave = 148 * 3, kMostSlices = 64;
+    const int least = (vocab + 16383) / 16384;
+    int slices = least < kMostSlices ? (kOneWave / rows < least ? least : kOneWave / rows > kMostSlices ? kMostSlices : kOneWave / rows) : least;
+    p.slice = ((vocab + slices - 1) / slices + 31) / 32 * 32;
+    slices = (vocab + p.slice - 1) / p.slice;
+    const size_t smem = needs_words ? ((size_t)p.slice + 8) * 4 : 0;
+    return logits_type == KAP_LOGITS_F32 ? launch_logits<float>(p, slices, smem, (cudaStream_t)cuda_stream)
+                                         : launch_logits<__nv_bfloat16>(p, slices, smem, (cudaStream_t)cuda_stream);
 }
