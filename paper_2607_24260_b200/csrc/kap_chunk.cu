@@ -85,7 +85,7 @@ extern "C" kap_status kap_chunk_attn(
     p.cuts = reinterpret_cast<ChunkCut*>(ws->d_part_o + 2ll * n_cta * kChunkUnitRows * kHeadDim);
     p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ws->d_status;
     p.num_pool_pages = num_pool_pages; p.batch = batch; p.total_rows = total_rows;
-    p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G; p.window = window; p.n_sink = window ? n_sink : 0;
+    p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G; p.log2_g = __builtin_ctz((unsigned)G); p.window = window; p.n_sink = window ? n_sink : 0;
     p.scale_log2 = sm_scale * 1.4426950408889634f;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -6,7 +6,8 @@
 
 namespace kap {
 
-constexpr int kChunkThreads = 384;
+constexpr int kChunkSoftmaxWarps = 8;                                 // 4 a stream
+constexpr int kChunkThreads = 32 * (kChunkSoftmaxWarps + 4);
 constexpr int kChunkTileRows = 128;                                    // query rows of one tile (TMEM lanes)
 constexpr int kChunkUnitRows = 2 * kChunkTileRows;
 constexpr int kChunkStepPages = 5;
@@ -61,7 +62,7 @@ struct ChunkParams {
     float* lse;
     int32_t* status;
     long long num_pool_pages;
-    int32_t batch, total_rows, hq, hkv, G, window, n_sink;
+    int32_t batch, total_rows, hq, hkv, G, log2_g, window, n_sink;
     float scale_log2;
 };
 
@@ -82,15 +83,14 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams& p, int b, bool&
     return s;
 }
 __device__ __forceinline__ int chunk_tiles(const ChunkParams& p, int n) {
-    const int R = kChunkUnitRows / p.G;
-    return (n + R - 1) / R;
+    return (n + (kChunkUnitRows >> p.log2_g) - 1) >> (8 - p.log2_g);
 }
 // cost of the first k tiles of a sequence, for one KV head
 __device__ __forceinline__ long long chunk_cost(const ChunkParams& p, const ChunkSeq& s, int k) {
     if (k <= 0) return 0;
-    const int R = kChunkUnitRows / p.G, t = chunk_tiles(p, s.n), whole = min(k, t - 1);
+    const int R = kChunkUnitRows >> p.log2_g, t = chunk_tiles(p, s.n), whole = min(k, t - 1);
     const long long lo = max(0, s.length - s.n), knee = (long long)p.window + p.n_sink;   // where the window begins to leave tokens out
-    const long long m = p.window ? min((long long)whole, max(0ll, (knee - lo + R - 1) / R)) : whole;
+    const long long m = p.window ? min((long long)whole, max(0ll, (knee - lo + R - 1) >> (8 - p.log2_g))) : whole;
     long long c = 2 * (whole * (long long)kChunkUnitCost + m * lo + R * (m * (m + 1) / 2) + (whole - m) * (knee + R));
     if (k == t) {
         const int rest = s.n - (t - 1) * R;
@@ -110,7 +110,7 @@ __device__ __forceinline__ ChunkPages chunk_pages(const ChunkParams& p, int lo, 
     return g;
 }
 __device__ __forceinline__ int chunk_steps(const ChunkParams& p, const ChunkSeq& s, int tile) {
-    const int R = kChunkUnitRows / p.G, lo = s.length - s.n + tile * R, hi = min(lo + R, s.length) - 1;
+    const int R = (kChunkUnitRows >> p.log2_g), lo = s.length - s.n + tile * R, hi = min(lo + R, s.length) - 1;
     return (chunk_pages(p, lo, hi).n + kChunkStepPages - 1) / kChunkStepPages;
 }
 
@@ -145,7 +145,7 @@ __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c
     const long long parts = max(1ll, min((long long)gridDim.x, total / kChunkLeastCost));
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const long long i = min((long long)blockIdx.x + e, parts), x = total / parts * i + total % parts * i / parts;
+        const long long i = min((long long)blockIdx.x + e, parts), x = i == parts ? total : (long long)((double)total * ((double)i / (double)parts));
         if (x < before || x >= before + mine) continue;
         long long rest = x - before;
         for (int k = 0; k < per; ++k) {
@@ -168,9 +168,10 @@ __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c
         if (b < p.batch) {
             bool bad;
             const ChunkSeq s = chunk_seq(p, b, bad);
-            const int t = chunk_tiles(p, s.n), R = kChunkUnitRows / p.G;
+            const int t = chunk_tiles(p, s.n), R = (kChunkUnitRows >> p.log2_g);
             const long long one = chunk_cost(p, s, t);
-            const int head = min((int)(c.cut_rest[warp] / one), p.hkv - 1);
+            int head = min((int)((double)c.cut_rest[warp] / (double)one), p.hkv - 1);
+            if (head * one > c.cut_rest[warp]) --head;                 // (a quotient that was rounded up)
             const long long y = c.cut_rest[warp] - head * one;
             int k = 0, hi = t;                                         // cost(k) <= y < cost(hi)
             while (hi - k > 1) {
@@ -181,8 +182,8 @@ __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c
                 k = at;
             }
             const int steps = chunk_steps(p, s, k), rows = min(R, s.n - k * R) * p.G;
-            const long long z = (y - chunk_cost(p, s, k)) / (rows > kChunkTileRows ? 2 : 1) - kChunkUnitCost;
-            step = (int)min((long long)steps, max(0ll, (z + kChunkStepTokens / 2) / kChunkStepTokens));
+            const int z = (int)((y - chunk_cost(p, s, k)) >> (rows > kChunkTileRows ? 1 : 0)) - kChunkUnitCost;     // (below 2^31: a context's tokens and a tile's)
+            step = min(steps, max(0, (z + kChunkStepTokens / 2) / kChunkStepTokens));
             unit = head * t + k;
             inside = step > 0 && step < steps;
             tok0 = s.row0 + k * R;
@@ -206,7 +207,7 @@ __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c
 // the next segments of this CTA; called by one warp
 __device__ __forceinline__ void chunk_segments(const ChunkParams& p, ChunkShared& sh) {
     ChunkControl& c = sh.c;
-    const int lane = threadIdx.x & 31, R = kChunkUnitRows / p.G;
+    const int lane = threadIdx.x & 31, R = (kChunkUnitRows >> p.log2_g);
     int seq = c.seq, unit = c.unit, step = c.step, first_done = c.first_done, n = 0;
     const int end_seq = c.end_seq, end_unit = c.end_unit, end_step = c.end_step;
     const int last_seq = end_unit > 0 || end_step > 0 ? end_seq : end_seq - 1;
@@ -330,7 +331,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
             mbar_init(smem_u32(&c->q_full[i]), 1);
             mbar_init(smem_u32(&c->q_free[i]), 1);
             mbar_init(smem_u32(&c->s_ready[i]), 1);
-            mbar_init(smem_u32(&c->s_free[i]), 4);                     // the stream's four softmax warps
+            mbar_init(smem_u32(&c->s_free[i]), 4);                     // the stream's softmax warps
             mbar_init(smem_u32(&c->p_ready[i]), 4);
             mbar_init(smem_u32(&c->pv_done[i]), 1);
         }
@@ -357,24 +358,59 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     auto wait = [&](unsigned long long& bar, uint32_t parity) { return mbar_wait(smem_u32(&bar), parity, deadline, late); };
 
     // state of the roles, kept over the rounds
-    int slot = 0, loads = 0, q_use[2] = {0, 0}, q_slot = 0, step0 = 0, count0 = 0, count1 = 0, count = 0;
-    uint32_t parity = 1, q_parity = 0;
+    int k_loads = 0, v_loads = 0, pending = 0, q_use[2] = {0, 0}, q_slot = 0, step0 = 0, count0 = 0, count1 = 0, count = 0;
+    uint32_t q_parity = 0;
     bool ok = true;
     uint64_t keep;
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(keep));
 
     for (;;) {
-    if (warp == 11) chunk_segments(p, sh);
+    if (warp == kChunkSoftmaxWarps + 2) chunk_segments(p, sh);
     __syncthreads();
     const int n_segments = c->n_segments, more_rounds = c->more;
-    if (warp == 8) {
+    if (warp == kChunkSoftmaxWarps) {
         // ---- TMA: up to 20 copies a step (five pages, K and V, two halves of 64 columns), issued by one elected lane with
-        // warp-uniform coordinates
+        // warp-uniform coordinates.  V is needed later than K, by as many steps as S runs ahead of P V: its copies follow that much later,
+        // so that what lies in the ring is what comes next.
+        int32_t old_page[kChunkStepPages], new_page[kChunkStepPages];  // of the V tiles that are still to come, at most two steps
+        int old_n = 0, new_n = 0, old_head = 0, new_head = 0;
+        auto load = [&](int v, int at, const int32_t (&page)[kChunkStepPages], int n, int kv_head) {
+            const int slot = 2 * (at % (kChunkSlots / 2)) + v;
+            ok = wait(c->free[slot], ((uint32_t)(at / (kChunkSlots / 2)) & 1u) ^ 1u);      // (the first round does not wait)
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return;
+            if (elect_one()) {
+                const uint32_t bar = smem_u32(&c->full[slot]), dst = smem_u32(slots) + slot * kChunkSlotBytes;
+                mbar_expect_tx(bar, (uint32_t)n * kTileBytes);
+#pragma unroll
+                for (int i = 0; i < kChunkStepPages; ++i) {
+                    if (i >= n) break;
+                    if (kNhd) {
+                        const int z = (page[i] * 2 + v) * kPageSize;
+                        tma_load_3d(dst + i * kHalfTileBytes, &kv_map, 0, kv_head, z, bar, keep);
+                        tma_load_3d(dst + kChunkPlaneBytes + i * kHalfTileBytes, &kv_map, 64, kv_head, z, bar, keep);
+                    } else {
+                        const int y = ((page[i] * 2 + v) * p.hkv + kv_head) * kPageSize;
+                        tma_load_2d(dst + i * kHalfTileBytes, &kv_map, 0, y, bar, keep);
+                        tma_load_2d(dst + kChunkPlaneBytes + i * kHalfTileBytes, &kv_map, 64, y, bar, keep);
+                    }
+                }
+            }
+            __syncwarp();
+        };
+        auto load_v = [&]() {
+            load(1, v_loads, old_page, old_n, old_head);
+            if (ok) ++v_loads;
+#pragma unroll
+            for (int i = 0; i < kChunkStepPages; ++i) old_page[i] = new_page[i];
+            old_n = new_n; old_head = new_head;
+            --pending;
+        };
         for (int k = 0; k < n_segments && ok; ++k) {
             const ChunkSegment s = sh.segments[k];
             deadline = global_ns() + kWaitBudgetNs;
             const int rows = s.rows_head & 0xffff, kv_head = s.rows_head >> 16;
-            const ChunkPages g = chunk_pages(p, s.lo, s.lo + rows / p.G - 1);
+            const ChunkPages g = chunk_pages(p, s.lo, s.lo + (rows >> p.log2_g) - 1);
             const int n_steps = s.step_end - s.step_begin, page0 = s.step_begin * kChunkStepPages;
             const int n_pages = min(g.n - page0, n_steps * kChunkStepPages);
             const bool pair = rows > kChunkTileRows;
@@ -388,15 +424,22 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
             int32_t ids = 0, next_ids = lane < 30 ? fetch(lane) : 0;
             for (int t = 0; t < (pair ? 2 : 1) && ok; ++t) {
                 const int to = pair ? t : q_slot;
-                ok = q_use[to] == 0 || wait(c->q_free[to], (uint32_t)(q_use[to] - 1) & 1u);
+                if (q_use[to] > 0) {
+                    // The products that free the tile may need the V tiles that are still to come (a segment's last ones come before the next
+                    // one's first S): they are not held back over a wait.
+                    const uint32_t phase = (uint32_t)(q_use[to] - 1) & 1u;
+                    if (!__all_sync(0xffffffffu, mbar_try_wait(smem_u32(&c->q_free[to]), phase)))
+                        while (pending > 0 && ok) load_v();
+                    ok = ok && wait(c->q_free[to], phase);
+                }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (elect_one()) {
                     const uint32_t bar = smem_u32(&c->q_full[to]), dst = smem_u32(q_tiles) + to * kChunkQBytes;
-                    const int tok = s.tok0 + t * (kChunkTileRows / p.G);
+                    const int tok = s.tok0 + t * (kChunkTileRows >> p.log2_g), head = kv_head << p.log2_g;
                     mbar_expect_tx(bar, kChunkQBytes);
-                    tma_load_3d(dst, &q_map, 0, kv_head * p.G, tok, bar, keep);
-                    tma_load_3d(dst + kChunkQHalfBytes, &q_map, 64, kv_head * p.G, tok, bar, keep);
+                    tma_load_3d(dst, &q_map, 0, head, tok, bar, keep);
+                    tma_load_3d(dst + kChunkQHalfBytes, &q_map, 64, head, tok, bar, keep);
                 }
                 __syncwarp();
                 ++q_use[to];
@@ -414,35 +457,25 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < kChunkStepPages; ++i) page[i] = __shfl_sync(0xffffffffu, ids, in_batch * kChunkStepPages + i);
                 if (++in_batch == kBatch) in_batch = 0;
-#pragma unroll 1
-                for (int v = 0; v < 2 && ok; ++v) {
-                    ok = wait(c->free[slot], parity);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    if (elect_one()) {
-                        const uint32_t bar = smem_u32(&c->full[slot]), dst = smem_u32(slots) + slot * kChunkSlotBytes;
-                        mbar_expect_tx(bar, (uint32_t)n * kTileBytes);
+                load(0, k_loads, page, n, kv_head);
+                if (!ok) break;
+                ++k_loads;
+                if (pending == 0) {
 #pragma unroll
-                        for (int i = 0; i < kChunkStepPages; ++i) {
-                            if (i >= n) break;
-                            if (kNhd) {
-                                const int z = (page[i] * 2 + v) * kPageSize;
-                                tma_load_3d(dst + i * kHalfTileBytes, &kv_map, 0, kv_head, z, bar, keep);
-                                tma_load_3d(dst + kChunkPlaneBytes + i * kHalfTileBytes, &kv_map, 64, kv_head, z, bar, keep);
-                            } else {
-                                const int y = ((page[i] * 2 + v) * p.hkv + kv_head) * kPageSize;
-                                tma_load_2d(dst + i * kHalfTileBytes, &kv_map, 0, y, bar, keep);
-                                tma_load_2d(dst + kChunkPlaneBytes + i * kHalfTileBytes, &kv_map, 64, y, bar, keep);
-                            }
-                        }
-                    }
-                    __syncwarp();
-                    ++loads;
-                    if (++slot == kChunkSlots) { slot = 0; parity ^= 1u; }
+                    for (int i = 0; i < kChunkStepPages; ++i) old_page[i] = page[i];
+                    old_n = n; old_head = kv_head;
+                } else {
+                    if (pending == 2) load_v();
+#pragma unroll
+                    for (int i = 0; i < kChunkStepPages; ++i) new_page[i] = page[i];
+                    new_n = n; new_head = kv_head;
                 }
+                ++pending;
+                if (pair && pending == 2 && ok) load_v();
             }
         }
-    } else if (warp == 9) {
+        while (pending > 0 && ok) load_v();
+    } else if (warp == kChunkSoftmaxWarps + 1) {
         // ---- tensor core: one elected lane runs through a whole segment, waits included, with warp-uniform operands
         constexpr uint32_t idesc_o = umma_idesc(kChunkTileRows, kHeadDim, true);
         const uint64_t q_desc = umma_smem_desc(smem_u32(q_tiles), 16, 1024), k_desc = umma_smem_desc(smem_u32(slots), 16, 1024);
@@ -452,7 +485,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
             const ChunkSegment seg = sh.segments[k];
             deadline = global_ns() + kWaitBudgetNs;
             const int rows = __shfl_sync(0xffffffffu, seg.rows_head & 0xffff, 0);
-            const ChunkPages g = chunk_pages(p, seg.lo, seg.lo + rows / p.G - 1);
+            const ChunkPages g = chunk_pages(p, seg.lo, seg.lo + (rows >> p.log2_g) - 1);
             const int n_steps = __shfl_sync(0xffffffffu, seg.step_end - seg.step_begin, 0);
             const int n_pages = __shfl_sync(0xffffffffu, g.n - seg.step_begin * kChunkStepPages, 0);
             const int pair = rows > kChunkTileRows ? 1 : 0;
@@ -494,22 +527,22 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                     wait(c->q_full[1], q_parity >> 1);
                     for (int j = 0; j < n_steps; ++j) {
                         issue_s(0, base0 + j, j, false);
+                        if (j == n_steps - 1) umma_commit(smem_u32(&c->q_free[0]));
                         if (j > 0) issue_pv(0, base0 + j - 1, j - 1, j == 1, false);
                         issue_s(1, base1 + j, j, true);
+                        if (j == n_steps - 1) umma_commit(smem_u32(&c->q_free[1]));
                         if (j > 0) issue_pv(1, base1 + j - 1, j - 1, j == 1, true);
                     }
                     issue_pv(0, base0 + n_steps - 1, n_steps - 1, n_steps == 1, false);
                     issue_pv(1, base1 + n_steps - 1, n_steps - 1, n_steps == 1, true);
-                    umma_commit(smem_u32(&c->q_free[0]));              // (all products of the segment are among those waited for)
-                    umma_commit(smem_u32(&c->q_free[1]));
                 } else {                                               // step j: work j / 2 of stream j mod 2
                     for (int j = 0; j < n_steps; ++j) {
                         issue_s(j & 1, (j & 1 ? base1 : base0) + (j >> 1), j, true);
+                        if (j == n_steps - 1) umma_commit(smem_u32(&c->q_free[q_at]));
                         if (j > 1) issue_pv(j & 1, (j & 1 ? base1 : base0) + (j >> 1) - 1, j - 2, j < 4, true);
                     }
                     for (int j = max(0, n_steps - 2); j < n_steps; ++j)
                         issue_pv(j & 1, (j & 1 ? base1 : base0) + (j >> 1), j, j < 2, true);
-                    umma_commit(smem_u32(&c->q_free[q_at]));
                 }
             }
             __syncwarp();
@@ -519,7 +552,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
             q_parity ^= pair ? 3u : 1u << q_slot;
             if (!pair) q_slot ^= 1;
         }
-    } else if (warp < 8) {
+    } else if (warp < kChunkSoftmaxWarps) {
         // ---- softmax: stream = warp group, one query row per thread
         const int stream = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + stream * 256, t_p = t_s + kChunkTmemP, t_o = t_s + kChunkTmemO;
@@ -534,12 +567,12 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
             const bool valid = R < rows, any_valid = tile * kChunkTileRows + (warp & 3) * 32 < rows;
             // The row sees tokens [0, sink_end) and [from, to), counted along the segment's pages
             int sink_end = 0, from = 0, to = 0;
-            const int hi = seg.lo + rows / p.G - 1;
+            const int hi = seg.lo + (rows >> p.log2_g) - 1;
             const ChunkPages g = chunk_pages(p, seg.lo, hi);
             // the last step holds the page in which the sequence ends
             const bool tail = g.n - seg.step_begin * kChunkStepPages <= n_steps * kChunkStepPages && seg.length % kPageSize != 0 && hi / kPageSize == (seg.length - 1) / kPageSize;
             if (valid) {
-                const int pos = seg.lo + R / p.G, shift = (g.first - g.head) * kPageSize;
+                const int pos = seg.lo + (R >> p.log2_g), shift = (g.first - g.head) * kPageSize;
                 to = pos + 1 - shift;
                 if (p.window) {
                     from = (int)max((long long)pos - p.window + 1, 0ll) - shift;
@@ -652,7 +685,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                 const uint32_t t_first = pair ? t_o : t_lane + kChunkTmemO, t_second = t_lane + 256 + kChunkTmemO;
                 const float f0 = pair || stream == 0 ? factor0 : factor1, f1 = stream == 0 ? factor1 : factor0;
                 const float inv = seg.slot >= 0 ? 1.f : l > 0.f ? 1.f / l : 0.f;
-                const int tok = seg.tok0 + R / p.G, h = kv_head * p.G + R % p.G;
+                const int tok = seg.tok0 + (R >> p.log2_g), h = (kv_head << p.log2_g) + (R & (p.G - 1));
                 const long long cell = (long long)tok * p.hq + h, state = (long long)seg.slot * kChunkUnitRows + R;
 #pragma unroll 1
                 for (int i = col0; i < col1; i += 32) {
@@ -703,14 +736,18 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     __syncthreads();                                                   // everybody has read this round's segments
     }
 
-    if (warp == 8 && *late) {                                          // copies in flight must land before the CTA ends
+    if (warp == kChunkSoftmaxWarps && *late) {                         // copies in flight must land before the CTA ends
         const uint64_t last = global_ns() + kWaitBudgetNs;
         int32_t more = 0;
-        for (int s = max(0, loads - kChunkSlots); s < loads; ++s) mbar_wait(smem_u32(&c->full[s % kChunkSlots]), (uint32_t)(s / kChunkSlots) & 1u, last, &more);
+        for (int v = 0; v < 2; ++v) {
+            const int n = v ? v_loads : k_loads;
+            for (int i = max(0, n - kChunkSlots / 2); i < n; ++i)
+                mbar_wait(smem_u32(&c->full[2 * (i % (kChunkSlots / 2)) + v]), (uint32_t)(i / (kChunkSlots / 2)) & 1u, last, &more);
+        }
         for (int s = 0; s < 2; ++s)
             if (q_use[s]) mbar_wait(smem_u32(&c->q_full[s]), (uint32_t)(q_use[s] - 1) & 1u, last, &more);
     }
-    if (warp == 9) {
+    if (warp == kChunkSoftmaxWarps + 1) {
         if (elect_one()) umma_commit(smem_u32(&c->drained));           // everything issued, whatever happened
         int32_t more = 0;
         mbar_wait(smem_u32(&c->drained), 0, global_ns() + kWaitBudgetNs, &more);

@@ -15,7 +15,7 @@ bool launch_programmatically();
 
 namespace {
 
-constexpr int kTableThreads = 1024, kTableWarps = kTableThreads / 32;
+constexpr int kTableThreads = 1024, kFewThreads = 128;        // of the first kernel, for batches of up to 128 sequences the second number
 constexpr int kFillThreads = 256, kFillEntries = 2048;
 constexpr int32_t kMaxRequests = 1 << 20;                     // a bit each in the first kernel's shared memory
 
@@ -52,59 +52,60 @@ __device__ __forceinline__ Entry load_entry(const TableParams& p, int b, uint32_
     return e;
 }
 
-// inclusive sums over the block; `carry` comes before, and is moved on
+// Inclusive sums over the block, and the block's totals.  (All threads; the shared arrays may be used again after another barrier.)
 struct Sums { long long pages, moved, rows; };
-__device__ __forceinline__ Sums block_scan(Sums v, Sums& carry, Sums* warp_sums) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) { return {a.pages + b.pages, a.moved + b.moved, a.rows + b.rows}; }
+__device__ __forceinline__ Sums warp_scan(Sums v) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-        const long long a = __shfl_up_sync(0xffffffffu, v.pages, d), b = __shfl_up_sync(0xffffffffu, v.moved, d), c = __shfl_up_sync(0xffffffffu, v.rows, d);
-        if (lane >= d) { v.pages += a; v.moved += b; v.rows += c; }
+        const Sums o{__shfl_up_sync(0xffffffffu, v.pages, d), __shfl_up_sync(0xffffffffu, v.moved, d), __shfl_up_sync(0xffffffffu, v.rows, d)};
+        if (lane >= d) v = v + o;
     }
-    __syncthreads();
-    if (lane == 31) warp_sums[warp] = v;
-    __syncthreads();
-    Sums total = carry;
-#pragma unroll 4
-    for (int w = 0; w < kTableWarps; ++w) {
-        if (w == warp) { v.pages += total.pages; v.moved += total.moved; v.rows += total.rows; }
-        total.pages += warp_sums[w].pages; total.moved += warp_sums[w].moved; total.rows += warp_sums[w].rows;
-    }
-    carry = total;
     return v;
 }
+template <int kWarps>
+__device__ __forceinline__ Sums block_scan(Sums v, Sums& all, Sums* warp_sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    v = warp_scan(v);
+    if (lane == 31) warp_sums[warp] = v;
+    __syncthreads();
+    const Sums w = warp_scan(lane < kWarps ? warp_sums[lane] : Sums{0, 0, 0});         // by every warp for itself
+    const Sums none{0, 0, 0}, before{__shfl_sync(0xffffffffu, w.pages, warp ? warp - 1 : 0), __shfl_sync(0xffffffffu, w.moved, warp ? warp - 1 : 0),
+                                     __shfl_sync(0xffffffffu, w.rows, warp ? warp - 1 : 0)};
+    all = {__shfl_sync(0xffffffffu, w.pages, 31), __shfl_sync(0xffffffffu, w.moved, 31), __shfl_sync(0xffffffffu, w.rows, 31)};
+    return v + (warp ? before : none);
+}
 
-template <bool kRelease>
-__global__ void __launch_bounds__(kTableThreads)
+template <bool kRelease, int kThreads>
+__global__ void __launch_bounds__(kThreads)
 kap_tables_kernel(const TableParams p)
 {
     extern __shared__ uint32_t seen[];
-    __shared__ Sums warp_sums[kTableWarps];
-    __shared__ int32_t upto[kTableThreads], first[kTableThreads], request[kTableThreads];
+    __shared__ Sums warp_sums[kThreads / 32];
+    __shared__ int32_t upto[kThreads], first[kThreads], request[kThreads];
     const int tid = threadIdx.x;
-    for (int i = tid; i < (p.num_requests + 31) / 32; i += kTableThreads) seen[i] = 0u;
+    for (int i = tid; i < (p.num_requests + 31) / 32; i += kThreads) seen[i] = 0u;
     if (!kRelease) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the second kernel, which waits
-    __syncthreads();
     const int count = *p.free_count;
+    __syncthreads();
     // ---- what the step needs, and whether that can be had
-    Sums total{0, 0, 0};
-    bool bad = false, full = false;
+    Sums total{0, 0, 0}, all{0, 0, 0};
+    bool bad = count < 0 || count > p.free_capacity, full = false;
     const Entry e0 = load_entry<kRelease>(p, tid, seen);
-    for (int b0 = 0; b0 < p.batch; b0 += kTableThreads) {
+    for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
         const Entry e = b0 == 0 ? e0 : load_entry<kRelease>(p, b0 + tid, seen);
         bad |= e.bad;
         full |= e.full;
-        total.pages += e.pages; total.moved += e.moved; total.rows += e.n;
+        total = total + Sums{e.pages, e.moved, e.n};
     }
-    Sums all{0, 0, 0};
-    const Sums mine0 = block_scan(total, all, warp_sums);     // (sums of the first 1024 sequences, when there are no more)
-    bad |= count < 0 || count > p.free_capacity;
+    const Sums mine0 = block_scan<kThreads / 32>(total, all, warp_sums);     // (sums of the sequences themselves, when each has a thread)
     bad = __syncthreads_or(bad);
     if (kRelease) full = all.moved > (long long)p.free_capacity - count;
     else full = __syncthreads_or(full) || all.moved > count || all.pages > p.bt_capacity || all.rows > p.row_capacity;
     if (bad || full) {                                        // nothing is taken: a step without pages and rows
         if (!kRelease)
-            for (int b = tid; b <= p.batch; b += kTableThreads) {
+            for (int b = tid; b <= p.batch; b += kThreads) {
                 p.bt_indptr[b] = 0;
                 if (p.new_indptr) p.new_indptr[b] = 0;
             }
@@ -117,43 +118,41 @@ kap_tables_kernel(const TableParams p)
         p.bt_indptr[0] = 0;
         if (p.new_indptr) p.new_indptr[0] = 0;
     }
-    for (int b0 = 0; b0 < p.batch; b0 += kTableThreads) {
+    for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
         const int b = b0 + tid;
         const Entry e = b0 == 0 ? e0 : load_entry<kRelease>(p, b, nullptr);
-        const long long moved0 = carry.moved;
-        Sums v{e.pages, e.moved, e.n};
-        if (p.batch <= kTableThreads) { v = mine0; carry = all; }
-        else v = block_scan(v, carry, warp_sums);
+        Sums v = mine0, here = all;
+        if (p.batch > kThreads) v = block_scan<kThreads / 32>(Sums{e.pages, e.moved, e.n}, here, warp_sums);
         if (b < p.batch) {
             if (!kRelease) {
-                p.bt_indptr[b + 1] = (int32_t)v.pages;
-                if (p.new_indptr) p.new_indptr[b + 1] = (int32_t)v.rows;
+                p.bt_indptr[b + 1] = (int32_t)(carry.pages + v.pages);
+                if (p.new_indptr) p.new_indptr[b + 1] = (int32_t)(carry.rows + v.rows);
             }
             if (e.moved > 0) p.pages_held[e.request] = e.pages;
         }
-        upto[tid] = (int32_t)(v.moved - moved0);
+        upto[tid] = (int32_t)v.moved;
         first[tid] = kRelease ? e.pages : e.held;
         request[tid] = e.request;
         __syncthreads();
-        const int moved = (int)(carry.moved - moved0);
-        for (int i = tid; i < moved; i += kTableThreads) {
+        for (int i = tid; i < (int)here.moved; i += kThreads) {
             int lo = 0;                                       // the owner: sequences whose pages all come before i
 #pragma unroll
-            for (int d = kTableThreads / 2; d > 0; d /= 2)
+            for (int d = kThreads / 2; d > 0; d /= 2)
                 if (upto[lo + d - 1] <= i) lo += d;
             const int before = lo ? upto[lo - 1] : 0;
             int32_t* entry = p.page_table + request[lo] * p.table_stride + first[lo] + (i - before);
             // the i-th page moved, in the batch's order, is the i-th from the larger of the two tops
-            if (kRelease) p.free_pages[count + all.moved - 1 - (moved0 + i)] = *entry;
-            else *entry = p.free_pages[count - 1 - (moved0 + i)];
+            if (kRelease) p.free_pages[count + all.moved - 1 - (carry.moved + i)] = *entry;
+            else *entry = p.free_pages[count - 1 - (carry.moved + i)];
         }
-        __syncthreads();
+        carry = carry + here;
+        if (b0 + kThreads < p.batch) __syncthreads();
     }
     if (tid == 0 && all.moved > 0) *p.free_count = (int32_t)(kRelease ? count + all.moved : count - all.moved);
 }
 
 // the last sequence whose entries begin at or before i
-__device__ __forceinline__ int owner_of(const int32_t* __restrict__ indptr, int lo, int hi, int i) {
+__device__ __forceinline__ int owner_of(const int32_t* indptr, int lo, int hi, int i) {
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (indptr[mid] <= i) lo = mid;
@@ -162,15 +161,24 @@ __device__ __forceinline__ int owner_of(const int32_t* __restrict__ indptr, int 
     return lo;
 }
 
+constexpr int kFillStaged = 4096;                             // sequences whose offsets are searched in shared memory
 __global__ void __launch_bounds__(kFillThreads)
 kap_fill_tables_kernel(const TableParams p, const int list_blocks)
 {
+    __shared__ int32_t staged[kFillStaged + 1];
+    const bool lists = (int)blockIdx.x < list_blocks;
+    const int32_t* const offsets = lists ? p.bt_indptr : p.new_indptr;
+    const int at = (lists ? blockIdx.x : blockIdx.x - list_blocks) * kFillEntries;
     // (It lets nothing start before it ends: attention kernels read block tables ahead of their dependency wait.)
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const bool lists = (int)blockIdx.x < list_blocks;
-    const int32_t* const indptr = lists ? p.bt_indptr : p.new_indptr;
-    const int total = indptr[p.batch], at = (lists ? blockIdx.x : blockIdx.x - list_blocks) * kFillEntries, end = min(at + kFillEntries, total);
+    const int total = offsets[p.batch], end = min(at + kFillEntries, total);
     if (at >= total) return;
+    const bool stage = p.batch <= kFillStaged;
+    if (stage) {
+        for (int b = threadIdx.x; b <= p.batch; b += kFillThreads) staged[b] = offsets[b];
+        __syncthreads();
+    }
+    const int32_t* const indptr = stage ? staged : offsets;
     const int b0 = owner_of(indptr, 0, p.batch, at), b1 = owner_of(indptr, b0, p.batch, end - 1) + 1;
 #pragma unroll 4
     for (int i = at + threadIdx.x; i < end; i += kFillThreads) {
@@ -200,13 +208,16 @@ kap_status check_state(int32_t batch, int32_t page_size, const void* page_table,
     return KAP_OK;
 }
 
-template <typename K>
-kap_status launch(K kernel, dim3 grid, int threads, size_t smem, cudaStream_t stream, const TableParams& p) {
+template <bool kRelease>
+kap_status launch(const TableParams& p, cudaStream_t stream) {
+    const bool few = p.batch <= kFewThreads;
+    auto* kernel = few ? kap_tables_kernel<kRelease, kFewThreads> : kap_tables_kernel<kRelease, kTableThreads>;
+    const size_t smem = (size_t)(p.num_requests + 31) / 32 * 4;
     if (smem > 32 * 1024) {                                   // with the kernel's own arrays more than the default 48 KiB
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "cudaFuncSetAttribute failed: %s", cudaGetErrorString(e));
     }
-    kernel<<<grid, threads, smem, stream>>>(p);
+    kernel<<<1, few ? kFewThreads : kTableThreads, smem, stream>>>(p);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "block table kernel launch failed: %s", cudaGetErrorString(e));
     count_launch();
@@ -245,7 +256,7 @@ extern "C" kap_status kap_build_block_tables(
         if (e == cudaSuccess && new_indptr) e = cudaMemsetAsync(new_indptr, 0, sizeof(int32_t), stream);
         return e == cudaSuccess ? KAP_OK : fail(KAP_ERR_CUDA, "cudaMemsetAsync failed: %s", cudaGetErrorString(e));
     }
-    st = launch(kap_tables_kernel<false>, dim3(1), kTableThreads, (size_t)(num_requests + 31) / 32 * 4, stream, p);
+    st = launch<false>(p, stream);
     if (st != KAP_OK) return st;
     const int64_t list_blocks = (p.bt_capacity + kFillEntries - 1) / kFillEntries;
     const int64_t row_blocks = slot || position ? (p.row_capacity + kFillEntries - 1) / kFillEntries : 0;
@@ -276,5 +287,5 @@ extern "C" kap_status kap_release_pages(
     p.request = request; p.ctx_len = keep_tokens; p.page_table = page_table; p.pages_held = pages_held;
     p.free_pages = free_pages; p.free_count = free_count; p.status = device_status; p.table_stride = table_stride;
     p.batch = n; p.page_size = page_size; p.num_requests = num_requests; p.free_capacity = free_capacity;
-    return launch(kap_tables_kernel<true>, dim3(1), kTableThreads, (size_t)(num_requests + 31) / 32 * 4, (cudaStream_t)cuda_stream, p);
+    return launch<true>(p, (cudaStream_t)cuda_stream);
 }
