@@ -161,29 +161,33 @@ __device__ __forceinline__ int owner_of(const int32_t* indptr, int lo, int hi, i
     return lo;
 }
 
-constexpr int kFillStaged = 4096;                             // sequences whose offsets are searched in shared memory
+constexpr int kFillStaged = 2048;                             // sequences whose offsets and requests are looked up in shared memory
 __global__ void __launch_bounds__(kFillThreads)
 kap_fill_tables_kernel(const TableParams p, const int list_blocks)
 {
-    __shared__ int32_t staged[kFillStaged + 1];
-    const bool lists = (int)blockIdx.x < list_blocks;
-    const int32_t* const offsets = lists ? p.bt_indptr : p.new_indptr;
+    __shared__ int32_t staged[kFillStaged + 1], staged_request[kFillStaged];
+    const bool lists = (int)blockIdx.x < list_blocks, stage = p.batch <= kFillStaged;
     const int at = (lists ? blockIdx.x : blockIdx.x - list_blocks) * kFillEntries;
     // (It lets nothing start before it ends: attention kernels read block tables ahead of their dependency wait.)
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int total = offsets[p.batch], end = min(at + kFillEntries, total);
-    if (at >= total) return;
-    const bool stage = p.batch <= kFillStaged;
+    const int32_t* indptr = lists ? p.bt_indptr : p.new_indptr;
     if (stage) {
-        for (int b = threadIdx.x; b <= p.batch; b += kFillThreads) staged[b] = offsets[b];
+        for (int b = threadIdx.x; b <= p.batch; b += kFillThreads) {
+            staged[b] = indptr[b];
+            if (b < p.batch) staged_request[b] = p.request ? p.request[b] : b;
+        }
         __syncthreads();
+        indptr = staged;
     }
-    const int32_t* const indptr = stage ? staged : offsets;
-    const int b0 = owner_of(indptr, 0, p.batch, at), b1 = owner_of(indptr, b0, p.batch, end - 1) + 1;
+    const int end = min(at + kFillEntries, indptr[p.batch]);
+    if (at >= end) return;
+    const int b1 = owner_of(indptr, 0, p.batch, end - 1) + 1;
+    int b = owner_of(indptr, 0, b1, at);
 #pragma unroll 4
     for (int i = at + threadIdx.x; i < end; i += kFillThreads) {
-        const int b = owner_of(indptr, b0, b1, i), place = i - indptr[b];
-        const long long row = (p.request ? p.request[b] : b) * p.table_stride;
+        if (i >= indptr[b + 1]) b = owner_of(indptr, b, b1, i);
+        const int place = i - indptr[b];
+        const long long row = (stage ? staged_request[b] : p.request ? p.request[b] : b) * p.table_stride;
         if (lists) {
             p.bt_pages[i] = p.page_table[row + place];
         } else {
