@@ -15,10 +15,7 @@
 // Layout: one CTA per token row, 128 threads; a thread task is two 16-byte pieces of one head that hold
 // both partners of eight pairs, so a rotation never crosses threads and q may be rotated in place.  What hides the look-ups is other
 // CTAs on the SM: reading a thread's values before them costs registers and was slower (2 x 8192 rows: 72 us with the 10 CTAs that then fit on an SM, 68 with 12, 66 with 16).
-#include <cuda_bf16.h>
-#include <cuda_runtime.h>
-
-#include "kap_internal.h"
+#include "kap_ptx.cuh"
 
 namespace kap {
 void count_launch();
@@ -62,46 +59,77 @@ __device__ __forceinline__ uint32_t rotate_neighbours(uint32_t v, const float2 t
     return *reinterpret_cast<const uint32_t*>(&x);
 }
 
-// Weights of a norm for the eight columns of one 16-byte piece.
-__device__ __forceinline__ void load_weights(const NormParams& n, const void* w, int at, float (&f)[8]) {
-    if (!w) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = 1.f;
-        return;
-    }
-    if (n.f32) {
-        const float4 a = __ldg(reinterpret_cast<const float4*>((const float*)w + at)), b = __ldg(reinterpret_cast<const float4*>((const float*)w + at) + 1);
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    } else {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)w + at));
-        const uint32_t v[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(v[e] << 16); f[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u); }
-    }
-    if (n.unit_offset)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] += 1.f;
-}
-__device__ __forceinline__ void widen(const uint4 a, float (&f)[8]) {
-    const uint32_t v[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(v[e] << 16); f[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u); }
-}
-__device__ __forceinline__ uint4 narrow(const float (&f)[8]) {
-    uint32_t v[4];
+// Two times eight values in pairs, from the two pieces of a task: the first and the second partners where neighbours rotate (the words'
+// lower and upper halves), else the pieces one after the other; and back, rounded.
+struct Halves { uint64_t a[4], b[4]; };
+template <bool neighbours>
+__device__ __forceinline__ Halves widen(const uint4& x, const uint4& y) {
+    const uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+    Halves h;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const __nv_bfloat162 x = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
-        v[e] = *reinterpret_cast<const uint32_t*>(&x);
+        const uint32_t p = neighbours ? (e < 2 ? u[2 * e] : v[2 * e - 4]) : u[e], q = neighbours ? (e < 2 ? u[2 * e + 1] : v[2 * e - 3]) : v[e];
+        h.a[e] = neighbours ? pack_f32x2(bf16_lo(p), bf16_lo(q)) : pack_f32x2(bf16_lo(p), bf16_hi(p));
+        h.b[e] = neighbours ? pack_f32x2(bf16_hi(p), bf16_hi(q)) : pack_f32x2(bf16_lo(q), bf16_hi(q));
     }
-    return make_uint4(v[0], v[1], v[2], v[3]);
+    return h;
+}
+template <bool neighbours>
+__device__ __forceinline__ void narrow(const Halves& h, uint4& x, uint4& y) {
+    uint32_t u[4], v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float a0, a1, b0, b1;
+        unpack_f32x2(h.a[e], a0, a1);
+        unpack_f32x2(h.b[e], b0, b1);
+        u[e] = neighbours ? pack_bf16(a0, b0) : pack_bf16(a0, a1);
+        v[e] = neighbours ? pack_bf16(a1, b1) : pack_bf16(b0, b1);
+    }
+    x = neighbours ? make_uint4(u[0], v[0], u[1], v[1]) : make_uint4(u[0], u[1], u[2], u[3]);
+    y = neighbours ? make_uint4(u[2], v[2], u[3], v[3]) : make_uint4(v[0], v[1], v[2], v[3]);
+}
+// The weights of a task's columns, arranged like its values.
+template <bool neighbours>
+__device__ __forceinline__ Halves load_weights(const NormParams& n, const void* of, int first, int second) {
+    Halves h;
+    if (!of) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h.a[e] = h.b[e] = pack_f32x2(1.f, 1.f);
+        return h;
+    }
+    if (n.f32) {
+        const float4 *f = reinterpret_cast<const float4*>((const float*)of + first), *g = reinterpret_cast<const float4*>((const float*)of + second);
+        const float4 q[4] = {__ldg(f), __ldg(f + 1), __ldg(g), __ldg(g + 1)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float4 u = neighbours ? q[e] : q[e >> 1], v = neighbours ? q[e] : q[2 + (e >> 1)];
+            h.a[e] = neighbours ? pack_f32x2(u.x, u.z) : e & 1 ? pack_f32x2(u.z, u.w) : pack_f32x2(u.x, u.y);
+            h.b[e] = neighbours ? pack_f32x2(v.y, v.w) : e & 1 ? pack_f32x2(v.z, v.w) : pack_f32x2(v.x, v.y);
+        }
+    } else {
+        h = widen<neighbours>(__ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)of + first)), __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)of + second)));
+    }
+    if (n.unit_offset) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            h.a[e] = add_f32x2(h.a[e], pack_f32x2(1.f, 1.f));
+            h.b[e] = add_f32x2(h.b[e], pack_f32x2(1.f, 1.f));
+        }
+    }
+    return h;
+}
+__device__ __forceinline__ void load_pairs(const float* at, uint64_t (&v)[4]) {          // eight values, 16-byte aligned
+    const ulonglong2 p = *reinterpret_cast<const ulonglong2*>(at), q = *(reinterpret_cast<const ulonglong2*>(at) + 1);
+    v[0] = p.x; v[1] = p.y; v[2] = q.x; v[3] = q.y;
 }
 
-template <bool kNorm>
-__global__ void __launch_bounds__(kRopeThreads, kNorm ? 10 : 16)
+template <bool kNorm, bool kNeighbours>                        // the second: of calls with norms, where neighbouring columns rotate
+__global__ void __launch_bounds__(kRopeThreads, kNorm ? 8 : 16)
 kap_append_kv_rope_kernel(const RopeParams p, const NormParams n)
 {
-    __shared__ float2 turn[kHeadDim / 2];           // (cos, sin) of this row's pairs
+    __shared__ float2 turn[kNorm ? 1 : kHeadDim / 2];           // (cos, sin) of this row's pairs
+    // with norms: cos, sin and -sin apart, for arithmetic on pairs
+    __shared__ alignas(16) float cosine[kNorm ? kHeadDim / 2 : 1], sine[kNorm ? kHeadDim / 2 : 1], minus_sine[kNorm ? kHeadDim / 2 : 1];
     const int row = blockIdx.x, tid = threadIdx.x;
     // the sequence that owns the row, the last one that begins at or before it: 32 probes at a time (a bisection waits for one
     // probe after the other; 2928 rows of 24 sequences 17.6 us with it, 17.1 so)
@@ -119,6 +147,27 @@ kap_append_kv_rope_kernel(const RopeParams p, const NormParams n)
         b = lo;
         place = row - p.new_indptr[lo];
     }
+    const int q_tasks = p.q ? p.hq * kTasks : 0, k_tasks = p.hkv * kTasks, n_tasks = q_tasks + 2 * k_tasks;
+    const int rotated = p.half / 8;                 // tasks of a head that rotate
+    struct Task { bool is_q, is_v, apart; int head, t, c0, c1; };      // c0, c1: the two pieces, partners half a rotation apart, or neighbours
+    auto task = [&](int i) {
+        Task k;
+        k.is_q = i < q_tasks; k.is_v = i >= q_tasks + k_tasks;
+        const int j = k.is_q ? i : k.is_v ? i - q_tasks - k_tasks : i - q_tasks;
+        k.head = j / kTasks; k.t = j % kTasks;
+        k.apart = !(kNorm ? kNeighbours : p.interleaved) && k.t < rotated && !k.is_v;
+        k.c0 = k.apart ? k.t : 2 * k.t; k.c1 = k.apart ? k.t + rotated : 2 * k.t + 1;
+        return k;
+    };
+    auto fetch = [&](int i, uint4& x, uint4& y) {
+        const Task k = task(i);
+        const __nv_bfloat16* src = k.is_q ? p.q + row * p.q_stride : k.is_v ? p.v + row * p.v_stride : p.k + row * p.k_stride;
+        const uint4* s4 = reinterpret_cast<const uint4*>(src + k.head * kHeadDim);
+        x = s4[k.c0]; y = s4[k.c1];
+    };
+    // With norms a thread's values are loaded a task ahead, the first ones before the look-ups.
+    uint4 next_x = make_uint4(0u, 0u, 0u, 0u), next_y = next_x;
+    if (kNorm && tid < n_tasks) fetch(tid, next_x, next_y);
     const int L = p.ctx_len[b];
     const long long at = (long long)L + place;      // logical index of the token
     const int list0 = p.bt_indptr[b], n_bt = p.bt_indptr[b + 1] - list0;
@@ -133,58 +182,55 @@ kap_append_kv_rope_kernel(const RopeParams p, const NormParams n)
         t -= rint(t);
         float s, c;
         sincospif((float)(2.0 * t), &s, &c);
-        turn[tid] = make_float2(c, s);
+        if (kNorm) { cosine[tid] = c; sine[tid] = s; minus_sine[tid] = -s; }
+        else turn[tid] = make_float2(c, s);
     }
     __syncthreads();
     if (p.ctx_out && tid == 0) p.ctx_out[b] = L + 1;   // one row a sequence: no other CTA reads ctx_len[b]
 
-    const int q_tasks = p.q ? p.hq * kTasks : 0, k_tasks = p.hkv * kTasks;
-    const int rotated = p.half / 8;                 // tasks of a head that rotate
-    for (int i = tid; i < q_tasks + 2 * k_tasks; i += kRopeThreads) {
-        const bool is_q = i < q_tasks, is_v = i >= q_tasks + k_tasks;
-        const int j = is_q ? i : is_v ? i - q_tasks - k_tasks : i - q_tasks;
-        const int head = j / kTasks, t = j % kTasks;
-        // the two pieces: partners half a rotation apart, or neighbours
-        const bool apart = !p.interleaved && t < rotated && !is_v;
-        const int c0 = apart ? t : 2 * t, c1 = apart ? t + rotated : 2 * t + 1;
-        const __nv_bfloat16* src = is_q ? p.q + row * p.q_stride : is_v ? p.v + row * p.v_stride : p.k + row * p.k_stride;
-        const uint4* s4 = reinterpret_cast<const uint4*>(src + head * kHeadDim);
+    for (int i = tid; i < n_tasks; i += kRopeThreads) {
+        const Task k = task(i);
+        const bool is_q = k.is_q, is_v = k.is_v, apart = k.apart;
+        const int head = k.head, t = k.t, c0 = k.c0, c1 = k.c1;
+        uint4 x = next_x, y = next_y;
+        if (kNorm && i + kRopeThreads < n_tasks) fetch(i + kRopeThreads, next_x, next_y);
         if (!is_q && !stored) continue;
-        uint4 x = s4[c0], y = s4[c1];
+        if (!kNorm) fetch(i, x, y);
         if (kNorm && !is_v) {
             // a head's eight threads are neighbours: its sum of squares takes three exchanges
-            float a[8], b[8], w[8];
-            widen(x, a); widen(y, b);
-            float sum = 0.f;
+            Halves h = widen<kNeighbours>(x, y);
+            uint64_t sum2 = mul_f32x2(h.a[0], h.a[0]);
+            sum2 = fma_f32x2(h.b[0], h.b[0], sum2);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += a[e] * a[e] + b[e] * b[e];
+            for (int e = 1; e < 4; ++e) sum2 = fma_f32x2(h.b[e], h.b[e], fma_f32x2(h.a[e], h.a[e], sum2));
+            float lo, hi;
+            unpack_f32x2(sum2, lo, hi);
+            float sum = lo + hi;
             const uint32_t group = 0xffu << (tid & 24);
 #pragma unroll
             for (int d = 1; d < kTasks; d *= 2) sum += __shfl_xor_sync(group, sum, d);
             const float r = rsqrtf(sum * (1.f / kHeadDim) + n.eps);
-            const void* weight = is_q ? n.q_weight : n.k_weight;
+            const uint64_t r2 = pack_f32x2(r, r);
             const int at = head * (is_q ? n.q_head_stride : n.k_head_stride);
-            load_weights(n, weight, at + c0 * 8, w);
+            const Halves w = load_weights<kNeighbours>(n, is_q ? n.q_weight : n.k_weight, at + c0 * 8, at + c1 * 8);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] *= r * w[e];
-            load_weights(n, weight, at + c1 * 8, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) b[e] *= r * w[e];
+            for (int e = 0; e < 4; ++e) {
+                h.a[e] = mul_f32x2(h.a[e], mul_f32x2(r2, w.a[e]));
+                h.b[e] = mul_f32x2(h.b[e], mul_f32x2(r2, w.b[e]));
+            }
             if (t < rotated) {
-                const float2* f = turn + t * 8;
+                uint64_t c[4], v[4], m[4];
+                load_pairs(&cosine[t * 8], c);
+                load_pairs(&sine[t * 8], v);
+                load_pairs(&minus_sine[t * 8], m);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (apart) {
-                        const float u = a[e] * f[e].x - b[e] * f[e].y, v = b[e] * f[e].x + a[e] * f[e].y;
-                        a[e] = u; b[e] = v;
-                    } else {                         // pairs 0 to 3 in the first piece, 4 to 7 in the second
-                        float* z = e < 4 ? a + 2 * e : b + 2 * (e - 4);
-                        const float u = z[0] * f[e].x - z[1] * f[e].y, v = z[1] * f[e].x + z[0] * f[e].y;
-                        z[0] = u; z[1] = v;
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const uint64_t a = h.a[e], b = h.b[e];
+                    h.a[e] = fma_f32x2(a, c[e], mul_f32x2(b, m[e]));
+                    h.b[e] = fma_f32x2(b, c[e], mul_f32x2(a, v[e]));
                 }
             }
-            x = narrow(a); y = narrow(b);
+            narrow<kNeighbours>(h, x, y);
         } else if (apart) {
             const float2* f = turn + t * 8;
             rotate(x.x, y.x, f[0], f[1]); rotate(x.y, y.y, f[2], f[3]);
@@ -276,8 +322,8 @@ kap_status append_rope(
     p.interleaved = interleaved != 0; p.nhd = kv_layout == KAP_KV_NHD;
     if (freq_axis)
         for (int i = 0; i < p.half; ++i) p.axis[i] = freq_axis[i];
-    if (norm) kap_append_kv_rope_kernel<true><<<(unsigned)total_rows, kRopeThreads, 0, (cudaStream_t)cuda_stream>>>(p, *norm);
-    else kap_append_kv_rope_kernel<false><<<(unsigned)total_rows, kRopeThreads, 0, (cudaStream_t)cuda_stream>>>(p, NormParams{});
+    auto* kernel = !norm ? kap_append_kv_rope_kernel<false, false> : interleaved ? kap_append_kv_rope_kernel<true, true> : kap_append_kv_rope_kernel<true, false>;
+    kernel<<<(unsigned)total_rows, kRopeThreads, 0, (cudaStream_t)cuda_stream>>>(p, norm ? *norm : NormParams{});
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "launch failed: %s", cudaGetErrorString(e));
     count_launch();
