@@ -123,12 +123,13 @@ bool offsets_fit_ring(int64_t batch, bool verify, int ring_slots) {
 
 // Tensor map over one layer's pool viewed as a 2-D bf16 matrix [pages*2*Hkv*P rows][128 cols];
 // box = 16 rows x 64 columns (one half of a page-head's K or V), 128-byte swizzle.
+// whole_pages: the box is a page's K (or V) of one head, see workspace_page_map; otherwise half of its columns
 kap_status get_tensor_map(kap_workspace* ws, const void* pool, int64_t pages, int32_t hkv,
-                          const CUtensorMap** out) {
+                          const CUtensorMap** out, bool whole_pages = false) {
     const int32_t layout = ws->kv_layout;
     for (int i = 0; i < ws->map_count; ++i) {
         auto& s = ws->maps[i];
-        if (s.base == pool && s.pages == pages && s.hkv == hkv && s.layout == layout) {
+        if (s.base == pool && s.pages == pages && s.hkv == hkv && s.layout == layout && s.whole_pages == whole_pages) {
             *out = reinterpret_cast<const CUtensorMap*>(s.map);
             return KAP_OK;
         }
@@ -139,7 +140,19 @@ kap_status get_tensor_map(kap_workspace* ws, const void* pool, int64_t pages, in
     if (rows >= (1ull << 31)) return fail(KAP_ERR_UNSUPPORTED, "pool of %lld pages is too large", (long long)pages);
     auto& slot = ws->maps[ws->map_next];
     CUresult r;
-    if (layout == KAP_KV_NHD) {
+    if (whole_pages) {
+        // (64 columns, 8 tokens, half of the columns, 8-token group, head): the box lands as [group][half][token][64]
+        const cuuint64_t token = layout == KAP_KV_NHD ? (cuuint64_t)hkv * kHeadDim * 2 : kHeadDim * 2;     // bytes between tokens
+        const cuuint64_t groups = (layout == KAP_KV_NHD ? (cuuint64_t)pages * 2 * kPageSize : rows) / 8;
+        cuuint64_t dims[5] = {64, 8, 2, groups, layout == KAP_KV_NHD ? (cuuint64_t)hkv : 1};
+        cuuint64_t strides[4] = {token, kHeadDim, 8 * token, kHeadDim * 2};
+        cuuint32_t box[5] = {64, 8, 2, (cuuint32_t)(kPageSize / 8), 1};
+        cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+        r = enc(reinterpret_cast<CUtensorMap*>(slot.map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5,
+                const_cast<void*>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    } else if (layout == KAP_KV_NHD) {
         // (d, head, token row): a head's row is 256 contiguous bytes, rows of one head are
         // Hkv * 256 bytes apart; the box takes 64 columns of one head for the 16 tokens of a page
         cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)hkv, (cuuint64_t)pages * 2 * kPageSize};
@@ -161,7 +174,7 @@ kap_status get_tensor_map(kap_workspace* ws, const void* pool, int64_t pages, in
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     }
     if (r != CUDA_SUCCESS) return fail(KAP_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d", (int)r);
-    slot.base = pool; slot.pages = pages; slot.hkv = hkv; slot.layout = layout;
+    slot.base = pool; slot.pages = pages; slot.hkv = hkv; slot.layout = layout; slot.whole_pages = whole_pages;
     *out = reinterpret_cast<const CUtensorMap*>(slot.map);
     ws->map_next = (ws->map_next + 1) % kap_workspace::kMapSlots;
     if (ws->map_count < kap_workspace::kMapSlots) ++ws->map_count;
@@ -299,6 +312,11 @@ kap_status check_shape(int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_
 // for kap_shared_prefix_attn: the pool's tensor map (as above, cached in the workspace) and a map over query rows
 kap_status workspace_kv_map(kap_workspace* ws, const void* pool, int64_t pages, int32_t hkv, const void** map) {
     return get_tensor_map(ws, pool, pages, hkv, reinterpret_cast<const CUtensorMap**>(map));
+}
+// K or V of a page and head in one copy (coordinates 0, 0, 0, first token row / 8, head): two groups of 8 tokens, each the columns 0-63 and
+// then 64-127 of its tokens, 1 KiB apiece.
+kap_status workspace_page_map(kap_workspace* ws, const void* pool, int64_t pages, int32_t hkv, const void** map) {
+    return get_tensor_map(ws, pool, pages, hkv, reinterpret_cast<const CUtensorMap**>(map), true);
 }
 kap_status encode_query_map(void* map, const void* q, int64_t rows, int32_t hq, int32_t G, int32_t tile_rows) {
     EncodeTiledFn enc = encode_tiled_fn();

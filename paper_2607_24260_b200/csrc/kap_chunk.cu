@@ -5,7 +5,7 @@
 
 namespace kap {
 void count_launch();
-kap_status workspace_kv_map(kap_workspace* ws, const void* pool, int64_t pages, int32_t hkv, const void** map);
+kap_status workspace_page_map(kap_workspace* ws, const void* pool, int64_t pages, int32_t hkv, const void** map);
 kap_status encode_query_map(void* map, const void* q, int64_t rows, int32_t hq, int32_t G, int32_t tile_rows);
 bool launch_programmatically();
 
@@ -70,7 +70,7 @@ extern "C" kap_status kap_chunk_attn(
         return fail(KAP_ERR_INVALID_ARG, "the workspace belongs to device %d but device %d is current", ws->device, dev);
     const void* kv_map = nullptr;
     alignas(64) CUtensorMap q_map;
-    kap_status st = workspace_kv_map(ws, kv_pool, num_pool_pages, num_kv_heads, &kv_map);
+    kap_status st = workspace_page_map(ws, kv_pool, num_pool_pages, num_kv_heads, &kv_map);
     if (st == KAP_OK) st = encode_query_map(&q_map, q, total_rows, num_q_heads, G, kChunkTileRows);
     if (st != KAP_OK) return st;
     const bool nhd = ws->kv_layout == KAP_KV_NHD;

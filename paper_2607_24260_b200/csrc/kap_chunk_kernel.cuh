@@ -13,8 +13,10 @@ constexpr int kChunkUnitRows = 2 * kChunkTileRows;
 constexpr int kChunkStepPages = 5;
 constexpr int kChunkStepTokens = kChunkStepPages * kPageSize;          // 80
 constexpr int kChunkSlots = 8;                                         // step n: K in slot 2 n, V in slot 2 n + 1 (mod 8)
-constexpr int kChunkPlaneBytes = kChunkStepTokens * 128;               // 80 tokens x 64 columns: 10 KiB
-constexpr int kChunkSlotBytes = 2 * kChunkPlaneBytes;                  // columns 0-63 | 64-127
+// A slot holds the step's pages one after the other, each as [two groups of 8 tokens][columns 0-63, 64-127][token]: one copy a page, and the
+// groups of all pages lie 2 KiB apart, as the products' operands want it.
+constexpr int kChunkSlotBytes = kChunkStepPages * kTileBytes;          // 20 KiB
+constexpr int kChunkGroupBytes = 2048, kChunkHalfBytes = 1024;
 constexpr int kChunkQHalfBytes = kChunkTileRows * 128;                 // 128 rows x 64 columns: 16 KiB
 constexpr int kChunkQBytes = 2 * kChunkQHalfBytes;
 constexpr int kChunkTmemP = 80, kChunkTmemO = 128;                     // columns of a stream's 256; S from 0
@@ -369,8 +371,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     __syncthreads();
     const int n_segments = c->n_segments, more_rounds = c->more;
     if (warp == kChunkSoftmaxWarps) {
-        // ---- TMA: up to 20 copies a step (five pages, K and V, two halves of 64 columns), issued by one elected lane with
-        // warp-uniform coordinates.  V is needed later than K, by as many steps as S runs ahead of P V: its copies follow that much later,
+        // ---- TMA: up to ten copies a step (five pages, K and V), issued by one elected lane with warp-uniform coordinates.  V is needed later than K, by as many steps as S runs ahead of P V: its copies follow that much later,
         // so that what lies in the ring is what comes next.
         int32_t old_page[kChunkStepPages], new_page[kChunkStepPages];  // of the V tiles that are still to come, at most two steps
         int old_n = 0, new_n = 0, old_head = 0, new_head = 0;
@@ -385,15 +386,8 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < kChunkStepPages; ++i) {
                     if (i >= n) break;
-                    if (kNhd) {
-                        const int z = (page[i] * 2 + v) * kPageSize;
-                        tma_load_3d(dst + i * kHalfTileBytes, &kv_map, 0, kv_head, z, bar, keep);
-                        tma_load_3d(dst + kChunkPlaneBytes + i * kHalfTileBytes, &kv_map, 64, kv_head, z, bar, keep);
-                    } else {
-                        const int y = ((page[i] * 2 + v) * p.hkv + kv_head) * kPageSize;
-                        tma_load_2d(dst + i * kHalfTileBytes, &kv_map, 0, y, bar, keep);
-                        tma_load_2d(dst + kChunkPlaneBytes + i * kHalfTileBytes, &kv_map, 64, y, bar, keep);
-                    }
+                    const int row = kNhd ? (page[i] * 2 + v) * kPageSize : ((page[i] * 2 + v) * p.hkv + kv_head) * kPageSize;
+                    tma_load_5d(dst + i * kTileBytes, &kv_map, row / 8, kNhd ? kv_head : 0, bar, keep);
                 }
             }
             __syncwarp();
@@ -478,9 +472,9 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     } else if (warp == kChunkSoftmaxWarps + 1) {
         // ---- tensor core: one elected lane runs through a whole segment, waits included, with warp-uniform operands
         constexpr uint32_t idesc_o = umma_idesc(kChunkTileRows, kHeadDim, true);
-        const uint64_t q_desc = umma_smem_desc(smem_u32(q_tiles), 16, 1024), k_desc = umma_smem_desc(smem_u32(slots), 16, 1024);
-        // V: 16 tokens (K) x 128 columns (N), N contiguous; columns 64-127 one plane further, 8 tokens = 1 KiB
-        const uint64_t v_desc = umma_smem_desc(smem_u32(slots), kChunkPlaneBytes, 1024);
+        const uint64_t q_desc = umma_smem_desc(smem_u32(q_tiles), 16, 1024), k_desc = umma_smem_desc(smem_u32(slots), 16, kChunkGroupBytes);
+        // V: 16 tokens (K) x 128 columns (N), N contiguous; columns 64-127 in the other half of a group
+        const uint64_t v_desc = umma_smem_desc(smem_u32(slots), kChunkHalfBytes, kChunkGroupBytes);
         for (int k = 0; k < n_segments; ++k) {
             const ChunkSegment seg = sh.segments[k];
             deadline = global_ns() + kWaitBudgetNs;
@@ -504,7 +498,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
                         umma_ss(tmem + t * 256, q + ((ks >> 2) * kChunkQHalfBytes + (ks & 3) * 32) / 16,
-                                kd + ((ks >> 2) * kChunkPlaneBytes + (ks & 3) * 32) / 16, idesc_s, ks > 0);
+                                kd + ((ks >> 2) * kChunkHalfBytes + (ks & 3) * 32) / 16, idesc_s, ks > 0);
                     umma_commit(smem_u32(&c->s_ready[t]));
                     if (last_user) umma_commit(smem_u32(&c->free[slot]));
                 };
@@ -518,7 +512,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                     const int pages = min(kChunkStepPages, n_pages - j * kChunkStepPages);
 #pragma unroll
                     for (int pg = 0; pg < kChunkStepPages; ++pg)
-                        if (pg < pages) umma_ts(o, w + pg * 8, v + pg * (kHalfTileBytes / 16), idesc_o, !first || pg > 0);
+                        if (pg < pages) umma_ts(o, w + pg * 8, v + pg * (kTileBytes / 16), idesc_o, !first || pg > 0);
                     umma_commit(smem_u32(&c->pv_done[t]));
                     if (last_user) umma_commit(smem_u32(&c->free[slot]));
                 };
@@ -643,11 +637,10 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                     const int v_step = step0 + j, v_slot = (2 * v_step) % kChunkSlots + 1;
                     wait(c->full[v_slot], (uint32_t)(v_step / (kChunkSlots / 2)) & 1u);
                     __syncwarp();
-                    unsigned char* v = slots + v_slot * kChunkSlotBytes + (g.n - 1) % kChunkStepPages * kHalfTileBytes;
-                    for (int i = lane; i < 2 * kPageSize * 8; i += 32) {       // (plane, token, 16 bytes)
-                        const int tok = i >> 3 & (kPageSize - 1);
-                        if (tok >= seg.length % kPageSize)
-                            *reinterpret_cast<uint4*>(v + (i >> 7) * kChunkPlaneBytes + tok * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    unsigned char* v = slots + v_slot * kChunkSlotBytes + (g.n - 1) % kChunkStepPages * kTileBytes;
+                    for (int i = lane; i < kTileBytes / 16; i += 32) {         // (group, half of the columns, token of the group, 16 bytes)
+                        const int tok = (i >> 7) * 8 + (i >> 3 & 7);
+                        if (tok >= seg.length % kPageSize) *reinterpret_cast<uint4*>(v + i * 16) = make_uint4(0, 0, 0, 0);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }

@@ -74,8 +74,8 @@ struct kap_workspace {
     int32_t* h_status = nullptr;             // pinned read-back
     void* upload_event = nullptr;            // cudaEvent_t: last schedule upload done
     // cached tensor maps, keyed by (pool pointer, pages, Hkv)
-    struct MapSlot { const void* base; int64_t pages; int32_t hkv, layout; alignas(64) unsigned char map[128]; };
-    static constexpr int kMapSlots = 64;
+    struct MapSlot { const void* base; int64_t pages; int32_t hkv, layout; bool whole_pages; alignas(64) unsigned char map[128]; };
+    static constexpr int kMapSlots = 128;
     MapSlot* maps = nullptr;
     int32_t map_next = 0, map_count = 0;
     std::vector<int32_t>* schedule_key = nullptr;   // inputs of the schedule held on the device
