@@ -309,6 +309,17 @@ __device__ __forceinline__ float chunk_weights(const float (&s)[kChunkStepTokens
     unpack_f32x2(add_f32x2(sum[0], sum[1]), a, b);
     return a + b;
 }
+// The waiting is done in a function of its own: with its loop at every wait, a barrier that had long been passed cost 50 cycles more (a group of eight
+// products and two such waits 525 cycles, 435 with this and both barriers tried together).
+__device__ __noinline__ bool wait_slowly(uint32_t bar, uint32_t parity, uint64_t deadline, volatile int32_t* late) { return mbar_wait(bar, parity, deadline, late); }
+__device__ __forceinline__ bool both_passed(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p, q;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tmbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
+                 "and.pred p, p, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar0), "r"(parity0), "r"(bar1), "r"(parity1) : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
 template <bool kNhd>
@@ -357,7 +368,14 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     chunk_plan(p, *c);
     uint64_t deadline = global_ns() + kWaitBudgetNs;                   // of a segment's waits; every role sets it anew
     volatile int32_t* const late = &c->timed_out;
-    auto wait = [&](unsigned long long& bar, uint32_t parity) { return mbar_wait(smem_u32(&bar), parity, deadline, late); };
+    auto wait = [&](unsigned long long& bar, uint32_t parity) {
+        return mbar_try_wait(smem_u32(&bar), parity) || wait_slowly(smem_u32(&bar), parity, deadline, late);
+    };
+    auto wait_both = [&](unsigned long long& bar0, uint32_t parity0, unsigned long long& bar1, uint32_t parity1) {
+        if (both_passed(smem_u32(&bar0), parity0, smem_u32(&bar1), parity1)) return;
+        wait_slowly(smem_u32(&bar0), parity0, deadline, late);
+        wait_slowly(smem_u32(&bar1), parity1, deadline, late);
+    };
 
     // state of the roles, kept over the rounds
     int k_loads = 0, v_loads = 0, pending = 0, q_use[2] = {0, 0}, q_slot = 0, step0 = 0, count0 = 0, count1 = 0, count = 0;
@@ -489,8 +507,8 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                 // S of step j for stream t (its work n)
                 auto issue_s = [&](int t, int n, int j, bool last_user) {
                     const int slot = (2 * (base + j)) % kChunkSlots;
-                    wait(c->full[slot], (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u);
-                    if (n > 0) wait(c->s_free[t], (uint32_t)(n - 1) & 1u);     // the softmax warps have read the scores before
+                    // the tile is there, and the softmax warps have read the scores before (a barrier's phase before its first has passed)
+                    wait_both(c->full[slot], (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u, c->s_free[t], (uint32_t)(n - 1) & 1u);
                     tc_fence_after();
                     const uint64_t q = q_desc + (uint32_t)(pair ? t : q_at) * (kChunkQBytes / 16), kd = k_desc + (uint32_t)slot * (kChunkSlotBytes / 16);
                     const int pages = min(kChunkStepPages, n_pages - j * kChunkStepPages);
@@ -504,8 +522,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                 };
                 auto issue_pv = [&](int t, int n, int j, bool first, bool last_user) {
                     const int slot = (2 * (base + j)) % kChunkSlots + 1;
-                    wait(c->full[slot], (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u);
-                    wait(c->p_ready[t], (uint32_t)n & 1u);
+                    wait_both(c->full[slot], (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u, c->p_ready[t], (uint32_t)n & 1u);
                     tc_fence_after();
                     const uint64_t v = v_desc + (uint32_t)slot * (kChunkSlotBytes / 16);
                     const uint32_t o = tmem + t * 256 + kChunkTmemO, w = tmem + t * 256 + kChunkTmemP;
