@@ -18,9 +18,9 @@ namespace {
             return fail(KAP_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));         \
     } while (0)
 
-// rows of the partial buffer: two states of 256 rows for each CTA, and behind them the cuts
-int64_t cut_rows(int32_t n_cta) { return ((n_cta + 1) * (int64_t)sizeof(ChunkCut) + kHeadDim * 4 - 1) / (kHeadDim * 4); }
-int64_t rows_needed(int32_t n_cta) { return 2ll * n_cta * kChunkUnitRows + cut_rows(n_cta); }
+// rows of the partial buffer: the CTAs' states, and behind them how the work was divided
+int64_t cut_rows(int32_t n_cta) { return ((n_cta + 1) * (int64_t)sizeof(ChunkCut) + sizeof(ChunkInStep) + kHeadDim * 4 - 1) / (kHeadDim * 4); }
+int64_t rows_needed(int32_t n_cta) { return (int64_t)kChunkStates * n_cta * kChunkUnitRows + cut_rows(n_cta); }
 
 }  // namespace
 }  // namespace kap
@@ -82,7 +82,8 @@ extern "C" kap_status kap_chunk_attn(
     ChunkParams p{};
     p.q_indptr = q_indptr; p.bt_indptr = bt_indptr; p.bt_pages = bt_pages; p.ctx_len = ctx_len;
     p.part_o = ws->d_part_o; p.part_ml = ws->d_part_ml;
-    p.cuts = reinterpret_cast<ChunkCut*>(ws->d_part_o + 2ll * n_cta * kChunkUnitRows * kHeadDim);
+    p.cuts = reinterpret_cast<ChunkCut*>(ws->d_part_o + (int64_t)kChunkStates * n_cta * kChunkUnitRows * kHeadDim);
+    p.in_step = reinterpret_cast<ChunkInStep*>(p.cuts + n_cta + 1);
     p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ws->d_status;
     p.num_pool_pages = num_pool_pages; p.batch = batch; p.total_rows = total_rows;
     p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G; p.log2_g = __builtin_ctz((unsigned)G); p.window = window; p.n_sink = window ? n_sink : 0;

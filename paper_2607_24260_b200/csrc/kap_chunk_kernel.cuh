@@ -34,6 +34,11 @@ struct alignas(16) ChunkSegment {                                      // what o
     int32_t slot;                                                      // of its partial state; -1: the whole unit, writes the output
 };
 struct ChunkCut { long long unit; int32_t inside, tok0, rows_head, pad; };   // where a CTA begins; inside: in the middle of this unit
+// In step (see chunk_plan): units of one sequence, the first ones whole, the last n_cut cut into `pieces` each; pieces = 0: not in step.
+struct ChunkInStep { int32_t pieces, n_cut, whole, seq; };
+constexpr int kChunkStates = 4;                                        // states a CTA, 256 rows each, that the workspace holds
+constexpr int kChunkMostPieces = 16, kChunkPieceCost = 8;              // cost of a piece beyond its steps (products to fill, state), in steps
+constexpr long long kChunkInStepBytes = 48ll << 20;
 
 struct ChunkControl {
     unsigned long long full[kChunkSlots], free[kChunkSlots];
@@ -43,6 +48,8 @@ struct ChunkControl {
     uint32_t tmem_base;
     int32_t timed_out;
     int32_t n_segments, more;                                          // of this round; another round follows
+    int32_t active, active_seq;                                        // sequences with rows, one of them
+    ChunkInStep in_step;
     // plan: this CTA's range of the tape
     int32_t seq, unit, step, end_seq, end_unit, end_step, first_done;
     long long warp_sum[kChunkThreads / 32];
@@ -60,6 +67,7 @@ struct ChunkParams {
     const int32_t *q_indptr, *bt_indptr, *bt_pages, *ctx_len;
     float *part_o, *part_ml;
     ChunkCut* cuts;                                                    // [gridDim.x + 1]
+    ChunkInStep* in_step;
     __nv_bfloat16* out;
     float* lse;
     int32_t* status;
@@ -116,6 +124,31 @@ __device__ __forceinline__ int chunk_steps(const ChunkParams& p, const ChunkSeq&
     return (chunk_pages(p, lo, hi).n + kChunkStepPages - 1) / kChunkStepPages;
 }
 
+// How one sequence whose rows all see a long context is divided: instead of a range of the tape, which begins anywhere in a unit, CTA i takes the
+// units i, i + n, ... as far as they go round, and of the rest, each cut into pieces, the pieces i, i + n, ... in the order of the context.  All CTAs
+// then walk the same tokens at about the same time, tiles of one head next to each other, so that K and V come from L2 (2048 tokens behind 128K: the tape
+// reads 16 GB from memory).  Called by one warp.
+__device__ __forceinline__ void chunk_in_step(const ChunkParams& p, ChunkControl& c) {
+    const int lane = threadIdx.x & 31, n_cta = gridDim.x;
+    bool bad;
+    const ChunkSeq s = chunk_seq(p, c.active_seq, bad);
+    const int t = chunk_tiles(p, s.n), units = t * p.hkv, rest = units % n_cta, steps = chunk_steps(p, s, t - 1);
+    const long long seen = p.window ? min((long long)s.length, (long long)p.window + p.n_sink + s.n) : s.length;
+    ChunkInStep v{0, rest, units - rest, c.active_seq};
+    if (t >= 2 && s.length / 8 >= s.n && seen * p.hkv * (4 * kHeadDim) >= kChunkInStepBytes) {
+        // the number of pieces that ends first
+        const int k = lane + 1, rounds = (rest * k + n_cta - 1) / n_cta;
+        int cost = k > kChunkMostPieces || rest * k > kChunkStates * n_cta ? INT32_MAX >> 8 : rounds * ((steps + k - 1) / k + (k > 1 ? kChunkPieceCost : 0));
+        cost = (cost << 5 | lane);                                     // (steps: below 2^23, tokens below 2^31 / 2)
+        v.pieces = (__reduce_min_sync(0xffffffffu, cost) & 31) + 1;
+    }
+    if (lane == 0) {
+        c.in_step = v;
+        if (blockIdx.x == 0) *p.in_step = v;
+        c.unit = 0;                                                    // segments planned so far
+    }
+}
+
 // this CTA's ends; called by all threads
 __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = (p.batch + kChunkThreads - 1) / kChunkThreads;
@@ -126,6 +159,7 @@ __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c
         bool bad;
         const ChunkSeq s = chunk_seq(p, b, bad);
         if (bad && blockIdx.x == 0) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
+        if (s.n > 0) { atomicAdd(&c.active, 1); c.active_seq = b; }
         mine += chunk_cost(p, s, chunk_tiles(p, s.n)) * p.hkv;
     }
     long long upto = mine;
@@ -137,6 +171,13 @@ __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c
     if (lane == 31) c.warp_sum[warp] = upto;
     if (tid < 2) c.cut_seq[tid] = p.batch;                             // the tape's end
     __syncthreads();
+    if (c.active == 1) {
+        if (warp == 0) chunk_in_step(p, c);
+        __syncthreads();
+        if (c.in_step.pieces) return;
+    } else if (tid == 0 && blockIdx.x == 0) {
+        p.in_step->pieces = 0;
+    }
     long long total = 0, before = 0;
 #pragma unroll
     for (int w = 0; w < kChunkThreads / 32; ++w) {
@@ -210,6 +251,30 @@ __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c
 __device__ __forceinline__ void chunk_segments(const ChunkParams& p, ChunkShared& sh) {
     ChunkControl& c = sh.c;
     const int lane = threadIdx.x & 31, R = (kChunkUnitRows >> p.log2_g);
+    if (c.in_step.pieces) {
+        const ChunkInStep v = c.in_step;
+        bool bad;
+        const ChunkSeq s = chunk_seq(p, v.seq, bad);
+        const int t = chunk_tiles(p, s.n), n_cta = gridDim.x, first = c.unit, rounds = v.whole / n_cta, cut = v.n_cut * v.pieces;
+        const int all = rounds + ((int)blockIdx.x < cut ? (cut - 1 - (int)blockIdx.x) / n_cta + 1 : 0), take = min(all - first, kChunkMaxSegments);
+        for (int k = lane; k < take; k += 32) {
+            const int at = first + k, q = (at - rounds) * n_cta + (int)blockIdx.x;      // q: of the pieces
+            const bool whole = at < rounds;
+            const int piece = whole ? 0 : q / v.n_cut, u = whole ? at * n_cta + (int)blockIdx.x : v.whole + q % v.n_cut, head = u / t, tile = u % t;
+            const int steps = chunk_steps(p, s, tile), pieces = whole ? 1 : v.pieces;
+            ChunkSegment g;
+            g.list_at = s.list_at; g.tok0 = s.row0 + tile * R; g.lo = s.length - s.n + tile * R;
+            g.rows_head = (min(R, s.n - tile * R) << p.log2_g) | head << 16;
+            g.step_begin = (int)((long long)steps * piece / pieces);
+            g.step_end = (int)((long long)steps * (piece + 1) / pieces);
+            g.length = s.length;
+            g.slot = pieces == 1 ? -1 : q;
+            sh.segments[k] = g;
+        }
+        __syncwarp();
+        if (lane == 0) { c.n_segments = take; c.more = first + take < all; c.unit = first + take; }
+        return;
+    }
     int seq = c.seq, unit = c.unit, step = c.step, first_done = c.first_done, n = 0;
     const int end_seq = c.end_seq, end_unit = c.end_unit, end_step = c.end_step;
     const int last_seq = end_unit > 0 || end_step > 0 ? end_seq : end_seq - 1;
@@ -350,6 +415,8 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
         }
         mbar_init(smem_u32(&c->drained), 1);
         c->timed_out = 0;
+        c->active = 0;
+        c->in_step.pieces = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&kv_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
@@ -770,7 +837,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
 }
 
 // ---- joins the states of the units that were cut.  Block (c, part): the unit in which CTA c begins, if no CTA before it begins in its middle;
-// CTA c - 1 began it, the CTAs that follow as long as their cuts lie in it hold the rest.  A warp takes a row at a time, a lane
+// CTA c - 1 began it, the CTAs that follow as long as their cuts lie in it hold the rest.  In step: the c-th of the units cut into pieces.  A warp takes a row at a time, a lane
 // four columns.
 constexpr int kChunkMergeThreads = 256;
 constexpr int kChunkMergeParts = kChunkUnitRows / 32;
@@ -779,22 +846,31 @@ kap_chunk_merge_kernel(const ChunkParams p, const int n_cta)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = 1 + blockIdx.x / kChunkMergeParts, part = blockIdx.x % kChunkMergeParts;
     pdl_wait();
-    const ChunkCut cut = p.cuts[c];
-    if (!cut.inside) return;
-    const ChunkCut prior = p.cuts[c - 1];
-    if (prior.inside && prior.unit == cut.unit) return;
-    const int rows = cut.rows_head & 0xffff, head = cut.rows_head >> 16;
-    if (part * 32 >= rows) return;
-    int n = 1;                                                         // cuts inside the unit
-    for (;;) {
-        const int i = c + n + lane;
-        const bool same = i < n_cta && p.cuts[i].inside && p.cuts[i].unit == cut.unit;
-        const uint32_t m = __ballot_sync(0xffffffffu, same);
-        const int more = m == 0xffffffffu ? 32 : __ffs(~m) - 1;
-        n += more;
-        if (more < 32) break;
+    const ChunkInStep in_step = *p.in_step;
+    int rows, head, tok0, total;                                       // the unit's query rows, its KV head and first token row; states
+    if (in_step.pieces) {
+        if (in_step.pieces == 1 || c > in_step.n_cut) return;
+        bool bad;
+        const ChunkSeq s = chunk_seq(p, in_step.seq, bad);
+        const int t = chunk_tiles(p, s.n), u = in_step.whole + c - 1, R = kChunkUnitRows >> p.log2_g, tile = u % t;
+        head = u / t; tok0 = s.row0 + tile * R; rows = min(R, s.n - tile * R) << p.log2_g; total = in_step.pieces;
+    } else {
+        const ChunkCut cut = p.cuts[c];
+        if (!cut.inside) return;
+        const ChunkCut prior = p.cuts[c - 1];
+        if (prior.inside && prior.unit == cut.unit) return;
+        int n = 1;                                                     // cuts inside the unit
+        for (;;) {
+            const int i = c + n + lane;
+            const bool same = i < n_cta && p.cuts[i].inside && p.cuts[i].unit == cut.unit;
+            const uint32_t m = __ballot_sync(0xffffffffu, same);
+            const int more = m == 0xffffffffu ? 32 : __ffs(~m) - 1;
+            n += more;
+            if (more < 32) break;
+        }
+        rows = cut.rows_head & 0xffff; head = cut.rows_head >> 16; tok0 = cut.tok0; total = n + 1;
     }
-    const int total = n + 1;
+    if (part * 32 >= rows) return;
     for (int R = part * 32 + warp; R < min(rows, part * 32 + 32); R += kChunkMergeThreads / 32) {
         Merged acc;
         acc.m = -INFINITY; acc.l = 0.f; acc.o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -805,7 +881,8 @@ kap_chunk_merge_kernel(const ChunkParams p, const int n_cta)
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 const int i = min(i0 + j, total - 1);
-                const long long row = ((long long)(c - 1 + i) * 2 + (i < total - 1 ? 1 : 0)) * kChunkUnitRows + R;
+                const long long slot = in_step.pieces ? (c - 1) + (long long)i * in_step.n_cut : (long long)(c - 1 + i) * 2 + (i < total - 1 ? 1 : 0);
+                const long long row = slot * kChunkUnitRows + R;
                 ml[j] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + row * 2));
                 o[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + row * kHeadDim) + lane);
             }
@@ -813,7 +890,7 @@ kap_chunk_merge_kernel(const ChunkParams p, const int n_cta)
             for (int j = 0; j < kBatch; ++j)
                 if (i0 + j < total && ml[j].y > 0.f) merge_into(acc, ml[j].x, ml[j].y, o[j]);
         }
-        const long long cell = (long long)(cut.tok0 + R / p.G) * p.hq + head * p.G + R % p.G;
+        const long long cell = (long long)(tok0 + (R >> p.log2_g)) * p.hq + (head << p.log2_g) + (R & (p.G - 1));
         const float inv = acc.l > 0.f ? 1.f / acc.l : 0.f;
         uint2 v;
         v.x = pack_bf16(acc.o.x * inv, acc.o.y * inv);

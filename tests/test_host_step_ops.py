@@ -89,8 +89,8 @@ def test_adjust_logits_of_nothing():
 
 
 def test_chunk_attn_items():
-    # two states of 256 rows for each of 148 SMs and the places of their cuts, in items of 64 or of 5 rows
-    rows = 2 * 148 * 256
+    # four states of 256 rows for each of 148 SMs and how the work was divided, in items of 64 or of 5 rows
+    rows = 4 * 148 * 256
     assert rows < kap.chunk_attn_items(64, 148) * 64 < rows + 64 * 2
     assert rows < kap.chunk_attn_items(5, 148) * 5 < rows + 20
     assert kap.chunk_attn_items() == kap.chunk_attn_items(64, 148)
