@@ -21,9 +21,11 @@ constexpr int kChunkQHalfBytes = kChunkTileRows * 128;                 // 128 ro
 constexpr int kChunkQBytes = 2 * kChunkQHalfBytes;
 constexpr int kChunkTmemP = 80, kChunkTmemO = 128;                     // columns of a stream's 256; S from 0
 constexpr int kChunkMaxSegments = 72;                                  // planned at a time
-// Cost of a unit beyond its tokens (query load, first products, epilogue), in tokens; it places the cuts, nothing else.
-constexpr int kChunkUnitCost = 160;
-constexpr int kChunkLeastCost = 640;                                   // of a CTA's share: fewer CTAs work when there is little to do
+// What a unit costs, to place the cuts and for nothing else: its tokens and, for the first products and the epilogue, some more, times 5 with two tiles
+// and 3 with one, for which a step's products are half and its copies the same.  (Windowed batch 944 us, with 2 : 1 980, 4 : 3 1023; whole prompts
+// 264 us, with 160 tokens more 295.)
+constexpr int kChunkUnitCost = 320, kChunkPairCost = 5, kChunkSoloCost = 3;
+constexpr int kChunkLeastCost = 1600;                                   // of a CTA's share: fewer CTAs work when there is little to do
 
 struct alignas(16) ChunkSegment {                                      // what one CTA does of one unit (query tile pair, KV head)
     int32_t list_at;                                                   // the sequence's first entry in bt_pages
@@ -101,11 +103,11 @@ __device__ __forceinline__ long long chunk_cost(const ChunkParams& p, const Chun
     const int R = kChunkUnitRows >> p.log2_g, t = chunk_tiles(p, s.n), whole = min(k, t - 1);
     const long long lo = max(0, s.length - s.n), knee = (long long)p.window + p.n_sink;   // where the window begins to leave tokens out
     const long long m = p.window ? min((long long)whole, max(0ll, (knee - lo + R - 1) >> (8 - p.log2_g))) : whole;
-    long long c = 2 * (whole * (long long)kChunkUnitCost + m * lo + R * (m * (m + 1) / 2) + (whole - m) * (knee + R));
+    long long c = kChunkPairCost * (whole * (long long)kChunkUnitCost + m * lo + R * (m * (m + 1) / 2) + (whole - m) * (knee + R));
     if (k == t) {
         const int rest = s.n - (t - 1) * R;
         const long long at = lo + (long long)(t - 1) * R, seen = p.window && at >= knee ? knee + rest : at + rest;
-        c += (rest * p.G > kChunkTileRows ? 2 : 1) * (kChunkUnitCost + seen);
+        c += (rest * p.G > kChunkTileRows ? kChunkPairCost : kChunkSoloCost) * (kChunkUnitCost + seen);
     }
     return c;
 }
@@ -225,7 +227,7 @@ __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c
                 k = at;
             }
             const int steps = chunk_steps(p, s, k), rows = min(R, s.n - k * R) * p.G;
-            const int z = (int)((y - chunk_cost(p, s, k)) >> (rows > kChunkTileRows ? 1 : 0)) - kChunkUnitCost;     // (below 2^31: a context's tokens and a tile's)
+            const int z = (int)((y - chunk_cost(p, s, k)) / (rows > kChunkTileRows ? kChunkPairCost : kChunkSoloCost)) - kChunkUnitCost;     // (below 2^31: a context's tokens and a tile's)
             step = min(steps, max(0, (z + kChunkStepTokens / 2) / kChunkStepTokens));
             unit = head * t + k;
             inside = step > 0 && step < steps;
@@ -404,16 +406,16 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     if (tid == 0) {
-        for (int i = 0; i < kChunkSlots; ++i) { mbar_init(smem_u32(&c->full[i]), 1); mbar_init(smem_u32(&c->free[i]), 1); }
+        for (int i = 0; i < kChunkSlots; ++i) { mbar_init(smem_u32(&c->full[i]), 1); mbar_init(smem_u32(&c->free[i]), 2); }   // free: both issuers
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&c->q_full[i]), 1);
-            mbar_init(smem_u32(&c->q_free[i]), 1);
+            mbar_init(smem_u32(&c->q_free[i]), 2);
             mbar_init(smem_u32(&c->s_ready[i]), 1);
             mbar_init(smem_u32(&c->s_free[i]), 4);                     // the stream's softmax warps
             mbar_init(smem_u32(&c->p_ready[i]), 4);
             mbar_init(smem_u32(&c->pv_done[i]), 1);
         }
-        mbar_init(smem_u32(&c->drained), 1);
+        mbar_init(smem_u32(&c->drained), 2);
         c->timed_out = 0;
         c->active = 0;
         c->in_step.pieces = 0;
@@ -445,46 +447,20 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     };
 
     // state of the roles, kept over the rounds
-    int k_loads = 0, v_loads = 0, pending = 0, q_use[2] = {0, 0}, q_slot = 0, step0 = 0, count0 = 0, count1 = 0, count = 0;
+    int loads = 0, q_use[2] = {0, 0}, q_slot = 0, step0 = 0, count = 0;
     uint32_t q_parity = 0;
     bool ok = true;
     uint64_t keep;
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(keep));
 
     for (;;) {
-    if (warp == kChunkSoftmaxWarps + 2) chunk_segments(p, sh);
+    if (warp == kChunkSoftmaxWarps + 3) chunk_segments(p, sh);
     __syncthreads();
     const int n_segments = c->n_segments, more_rounds = c->more;
-    if (warp == kChunkSoftmaxWarps) {
-        // ---- TMA: up to ten copies a step (five pages, K and V), issued by one elected lane with warp-uniform coordinates.  V is needed later than K, by as many steps as S runs ahead of P V: its copies follow that much later,
-        // so that what lies in the ring is what comes next.
-        int32_t old_page[kChunkStepPages], new_page[kChunkStepPages];  // of the V tiles that are still to come, at most two steps
-        int old_n = 0, new_n = 0, old_head = 0, new_head = 0;
-        auto load = [&](int v, int at, const int32_t (&page)[kChunkStepPages], int n, int kv_head) {
-            const int slot = 2 * (at % (kChunkSlots / 2)) + v;
-            ok = wait(c->free[slot], ((uint32_t)(at / (kChunkSlots / 2)) & 1u) ^ 1u);      // (the first round does not wait)
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) return;
-            if (elect_one()) {
-                const uint32_t bar = smem_u32(&c->full[slot]), dst = smem_u32(slots) + slot * kChunkSlotBytes;
-                mbar_expect_tx(bar, (uint32_t)n * kTileBytes);
-#pragma unroll
-                for (int i = 0; i < kChunkStepPages; ++i) {
-                    if (i >= n) break;
-                    const int row = kNhd ? (page[i] * 2 + v) * kPageSize : ((page[i] * 2 + v) * p.hkv + kv_head) * kPageSize;
-                    tma_load_5d(dst + i * kTileBytes, &kv_map, row / 8, kNhd ? kv_head : 0, bar, keep);
-                }
-            }
-            __syncwarp();
-        };
-        auto load_v = [&]() {
-            load(1, v_loads, old_page, old_n, old_head);
-            if (ok) ++v_loads;
-#pragma unroll
-            for (int i = 0; i < kChunkStepPages; ++i) old_page[i] = new_page[i];
-            old_n = new_n; old_head = new_head;
-            --pending;
-        };
+    if (warp == kChunkSoftmaxWarps || warp == kChunkSoftmaxWarps + 3) {
+        // ---- copies: one warp brings the query tiles and K, another V, which is needed later, so that neither waits for the other's slots.  Up
+        // to five a step, issued by one elected lane with warp-uniform coordinates.
+        const int v = warp == kChunkSoftmaxWarps ? 0 : 1;
         for (int k = 0; k < n_segments && ok; ++k) {
             const ChunkSegment s = sh.segments[k];
             deadline = global_ns() + kWaitBudgetNs;
@@ -496,67 +472,61 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
             if (n_steps <= 0) continue;
             auto fetch = [&](int i) {                                  // physical page of the segment's i-th
                 if (i >= n_pages) return 0;
-                const int v = page0 + i;
-                return p.bt_pages[s.list_at + (v < g.head ? v : v - g.head + g.first)];
+                const int at = page0 + i;
+                return p.bt_pages[s.list_at + (at < g.head ? at : at - g.head + g.first)];
             };
             constexpr int kBatch = 30 / kChunkStepPages;               // page ids, 30 at a time and one batch ahead
             int32_t ids = 0, next_ids = lane < 30 ? fetch(lane) : 0;
-            for (int t = 0; t < (pair ? 2 : 1) && ok; ++t) {
-                const int to = pair ? t : q_slot;
-                if (q_use[to] > 0) {
-                    // The products that free the tile may need the V tiles that are still to come (a segment's last ones come before the next
-                    // one's first S): they are not held back over a wait.
-                    const uint32_t phase = (uint32_t)(q_use[to] - 1) & 1u;
-                    if (!__all_sync(0xffffffffu, mbar_try_wait(smem_u32(&c->q_free[to]), phase)))
-                        while (pending > 0 && ok) load_v();
-                    ok = ok && wait(c->q_free[to], phase);
+            if (v == 0) {
+                for (int t = 0; t < (pair ? 2 : 1) && ok; ++t) {
+                    const int to = pair ? t : q_slot;
+                    ok = __all_sync(0xffffffffu, q_use[to] == 0 || wait(c->q_free[to], (uint32_t)(q_use[to] - 1) & 1u));
+                    if (!ok) break;
+                    if (elect_one()) {
+                        const uint32_t bar = smem_u32(&c->q_full[to]), dst = smem_u32(q_tiles) + to * kChunkQBytes;
+                        const int tok = s.tok0 + t * (kChunkTileRows >> p.log2_g), head = kv_head << p.log2_g;
+                        mbar_expect_tx(bar, kChunkQBytes);
+                        tma_load_3d(dst, &q_map, 0, head, tok, bar, keep);
+                        tma_load_3d(dst + kChunkQHalfBytes, &q_map, 64, head, tok, bar, keep);
+                    }
+                    __syncwarp();
+                    ++q_use[to];
                 }
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                if (elect_one()) {
-                    const uint32_t bar = smem_u32(&c->q_full[to]), dst = smem_u32(q_tiles) + to * kChunkQBytes;
-                    const int tok = s.tok0 + t * (kChunkTileRows >> p.log2_g), head = kv_head << p.log2_g;
-                    mbar_expect_tx(bar, kChunkQBytes);
-                    tma_load_3d(dst, &q_map, 0, head, tok, bar, keep);
-                    tma_load_3d(dst + kChunkQHalfBytes, &q_map, 64, head, tok, bar, keep);
-                }
-                __syncwarp();
-                ++q_use[to];
+                if (!pair) q_slot ^= 1;
             }
-            if (!pair) q_slot ^= 1;
             int in_batch = 0;
-            for (int j = 0; j < n_steps && ok; ++j) {
+            for (int j = 0; j < n_steps && ok; ++j, ++loads) {
                 if (in_batch == 0) {
                     ids = next_ids;
                     next_ids = lane < 30 ? fetch((j + kBatch) * kChunkStepPages + lane) : 0;
                     if (ids < 0 || ids >= p.num_pool_pages) { ids = 0; atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX); }
                 }
-                const int n = min(kChunkStepPages, n_pages - j * kChunkStepPages);
-                int32_t page[kChunkStepPages];
+                const int n = min(kChunkStepPages, n_pages - j * kChunkStepPages), slot = 2 * (loads % (kChunkSlots / 2)) + v;
+                int32_t row[kChunkStepPages];                          // first token row of each page's K or V, in groups of 8
 #pragma unroll
-                for (int i = 0; i < kChunkStepPages; ++i) page[i] = __shfl_sync(0xffffffffu, ids, in_batch * kChunkStepPages + i);
-                if (++in_batch == kBatch) in_batch = 0;
-                load(0, k_loads, page, n, kv_head);
-                if (!ok) break;
-                ++k_loads;
-                if (pending == 0) {
-#pragma unroll
-                    for (int i = 0; i < kChunkStepPages; ++i) old_page[i] = page[i];
-                    old_n = n; old_head = kv_head;
-                } else {
-                    if (pending == 2) load_v();
-#pragma unroll
-                    for (int i = 0; i < kChunkStepPages; ++i) new_page[i] = page[i];
-                    new_n = n; new_head = kv_head;
+                for (int i = 0; i < kChunkStepPages; ++i) {
+                    const int page = __shfl_sync(0xffffffffu, ids, in_batch * kChunkStepPages + i);
+                    row[i] = (kNhd ? page * 2 + v : (page * 2 + v) * p.hkv + kv_head) * (kPageSize / 8);
                 }
-                ++pending;
-                if (pair && pending == 2 && ok) load_v();
+                if (++in_batch == kBatch) in_batch = 0;
+                ok = __all_sync(0xffffffffu, wait(c->free[slot], ((uint32_t)(loads / (kChunkSlots / 2)) & 1u) ^ 1u));      // (the first round does not wait)
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t bar = smem_u32(&c->full[slot]), dst = smem_u32(slots) + slot * kChunkSlotBytes;
+                    mbar_expect_tx(bar, (uint32_t)n * kTileBytes);
+#pragma unroll
+                    for (int i = 0; i < kChunkStepPages; ++i)
+                        if (i < n) tma_load_5d(dst + i * kTileBytes, &kv_map, row[i], kNhd ? kv_head : 0, bar, keep);
+                }
+                __syncwarp();
             }
         }
-        while (pending > 0 && ok) load_v();
-    } else if (warp == kChunkSoftmaxWarps + 1) {
-        // ---- tensor core: one elected lane runs through a whole segment, waits included, with warp-uniform operands
+    } else if (warp == kChunkSoftmaxWarps + 1 || warp == kChunkSoftmaxWarps + 2) {
+        // ---- tensor core: an issuer for each stream, so that neither waits for the other's softmax: S of its next step, then O += P V of the one
+        // before.  One elected lane runs through a whole segment, waits included, with warp-uniform operands.  Both arrive on a tile's
+        // free barrier, with their products or, where the tile is not theirs, as soon as it is there (its last use is then over).
         constexpr uint32_t idesc_o = umma_idesc(kChunkTileRows, kHeadDim, true);
+        const int t = warp - (kChunkSoftmaxWarps + 1);
         const uint64_t q_desc = umma_smem_desc(smem_u32(q_tiles), 16, 1024), k_desc = umma_smem_desc(smem_u32(slots), 16, kChunkGroupBytes);
         // V: 16 tokens (K) x 128 columns (N), N contiguous; columns 64-127 in the other half of a group
         const uint64_t v_desc = umma_smem_desc(smem_u32(slots), kChunkHalfBytes, kChunkGroupBytes);
@@ -567,17 +537,23 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
             const ChunkPages g = chunk_pages(p, seg.lo, seg.lo + (rows >> p.log2_g) - 1);
             const int n_steps = __shfl_sync(0xffffffffu, seg.step_end - seg.step_begin, 0);
             const int n_pages = __shfl_sync(0xffffffffu, g.n - seg.step_begin * kChunkStepPages, 0);
-            const int pair = rows > kChunkTileRows ? 1 : 0;
+            const int pair = rows > kChunkTileRows ? 1 : 0, stride = pair ? 1 : 2, first = pair ? 0 : t;       // this stream's steps
             if (n_steps <= 0) continue;
-            const int base0 = count0, base1 = count1, base = step0, q_at = q_slot;
+            const int base = step0, work0 = count, q_at = pair ? t : q_slot;
             if (elect_one()) {
-                // S of step j for stream t (its work n)
-                auto issue_s = [&](int t, int n, int j, bool last_user) {
-                    const int slot = (2 * (base + j)) % kChunkSlots;
+                auto slot_of = [&](int j) { return 2 * ((base + j) % (kChunkSlots / 2)); };
+                auto phase_of = [&](int j) { return (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u; };
+                // of a step that is the other stream's
+                auto pass = [&](int j, int v) {
+                    wait(c->full[slot_of(j) + v], phase_of(j));
+                    mbar_arrive(smem_u32(&c->free[slot_of(j) + v]));
+                };
+                auto issue_s = [&](int j, int n) {                     // of step j, work n of the stream
+                    const int slot = slot_of(j);
                     // the tile is there, and the softmax warps have read the scores before (a barrier's phase before its first has passed)
-                    wait_both(c->full[slot], (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u, c->s_free[t], (uint32_t)(n - 1) & 1u);
+                    wait_both(c->full[slot], phase_of(j), c->s_free[t], (uint32_t)(n - 1) & 1u);
                     tc_fence_after();
-                    const uint64_t q = q_desc + (uint32_t)(pair ? t : q_at) * (kChunkQBytes / 16), kd = k_desc + (uint32_t)slot * (kChunkSlotBytes / 16);
+                    const uint64_t q = q_desc + (uint32_t)q_at * (kChunkQBytes / 16), kd = k_desc + (uint32_t)slot * (kChunkSlotBytes / 16);
                     const int pages = min(kChunkStepPages, n_pages - j * kChunkStepPages);
                     const uint32_t idesc_s = umma_idesc(kChunkTileRows, kPageSize, false) + ((uint32_t)(pages - 1) * (kPageSize >> 3) << 17);
 #pragma unroll
@@ -585,48 +561,46 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                         umma_ss(tmem + t * 256, q + ((ks >> 2) * kChunkQHalfBytes + (ks & 3) * 32) / 16,
                                 kd + ((ks >> 2) * kChunkHalfBytes + (ks & 3) * 32) / 16, idesc_s, ks > 0);
                     umma_commit(smem_u32(&c->s_ready[t]));
-                    if (last_user) umma_commit(smem_u32(&c->free[slot]));
+                    umma_commit(smem_u32(&c->free[slot]));
                 };
-                auto issue_pv = [&](int t, int n, int j, bool first, bool last_user) {
-                    const int slot = (2 * (base + j)) % kChunkSlots + 1;
-                    wait_both(c->full[slot], (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u, c->p_ready[t], (uint32_t)n & 1u);
+                auto issue_pv = [&](int j, int n) {
+                    const int slot = slot_of(j) + 1;
+                    wait_both(c->full[slot], phase_of(j), c->p_ready[t], (uint32_t)n & 1u);
                     tc_fence_after();
                     const uint64_t v = v_desc + (uint32_t)slot * (kChunkSlotBytes / 16);
                     const uint32_t o = tmem + t * 256 + kChunkTmemO, w = tmem + t * 256 + kChunkTmemP;
                     const int pages = min(kChunkStepPages, n_pages - j * kChunkStepPages);
 #pragma unroll
                     for (int pg = 0; pg < kChunkStepPages; ++pg)
-                        if (pg < pages) umma_ts(o, w + pg * 8, v + pg * (kTileBytes / 16), idesc_o, !first || pg > 0);
+                        if (pg < pages) umma_ts(o, w + pg * 8, v + pg * (kTileBytes / 16), idesc_o, n > work0 || pg > 0);
                     umma_commit(smem_u32(&c->pv_done[t]));
-                    if (last_user) umma_commit(smem_u32(&c->free[slot]));
+                    umma_commit(smem_u32(&c->free[slot]));
                 };
-                wait(c->q_full[pair ? 0 : q_at], (q_parity >> (pair ? 0 : q_at)) & 1u);
-                if (pair) {
-                    wait(c->q_full[1], q_parity >> 1);
-                    for (int j = 0; j < n_steps; ++j) {
-                        issue_s(0, base0 + j, j, false);
-                        if (j == n_steps - 1) umma_commit(smem_u32(&c->q_free[0]));
-                        if (j > 0) issue_pv(0, base0 + j - 1, j - 1, j == 1, false);
-                        issue_s(1, base1 + j, j, true);
-                        if (j == n_steps - 1) umma_commit(smem_u32(&c->q_free[1]));
-                        if (j > 0) issue_pv(1, base1 + j - 1, j - 1, j == 1, true);
-                    }
-                    issue_pv(0, base0 + n_steps - 1, n_steps - 1, n_steps == 1, false);
-                    issue_pv(1, base1 + n_steps - 1, n_steps - 1, n_steps == 1, true);
-                } else {                                               // step j: work j / 2 of stream j mod 2
-                    for (int j = 0; j < n_steps; ++j) {
-                        issue_s(j & 1, (j & 1 ? base1 : base0) + (j >> 1), j, true);
-                        if (j == n_steps - 1) umma_commit(smem_u32(&c->q_free[q_at]));
-                        if (j > 1) issue_pv(j & 1, (j & 1 ? base1 : base0) + (j >> 1) - 1, j - 2, j < 4, true);
-                    }
-                    for (int j = max(0, n_steps - 2); j < n_steps; ++j)
-                        issue_pv(j & 1, (j & 1 ? base1 : base0) + (j >> 1), j, j < 2, true);
+                wait(c->q_full[q_at], q_parity >> q_at & 1u);
+                int n = work0, passed = 0;                             // passed: steps of the other stream up to here have been passed for V
+                auto pass_v = [&](int upto) {
+                    if (!pair)
+                        for (; passed < upto; ++passed)
+                            if ((passed & 1) != t) pass(passed, 1);
+                };
+                for (int j = first; j < n_steps; j += stride, ++n) {
+                    if (!pair && j > 0) pass(j - 1, 0);
+                    issue_s(j, n);
+                    if (j + stride >= n_steps) umma_commit(smem_u32(&c->q_free[q_at]));
+                    if (n > work0) { pass_v(j - stride); issue_pv(j - stride, n - 1); }
+                }
+                if (!pair && ((n_steps - 1) & 1) != t) pass(n_steps - 1, 0);
+                if (n > work0) { const int last = first + (n - 1 - work0) * stride; pass_v(last); issue_pv(last, n - 1); }
+                else mbar_arrive(smem_u32(&c->q_free[q_at]));          // (one step: nothing for the second stream)
+                pass_v(n_steps);
+                if (pair) {                                            // the other stream's query tile
+                    wait(c->q_full[t ^ 1], q_parity >> (t ^ 1) & 1u);
+                    mbar_arrive(smem_u32(&c->q_free[t ^ 1]));
                 }
             }
             __syncwarp();
             step0 += n_steps;
-            count0 += pair ? n_steps : (n_steps + 1) >> 1;
-            count1 += pair ? n_steps : n_steps >> 1;
+            count += pair ? n_steps : (n_steps + 1 - t) >> 1;
             q_parity ^= pair ? 3u : 1u << q_slot;
             if (!pair) q_slot ^= 1;
         }
@@ -813,18 +787,16 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     __syncthreads();                                                   // everybody has read this round's segments
     }
 
-    if (warp == kChunkSoftmaxWarps && *late) {                         // copies in flight must land before the CTA ends
+    if ((warp == kChunkSoftmaxWarps || warp == kChunkSoftmaxWarps + 3) && *late) {      // copies in flight must land before the CTA ends
         const uint64_t last = global_ns() + kWaitBudgetNs;
         int32_t more = 0;
-        for (int v = 0; v < 2; ++v) {
-            const int n = v ? v_loads : k_loads;
-            for (int i = max(0, n - kChunkSlots / 2); i < n; ++i)
-                mbar_wait(smem_u32(&c->full[2 * (i % (kChunkSlots / 2)) + v]), (uint32_t)(i / (kChunkSlots / 2)) & 1u, last, &more);
-        }
+        const int v = warp == kChunkSoftmaxWarps ? 0 : 1;
+        for (int i = max(0, loads - kChunkSlots / 2); i < loads; ++i)
+            mbar_wait(smem_u32(&c->full[2 * (i % (kChunkSlots / 2)) + v]), (uint32_t)(i / (kChunkSlots / 2)) & 1u, last, &more);
         for (int s = 0; s < 2; ++s)
             if (q_use[s]) mbar_wait(smem_u32(&c->q_full[s]), (uint32_t)(q_use[s] - 1) & 1u, last, &more);
     }
-    if (warp == kChunkSoftmaxWarps + 1) {
+    if (warp == kChunkSoftmaxWarps + 1 || warp == kChunkSoftmaxWarps + 2) {
         if (elect_one()) umma_commit(smem_u32(&c->drained));           // everything issued, whatever happened
         int32_t more = 0;
         mbar_wait(smem_u32(&c->drained), 0, global_ns() + kWaitBudgetNs, &more);
