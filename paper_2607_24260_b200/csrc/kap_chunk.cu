@@ -18,6 +18,7 @@ namespace {
             return fail(KAP_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));         \
     } while (0)
 
+constexpr int64_t kFewMergeRows = 16384;
 // rows of the partial buffer: the CTAs' states, and behind them how the work was divided
 int64_t cut_rows(int32_t n_cta) { return ((n_cta + 1) * (int64_t)sizeof(ChunkCut) + sizeof(ChunkInStep) + kHeadDim * 4 - 1) / (kHeadDim * 4); }
 int64_t rows_needed(int32_t n_cta) { return (int64_t)kChunkStates * n_cta * kChunkUnitRows + cut_rows(n_cta); }
@@ -87,6 +88,7 @@ extern "C" kap_status kap_chunk_attn(
     p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ws->d_status;
     p.num_pool_pages = num_pool_pages; p.batch = batch; p.total_rows = total_rows;
     p.hq = num_q_heads; p.hkv = num_kv_heads; p.G = G; p.log2_g = __builtin_ctz((unsigned)G); p.window = window; p.n_sink = window ? n_sink : 0;
+    p.wide_out = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
     p.scale_log2 = sm_scale * 1.4426950408889634f;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -103,10 +105,12 @@ extern "C" kap_status kap_chunk_attn(
     else KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_chunk_kernel<false>, kv, q_map, p));
     count_launch();
     if (n_cta > 1) {
-        cfg.gridDim = dim3((unsigned)(n_cta - 1) * kChunkMergeParts);
+        // Few rows: one a warp, their states are all that is waited for.  Many: four a warp one after the other, a quarter of the blocks.
+        const int part_rows = (int64_t)total_rows * num_q_heads <= kFewMergeRows ? kChunkMergeThreads / 32 : kChunkMergeThreads / 8;
+        cfg.gridDim = dim3((unsigned)(n_cta - 1) * (kChunkUnitRows / part_rows));
         cfg.blockDim = dim3(kChunkMergeThreads);
         cfg.dynamicSmemBytes = 0;
-        KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_chunk_merge_kernel, p, n_cta));
+        KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_chunk_merge_kernel, p, n_cta, part_rows));
         count_launch();
     }
     return KAP_OK;

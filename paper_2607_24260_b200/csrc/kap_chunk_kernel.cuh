@@ -21,11 +21,10 @@ constexpr int kChunkQHalfBytes = kChunkTileRows * 128;                 // 128 ro
 constexpr int kChunkQBytes = 2 * kChunkQHalfBytes;
 constexpr int kChunkTmemP = 80, kChunkTmemO = 128;                     // columns of a stream's 256; S from 0
 constexpr int kChunkMaxSegments = 72;                                  // planned at a time
-// What a unit costs, to place the cuts and for nothing else: its tokens and, for the first products and the epilogue, some more, times 5 with two tiles
-// and 3 with one, for which a step's products are half and its copies the same.  (Windowed batch 944 us, with 2 : 1 980, 4 : 3 1023; whole prompts
-// 264 us, with 160 tokens more 295.)
-constexpr int kChunkUnitCost = 320, kChunkPairCost = 5, kChunkSoloCost = 3;
-constexpr int kChunkLeastCost = 1600;                                   // of a CTA's share: fewer CTAs work when there is little to do
+// What a unit costs, to place the cuts and for nothing else: its tokens and, for the first products and the epilogue, some more, times 2 with two
+// tiles.  (Windowed batch 835 us, with 5 : 3 910, 3 : 1 895; whole prompts 259 us, with 320 tokens more 268, with 240 278.)
+constexpr int kChunkUnitCost = 400, kChunkPairCost = 2, kChunkSoloCost = 1;
+constexpr int kChunkLeastCost = 640;                                   // of a CTA's share: fewer CTAs work when there is little to do
 
 struct alignas(16) ChunkSegment {                                      // what one CTA does of one unit (query tile pair, KV head)
     int32_t list_at;                                                   // the sequence's first entry in bt_pages
@@ -74,7 +73,7 @@ struct ChunkParams {
     float* lse;
     int32_t* status;
     long long num_pool_pages;
-    int32_t batch, total_rows, hq, hkv, G, log2_g, window, n_sink;
+    int32_t batch, total_rows, hq, hkv, G, log2_g, window, n_sink, wide_out;      // wide_out: out lies on a 32-byte boundary
     float scale_log2;
 };
 
@@ -763,9 +762,14 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                         uint32_t v[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) v[e] = l > 0.f ? pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv) : 0u;
-                        uint4* dst = reinterpret_cast<uint4*>(p.out + cell * kHeadDim + i);
+                        __nv_bfloat16* dst = p.out + cell * kHeadDim + i;
+                        if (p.wide_out) {                              // (every lane has a row of its own: the fewer instructions, the better)
+                            store_32b(dst, &v[0]);
+                            store_32b(dst + 16, &v[8]);
+                        } else {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) dst[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                            for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(dst)[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                        }
                     } else if (valid) {
                         // 32-byte stores: each lane has a row of its own, so an instruction touches 32 lines whatever its width
 #pragma unroll
@@ -810,13 +814,12 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
 
 // ---- joins the states of the units that were cut.  Block (c, part): the unit in which CTA c begins, if no CTA before it begins in its middle;
 // CTA c - 1 began it, the CTAs that follow as long as their cuts lie in it hold the rest.  In step: the c-th of the units cut into pieces.  A warp takes a row at a time, a lane
-// four columns.
+// four columns; a block has part_rows rows.
 constexpr int kChunkMergeThreads = 256;
-constexpr int kChunkMergeParts = kChunkUnitRows / 32;
 __global__ void __launch_bounds__(kChunkMergeThreads)
-kap_chunk_merge_kernel(const ChunkParams p, const int n_cta)
+kap_chunk_merge_kernel(const ChunkParams p, const int n_cta, const int part_rows)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = 1 + blockIdx.x / kChunkMergeParts, part = blockIdx.x % kChunkMergeParts;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = kChunkUnitRows / part_rows, c = 1 + blockIdx.x / parts, row0 = blockIdx.x % parts * part_rows;
     pdl_wait();
     const ChunkInStep in_step = *p.in_step;
     int rows, head, tok0, total;                                       // the unit's query rows, its KV head and first token row; states
@@ -842,8 +845,8 @@ kap_chunk_merge_kernel(const ChunkParams p, const int n_cta)
         }
         rows = cut.rows_head & 0xffff; head = cut.rows_head >> 16; tok0 = cut.tok0; total = n + 1;
     }
-    if (part * 32 >= rows) return;
-    for (int R = part * 32 + warp; R < min(rows, part * 32 + 32); R += kChunkMergeThreads / 32) {
+    if (row0 >= rows) return;
+    for (int R = row0 + warp; R < min(rows, row0 + part_rows); R += kChunkMergeThreads / 32) {
         Merged acc;
         acc.m = -INFINITY; acc.l = 0.f; acc.o = make_float4(0.f, 0.f, 0.f, 0.f);
         constexpr int kBatch = 8;
