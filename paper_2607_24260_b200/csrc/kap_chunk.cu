@@ -18,7 +18,7 @@ namespace {
             return fail(KAP_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));         \
     } while (0)
 
-constexpr int64_t kFewMergeRows = 16384;
+constexpr int64_t kFewMergeCells = 16384;                                  // rows x heads (see the two merge kernels)
 // rows of the partial buffer: the CTAs' states, and behind them how the work was divided
 int64_t cut_rows(int32_t n_cta) { return ((n_cta + 1) * (int64_t)sizeof(ChunkCut) + sizeof(ChunkInStep) + kHeadDim * 4 - 1) / (kHeadDim * 4); }
 int64_t rows_needed(int32_t n_cta) { return (int64_t)kChunkStates * n_cta * kChunkUnitRows + cut_rows(n_cta); }
@@ -105,12 +105,12 @@ extern "C" kap_status kap_chunk_attn(
     else KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_chunk_kernel<false>, kv, q_map, p));
     count_launch();
     if (n_cta > 1) {
-        // Few rows: one a warp, their states are all that is waited for.  Many: four a warp one after the other, a quarter of the blocks.
-        const int part_rows = (int64_t)total_rows * num_q_heads <= kFewMergeRows ? kChunkMergeThreads / 32 : kChunkMergeThreads / 8;
-        cfg.gridDim = dim3((unsigned)(n_cta - 1) * (kChunkUnitRows / part_rows));
+        const int64_t cells = (int64_t)total_rows * num_q_heads, warps = kChunkMergeThreads / 32;
+        const bool few = cells <= kFewMergeCells;
+        cfg.gridDim = dim3(few ? (unsigned)((cells + warps - 1) / warps) : (unsigned)(n_cta - 1) * (kChunkUnitRows / kChunkMergeRows));
         cfg.blockDim = dim3(kChunkMergeThreads);
         cfg.dynamicSmemBytes = 0;
-        KAP_CUDA(cudaLaunchKernelEx(&cfg, kap_chunk_merge_kernel, p, n_cta, part_rows));
+        KAP_CUDA(cudaLaunchKernelEx(&cfg, few ? kap_chunk_merge_rows_kernel : kap_chunk_merge_kernel, p, n_cta));
         count_launch();
     }
     return KAP_OK;

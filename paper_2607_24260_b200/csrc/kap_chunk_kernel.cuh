@@ -812,23 +812,63 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
 }
 
-// ---- joins the states of the units that were cut.  Block (c, part): the unit in which CTA c begins, if no CTA before it begins in its middle;
-// CTA c - 1 began it, the CTAs that follow as long as their cuts lie in it hold the rest.  In step: the c-th of the units cut into pieces.  A warp takes a row at a time, a lane
-// four columns; a block has part_rows rows.
+// ---- joins the states of the units that were cut: those of a unit are the last of CTA c - 1, which began it, and the ones of the CTAs from c on as
+// long as their cuts lie in it; in step, one for each piece.  A warp takes a row at a time, a lane four columns.
 constexpr int kChunkMergeThreads = 256;
+struct ChunkStates { long long first, stride, last; int32_t n; };      // slots of a unit's states: first + i stride, the last one apart
+__device__ __forceinline__ ChunkStates cut_states(int c, int cuts) {   // cuts c .. c + cuts - 1 lie in the unit
+    return {2ll * (c - 1) + 1, 2, 2ll * (c - 1 + cuts), cuts + 1};
+}
+__device__ __forceinline__ ChunkStates piece_states(const ChunkInStep& v, int of) {
+    return {of, v.n_cut, of + (long long)(v.pieces - 1) * v.n_cut, v.pieces};
+}
+__device__ __forceinline__ void chunk_merge_row(const ChunkParams& p, const ChunkStates& of, int R, int tok0, int head) {
+    const int lane = threadIdx.x & 31;
+    Merged acc;
+    acc.m = -INFINITY; acc.l = 0.f; acc.o = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kBatch = 8;
+    for (int i0 = 0; i0 < of.n; i0 += kBatch) {
+        float2 ml[kBatch];
+        float4 o[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int i = min(i0 + j, of.n - 1);
+            const long long row = (i < of.n - 1 ? of.first + i * of.stride : of.last) * kChunkUnitRows + R;
+            ml[j] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + row * 2));
+            o[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + row * kHeadDim) + lane);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (i0 + j < of.n && ml[j].y > 0.f) merge_into(acc, ml[j].x, ml[j].y, o[j]);
+    }
+    const long long cell = (long long)(tok0 + (R >> p.log2_g)) * p.hq + (head << p.log2_g) + (R & (p.G - 1));
+    const float inv = acc.l > 0.f ? 1.f / acc.l : 0.f;
+    uint2 v;
+    v.x = pack_bf16(acc.o.x * inv, acc.o.y * inv);
+    v.y = pack_bf16(acc.o.z * inv, acc.o.w * inv);
+    *reinterpret_cast<uint2*>(p.out + cell * kHeadDim + lane * 4) = v;
+    if (p.lse && lane == 0) p.lse[cell] = acc.l > 0.f ? (acc.m + log2f(acc.l)) * 0.6931471805599453f : -INFINITY;
+}
+
+// Many rows: most are in units that one CTA finished.  Block (c, part): 32 rows of the unit in which CTA c begins, if no CTA before it begins in its
+// middle (in step: of the c-th unit cut).
+constexpr int kChunkMergeRows = 32;
 __global__ void __launch_bounds__(kChunkMergeThreads)
-kap_chunk_merge_kernel(const ChunkParams p, const int n_cta, const int part_rows)
+kap_chunk_merge_kernel(const ChunkParams p, const int n_cta)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = kChunkUnitRows / part_rows, c = 1 + blockIdx.x / parts, row0 = blockIdx.x % parts * part_rows;
+    constexpr int kParts = kChunkUnitRows / kChunkMergeRows;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = 1 + blockIdx.x / kParts, row0 = blockIdx.x % kParts * kChunkMergeRows;
     pdl_wait();
     const ChunkInStep in_step = *p.in_step;
-    int rows, head, tok0, total;                                       // the unit's query rows, its KV head and first token row; states
+    int rows, head, tok0;                                              // the unit's query rows, its KV head and first token row
+    ChunkStates states;
     if (in_step.pieces) {
         if (in_step.pieces == 1 || c > in_step.n_cut) return;
         bool bad;
         const ChunkSeq s = chunk_seq(p, in_step.seq, bad);
         const int t = chunk_tiles(p, s.n), u = in_step.whole + c - 1, R = kChunkUnitRows >> p.log2_g, tile = u % t;
-        head = u / t; tok0 = s.row0 + tile * R; rows = min(R, s.n - tile * R) << p.log2_g; total = in_step.pieces;
+        head = u / t; tok0 = s.row0 + tile * R; rows = min(R, s.n - tile * R) << p.log2_g;
+        states = piece_states(in_step, c - 1);
     } else {
         const ChunkCut cut = p.cuts[c];
         if (!cut.inside) return;
@@ -843,36 +883,50 @@ kap_chunk_merge_kernel(const ChunkParams p, const int n_cta, const int part_rows
             n += more;
             if (more < 32) break;
         }
-        rows = cut.rows_head & 0xffff; head = cut.rows_head >> 16; tok0 = cut.tok0; total = n + 1;
+        rows = cut.rows_head & 0xffff; head = cut.rows_head >> 16; tok0 = cut.tok0;
+        states = cut_states(c, n);
     }
-    if (row0 >= rows) return;
-    for (int R = row0 + warp; R < min(rows, row0 + part_rows); R += kChunkMergeThreads / 32) {
-        Merged acc;
-        acc.m = -INFINITY; acc.l = 0.f; acc.o = make_float4(0.f, 0.f, 0.f, 0.f);
-        constexpr int kBatch = 8;
-        for (int i0 = 0; i0 < total; i0 += kBatch) {
-            float2 ml[kBatch];
-            float4 o[kBatch];
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                const int i = min(i0 + j, total - 1);
-                const long long slot = in_step.pieces ? (c - 1) + (long long)i * in_step.n_cut : (long long)(c - 1 + i) * 2 + (i < total - 1 ? 1 : 0);
-                const long long row = slot * kChunkUnitRows + R;
-                ml[j] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + row * 2));
-                o[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + row * kHeadDim) + lane);
-            }
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j)
-                if (i0 + j < total && ml[j].y > 0.f) merge_into(acc, ml[j].x, ml[j].y, o[j]);
+    for (int R = row0 + warp; R < min(rows, row0 + kChunkMergeRows); R += kChunkMergeThreads / 32) chunk_merge_row(p, states, R, tok0, head);
+}
+
+// Few rows, most of them in units cut many times: a warp for each (row, head), which finds its unit's states itself.  (50 rows at 4K: the call 26 us,
+// with blocks for all places where a unit could be cut 31.)
+__global__ void __launch_bounds__(kChunkMergeThreads)
+kap_chunk_merge_rows_kernel(const ChunkParams p, const int n_cta)
+{
+    const int lane = threadIdx.x & 31, cell = blockIdx.x * (kChunkMergeThreads / 32) + (threadIdx.x >> 5), row = cell / p.hq, h = cell % p.hq;
+    pdl_wait();
+    if (row >= p.total_rows) return;
+    const ChunkInStep in_step = *p.in_step;
+    int lo = 0, hi = p.batch;                                          // the sequence that owns the row, 32 probes at a time
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, probe = lo + lane * step;
+        const uint32_t below = __ballot_sync(0xffffffffu, probe < hi && p.q_indptr[probe] <= row);
+        lo += max(31 - __clz(below), 0) * step;
+        hi = min(hi, lo + step);
+    }
+    bool bad;
+    const ChunkSeq s = chunk_seq(p, lo, bad);
+    if (row < s.row0 || row >= s.row0 + s.n) return;                   // nobody's
+    const int R = kChunkUnitRows >> p.log2_g, t = chunk_tiles(p, s.n), tile = (row - s.row0) / R, head = h >> p.log2_g, unit = head * t + tile;
+    ChunkStates states;
+    if (in_step.pieces) {
+        if (in_step.pieces == 1 || unit < in_step.whole) return;
+        states = piece_states(in_step, unit - in_step.whole);
+    } else {
+        int first = 0, n = 0;
+        for (int c0 = 1; c0 < n_cta; c0 += 32) {
+            const int c = c0 + lane;
+            const bool same = c < n_cta && p.cuts[c].inside && p.cuts[c].unit == ((long long)lo << 32 | (unsigned)unit);
+            const uint32_t m = __ballot_sync(0xffffffffu, same);
+            if (m && n == 0) first = c0 + __ffs(m) - 1;
+            n += __popc(m);
         }
-        const long long cell = (long long)(tok0 + (R >> p.log2_g)) * p.hq + (head << p.log2_g) + (R & (p.G - 1));
-        const float inv = acc.l > 0.f ? 1.f / acc.l : 0.f;
-        uint2 v;
-        v.x = pack_bf16(acc.o.x * inv, acc.o.y * inv);
-        v.y = pack_bf16(acc.o.z * inv, acc.o.w * inv);
-        *reinterpret_cast<uint2*>(p.out + cell * kHeadDim + lane * 4) = v;
-        if (p.lse && lane == 0) p.lse[cell] = acc.l > 0.f ? (acc.m + log2f(acc.l)) * 0.6931471805599453f : -INFINITY;
+        if (n == 0) return;                                            // one CTA did the whole unit
+        states = cut_states(first, n);
     }
+    const int tok0 = s.row0 + tile * R;
+    chunk_merge_row(p, states, ((row - tok0) << p.log2_g) + (h & (p.G - 1)), tok0, head);
 }
 
 }  // namespace kap
