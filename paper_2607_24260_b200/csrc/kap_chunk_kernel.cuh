@@ -1,5 +1,31 @@
 // Attention of many new tokens over the paged cache on the tensor cores (tcgen05.mma, accumulators in tensor memory): prompt chunks and
 // single tokens of one batch in one launch, causal, with an optional sliding window and first tokens that stay visible.
+//
+// Mathematics: one pass with a running maximum and sum.  For a tile of up to 128 query rows (a token's heads of one KV head are rows of the same tile) and
+// steps of 80 tokens,
+//     S = Q K^T (128 x 80),   p = 2^(S scale - m),   l += sum p,   O += P V (128 x 128),
+// with a lazy reference m: it moves only when a step's maximum exceeds it by more than 8 (weights stay below 256), and then l and O are rescaled.  P is
+// rounded to bf16 for the product (the tensor core's operand type; 2^-8 of each weight, averaged by the sum); l adds the unrounded weights in fp32, so lse
+// keeps fp32 accuracy.  Parts of a unit leave (m, l, O) in fp32, and states of the same row join as M = max m, l = sum 2^(m_i - M) l_i, O likewise.
+//
+// A unit is two tiles of one sequence and KV head (256 rows, a pair), or its last rows if they fit one tile (solo), over the pages that they see: all
+// up to the last row's own, or the sinks' pages and those from the first row's window on.  A pair gives each of two streams a tile and both the same K and V;
+// a solo unit alternates its steps between the streams.  One CTA per SM, 12 warps:
+//   warps 0-3, 4-7  softmax of stream 0 and stream 1: one query row per thread (TMEM lane), 80 scores at a time
+//   warp 8, 11      copies: query tiles and K; V.  A ring of four steps; a page's K (or V) is one copy of 4 KiB
+//   warp 9, 10      the products of stream 0 and of stream 1
+// Tensor memory, 256 of the 512 columns per stream: S (80), P (40), O (128).  Steps of 80 tokens are the longest whose weights fit beside the scores, so that
+// S of the next step runs as soon as the scores have been read.
+//
+// Bounds.  Single tokens (64 x 16K, 32 / 8 heads): memory, 645 us, 6.66 TB/s; what it took is a short way round the ring (copies of V that do not stand in
+// K's way, satisfied barriers that cost little).  Chunks: a product 128 x 80 x 16 reads 6.5 KiB of shared memory, 52 cycles, and P V 64, together 1432 cycles
+// for a pair's step; 2160 pass, of which copies into shared memory (40 KiB a step, 320 cycles of its bandwidth) explain some, and under load the
+// board's power limit holds the clock at 1.4 to 1.5 GHz (2048 rows behind 128K: 3.8 ms in a burst, 4.06 ms = 1.09 PFLOP/s sustained, of 1.37 that a plain product
+// sustains).  Sixteen softmax warps with half a row each took the same time, sixteen with quarter rows (16-lane loads) 1.6 times as long.
+//
+// Every wait on an mbarrier is bounded, anew for each segment; when one runs out the CTA sets KAP_ERR_TIMEOUT, later waits return at once, the roles run
+// to their end inside this CTA's shared and tensor memory, copies and products in flight are waited for (bounded again), tensor memory is freed and
+// the kernel returns.
 #pragma once
 
 #include "kap_ptx.cuh"
@@ -79,7 +105,8 @@ struct ChunkParams {
 
 // ------------------------------------------------------------------------------------------------------------------ plan
 // All units of the batch, ordered by sequence, KV head and tile, lie on a tape whose length is their cost; CTA i of n takes the tape from
-// i / n to (i + 1) / n of it.  Every CTA finds its two ends by itself, from closed forms, so that lengths may live on the device.
+// i / n to (i + 1) / n of it.  Every CTA finds its two ends by itself, from closed forms, so that lengths may live on the device (4 us from the start of
+// the kernel to the first copy; a unit is cut at most as often as CTAs share it, two states a CTA).
 struct ChunkSeq { int32_t row0, n, length, list_at; };                 // first row of q, rows, tokens, block table
 
 __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams& p, int b, bool& bad) {
@@ -90,7 +117,7 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams& p, int b, bool&
     s.n = max(min(r1, p.total_rows) - s.row0, 0);
     s.length = (int)min((long long)max(L, 0), listed);
     s.list_at = l0;
-    bad = r0 != s.row0 || r1 != s.row0 + s.n || L != s.length;
+    bad = r0 != s.row0 || r1 != s.row0 + s.n || (s.n > 0 && L != s.length);      // (a sequence without rows may have any length)
     return s;
 }
 __device__ __forceinline__ int chunk_tiles(const ChunkParams& p, int n) {

@@ -541,16 +541,17 @@ def append_kv(k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, new_indptr=No
 def _page_state(page_table, pages_held, free_pages, free_count):
     """(requests, table_stride, device) of the arrays that build_block_tables and release_pages keep"""
     _torch_module()
-    dev = page_table.get_device()
-    if page_table.dtype is not _I32 or page_table.dim() != 2 or dev < 0 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-        raise KapError(ERR_INVALID_ARG, f"page_table is {page_table.dtype} {tuple(page_table.shape)} with strides {page_table.stride()} on "
-                       f"{page_table.device}, expected an int32 [requests, pages] tensor on a GPU")
-    requests, wide = page_table.shape
-    if requests > 1 and page_table.stride(0) != wide:
-        raise KapError(ERR_INVALID_ARG, f"page_table has strides {page_table.stride()}: its rows must lie one behind the other")
-    _check_index("pages_held", pages_held, requests, dev)
-    _check_index("free_pages", free_pages, 0, dev)
-    _check_index("free_count", free_count, 1, dev)
+    i32, dev, shape = _I32, page_table.get_device(), page_table.shape
+    if dev < 0 or len(shape) != 2 or page_table.dtype is not i32 or not page_table.is_contiguous():
+        raise KapError(ERR_INVALID_ARG, f"page_table is {page_table.dtype} {tuple(shape)} with strides {page_table.stride()} on "
+                       f"{page_table.device}, expected a contiguous int32 [requests, pages] tensor on a GPU")
+    requests, wide = shape
+    if pages_held.dtype is not i32 or free_pages.dtype is not i32 or free_count.dtype is not i32 or pages_held.get_device() != dev or \
+            free_pages.get_device() != dev or free_count.get_device() != dev or not pages_held.is_contiguous() or \
+            not free_pages.is_contiguous() or pages_held.numel() < requests or free_count.numel() < 1:
+        _check_index("pages_held", pages_held, requests, dev)
+        _check_index("free_pages", free_pages, 0, dev)
+        _check_index("free_count", free_count, 1, dev)
     return requests, wide, dev
 
 
@@ -561,21 +562,39 @@ def build_block_tables(ctx_len, page_table, pages_held, free_pages, free_count, 
     from free_pages[:free_count].  page_table [requests, pages], pages_held [requests], free_pages and free_count [1] are kept up to
     date; new_indptr [batch + 1], slot and position [rows] are optional."""
     requests, wide, dev = _page_state(page_table, pages_held, free_pages, free_count)
-    batch = ctx_len.shape[0]
-    _check_index("ctx_len", ctx_len, batch, dev)
-    _check_index("bt_indptr", bt_indptr, batch + 1, dev)
-    _check_index("bt_pages", bt_pages, 0, dev)
-    for name, t, least in (("n_new", n_new, batch), ("request", request, batch), ("new_indptr", new_indptr, batch + 1),
-                           ("position", position, 0), ("device_status", device_status, 1)):
-        if t is not None:
-            _check_index(name, t, least, dev)
-    if slot is not None and (slot.dtype is not _torch.int64 or slot.get_device() != dev or not slot.is_contiguous()):
-        raise KapError(ERR_INVALID_ARG, f"slot is {slot.dtype} with strides {slot.stride()} on {slot.device}, expected a contiguous int64 tensor on GPU {dev}")
-    rows = [t.numel() for t in (slot, position) if t is not None]
+    batch, lists = ctx_len.shape[0], bt_pages.numel()
+    if ctx_len.dtype is not _I32 or bt_indptr.dtype is not _I32 or bt_pages.dtype is not _I32 or ctx_len.get_device() != dev or \
+            bt_indptr.get_device() != dev or bt_pages.get_device() != dev or not ctx_len.is_contiguous() or \
+            not bt_indptr.is_contiguous() or not bt_pages.is_contiguous() or bt_indptr.numel() <= batch:
+        _check_index("ctx_len", ctx_len, batch, dev)
+        _check_index("bt_indptr", bt_indptr, batch + 1, dev)
+        _check_index("bt_pages", bt_pages, 0, dev)
+    n_new_at = request_at = new_at = slot_at = position_at = status_at = None
+    rows = -1
+    if n_new is not None:
+        _check_index("n_new", n_new, batch, dev)
+        n_new_at = n_new.data_ptr()
+    if request is not None:
+        _check_index("request", request, batch, dev)
+        request_at = request.data_ptr()
+    if new_indptr is not None:
+        _check_index("new_indptr", new_indptr, batch + 1, dev)
+        new_at = new_indptr.data_ptr()
+    if slot is not None:
+        if slot.dtype is not _torch.int64 or slot.get_device() != dev or not slot.is_contiguous():
+            raise KapError(ERR_INVALID_ARG, f"slot is {slot.dtype} with strides {slot.stride()} on {slot.device}, expected a contiguous int64 tensor on GPU {dev}")
+        slot_at, rows = slot.data_ptr(), slot.numel()
+    if position is not None:
+        _check_index("position", position, 0, dev)
+        position_at, n = position.data_ptr(), position.numel()
+        rows = n if rows < 0 or n < rows else rows
+    if device_status is not None:
+        _check_index("device_status", device_status, 1, dev)
+        status_at = device_status.data_ptr()
     _check(lib().kap_build_block_tables(
-        _dptr(request), ctx_len.data_ptr(), _dptr(n_new), batch, page_size, page_table.data_ptr(), requests, wide, pages_held.data_ptr(),
-        free_pages.data_ptr(), free_pages.numel(), free_count.data_ptr(), bt_indptr.data_ptr(), bt_pages.data_ptr(), bt_pages.numel(),
-        _dptr(new_indptr), _dptr(slot), _dptr(position), min(rows) if rows else 0, _dptr(device_status), _stream_on(dev, stream)))
+        request_at, ctx_len.data_ptr(), n_new_at, batch, page_size, page_table.data_ptr(), requests, wide, pages_held.data_ptr(),
+        free_pages.data_ptr(), free_pages.numel(), free_count.data_ptr(), bt_indptr.data_ptr(), bt_pages.data_ptr(), lists,
+        new_at, slot_at, position_at, max(rows, 0), status_at, _stream_on(dev, stream)))
 
 
 def release_pages(request, page_table, pages_held, free_pages, free_count, keep_tokens=None, page_size=16, device_status=None,
@@ -583,13 +602,20 @@ def release_pages(request, page_table, pages_held, free_pages, free_count, keep_
     """kap_release_pages on torch CUDA tensors: the pages of the requests beyond keep_tokens (None: all) go back to the
     stack; request None names every row of page_table."""
     requests, wide, dev = _page_state(page_table, pages_held, free_pages, free_count)
-    n = requests if request is None else request.numel()
-    for name, t, least in (("request", request, n), ("keep_tokens", keep_tokens, n), ("device_status", device_status, 1)):
-        if t is not None:
-            _check_index(name, t, least, dev)
+    n, request_at, keep_at, status_at = requests, None, None, None
+    if request is not None:
+        n = request.numel()
+        _check_index("request", request, n, dev)
+        request_at = request.data_ptr()
+    if keep_tokens is not None:
+        _check_index("keep_tokens", keep_tokens, n, dev)
+        keep_at = keep_tokens.data_ptr()
+    if device_status is not None:
+        _check_index("device_status", device_status, 1, dev)
+        status_at = device_status.data_ptr()
     _check(lib().kap_release_pages(
-        _dptr(request), n, _dptr(keep_tokens), page_size, page_table.data_ptr(), requests, wide, pages_held.data_ptr(), free_pages.data_ptr(),
-        free_pages.numel(), free_count.data_ptr(), _dptr(device_status), _stream_on(dev, stream)))
+        request_at, n, keep_at, page_size, page_table.data_ptr(), requests, wide, pages_held.data_ptr(), free_pages.data_ptr(),
+        free_pages.numel(), free_count.data_ptr(), status_at, _stream_on(dev, stream)))
 
 
 def _head_rows(name, t, rows, heads, d, dev):
@@ -688,6 +714,7 @@ def _append_rope(norm, q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, i
         _check_index("position_offset", position_offset, batch, dev)
     if device_status is not None:
         _check_index("device_status", device_status, 1, dev)
+    middle = () if norm is None else _norm_arguments(norm, Hq, Hkv, d, dev)
     first = (_dptr(q), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, _dptr(q_out), os_, _dptr(new_indptr), rows)
     rest = (inv_freq.data_ptr(), rot, 1 if interleaved else 0, _dptr(positions), pos_stride, axes, axis,
             _dptr(position_offset), kv_pool.data_ptr(), pages, bt_indptr.data_ptr(), bt_pages.data_ptr(),
@@ -696,7 +723,7 @@ def _append_rope(norm, q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, i
     if norm is None:
         _check(lib().kap_append_kv_rope(*first, *rest))
     else:
-        _check(lib().kap_append_kv_norm_rope(*first, *_norm_arguments(norm, Hq, Hkv, d, dev), *rest))
+        _check(lib().kap_append_kv_norm_rope(*first, *middle, *rest))
 
 
 def adjust_logits(logits, out=None, history=None, history_at=None, repetition=None, presence=None, frequency=None, bias_indptr=None,

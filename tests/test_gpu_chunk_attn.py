@@ -82,10 +82,12 @@ class Case:
             self.ws.check()
         return out, lse
 
-    def expected(self, b):
-        """out, lse and the weighted mean of |V| of sequence b in 64 bits"""
-        n, length, G = int(self.n_q[b]), int(self.ctx[b]), self.hq // self.hkv
-        t = torch.arange(length, device=gu.DEV)
+    def expected(self, b, lo=0, hi=None):
+        """out, lse and the weighted mean of |V| of rows lo .. hi - 1 of sequence b in 64 bits"""
+        G = self.hq // self.hkv
+        hi = int(self.n_q[b]) if hi is None else hi
+        n, length, first = hi - lo, int(self.ctx[b]) - int(self.n_q[b]) + hi, int(self.q_indptr[b]) + lo
+        t = torch.arange(max(length, 0), device=gu.DEV)
         if self.window:
             t = t[(t < self.sink) | (t > length - n - self.window)]
         p = torch.arange(length - n, length, device=gu.DEV)
@@ -94,7 +96,7 @@ class Case:
             sees &= (t[None] > p[:, None] - self.window) | (t[None] < self.sink)
         entry = torch.from_numpy(self.bt[self.bt_indptr[b]:self.bt_indptr[b + 1]].astype(np.int64)).to(gu.DEV)
         kv = self.heads_first()[entry[t // PAGE], :, :, t % PAGE].double()          # [tokens, 2, Hkv, D]
-        q = self.q[int(self.q_indptr[b]):int(self.q_indptr[b + 1])].double().view(n, self.hkv, G, D)
+        q = self.q[first:first + n].double().view(n, self.hkv, G, D)
         z = torch.einsum("nhgd,thd->hgnt", q, kv[:, 0]) * self.scale
         z = torch.where(sees, z, -torch.inf)
         lse = torch.logsumexp(z, -1)
@@ -102,12 +104,17 @@ class Case:
         flat = lambda x: x.permute(2, 0, 1, *range(3, x.dim())).reshape(n, self.hq, *x.shape[3:])     # noqa: E731
         return [flat(x) for x in (torch.einsum("hgnt,thd->hgnd", w, kv[:, 1]), lse, torch.einsum("hgnt,thd->hgnd", w, kv[:, 1].abs()))]
 
-    def check(self, out, lse, only=None):
+    def check(self, out, lse, only=None, rows=None):
+        """rows: so many rows at a time, the first, the last and some between"""
+        parts = []
         for b in range(len(self.n_q)) if only is None else only:
-            if not self.n_q[b]:
-                continue
-            rows = slice(int(self.q_indptr[b]), int(self.q_indptr[b + 1]))
-            o, l, size = self.expected(b)
+            n = int(self.n_q[b])
+            starts = [0] if rows is None or n <= rows else [0, n - rows] + list(range(rows, n - rows, max(rows, n // 5)))
+            parts += [(b, lo, min(n, lo + (rows or n))) for lo in starts if n]
+        for b, lo, hi in parts:
+            first = int(self.q_indptr[b])
+            rows = slice(first + lo, first + hi)
+            o, l, size = self.expected(b, lo, hi)
             bound = 2.0 ** -8 * (size + o.abs()) + 2e-4 * self.hot * size + 1e-30
             err = (out[rows].double() - o).abs()
             assert bool((err <= bound).all()), f"sequence {b}: {int((err > bound).sum())} values off, worst {float((err / bound).max())} of the bound"
@@ -178,6 +185,24 @@ def test_scales():
         c = Case(9, [(70, 300), (1, 500)], 8, 2, scale=scale)
         c.hot = max(1.0, scale / D ** -0.5)
         c.check(*c.call())
+
+
+# A sequence alone behind a context whose K and V are too much for the caches is divided differently (all CTAs walk it together): from 48 MiB on, 8 KV
+# heads that is 12288 tokens, and with at least eight tokens for each row.
+@pytest.mark.parametrize("n,ctx,hq,hkv,window,sink", [
+    (70, 12300, 32, 8, 0, 0),          # 2 tiles a head, 16 units: none whole
+    (1100, 13001, 32, 8, 0, 0),        # 18 tiles, 144 units
+    (1500, 12777, 32, 8, 0, 0),        # 24 tiles, 192 units: one round of whole units, 44 cut
+    (300, 20001, 8, 8, 13000, 21),     # through a window of that size
+    (513, 13000, 64, 8, 0, 0),         # 17 tiles, 136 units, the last tile one row
+    (40, 100003, 16, 1, 0, 0),
+])
+def test_a_long_context_that_all_walk_together(n, ctx, hq, hkv, window, sink):
+    for layout in (HND, NHD):
+        c = Case(30, [(0, 100), (n, ctx), (0, 0)], hq, hkv, layout, window=window, sink=sink, before=1)
+        out, lse = c.call()
+        # in pieces: the whole in 64 bits would not fit
+        c.check(out, lse, rows=40 if ctx * hq > 200000 else None)
 
 
 def test_agrees_with_verify_attn():
