@@ -4,10 +4,12 @@
 // Mathematics, for token t of a row with logit x: c = times t occurs in the answer so far, s = t occurs in the prompt or the answer,
 //     x1 = s ? (x > 0 ? x / r : x r) : x,   x2 = x1 - f c - p [c > 0],   x3 = x2 + bias_t,   out = allowed_t ? x3 : -inf,
 // in fp32, rounded to the logits' type once.
-// Layout: a cluster of CTAs per row; CTA i owns the i-th slice of the vocabulary and keeps a 32-bit word for each of its tokens in shared
-// memory (times in the answer; whether in the prompt; whether it has a bias).  The history is dealt out over the cluster and counted in the
-// owners' words through distributed shared memory, read once; the owner then passes over its slice once, logits and words together.
-// Its first logits are loaded before the history is counted.  Tokens with a bias are left to the biases' pass.
+// Layout: a row is cut into slices of the vocabulary, a CTA each.  The CTA keeps a 32-bit word for each of its tokens in shared memory (times in the
+// answer; whether in the prompt; whether it has a bias), reads the row's whole history and counts the tokens that are its own, and then passes over its slice
+// once, logits, words and mask together; its first logits are loaded before the history is counted.  Tokens with a bias are left to the biases' pass.
+// Bound: memory without a history (512 rows of 128256: 80 us, a plain copy's rate).  A history of 2000 to 4000 tokens a row makes it 118 us: 40 of the 82
+// million warp instructions are its words' (cleared, counted, found and corrected).  Words in a cluster's shared memory, the history dealt out: 210 us, since
+// frequent tokens meet at one address; a list of touched words corrected after the copy: 158, since their logits are then waited for once more.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -49,7 +51,7 @@ template <> __device__ __forceinline__ uint4 minus_inf_vector<__nv_bfloat16>() {
 struct Rules { float repetition, presence, frequency; };
 __device__ __forceinline__ float penalised(float x, uint32_t word, const Rules& r) {
     const uint32_t c = word & kCountMask;
-    if (word & (kInPrompt | kCountMask)) x = x > 0.f ? __fdiv_rn(x, r.repetition) : x * r.repetition;
+    if (word & ~kHasBias) x = x > 0.f ? __fdiv_rn(x, r.repetition) : x * r.repetition;
     if (c) x = x - r.frequency * (float)c - r.presence;
     return x;
 }
@@ -155,58 +157,100 @@ kap_adjust_logits_kernel(const LogitParams p)
 #pragma unroll 4
         for (int i = tid; i < head; i += kLogitThreads) single(v0 + i);
         for (int i = v0 + head + n_vec * kVec + tid; i < v1; i += kLogitThreads) single(i);
-        auto vector = [&](int i, uint4 x, bool loaded) {
-            const int t = v0 + head + i * kVec;
-            uint32_t open = (1u << kVec) - 1u;
-            if (q.mask) {
-                const int w = t >> 5, k = t & 31;
-                open = __ldg(q.mask + w) >> k;
-                if (k + kVec > 32) open |= __ldg(q.mask + w + 1) << (32 - k);
-                open &= (1u << kVec) - 1u;
-            }
-            if (open == 0u) { dst[i] = minus_inf_vector<T>(); return; }
-            uint32_t w[kVec], any = 0u;
-            if (counted) {
+        // The words of a vector, as a bit for each that is not 0; what has a bias is left alone.
+        auto find = [&](int i, uint32_t (&w)[kVec], uint32_t& left) {
+            uint32_t hits = 0u;
+            left = 0u;
 #pragma unroll
-                for (int j = 0; j < kVec; j += 4) {
-                    const uint4 z = *reinterpret_cast<const uint4*>(words + (t - v0) + j);
-                    w[j] = z.x; w[j + 1] = z.y; w[j + 2] = z.z; w[j + 3] = z.w;
-                    any |= z.x | z.y | z.z | z.w;
-                }
+            for (int j = 0; j < kVec; j += 4) {
+                const uint4 z = *reinterpret_cast<const uint4*>(words + head + i * kVec + j);
+                w[j] = z.x; w[j + 1] = z.y; w[j + 2] = z.z; w[j + 3] = z.w;
             }
-            if (any == 0u && open == (1u << kVec) - 1u) {
-                if (!in_place) __stcs(dst + i, x);
-                return;
-            }
-            if (!loaded) x = src[i];
-            T* e = reinterpret_cast<T*>(&x);
-            bool leave = false;
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) hits |= w[j];
+            if (hits == 0u) return 0u;
+            hits = 0u;
 #pragma unroll
             for (int j = 0; j < kVec; ++j) {
-                if (!(open >> j & 1u)) e[j] = from_float<T>(-INFINITY);
-                else if (any && (w[j] & kHasBias)) leave = true;
-                else if (any && w[j]) e[j] = from_float<T>(penalised(to_float(e[j]), w[j], q.r));
+                hits |= (w[j] & ~kHasBias ? 1u : 0u) << j;
+                left |= (w[j] >> 31) << j;
             }
-            if (!leave) { dst[i] = x; return; }
+            return hits & ~left;
+        };
+        auto correct = [&](uint4& x, const uint32_t (&w)[kVec], uint32_t hits) {
+            // most lanes have one, but not the same one: a turn of the loop for each, not a case for each place
+            T* e = reinterpret_cast<T*>(&x);
+            while (hits) {
+                const int at = __ffs(hits) - 1;
+                hits &= hits - 1u;
+                float v = 0.f;
+                uint32_t word = 0u;
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+                    if (j == at) { v = to_float(e[j]); word = w[j]; }
+                const T y = from_float<T>(penalised(v, word, q.r));
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+                    if (j == at) e[j] = y;
+            }
+        };
+        auto store = [&](int i, const uint4& x, uint32_t left) {
+            if (left == 0u) { __stcs(dst + i, x); return; }
+            const T* e = reinterpret_cast<const T*>(&x);
+            const int t = v0 + head + i * kVec;
 #pragma unroll
             for (int j = 0; j < kVec; ++j)
-                if (!(open >> j & 1u) || !(w[j] & kHasBias)) out[t + j] = e[j];
+                if (!(left >> j & 1u)) out[t + j] = e[j];
         };
-        if (!in_place) {
+        if (!q.mask) {
+            auto vector = [&](int i, uint4 x) {
+                uint32_t left = 0u;
+                if (counted) {
+                    uint32_t w[kVec];
+                    const uint32_t hits = find(i, w, left);
+                    if (in_place) {
+                        if (hits == 0u) return;
+                        x = src[i];
+                    }
+                    correct(x, w, hits);
+                }
+                store(i, x, left);
+            };
+            if (in_place) {
+                for (int i = tid; i < n_vec; i += kLogitThreads) vector(i, make_uint4(0u, 0u, 0u, 0u));
+            } else {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k)
-                if (tid + k * kLogitThreads < n_vec) vector(tid + k * kLogitThreads, ahead[k], true);
-            int i = tid + kAhead * kLogitThreads;
-            for (; i + (kAhead - 1) * kLogitThreads < n_vec; i += kAhead * kLogitThreads) {
-                uint4 x[kAhead];
+                for (int k = 0; k < kAhead; ++k)
+                    if (tid + k * kLogitThreads < n_vec) vector(tid + k * kLogitThreads, ahead[k]);
+                int i = tid + kAhead * kLogitThreads;
+                for (; i + (kAhead - 1) * kLogitThreads < n_vec; i += kAhead * kLogitThreads) {
+                    uint4 x[kAhead];
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) x[k] = __ldcs(src + i + k * kLogitThreads);
+                    for (int k = 0; k < kAhead; ++k) x[k] = __ldcs(src + i + k * kLogitThreads);
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) vector(i + k * kLogitThreads, x[k], true);
+                    for (int k = 0; k < kAhead; ++k) vector(i + k * kLogitThreads, x[k]);
+                }
+                for (; i < n_vec; i += kLogitThreads) vector(i, __ldcs(src + i));
             }
-            for (; i < n_vec; i += kLogitThreads) vector(i, __ldcs(src + i), true);
         } else {
-            for (int i = tid; i < n_vec; i += kLogitThreads) vector(i, make_uint4(0u, 0u, 0u, 0u), false);
+            constexpr uint32_t kAllOpen = (1u << kVec) - 1u;
+            for (int i = tid; i < n_vec; i += kLogitThreads) {
+                const int t = v0 + head + i * kVec, word = t >> 5, k = t & 31;
+                uint32_t open = __ldg(q.mask + word) >> k;
+                if (k + kVec > 32) open |= __ldg(q.mask + word + 1) << (32 - k);
+                open &= kAllOpen;
+                if (open == 0u) { __stcs(dst + i, minus_inf_vector<T>()); continue; }       // (nothing is read)
+                uint32_t w[kVec], left = 0u, hits = counted ? find(i, w, left) & open : 0u;
+                left &= open;
+                if (open == kAllOpen && hits == 0u && in_place) continue;
+                uint4 x = src[i];
+                T* e = reinterpret_cast<T*>(&x);
+                correct(x, w, hits);
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+                    if (!(open >> j & 1u)) e[j] = from_float<T>(-INFINITY);
+                store(i, x, left);
+            }
         }
     }
     if (q.b1 > q.b0) {
@@ -284,8 +328,8 @@ extern "C" kap_status kap_adjust_logits(
     const bool needs_words = history && (repetition || presence || frequency);
     if (!needs_words) p.history = nullptr;
     // Slices of at most 16384 tokens (64 KiB of words: three CTAs on an SM), and of fewer where there are rows too few to fill the device: every CTA of a
-    // row reads its whole history, so no more than that (512 rows of 128256, histories of 2000 to 4000: 8 slices 135 us, 16 167; one row
-    // with 20000: 8 slices 14 us, 64 7.6).
+    // row reads its whole history, so no more than that (512 rows of 128256, histories of 2000 to 4000: 8 slices 118 us, 10 120, 12
+    // 123; one row with 20000: 8 slices 14 us, 64 8).
     constexpr int kOneWave = 148 * 3, kMostSlices = 64;
     const int least = (vocab + 16383) / 16384;
     int slices = least < kMostSlices ? (kOneWave / rows < least ? least : kOneWave / rows > kMostSlices ? kMostSlices : kOneWave / rows) : least;
