@@ -36,6 +36,9 @@ constexpr int kChunkSoftmaxWarps = 8;                                 // 4 a str
 constexpr int kChunkThreads = 32 * (kChunkSoftmaxWarps + 4);
 constexpr int kChunkTileRows = 128;                                    // query rows of one tile (TMEM lanes)
 constexpr int kChunkUnitRows = 2 * kChunkTileRows;
+// Solo units of up to 64 rows use products of 64 rows, which take half the energy, and single tokens run into the board's power limit, too (windowed batch
+// sustained 970 us, with 128 rows 1040).  Row r of such a tile is lane r % 16 of the quarter r / 16.
+constexpr int kChunkSmallRows = 64;
 constexpr int kChunkStepPages = 5;
 constexpr int kChunkStepTokens = kChunkStepPages * kPageSize;          // 80
 constexpr int kChunkSlots = 8;                                         // step n: K in slot 2 n, V in slot 2 n + 1 (mod 8)
@@ -551,7 +554,6 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
         // ---- tensor core: an issuer for each stream, so that neither waits for the other's softmax: S of its next step, then O += P V of the one
         // before.  One elected lane runs through a whole segment, waits included, with warp-uniform operands.  Both arrive on a tile's
         // free barrier, with their products or, where the tile is not theirs, as soon as it is there (its last use is then over).
-        constexpr uint32_t idesc_o = umma_idesc(kChunkTileRows, kHeadDim, true);
         const int t = warp - (kChunkSoftmaxWarps + 1);
         const uint64_t q_desc = umma_smem_desc(smem_u32(q_tiles), 16, 1024), k_desc = umma_smem_desc(smem_u32(slots), 16, kChunkGroupBytes);
         // V: 16 tokens (K) x 128 columns (N), N contiguous; columns 64-127 in the other half of a group
@@ -566,6 +568,8 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
             const int pair = rows > kChunkTileRows ? 1 : 0, stride = pair ? 1 : 2, first = pair ? 0 : t;       // this stream's steps
             if (n_steps <= 0) continue;
             const int base = step0, work0 = count, q_at = pair ? t : q_slot;
+            const uint32_t idesc_o = rows <= kChunkSmallRows ? umma_idesc(kChunkSmallRows, kHeadDim, true) : umma_idesc(kChunkTileRows, kHeadDim, true);
+            const uint32_t idesc_page = rows <= kChunkSmallRows ? umma_idesc(kChunkSmallRows, kPageSize, false) : umma_idesc(kChunkTileRows, kPageSize, false);
             if (elect_one()) {
                 auto slot_of = [&](int j) { return 2 * ((base + j) % (kChunkSlots / 2)); };
                 auto phase_of = [&](int j) { return (uint32_t)((base + j) / (kChunkSlots / 2)) & 1u; };
@@ -581,7 +585,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                     tc_fence_after();
                     const uint64_t q = q_desc + (uint32_t)q_at * (kChunkQBytes / 16), kd = k_desc + (uint32_t)slot * (kChunkSlotBytes / 16);
                     const int pages = min(kChunkStepPages, n_pages - j * kChunkStepPages);
-                    const uint32_t idesc_s = umma_idesc(kChunkTileRows, kPageSize, false) + ((uint32_t)(pages - 1) * (kPageSize >> 3) << 17);
+                    const uint32_t idesc_s = idesc_page + ((uint32_t)(pages - 1) * (kPageSize >> 3) << 17);
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
                         umma_ss(tmem + t * 256, q + ((ks >> 2) * kChunkQHalfBytes + (ks & 3) * 32) / 16,
@@ -632,7 +636,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
         }
     } else if (warp < kChunkSoftmaxWarps) {
         // ---- softmax: stream = warp group, one query row per thread
-        const int stream = warp >> 2, r = (warp & 3) * 32 + lane;
+        const int stream = warp >> 2;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + stream * 256, t_p = t_s + kChunkTmemP, t_o = t_s + kChunkTmemO;
         const float sc = p.scale_log2;
         for (int k = 0; k < n_segments; ++k) {
@@ -641,8 +645,9 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
             const int rows = seg.rows_head & 0xffff, kv_head = seg.rows_head >> 16;
             const bool pair = rows > kChunkTileRows;
             const int n_steps = seg.step_end - seg.step_begin;
-            const int tile = pair ? stream : 0, R = tile * kChunkTileRows + r;
-            const bool valid = R < rows, any_valid = tile * kChunkTileRows + (warp & 3) * 32 < rows;
+            const bool small = rows <= kChunkSmallRows;
+            const int first_row = (pair ? stream * kChunkTileRows : 0) + (warp & 3) * (small ? 16 : 32), R = first_row + lane;
+            const bool valid = R < rows && (!small || lane < 16), any_valid = first_row < rows;
             // The row sees tokens [0, sink_end) and [from, to), counted along the segment's pages
             int sink_end = 0, from = 0, to = 0;
             const int hi = seg.lo + (rows >> p.log2_g) - 1;
