@@ -90,8 +90,9 @@ struct ChunkShared {
     ChunkControl c;
     alignas(16) ChunkSegment segments[kChunkMaxSegments];
 };
-constexpr int kChunkSmemBytes = 2 * kChunkQBytes + kChunkSlots * kChunkSlotBytes + 3072;
-static_assert(sizeof(ChunkShared) <= 3072 && kChunkSmemBytes <= 232448, "shared memory");
+constexpr int kChunkCtlBytes = 3 * 1024;
+constexpr int kChunkSmemBytes = 2 * kChunkQBytes + kChunkSlots * kChunkSlotBytes + kChunkCtlBytes;
+static_assert(sizeof(ChunkShared) <= kChunkCtlBytes && kChunkSmemBytes <= 232448, "shared memory");
 
 struct ChunkParams {
     const int32_t *q_indptr, *bt_indptr, *bt_pages, *ctx_len;
