@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kTableThreads = 1024, kFewThreads = 128;        // of the first kernel, for batches of up to 128 sequences the second number
 constexpr int kFillThreads = 256, kFillEntries = 2048;
+constexpr long long kMostEntries = INT32_MAX - kFillEntries;  // of a step's block table, and rows: the second kernel counts past them in 32 bits
 constexpr int32_t kMaxRequests = 1 << 20;                     // a bit each in the first kernel's shared memory
 
 struct TableParams {
@@ -36,7 +37,7 @@ __device__ __forceinline__ Entry load_entry(const TableParams& p, int b, uint32_
     e.request = p.request ? p.request[b] : b;
     const int L = p.ctx_len ? p.ctx_len[b] : 0;
     e.n = kRelease ? 0 : p.n_new ? p.n_new[b] : 1;
-    if (e.request < 0 || e.request >= p.num_requests || L < 0 || e.n < 0) { e.bad = true; e.n = 0; return e; }
+    if (e.request < 0 || e.request >= p.num_requests || L < 0 || e.n < 0 || L > INT32_MAX - e.n) { e.bad = true; e.n = 0; return e; }
     e.held = p.pages_held[e.request];
     if (seen) e.bad = atomicOr(&seen[e.request >> 5], 1u << (e.request & 31)) >> (e.request & 31) & 1u;   // named twice
     if (e.held < 0 || e.held > p.table_stride) { e.bad = true; e.held = 0; }
@@ -251,8 +252,8 @@ extern "C" kap_status kap_build_block_tables(
     p.request = request; p.ctx_len = ctx_len; p.n_new = n_new; p.page_table = page_table; p.pages_held = pages_held;
     p.free_pages = free_pages; p.free_count = free_count; p.bt_indptr = bt_indptr; p.bt_pages = bt_pages; p.new_indptr = new_indptr;
     p.slot = reinterpret_cast<long long*>(slot); p.position = position; p.status = device_status;
-    p.table_stride = table_stride; p.bt_capacity = bt_capacity < INT32_MAX ? bt_capacity : INT32_MAX;
-    p.row_capacity = (slot || position) && row_capacity < INT32_MAX ? row_capacity : INT32_MAX;
+    p.table_stride = table_stride; p.bt_capacity = bt_capacity < kMostEntries ? bt_capacity : kMostEntries;
+    p.row_capacity = (slot || position) && row_capacity < kMostEntries ? row_capacity : kMostEntries;
     p.batch = batch; p.page_size = page_size; p.num_requests = num_requests; p.free_capacity = free_capacity;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     if (batch == 0) {                                         // an empty table
