@@ -21,6 +21,7 @@ void count_launch();
 namespace {
 
 constexpr int kLogitThreads = 512;
+constexpr int kMostSlice = 16384, kMostWords = kMostSlice + 8;            // tokens of a CTA's slice, and words for it
 constexpr uint32_t kInPrompt = 1u << 30, kHasBias = 1u << 31, kCountMask = kInPrompt - 1;
 
 struct LogitParams {
@@ -274,7 +275,8 @@ template <typename T>
 kap_status launch_logits(const LogitParams& p, int slices, size_t smem, cudaStream_t stream) {
     auto* kernel = kap_adjust_logits_kernel<T>;
     cudaError_t e = cudaSuccess;
-    if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // (always to the most that a call may need: another thread's call must not find less than it asked for)
+    if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostWords * 4);
     if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "cudaFuncSetAttribute failed: %s", cudaGetErrorString(e));
     kernel<<<dim3((unsigned)slices, (unsigned)p.rows), kLogitThreads, smem, stream>>>(p);
     e = cudaGetLastError();
@@ -331,7 +333,7 @@ extern "C" kap_status kap_adjust_logits(
     // row reads its whole history, so no more than that (512 rows of 128256, histories of 2000 to 4000: 8 slices 118 us, 10 120, 12
     // 123; one row with 20000: 8 slices 14 us, 64 8).
     constexpr int kOneWave = 148 * 3, kMostSlices = 64;
-    const int least = (vocab + 16383) / 16384;
+    const int least = (vocab + kMostSlice - 1) / kMostSlice;
     int slices = least < kMostSlices ? (kOneWave / rows < least ? least : kOneWave / rows > kMostSlices ? kMostSlices : kOneWave / rows) : least;
     p.slice = ((vocab + slices - 1) / slices + 31) / 32 * 32;
     slices = (vocab + p.slice - 1) / p.slice;

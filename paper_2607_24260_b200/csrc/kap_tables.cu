@@ -219,7 +219,8 @@ kap_status launch(const TableParams& p, cudaStream_t stream) {
     auto* kernel = few ? kap_tables_kernel<kRelease, kFewThreads> : kap_tables_kernel<kRelease, kTableThreads>;
     const size_t smem = (size_t)(p.num_requests + 31) / 32 * 4;
     if (smem > 32 * 1024) {                                   // with the kernel's own arrays more than the default 48 KiB
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        // (always to the most that a call may need: another thread's call must not find less than it asked for)
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRequests / 8);
         if (e != cudaSuccess) return fail(KAP_ERR_CUDA, "cudaFuncSetAttribute failed: %s", cudaGetErrorString(e));
     }
     kernel<<<1, few ? kFewThreads : kTableThreads, smem, stream>>>(p);

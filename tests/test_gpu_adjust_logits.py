@@ -259,6 +259,36 @@ def test_captured_and_on_another_stream():
     assert torch.equal(first, out)
 
 
+def test_calls_of_two_threads():
+    # calls that need different amounts of shared memory, from two threads at once: both kernels of the shared-memory sizes that have to be asked for
+    import threading
+    cases = [Case(51, 128, 128256, longest=60, biases=0), Case(52, 128, 100000, longest=60, biases=0)]
+    want = []
+    for c in cases:
+        c.arguments, c.stream = c.args(), torch.cuda.Stream()
+        want.append(kap.adjust_logits(c.logits, c.out, **c.arguments).clone())
+    torch.cuda.synchronize()
+    failed = []
+
+    def calls(c):
+        try:
+            torch.cuda.set_device(0)
+            for _ in range(300):
+                kap.adjust_logits(c.logits, c.out, **c.arguments, stream=c.stream)
+            c.stream.synchronize()
+        except Exception as e:                                                     # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=calls, args=(c,)) for c in cases]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    for c, w in zip(cases, want):
+        assert torch.equal(c.out, w)
+
+
 def test_refusals():
     c = Case(18, 3, 100, masks=2)
     a = c.args()
