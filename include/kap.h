@@ -733,7 +733,7 @@ kap_status kap_shared_prefix_attn(
  * One workspace serves one call at a time: calls, and graphs that hold them, which may run at the same time on two streams need a workspace
  * each.  Results do not depend on timing; a row's sums run in an order that depends on the whole batch's lengths.
  * Reported through kap_workspace_check (KAP_ERR_DEVICE_INDEX; results of that sequence are not defined): a page outside the pool, a
- * q_indptr that falls or leaves 0 .. total_rows, a negative ctx_len or one beyond the block table.
+ * q_indptr that falls or leaves 0 .. total_rows, a negative bt_indptr, a negative ctx_len or one beyond the block table or 67108864 tokens.
  * Errors: as kap_verify_attn (the workspace needs no schedule), plus KAP_ERR_CAPACITY for a workspace that is too small and
  * KAP_ERR_INVALID_ARG for a negative window or n_sink, a misaligned array, or an sm_scale that is not a positive number.
  */

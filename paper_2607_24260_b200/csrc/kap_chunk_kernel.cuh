@@ -50,6 +50,8 @@ constexpr int kChunkQHalfBytes = kChunkTileRows * 128;                 // 128 ro
 constexpr int kChunkQBytes = 2 * kChunkQHalfBytes;
 constexpr int kChunkTmemP = 80, kChunkTmemO = 128;                     // columns of a stream's 256; S from 0
 constexpr int kChunkMaxSegments = 72;                                  // planned at a time
+// A sequence's tokens: a whole unit of so many takes a CTA a second, half of what its waits may take, and steps stay far below the sentinel of chunk_in_step.
+constexpr int kChunkMostTokens = 1 << 26;
 // What a unit costs, to place the cuts and for nothing else: its tokens and, for the first products and the epilogue, some more, times 2 with two
 // tiles.  (Windowed batch 835 us, with 5 : 3 910, 3 : 1 895; whole prompts 259 us, with 320 tokens more 268, with 240 278.)
 constexpr int kChunkUnitCost = 400, kChunkPairCost = 2, kChunkSoloCost = 1;
@@ -69,6 +71,7 @@ struct ChunkInStep { int32_t pieces, n_cut, whole, seq; };
 constexpr int kChunkStates = 4;                                        // states a CTA, 256 rows each, that the workspace holds
 constexpr int kChunkMostPieces = 16, kChunkPieceCost = 8;              // cost of a piece beyond its steps (products to fill, state), in steps
 constexpr long long kChunkInStepBytes = 48ll << 20;
+static_assert(kChunkMostTokens / kChunkStepTokens + 10 * kChunkMostPieces < (INT32_MAX >> 8), "the sentinel of chunk_in_step");
 
 struct ChunkControl {
     unsigned long long full[kChunkSlots], free[kChunkSlots];
@@ -119,7 +122,7 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams& p, int b, bool&
     ChunkSeq s;
     s.row0 = min(max(r0, 0), p.total_rows);
     s.n = max(min(r1, p.total_rows) - s.row0, 0);
-    s.length = (int)min((long long)max(L, 0), listed);
+    s.length = l0 < 0 ? 0 : (int)min((long long)min(max(L, 0), kChunkMostTokens), listed);
     s.list_at = l0;
     bad = r0 != s.row0 || r1 != s.row0 + s.n || (s.n > 0 && L != s.length);      // (a sequence without rows may have any length)
     return s;
@@ -171,7 +174,7 @@ __device__ __forceinline__ void chunk_in_step(const ChunkParams& p, ChunkControl
         // the number of pieces that ends first
         const int k = lane + 1, rounds = (rest * k + n_cta - 1) / n_cta;
         int cost = k > kChunkMostPieces || rest * k > kChunkStates * n_cta ? INT32_MAX >> 8 : rounds * ((steps + k - 1) / k + (k > 1 ? kChunkPieceCost : 0));
-        cost = (cost << 5 | lane);                                     // (steps: below 2^23, tokens below 2^31 / 2)
+        cost = (cost << 5 | lane);                                     // (steps: below 2^20)
         v.pieces = (__reduce_min_sync(0xffffffffu, cost) & 31) + 1;
     }
     if (lane == 0) {

@@ -347,6 +347,36 @@ def test_bad_pages_and_lengths_are_reported():
         torch.cuda.synchronize()
 
 
+def _repeated(tokens, listed=None, hq=1, list0=0):
+    """one token after `tokens` - 1 others in a cache whose block table names one page again and again; keys 0, values 1, 2, 4, ..."""
+    pool = torch.zeros((2, 2, 1, PAGE, D), dtype=torch.bfloat16, device=gu.DEV)
+    value = 2.0 ** (torch.arange(D, device=gu.DEV) % 8)
+    pool[1, 1] = value.to(torch.bfloat16)
+    table = torch.ones((listed or tokens + PAGE - 1) // PAGE, dtype=torch.int32, device=gu.DEV)
+    q = torch.ones((1, hq, D), dtype=torch.bfloat16, device=gu.DEV)
+    out, lse = torch.full_like(q, float("nan")), torch.full((1, hq), float("nan"), device=gu.DEV)
+    ws = kap.Workspace(max_items=kap.chunk_attn_items(), max_rows_per_item=64, max_batch=1)
+    kap.chunk_attn(q, gu.i32([0, 1]), pool, gu.i32([list0, list0 + len(table)]), table, gu.i32([tokens]), out, ws, lse=lse)
+    return ws, out, lse, value
+
+
+def test_the_longest_context():
+    # weights of 1, whose partial sums are whole numbers below 2^24: only lse is rounded (a logarithm of 2^26, 18.02: three roundings of 2^-24 of it)
+    ws, out, lse, value = _repeated(2 ** 26)
+    ws.check()
+    assert torch.equal(out[0, 0].float(), value)
+    assert abs(float(lse[0, 0]) - 26 * np.log(2.0)) <= 4e-6
+
+
+@pytest.mark.parametrize("tokens,list0", [(2 ** 26 + 1, 0), (100, -1), (100, -2 ** 31)])
+def test_lengths_and_lists_that_are_not_followed(tokens, list0):
+    ws, *_ = _repeated(tokens, list0=list0)
+    with pytest.raises(kap.KapError) as e:
+        ws.check()
+    assert e.value.code == kap.ERR_DEVICE_INDEX
+    ws.check()
+
+
 def test_refusals():
     c = Case(22, [(4, 40)], 8, 2)
     small = kap.Workspace(max_items=10, max_rows_per_item=64, max_batch=4)
