@@ -726,6 +726,7 @@ kap_status kap_shared_prefix_attn(
  * with a window).  out and lse as kap_selected_decode_attn; a row that sees no token (p < 0) gets out = 0, lse = -inf.  Rows outside
  * q_indptr[0] .. q_indptr[batch] - 1 are left alone.  Pages that no row of a sequence sees are not read: their entries in bt_pages may
  * hold anything.  Every token below ctx_len in the pages that are read must hold finite K and V; what lies behind ctx_len may hold anything.
+ * A query with NaN gets NaN, and no other query is changed by it.
  *
  * No schedule: the work is divided on the device, from q_indptr and ctx_len as they are when the kernel runs, so a captured call serves
  * steps of any lengths within total_rows.  Of the workspace the partial buffer of max_items * max_rows_per_item rows is used (a

@@ -770,7 +770,8 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                 const bool own = mine > 0, both = !pair && n_steps > 1, have = pair ? own : n_steps > 0;
                 const uint32_t t_first = pair ? t_o : t_lane + kChunkTmemO, t_second = t_lane + 256 + kChunkTmemO;
                 const float f0 = pair || stream == 0 ? factor0 : factor1, f1 = stream == 0 ? factor1 : factor0;
-                const float inv = seg.slot >= 0 ? 1.f : l > 0.f ? 1.f / l : 0.f;
+                const bool empty = l == 0.f;                           // (the sum of a query that is not finite is NaN, and so is its result)
+                const float inv = seg.slot >= 0 ? 1.f : empty ? 0.f : 1.f / l;
                 const int tok = seg.tok0 + (R >> p.log2_g), h = (kv_head << p.log2_g) + (R & (p.G - 1));
                 const long long cell = (long long)tok * p.hq + h, state = (long long)seg.slot * kChunkUnitRows + R;
 #pragma unroll 1
@@ -797,7 +798,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                     if (valid && seg.slot < 0) {
                         uint32_t v[16];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) v[e] = l > 0.f ? pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv) : 0u;
+                        for (int e = 0; e < 16; ++e) v[e] = empty ? 0u : pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
                         __nv_bfloat16* dst = p.out + cell * kHeadDim + i;
                         if (p.wide_out) {                              // (every lane has a row of its own: the fewer instructions, the better)
                             store_32b(dst, &v[0]);
@@ -814,7 +815,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                 }
                 if (valid && (pair || stream == 0)) {
                     if (seg.slot >= 0) *reinterpret_cast<float2*>(p.part_ml + state * 2) = make_float2(m_ref, l);
-                    else if (p.lse) p.lse[cell] = l > 0.f ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                    else if (p.lse) p.lse[cell] = empty ? -INFINITY : (m_ref + log2f(l)) * 0.6931471805599453f;
                 }
             }
             tc_fence_before();                                         // O has been read: the next segment's products may replace it
@@ -875,15 +876,15 @@ __device__ __forceinline__ void chunk_merge_row(const ChunkParams& p, const Chun
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
-            if (i0 + j < of.n && ml[j].y > 0.f) merge_into(acc, ml[j].x, ml[j].y, o[j]);
+            if (i0 + j < of.n && ml[j].y != 0.f) merge_into(acc, ml[j].x, ml[j].y, o[j]);
     }
     const long long cell = (long long)(tok0 + (R >> p.log2_g)) * p.hq + (head << p.log2_g) + (R & (p.G - 1));
-    const float inv = acc.l > 0.f ? 1.f / acc.l : 0.f;
+    const float inv = acc.l == 0.f ? 0.f : 1.f / acc.l;
     uint2 v;
     v.x = pack_bf16(acc.o.x * inv, acc.o.y * inv);
     v.y = pack_bf16(acc.o.z * inv, acc.o.w * inv);
     *reinterpret_cast<uint2*>(p.out + cell * kHeadDim + lane * 4) = v;
-    if (p.lse && lane == 0) p.lse[cell] = acc.l > 0.f ? (acc.m + log2f(acc.l)) * 0.6931471805599453f : -INFINITY;
+    if (p.lse && lane == 0) p.lse[cell] = acc.l == 0.f ? -INFINITY : (acc.m + log2f(acc.l)) * 0.6931471805599453f;
 }
 
 // Many rows: most are in units that one CTA finished.  Block (c, part): 32 rows of the unit in which CTA c begins, if no CTA before it begins in its

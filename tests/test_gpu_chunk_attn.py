@@ -347,6 +347,22 @@ def test_bad_pages_and_lengths_are_reported():
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("sequences,hq,hkv", [([(300, 700), (1, 5000), (40, 40)], 8, 2), ([(50, 4000)], 8, 2), ([(150, 150)], 2, 2), ([(1, 20000)], 16, 1)])
+def test_a_query_with_nan_gets_nan_alone(sequences, hq, hkv):
+    # in units of one CTA and in cut ones, of a pair, of one tile and of 64 rows
+    c = Case(33, sequences, hq, hkv)
+    good, good_lse = c.call()
+    rows = torch.tensor([int(c.q_indptr[b]) + int(n) - 1 for b, (n, _) in enumerate(sequences)] + [int(c.q_indptr[0])], device=gu.DEV)
+    c.q[rows, 1, 5] = float("nan")
+    out, lse = c.call()
+    hit = torch.zeros(c.rows, hq, dtype=torch.bool, device=gu.DEV)
+    hit[rows, 1] = True
+    assert bool(out[hit].isnan().all()) and bool(lse[hit].isnan().all())
+    used = slice(int(c.q_indptr[0]), int(c.q_indptr[-1]))
+    keep = ~hit[used]
+    assert torch.equal(out[used][keep], good[used][keep]) and torch.equal(lse[used][keep], good_lse[used][keep])
+
+
 def _repeated(tokens, listed=None, hq=1, list0=0):
     """one token after `tokens` - 1 others in a cache whose block table names one page again and again; keys 0, values 1, 2, 4, ..."""
     pool = torch.zeros((2, 2, 1, PAGE, D), dtype=torch.bfloat16, device=gu.DEV)
