@@ -69,9 +69,9 @@ __device__ __forceinline__ LogitRow load_row(const LogitParams& p, int row, bool
     LogitRow v;
     const float rep = p.repetition ? p.repetition[row] : 1.f, pres = p.presence ? p.presence[row] : 0.f, freq = p.frequency ? p.frequency[row] : 0.f;
     v.h0 = v.h1 = v.h2 = 0;
-    if (p.history) { v.h0 = p.history_at[row * 3ll]; v.h1 = p.history_at[row * 3ll + 1]; v.h2 = p.history_at[row * 3ll + 2]; }
-    v.b0 = p.bias_token ? p.bias_indptr[row] : 0;
-    v.b1 = p.bias_token ? p.bias_indptr[row + 1] : 0;
+    if (p.history_at) { v.h0 = p.history_at[row * 3ll]; v.h1 = p.history_at[row * 3ll + 1]; v.h2 = p.history_at[row * 3ll + 2]; }
+    v.b0 = p.bias_indptr ? p.bias_indptr[row] : 0;
+    v.b1 = p.bias_indptr ? p.bias_indptr[row + 1] : 0;
     const int m = !p.allowed ? -1 : p.allowed_row ? p.allowed_row[row] : row;
     bool bad = false;
     v.r.repetition = rep > 0.f ? rep : 1.f;
@@ -305,11 +305,12 @@ extern "C" kap_status kap_adjust_logits(
     if (rows == 0) return KAP_OK;
     if (!logits || !out) return fail(KAP_ERR_INVALID_ARG, "NULL logits or out");
     if (logits == out && row_stride != out_stride) return fail(KAP_ERR_INVALID_ARG, "in place, but with two row strides");
-    if (history_len < 0 || (history && !history_at)) return fail(KAP_ERR_INVALID_ARG, "history needs history_at and a length");
-    if (!history && (repetition || presence || frequency)) return fail(KAP_ERR_INVALID_ARG, "penalties need the history");
-    if ((bias_token != nullptr) != (bias_indptr != nullptr) || (bias_token != nullptr) != (bias_value != nullptr))
-        return fail(KAP_ERR_INVALID_ARG, "biases need bias_indptr, bias_token and bias_value");
+    if (history_len < 0 || (history && !history_at) || (history_at && !history && history_len > 0)) return fail(KAP_ERR_INVALID_ARG, "history needs history_at and a length");
+    if (!history_at && (repetition || presence || frequency)) return fail(KAP_ERR_INVALID_ARG, "penalties need the history");
     if (bias_len < 0) return fail(KAP_ERR_INVALID_ARG, "bias_len %lld", (long long)bias_len);
+    // (a list without entries needs no address)
+    if (bias_indptr ? bias_len > 0 && (!bias_token || !bias_value) : bias_len > 0 || bias_token || bias_value)
+        return fail(KAP_ERR_INVALID_ARG, "biases need bias_indptr, bias_token and bias_value");
     if (allowed ? num_masks < 1 || allowed_stride < (vocab + 31) / 32 : allowed_row != nullptr)
         return fail(KAP_ERR_INVALID_ARG, "%d masks of %lld words for %d logits", num_masks, (long long)allowed_stride, vocab);
     if (allowed && !allowed_row && num_masks < rows) return fail(KAP_ERR_INVALID_ARG, "%d masks for %d rows: allowed_row is needed", num_masks, rows);
@@ -327,8 +328,8 @@ extern "C" kap_status kap_adjust_logits(
     p.allowed = allowed; p.allowed_row = allowed_row; p.status = device_status;
     p.row_stride = row_stride; p.out_stride = out_stride; p.history_len = history_len; p.bias_len = bias_len; p.allowed_stride = allowed_stride;
     p.rows = rows; p.vocab = vocab; p.num_masks = num_masks;
-    const bool needs_words = history && (repetition || presence || frequency);
-    if (!needs_words) p.history = nullptr;
+    const bool needs_words = history_at && (repetition || presence || frequency);
+    if (!needs_words) p.history_at = nullptr;
     // Slices of at most 16384 tokens (64 KiB of words: three CTAs on an SM), and of fewer where there are rows too few to fill the device: every CTA of a
     // row reads its whole history, so no more than that (512 rows of 128256, histories of 2000 to 4000: 8 slices 118 us, 10 120, 12
     // 123; one row with 20000: 8 slices 14 us, 64 8).

@@ -259,6 +259,26 @@ def test_captured_and_on_another_stream():
     assert torch.equal(first, out)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+def test_lists_without_entries(in_place):
+    # the first step of a batch: nothing said yet, no biases; offsets that leave the empty lists are reported
+    c = Case(53, 3, 500)
+    empty = lambda t: torch.zeros(0, dtype=t, device=gu.DEV)                       # noqa: E731
+    a = dict(c.args(), history=empty(torch.int32), history_at=torch.zeros(3, 3, dtype=torch.int64, device=gu.DEV), bias_indptr=torch.zeros(4, dtype=torch.int32, device=gu.DEV),
+             bias_token=empty(torch.int32), bias_value=empty(F32), device_status=c.status)
+    before = c.logits.clone()
+    out = kap.adjust_logits(c.logits, None if in_place else c.out, **a)
+    assert torch.equal(out, before) and int(c.status[0]) == 0
+    a["history_at"][1, 2] = 1
+    assert torch.equal(kap.adjust_logits(c.logits, None if in_place else c.out, **a), before)
+    assert int(c.status[0]) == 1 << kap.ERR_DEVICE_INDEX
+    c.status.zero_()
+    a["history_at"].zero_()
+    a["bias_indptr"][3] = 2
+    assert torch.equal(kap.adjust_logits(c.logits, None if in_place else c.out, **a), before)
+    assert int(c.status[0]) == 1 << kap.ERR_DEVICE_INDEX
+
+
 def test_calls_of_two_threads():
     # calls that need different amounts of shared memory, from two threads at once: both kernels of the shared-memory sizes that have to be asked for
     import threading

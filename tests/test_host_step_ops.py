@@ -84,6 +84,12 @@ def test_adjust_logits_refusals(change, code):
     assert kap.lib().kap_last_error()
 
 
+@pytest.mark.parametrize("change", [dict(history=None, history_len=0, at=None), dict(bias_at=None, bias_token=None, bias_value=None), dict(bias_token=None, bias_value=None, bias_len=5),
+                                    dict(bias_at=None, bias_len=0)])
+def test_adjust_logits_refuses_half_a_rule(change):
+    assert _call("kap_adjust_logits", LOGITS, change) == INVALID
+
+
 def test_adjust_logits_of_nothing():
     assert _call("kap_adjust_logits", LOGITS, dict(rows=0)) == kap.OK
 
