@@ -574,9 +574,9 @@ kap_status kap_append_kv_rope(
  *   new_indptr [batch+1]                     first new row of each sequence (kap_append_kv_rope's new_indptr, kap_chunk_attn's q_indptr), or NULL
  *   slot, position [new_indptr[batch]]       page * page_size + place in it, and logical index, of each new row; each may be NULL
  * Entries behind the last one are left as they were.  All or nothing: a step that cannot be built (stack, table row, bt_capacity or
- * row_capacity too small: KAP_ERR_CAPACITY; a request out of range or named twice, a negative length, a sequence of 2^31 tokens and more, a pages_held or free_count out of
+ * row_capacity too small: KAP_ERR_CAPACITY; a request out of range or named twice, a negative length, a pages_held or free_count out of
  * range: KAP_ERR_DEVICE_INDEX; as 1 << code in *device_status) changes no state and leaves bt_indptr and new_indptr all 0, which the
- * append and attention calls take as a step without rows.
+ * append and attention calls take as a step without rows.  (A sequence of 2^31 tokens fits no table row, whatever the page size.)
  * kap_release_pages: of each request in request[0 .. n-1] (NULL: requests 0 .. n-1) the pages beyond ceil(keep_tokens / page_size) (NULL: all)
  * go back, the i-th to free_pages[free_count + all - 1 - i]: released at once, the pages of a step lie where it took them from.  A request
  * that holds fewer keeps them.  All or nothing as above (KAP_ERR_CAPACITY: free_capacity).

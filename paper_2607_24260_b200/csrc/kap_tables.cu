@@ -37,7 +37,7 @@ __device__ __forceinline__ Entry load_entry(const TableParams& p, int b, uint32_
     e.request = p.request ? p.request[b] : b;
     const int L = p.ctx_len ? p.ctx_len[b] : 0;
     e.n = kRelease ? 0 : p.n_new ? p.n_new[b] : 1;
-    if (e.request < 0 || e.request >= p.num_requests || L < 0 || e.n < 0 || L > INT32_MAX - e.n) { e.bad = true; e.n = 0; return e; }
+    if (e.request < 0 || e.request >= p.num_requests || L < 0 || e.n < 0) { e.bad = true; e.n = 0; return e; }
     e.held = p.pages_held[e.request];
     if (seen) e.bad = atomicOr(&seen[e.request >> 5], 1u << (e.request & 31)) >> (e.request & 31) & 1u;   // named twice
     if (e.held < 0 || e.held > p.table_stride) { e.bad = true; e.held = 0; }
@@ -46,7 +46,7 @@ __device__ __forceinline__ Entry load_entry(const TableParams& p, int b, uint32_
         e.pages = (int32_t)min(pages, (long long)e.held);
         e.moved = e.held - e.pages;
     } else {
-        if (pages > p.table_stride) { e.full = true; return e; }
+        if (pages > p.table_stride || L > INT32_MAX - e.n) { e.full = true; return e; }      // (a position has 32 bits)
         e.pages = (int32_t)pages;
         e.moved = max(0, e.pages - e.held);
     }

@@ -254,11 +254,11 @@ def test_many_requests():
 
 
 @pytest.mark.parametrize("ctx,new", [(2 ** 31 - 1, 5), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31 - 4, 4)])
-def test_a_sequence_of_2_to_the_31_tokens_is_reported(ctx, new):
+def test_a_sequence_of_2_to_the_31_tokens_is_refused(ctx, new):
     # with large pages its table is short, but its positions pass 32 bits
     s = Server(2, 4096, 4000, page=2 ** 20)
     s.step([0, 2 ** 31 - 8], [3, 5])
     got, *_ = s.build([7, ctx], [1, new], capacity=5000, rows=64)
-    assert int(s.status[0]) == 1 << kap.ERR_DEVICE_INDEX
+    assert int(s.status[0]) == 1 << kap.ERR_CAPACITY
     assert not got["bt_indptr"].any() and not got["new_indptr"].any() and (got["slot"] == -9).all()
     s.expect_state()
