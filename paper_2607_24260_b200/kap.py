@@ -757,7 +757,11 @@ def adjust_logits(logits, out=None, history=None, history_at=None, repetition=No
         masks, words = allowed.shape[0], allowed.stride(0) if allowed.shape[0] > 1 else allowed.shape[1]
         if allowed.shape[1] * 32 < vocab:
             raise KapError(ERR_INVALID_ARG, f"allowed has {allowed.shape[1]} words for {vocab} logits")
-    if bias_token is not None and bias_value is not None and bias_token.numel() != bias_value.numel():
+    if (history is None) != (history_at is None):
+        raise KapError(ERR_INVALID_ARG, "history and history_at go together")
+    if (bias_token is None) != (bias_indptr is None) or (bias_value is None) != (bias_indptr is None):
+        raise KapError(ERR_INVALID_ARG, "bias_indptr, bias_token and bias_value go together")
+    if bias_token is not None and bias_token.numel() != bias_value.numel():
         raise KapError(ERR_INVALID_ARG, f"{bias_token.numel()} bias tokens, {bias_value.numel()} values")
     _check(lib().kap_adjust_logits(
         logits.data_ptr(), kind, vocab if rows <= 1 else logits.stride(0), rows, vocab, out.data_ptr(), vocab if rows <= 1 else out.stride(0),

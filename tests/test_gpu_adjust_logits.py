@@ -279,6 +279,16 @@ def test_lists_without_entries(in_place):
     assert int(c.status[0]) == 1 << kap.ERR_DEVICE_INDEX
 
 
+def test_half_a_rule_is_refused():
+    c = Case(54, 3, 100)
+    a = c.args()
+    for change in (dict(history=None), dict(history_at=None), dict(bias_indptr=None), dict(bias_token=None), dict(bias_value=None), dict(bias_token=None, bias_value=None)):
+        with pytest.raises(kap.KapError) as e:
+            kap.adjust_logits(c.logits, c.out, **{**a, **change})
+        assert e.value.code == kap.ERR_INVALID_ARG
+    assert bool((c.out == 7).all())
+
+
 def test_calls_of_two_threads():
     # calls that need different amounts of shared memory, from two threads at once: both kernels of the shared-memory sizes that have to be asked for
     import threading
