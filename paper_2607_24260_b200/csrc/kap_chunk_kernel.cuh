@@ -859,32 +859,48 @@ __device__ __forceinline__ ChunkStates cut_states(int c, int cuts) {   // cuts c
 __device__ __forceinline__ ChunkStates piece_states(const ChunkInStep& v, int of) {
     return {of, v.n_cut, of + (long long)(v.pieces - 1) * v.n_cut, v.pieces};
 }
-__device__ __forceinline__ void chunk_merge_row(const ChunkParams& p, const ChunkStates& of, int R, int tok0, int head) {
+// kRows rows from R on, every `apart`-th, with kBatch states of each in flight; rows from `end` on are left out.
+template <int kRows, int kBatch>
+__device__ __forceinline__ void chunk_merge_rows(const ChunkParams& p, const ChunkStates& of, int R, int apart, int end, int tok0, int head) {
     const int lane = threadIdx.x & 31;
-    Merged acc;
-    acc.m = -INFINITY; acc.l = 0.f; acc.o = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int kBatch = 8;
+    Merged acc[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) { acc[r].m = -INFINITY; acc[r].l = 0.f; acc[r].o = make_float4(0.f, 0.f, 0.f, 0.f); }
     for (int i0 = 0; i0 < of.n; i0 += kBatch) {
-        float2 ml[kBatch];
-        float4 o[kBatch];
+        float2 ml[kRows][kBatch];
+        float4 o[kRows][kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-            const int i = min(i0 + j, of.n - 1);
-            const long long row = (i < of.n - 1 ? of.first + i * of.stride : of.last) * kChunkUnitRows + R;
-            ml[j] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + row * 2));
-            o[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + row * kHeadDim) + lane);
+            const int i = i0 + j;
+            const long long state = (i < of.n - 1 ? of.first + i * of.stride : of.last) * kChunkUnitRows;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                ml[r][j] = make_float2(-INFINITY, 0.f);
+                if (i < of.n && R + r * apart < end) {
+                    const long long row = state + R + r * apart;
+                    ml[r][j] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + row * 2));
+                    o[r][j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + row * kHeadDim) + lane);
+                }
+            }
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
-            if (i0 + j < of.n && ml[j].y != 0.f) merge_into(acc, ml[j].x, ml[j].y, o[j]);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+                if (ml[r][j].y != 0.f) merge_into(acc[r], ml[r][j].x, ml[r][j].y, o[r][j]);
     }
-    const long long cell = (long long)(tok0 + (R >> p.log2_g)) * p.hq + (head << p.log2_g) + (R & (p.G - 1));
-    const float inv = acc.l == 0.f ? 0.f : 1.f / acc.l;
-    uint2 v;
-    v.x = pack_bf16(acc.o.x * inv, acc.o.y * inv);
-    v.y = pack_bf16(acc.o.z * inv, acc.o.w * inv);
-    *reinterpret_cast<uint2*>(p.out + cell * kHeadDim + lane * 4) = v;
-    if (p.lse && lane == 0) p.lse[cell] = acc.l == 0.f ? -INFINITY : (acc.m + log2f(acc.l)) * 0.6931471805599453f;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int at = R + r * apart;
+        if (at >= end) break;
+        const long long cell = (long long)(tok0 + (at >> p.log2_g)) * p.hq + (head << p.log2_g) + (at & (p.G - 1));
+        const float inv = acc[r].l == 0.f ? 0.f : 1.f / acc[r].l;
+        uint2 v;
+        v.x = pack_bf16(acc[r].o.x * inv, acc[r].o.y * inv);
+        v.y = pack_bf16(acc[r].o.z * inv, acc[r].o.w * inv);
+        *reinterpret_cast<uint2*>(p.out + cell * kHeadDim + lane * 4) = v;
+        if (p.lse && lane == 0) p.lse[cell] = acc[r].l == 0.f ? -INFINITY : (acc[r].m + log2f(acc[r].l)) * 0.6931471805599453f;
+    }
 }
 
 // Many rows: most are in units that one CTA finished.  Block (c, part): 32 rows of the unit in which CTA c begins, if no CTA before it begins in its
@@ -923,7 +939,13 @@ kap_chunk_merge_kernel(const ChunkParams p, const int n_cta)
         rows = cut.rows_head & 0xffff; head = cut.rows_head >> 16; tok0 = cut.tok0;
         states = cut_states(c, n);
     }
-    for (int R = row0 + warp; R < min(rows, row0 + kChunkMergeRows); R += kChunkMergeThreads / 32) chunk_merge_row(p, states, R, tok0, head);
+    constexpr int kWarps = kChunkMergeThreads / 32, kEach = kChunkMergeRows / kWarps;
+    const int end = min(rows, row0 + kChunkMergeRows);
+    if (states.n == 2) {                                               // the usual cut: all rows of the warp at once
+        chunk_merge_rows<kEach, 2>(p, states, row0 + warp, kWarps, end, tok0, head);
+    } else {
+        for (int R = row0 + warp; R < end; R += kWarps) chunk_merge_rows<1, 8>(p, states, R, 0, end, tok0, head);
+    }
 }
 
 // Few rows, most of them in units cut many times: a warp for each (row, head), which finds its unit's states itself.  (50 rows at 4K: the call 26 us,
@@ -963,7 +985,8 @@ kap_chunk_merge_rows_kernel(const ChunkParams p, const int n_cta)
         states = cut_states(first, n);
     }
     const int tok0 = s.row0 + tile * R;
-    chunk_merge_row(p, states, ((row - tok0) << p.log2_g) + (h & (p.G - 1)), tok0, head);
+    const int at = ((row - tok0) << p.log2_g) + (h & (p.G - 1));
+    chunk_merge_rows<1, 8>(p, states, at, 0, at + 1, tok0, head);
 }
 
 }  // namespace kap
