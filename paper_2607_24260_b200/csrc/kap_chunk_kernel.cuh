@@ -66,8 +66,10 @@ struct alignas(16) ChunkSegment {                                      // what o
     int32_t slot;                                                      // of its partial state; -1: the whole unit, writes the output
 };
 struct ChunkCut { long long unit; int32_t inside, tok0, rows_head, pad; };   // where a CTA begins; inside: in the middle of this unit
-// In step (see chunk_plan): units of one sequence, the first ones whole, the last n_cut cut into `pieces` each; pieces = 0: not in step.
+// In step (see chunk_in_step): units of one sequence, the first ones whole, the last n_cut cut into `pieces` each; pieces = 0: not in step.
+// Dealt (see chunk_deal): seq = -1, pieces = 1, `whole` units, none cut.
 struct ChunkInStep { int32_t pieces, n_cut, whole, seq; };
+constexpr int kChunkDealSeqs = 16, kChunkDealRounds = 3;               // dealing: sequences at most, units for each CTA at least
 constexpr int kChunkStates = 4;                                        // states a CTA, 256 rows each, that the workspace holds
 constexpr int kChunkMostPieces = 16, kChunkPieceCost = 8;              // cost of a piece beyond its steps (products to fill, state), in steps
 constexpr long long kChunkInStepBytes = 48ll << 20;
@@ -82,6 +84,7 @@ struct ChunkControl {
     int32_t timed_out;
     int32_t n_segments, more;                                          // of this round; another round follows
     int32_t active, active_seq;                                        // sequences with rows, one of them
+    uint32_t has_rows[kChunkThreads / 32];                             // a bit for each sequence, in batches of up to kChunkThreads
     ChunkInStep in_step;
     // plan: this CTA's range of the tape
     int32_t seq, unit, step, end_seq, end_unit, end_step, first_done;
@@ -184,19 +187,115 @@ __device__ __forceinline__ void chunk_in_step(const ChunkParams& p, ChunkControl
     }
 }
 
+// Whole units dealt out: where there are many of falling cost, prompts above all, a range of the tape each leaves CTAs with cut units (states, and the join)
+// and with no more even shares than the costs are right.  Instead units are sorted by the tokens that they see, a counting sort in closed form: tile k of a
+// sequence is in class lo / R + 1 + k (lo: its cached tokens, R: tokens of a tile), a solo unit in that of a pair of its cost; and CTA i takes the units at
+// i, 2 n - 1 - i, 2 n + i, ... .  (Prompts of 3 x 5000 231 us, on the tape 250; 2 x 4096 286 and 310; 1 x 4096 158 and 178.)  Not where whole units cannot
+// be shared evenly: the last, incomplete round has to cost less than an eighth of a share (2 x 2048 behind 8K, 3.5 units a CTA: an estimate of 618 us, on the tape
+// 570), the dearest unit less than 3 / 5.
+struct ChunkDealt { int32_t base, pairs, solo; };                      // of a lane's sequence: first class and number of pairs, class of the solo unit or -1
+__device__ __forceinline__ ChunkDealt chunk_dealt(const ChunkParams& p, const ChunkControl& c, ChunkSeq& s) {
+    int b = -1, rank = threadIdx.x & 31;                               // the rank-th sequence with rows
+    if (rank < c.active) {
+#pragma unroll 1
+        for (int w = 0; w < kChunkThreads / 32; ++w) {
+            uint32_t has = c.has_rows[w];
+            const int n = __popc(has);
+            if (rank >= n) { rank -= n; continue; }
+            while (rank--) has &= has - 1u;
+            b = w * 32 + __ffs(has) - 1;
+            break;
+        }
+    }
+    ChunkDealt d{0, 0, -1};
+    s = ChunkSeq{0, 0, 0, 0};
+    if (b >= 0) {
+        bool bad;
+        s = chunk_seq(p, b, bad);
+        const int R = kChunkUnitRows >> p.log2_g, t = chunk_tiles(p, s.n), rest = s.n - (t - 1) * R, lo = max(0, s.length - s.n);
+        const long long knee = (long long)p.window + p.n_sink + rest, seen = p.window ? min((long long)s.length, knee) : s.length;
+        d.base = lo / R + 1;
+        d.pairs = t;
+        if (rest * p.G <= kChunkTileRows) { --d.pairs; d.solo = (int)max(0ll, seen / 2 - kChunkUnitCost / 2) / R; }
+    }
+    return d;
+}
+// of the sequences' units (of one KV head) those in class h and above
+__device__ __forceinline__ int chunk_dealt_from(const ChunkDealt& d, int active, int h) {
+    int n = 0;
+    for (int i = 0; i < active; ++i) {
+        const int base = __shfl_sync(0xffffffffu, d.base, i), pairs = __shfl_sync(0xffffffffu, d.pairs, i), solo = __shfl_sync(0xffffffffu, d.solo, i);
+        n += min(max(base + pairs - h, 0), pairs) + (solo >= h && solo >= 0 ? 1 : 0);
+    }
+    return n;
+}
+// the q-th of them, in falling classes: (lane of its sequence, tile); every lane has a q of its own
+__device__ __forceinline__ int2 chunk_dealt_at(const ChunkDealt& d, int active, int q) {
+    int lo = 0, hi = __reduce_max_sync(0xffffffffu, max(d.base + d.pairs, d.solo + 1));      // from(lo) > q >= from(hi)
+    for (int left = hi; left > 0; left >>= 1) {
+        const int mid = (lo + hi) >> 1;
+        const bool more = chunk_dealt_from(d, active, mid) > q;
+        if (hi - lo > 1) { if (more) lo = mid; else hi = mid; }
+    }
+    int rest = q - chunk_dealt_from(d, active, lo + 1);
+    int2 at = make_int2(0, 0);
+    bool found = false;
+    for (int i = 0; i < active; ++i) {
+        const int base = __shfl_sync(0xffffffffu, d.base, i), pairs = __shfl_sync(0xffffffffu, d.pairs, i), solo = __shfl_sync(0xffffffffu, d.solo, i);
+        if (lo >= base && lo < base + pairs) {
+            if (!found && rest == 0) { at = make_int2(i, lo - base); found = true; }
+            --rest;
+        }
+        if (solo == lo) {
+            if (!found && rest == 0) { at = make_int2(i, pairs); found = true; }
+            --rest;
+        }
+    }
+    return at;
+}
+// whether to deal; called by one warp
+__device__ __forceinline__ void chunk_deal(const ChunkParams& p, ChunkControl& c) {
+    const int lane = threadIdx.x & 31, n_cta = gridDim.x, active = c.active;
+    ChunkSeq s;
+    const ChunkDealt d = chunk_dealt(p, c, s);
+    const int units = __reduce_add_sync(0xffffffffu, chunk_tiles(p, s.n)) * p.hkv;
+    if (units < kChunkDealRounds * n_cta) return;
+    // the dearest unit, and the dearest of the last, incomplete round
+    const int last = units / n_cta * n_cta, q = lane == 0 || last == units ? 0 : last / p.hkv;
+    const int2 at = chunk_dealt_at(d, active, q);
+    ChunkSeq o;
+    o.row0 = 0; o.list_at = 0;
+    o.n = __shfl_sync(0xffffffffu, s.n, at.x); o.length = __shfl_sync(0xffffffffu, s.length, at.x);
+    const long long cost = chunk_cost(p, o, at.y + 1) - chunk_cost(p, o, at.y);
+    const long long dearest = __shfl_sync(0xffffffffu, cost, 0), tail = last == units ? 0 : __shfl_sync(0xffffffffu, cost, 1);
+    long long share = 0;
+    for (int w = 0; w < kChunkThreads / 32; ++w) share += c.warp_sum[w];
+    share /= n_cta;
+    if (8 * tail > share || 5 * dearest > 3 * share) return;
+    if (lane == 0) {
+        const ChunkInStep v{1, 0, units, -1};
+        c.in_step = v;
+        if (blockIdx.x == 0) *p.in_step = v;
+        c.unit = 0;
+    }
+}
+
 // this CTA's ends; called by all threads
 __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = (p.batch + kChunkThreads - 1) / kChunkThreads;
     long long mine = 0;
+    bool rows = false;
     for (int i = 0; i < per; ++i) {
         const int b = tid * per + i;
         if (b >= p.batch) break;
         bool bad;
         const ChunkSeq s = chunk_seq(p, b, bad);
         if (bad && blockIdx.x == 0) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
-        if (s.n > 0) { atomicAdd(&c.active, 1); c.active_seq = b; }
+        if (s.n > 0) { atomicAdd(&c.active, 1); c.active_seq = b; rows = true; }
         mine += chunk_cost(p, s, chunk_tiles(p, s.n)) * p.hkv;
     }
+    const uint32_t has_rows = __ballot_sync(0xffffffffu, rows);
+    if (lane == 0) c.has_rows[warp] = has_rows;
     long long upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -206,13 +305,17 @@ __device__ __forceinline__ void chunk_plan(const ChunkParams& p, ChunkControl& c
     if (lane == 31) c.warp_sum[warp] = upto;
     if (tid < 2) c.cut_seq[tid] = p.batch;                             // the tape's end
     __syncthreads();
-    if (c.active == 1) {
-        if (warp == 0) chunk_in_step(p, c);
+    const bool deals = c.active > 0 && c.active <= kChunkDealSeqs && per == 1;
+    if (c.active == 1 || deals) {
+        if (warp == 0) {
+            if (c.active == 1) chunk_in_step(p, c);
+            __syncwarp();
+            if (deals && !c.in_step.pieces) chunk_deal(p, c);
+        }
         __syncthreads();
         if (c.in_step.pieces) return;
-    } else if (tid == 0 && blockIdx.x == 0) {
-        p.in_step->pieces = 0;
     }
+    if (tid == 0 && blockIdx.x == 0) p.in_step->pieces = 0;
     long long total = 0, before = 0;
 #pragma unroll
     for (int w = 0; w < kChunkThreads / 32; ++w) {
@@ -288,6 +391,29 @@ __device__ __forceinline__ void chunk_segments(const ChunkParams& p, ChunkShared
     const int lane = threadIdx.x & 31, R = (kChunkUnitRows >> p.log2_g);
     if (c.in_step.pieces) {
         const ChunkInStep v = c.in_step;
+        if (v.seq < 0) {
+            ChunkSeq s;
+            const ChunkDealt d = chunk_dealt(p, c, s);
+            const int n_cta = gridDim.x, cta = blockIdx.x, first = c.unit, rounds = v.whole / n_cta, turn = rounds & 1 ? n_cta - 1 - cta : cta;
+            const int all = rounds + (rounds * n_cta + turn < v.whole ? 1 : 0), take = min(all - first, kChunkMaxSegments);
+            for (int k0 = 0; k0 < take; k0 += 32) {
+                const int k = first + min(k0 + lane, take - 1), q = k * n_cta + (k & 1 ? n_cta - 1 - cta : cta);
+                const int2 at = chunk_dealt_at(d, c.active, q / p.hkv);
+                ChunkSeq o;
+                o.row0 = __shfl_sync(0xffffffffu, s.row0, at.x); o.n = __shfl_sync(0xffffffffu, s.n, at.x);
+                o.length = __shfl_sync(0xffffffffu, s.length, at.x); o.list_at = __shfl_sync(0xffffffffu, s.list_at, at.x);
+                ChunkSegment g;
+                g.list_at = o.list_at; g.tok0 = o.row0 + at.y * R; g.lo = o.length - o.n + at.y * R;
+                g.rows_head = (min(R, o.n - at.y * R) << p.log2_g) | (q % p.hkv) << 16;
+                g.step_begin = 0; g.step_end = chunk_steps(p, o, at.y);
+                g.length = o.length;
+                g.slot = -1;
+                if (k0 + lane < take) sh.segments[k0 + lane] = g;
+            }
+            __syncwarp();
+            if (lane == 0) { c.n_segments = take; c.more = first + take < all; c.unit = first + take; }
+            return;
+        }
         bool bad;
         const ChunkSeq s = chunk_seq(p, v.seq, bad);
         const int t = chunk_tiles(p, s.n), n_cta = gridDim.x, first = c.unit, rounds = v.whole / n_cta, cut = v.n_cut * v.pieces;

@@ -205,6 +205,29 @@ def test_a_long_context_that_all_walk_together(n, ctx, hq, hkv, window, sink):
         c.check(out, lse, rows=40 if ctx * hq > 200000 else None)
 
 
+@pytest.mark.parametrize("layout", [HND, NHD])
+@pytest.mark.parametrize("sequences,hq,hkv,window,sink", [
+    ([(3600, 3600)], 32, 8, 0, 0), ([(3567, 3600)], 32, 8, 0, 0), ([(2000, 2000), (0, 30), (1801, 1801), (0, 0), (77, 200), (1, 700)], 32, 8, 0, 0),
+    ([(1200, 1300), (700, 3000), (2000, 1990), (33, 33)], 32, 8, 200, 10), ([(130 + 97 * i, 130 + 98 * i) for i in range(16)], 16, 4, 0, 0),
+    ([(130 + 97 * i, 130 + 98 * i) for i in range(17)], 16, 4, 0, 0), ([(0, 5)] * 360 + [(2500, 2500), (1100, 1100)], 32, 8, 0, 0), ([(4000, 4000), (3900, 3900)], 16, 1, 0, 0),
+    ([(4500, 4500), (1000, 1000)], 24, 24, 0, 0),
+])
+def test_many_whole_units(sequences, hq, hkv, window, sink, layout):
+    # prompts whose units are dealt out whole, on both sides of the limits of that
+    c = Case(40 + len(sequences), sequences, hq, hkv, layout, window=window, sink=sink)
+    out, lse = c.call()
+    c.check(out, lse, rows=150)
+
+
+def test_more_dealt_units_than_one_round_plans():
+    # 64 heads of 176 tiles, 76 units a CTA
+    c = Case(45, [(45056, 45056)], 64, 64, window=300, sink=3)
+    out, lse = c.call()
+    c.check(out, lse, rows=64)
+    again = c.call()
+    assert torch.equal(out.view(torch.int16), again[0].view(torch.int16)) and torch.equal(lse.view(torch.int32), again[1].view(torch.int32))
+
+
 def test_agrees_with_verify_attn():
     c = Case(10, [(4, 700), (1, 33), (8, 2000)], 8, 2, behind=0)
     out, lse = c.call()
