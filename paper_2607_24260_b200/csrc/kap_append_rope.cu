@@ -15,6 +15,12 @@
 // Layout: one CTA per token row, 128 threads; a thread task is two 16-byte pieces of one head that hold
 // both partners of eight pairs, so a rotation never crosses threads and q may be rotated in place.  What hides the look-ups is other
 // CTAs on the SM: reading a thread's values before them costs registers and was slower (2 x 8192 rows: 72 us with the 10 CTAs that then fit on an SM, 68 with 12, 66 with 16).
+//
+// kap_append_kv_norm_rope is the same kernel with the heads of q and k normalised first: y = x / sqrt(mean(x^2) + eps) w, then the rotation, all in fp32.
+// A head's eight threads are neighbours and exchange their sums of squares (three shuffles).  Bound: 2 x 8192 rows of 32 / 8 heads take 77 us, 5.2 TB/s,
+// at 64 % of the issue slots; without norms 66.  Arithmetic on pairs of values (55.7 million warp instructions, 69.9 without), values loaded a task
+// ahead, the first ones before the look-ups, 8 CTAs on an SM (the first ones behind the look-ups 79 us, only those ahead 84; 7 CTAs 76, but 83 instead of 79 with
+// half of a head rotated; 9 and 10 CTAs without loads ahead 79 and 84).  64 single rows: 4.6 us.
 #include "kap_ptx.cuh"
 
 namespace kap {

