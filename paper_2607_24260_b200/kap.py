@@ -656,6 +656,13 @@ def append_kv_norm_rope(q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, 
 def _norm_arguments(norm, Hq, Hkv, d, dev):
     """(q_weight, k_weight, type, per head, unit offset, eps) of kap_append_kv_norm_rope"""
     q_weight, k_weight, eps, unit_offset = norm
+    if Hq and q_weight is not None and k_weight is not None and q_weight.dtype is k_weight.dtype and (k_weight.dtype is _F32 or k_weight.dtype is _BF16) and \
+            q_weight.is_contiguous() and k_weight.is_contiguous() and q_weight.get_device() == dev and k_weight.get_device() == dev:
+        shapes, heads = (q_weight.shape, k_weight.shape), 0
+        if shapes == ((Hq, d), (Hkv, d)):
+            heads = 1
+        if heads or shapes == ((d,), (d,)):                       # the usual forms; all others, and what is wrong, below
+            return (q_weight.data_ptr(), k_weight.data_ptr(), NORM_F32 if k_weight.dtype is _F32 else NORM_BF16, heads, 1 if unit_offset else 0, eps)
     kinds = set()
     for name, w, heads in (("q_weight", q_weight, Hq), ("k_weight", k_weight, Hkv)):
         if w is None or (name == "q_weight" and Hq == 0):
@@ -726,6 +733,14 @@ def _append_rope(norm, q, k_new, v_new, kv_pool, bt_indptr, bt_pages, ctx_len, i
         _check(lib().kap_append_kv_norm_rope(*first, *middle, *rest))
 
 
+def _array(name, t, dtype, n, dev):
+    """the address of a contiguous tensor of n elements (n < 0: any number)"""
+    if t.dtype is not dtype or (n >= 0 and t.numel() != n) or not t.is_contiguous() or t.get_device() != dev:
+        raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}, expected a contiguous {dtype} "
+                       f"tensor{f' of {n}' if n >= 0 else ''} on GPU {dev}")
+    return t.data_ptr()
+
+
 def adjust_logits(logits, out=None, history=None, history_at=None, repetition=None, presence=None, frequency=None, bias_indptr=None,
                   bias_token=None, bias_value=None, allowed=None, allowed_row=None, device_status=None, stream=None):
     """kap_adjust_logits on torch CUDA tensors: logits and out fp32 or bf16 [rows, vocab] (any row stride; out None: in place);
@@ -741,14 +756,6 @@ def adjust_logits(logits, out=None, history=None, history_at=None, repetition=No
     elif out.dtype is not logits.dtype or out.shape != logits.shape or (vocab > 1 and out.stride(1) != 1) or out.get_device() != dev:
         raise KapError(ERR_INVALID_ARG, f"out is {out.dtype} {tuple(out.shape)} with strides {out.stride()} on {out.device}, logits {logits.dtype} {tuple(logits.shape)} on GPU {dev}")
 
-    def ptr(name, t, dt, n):
-        if t is None:
-            return None
-        if t.dtype is not dt or (t.numel() != n and n >= 0) or not t.is_contiguous() or t.get_device() != dev:
-            raise KapError(ERR_INVALID_ARG, f"{name} is {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}, expected a contiguous {dt} "
-                           f"tensor{f' of {n}' if n >= 0 else ''} on GPU {dev}")
-        return t.data_ptr()
-
     f32, i32 = _F32, _I32
     masks = words = 0
     if allowed is not None:
@@ -763,13 +770,20 @@ def adjust_logits(logits, out=None, history=None, history_at=None, repetition=No
         raise KapError(ERR_INVALID_ARG, "bias_indptr, bias_token and bias_value go together")
     if bias_token is not None and bias_token.numel() != bias_value.numel():
         raise KapError(ERR_INVALID_ARG, f"{bias_token.numel()} bias tokens, {bias_value.numel()} values")
+    wide = vocab if rows <= 1 else logits.stride(0)
     _check(lib().kap_adjust_logits(
-        logits.data_ptr(), kind, vocab if rows <= 1 else logits.stride(0), rows, vocab, out.data_ptr(), vocab if rows <= 1 else out.stride(0),
-        ptr("history", history, i32, -1), 0 if history is None else history.numel(), ptr("history_at", history_at, _torch.int64, 3 * rows),
-        ptr("repetition", repetition, f32, rows), ptr("presence", presence, f32, rows), ptr("frequency", frequency, f32, rows),
-        ptr("bias_indptr", bias_indptr, i32, rows + 1), ptr("bias_token", bias_token, i32, -1), ptr("bias_value", bias_value, f32, -1),
-        0 if bias_token is None else bias_token.numel(),
-        _dptr(allowed), masks, words, ptr("allowed_row", allowed_row, i32, rows), ptr("device_status", device_status, i32, 1), _stream_on(dev, stream)))
+        logits.data_ptr(), kind, wide, rows, vocab, out.data_ptr(), wide if out is logits else vocab if rows <= 1 else out.stride(0),
+        None if history is None else _array("history", history, i32, -1, dev), 0 if history is None else history.numel(),
+        None if history_at is None else _array("history_at", history_at, _torch.int64, 3 * rows, dev),
+        None if repetition is None else _array("repetition", repetition, f32, rows, dev),
+        None if presence is None else _array("presence", presence, f32, rows, dev),
+        None if frequency is None else _array("frequency", frequency, f32, rows, dev),
+        None if bias_indptr is None else _array("bias_indptr", bias_indptr, i32, rows + 1, dev),
+        None if bias_token is None else _array("bias_token", bias_token, i32, -1, dev),
+        None if bias_value is None else _array("bias_value", bias_value, f32, -1, dev), 0 if bias_token is None else bias_token.numel(),
+        None if allowed is None else allowed.data_ptr(), masks, words,
+        None if allowed_row is None else _array("allowed_row", allowed_row, i32, rows, dev),
+        None if device_status is None else _array("device_status", device_status, i32, 1, dev), _stream_on(dev, stream)))
     return out
 
 
