@@ -575,12 +575,14 @@ kap_status kap_append_kv_rope(
  *   slot, position [new_indptr[batch]]       page * page_size + place in it, and logical index, of each new row; each may be NULL
  * Entries behind the last one are left as they were.  All or nothing: a step that cannot be built (stack, table row, bt_capacity or
  * row_capacity too small: KAP_ERR_CAPACITY; a request out of range or named twice, a negative length, a pages_held or free_count out of
- * range: KAP_ERR_DEVICE_INDEX; as 1 << code in *device_status) changes no state and leaves bt_indptr and new_indptr all 0, which the
+ * range, a new row on a page that was given back: KAP_ERR_DEVICE_INDEX; as 1 << code in *device_status) changes no state and leaves bt_indptr and new_indptr all 0, which the
  * append and attention calls take as a step without rows.  (A sequence of 2^31 tokens fits no table row, whatever the page size.)
  * kap_release_pages: of each request in request[0 .. n-1] (NULL: requests 0 .. n-1) the pages beyond ceil(keep_tokens / page_size) (NULL: all)
  * go back, the i-th to free_pages[free_count + all - 1 - i]: released at once, the pages of a step lie where it took them from.  A request
  * that holds fewer keeps them.  All or nothing as above (KAP_ERR_CAPACITY: free_capacity).
- * The pages of a sliding window's past are not tracked: entries of page_table that no row sees may be overwritten by the caller, but count as held.
+ * Pages that no later row of a request sees (a sliding window's past) may be given back by the caller between two calls: put on the stack, free_count
+ * raised, and their entries of page_table set to a negative number.  Such entries count as held and are listed in bt_pages as they are; a release
+ * passes them over (they are not among its `all`), and a step whose new rows would lie on one is not built.  No other entry below pages_held may be changed.
  * Two calls that share state must be ordered.  Asynchronous on cuda_stream, without a workspace; can be captured into a CUDA graph.
  * Errors: KAP_ERR_INVALID_ARG (NULL or misaligned pointer, negative size, batch > num_requests, slot or position without new_indptr),
  * KAP_ERR_UNSUPPORTED (num_requests above 1048576), KAP_ERR_CUDA.

@@ -2,11 +2,12 @@
 // block tables and slot mappings, Section 3.1, are taken as given by its host runtime).
 //
 // Mathematics: with L tokens cached, n new ones and held pages, sequence b lists ceil((L + n) / P) pages and takes those it does not hold from the
-// top of a stack of free pages; where a sequence's list, new rows and taken pages begin are three prefix sums over the batch.
+// top of a stack of free pages; where a sequence's list, new rows and taken pages begin are three prefix sums over the batch.  A negative entry of the
+// page table is a page that its request has given back: a release passes it over, and a new row may not lie on it.
 // Layout: one CTA does the sums, the checks and the state (page table, held pages, stack), all or nothing; a second kernel, started while
 // the first runs, copies the lists and writes the slots, a CTA for each 2048 entries, whose owners it finds by bisection.
-// Bound: latency.  A step and its release are three kernels, each a chain of look-ups: 11 us for 64 sequences at 16K, 18 us for 512 of up to 128K (the bytes
-// alone 0.03 and 1.5 us).
+// Bound: latency.  A step and its release are three kernels, each a chain of look-ups: 11 us for 64 sequences at 16K, 19 us for 512 of up to 128K (the bytes
+// alone 0.03 and 1.5 us); of the 19, 0.7 look at the pages that first rows lie on and 0.4 at the released entries for negative ones.
 #include <cuda_runtime.h>
 
 #include "kap_internal.h"
@@ -30,16 +31,25 @@ struct TableParams {
     int32_t batch, page_size, num_requests, free_capacity;
 };
 
-struct Entry { int32_t request, held, pages, moved, n; bool bad, full; };   // pages: listed (build) or kept (release); moved: taken or given back
+struct Entry {
+    int32_t request, held, pages, moved, n;                   // pages: listed (build) or kept (release); moved: taken, or entries given up
+    bool bad, full, on_held;                                  // on_held: the first new row lies on a page held,
+    int32_t first_page;                                       // this one
+    __device__ __forceinline__ bool on_none() const { return on_held && first_page < 0; }      // it has been given back
+};
 
 template <bool kRelease>
 __device__ __forceinline__ Entry load_entry(const TableParams& p, int b, uint32_t* seen) {
-    Entry e{0, 0, 0, 0, 0, false, false};
+    Entry e{0, 0, 0, 0, 0, false, false, false, 0};
     if (b >= p.batch) return e;
     e.request = p.request ? p.request[b] : b;
     const int L = p.ctx_len ? p.ctx_len[b] : 0;
     e.n = kRelease ? 0 : p.n_new ? p.n_new[b] : 1;
     if (e.request < 0 || e.request >= p.num_requests || L < 0 || e.n < 0) { e.bad = true; e.n = 0; return e; }
+    const int32_t* const row = p.page_table + e.request * p.table_stride;
+    // the page of the first new row, which may be held already: loaded beside the number of those, not behind it, and looked at as late as can be
+    const int first = L / p.page_size;
+    if (!kRelease && seen && e.n > 0 && first < p.table_stride) e.first_page = row[first];
     e.held = p.pages_held[e.request];
     if (seen) e.bad = atomicOr(&seen[e.request >> 5], 1u << (e.request & 31)) >> (e.request & 31) & 1u;   // named twice
     if (e.held < 0 || e.held > p.table_stride) { e.bad = true; e.held = 0; }
@@ -51,6 +61,11 @@ __device__ __forceinline__ Entry load_entry(const TableParams& p, int b, uint32_
         if (pages > p.table_stride || L > INT32_MAX - e.n) { e.full = true; return e; }      // (a position has 32 bits)
         e.pages = (int32_t)pages;
         e.moved = max(0, e.pages - e.held);
+        if (seen && e.n > 0) {                                // new rows on pages held: not on entries that the caller has given back
+            const int end = min(e.held, e.pages);
+            e.on_held = first < end;
+            for (int i = first + 1; i < end; ++i) e.bad |= row[i] < 0;
+        }
     }
     return e;
 }
@@ -80,6 +95,16 @@ __device__ __forceinline__ Sums block_scan(Sums v, Sums& all, Sums* warp_sums) {
     return v + (warp ? before : none);
 }
 
+// The sequence that owns the i-th entry moved of those of a block's threads: upto[t] counts the entries of the first t + 1.
+template <int kThreads>
+__device__ __forceinline__ int moved_by(const int32_t* upto, int i) {
+    int lo = 0;                                               // sequences whose entries all come before i
+#pragma unroll
+    for (int d = kThreads / 2; d > 0; d /= 2)
+        if (upto[lo + d - 1] <= i) lo += d;
+    return lo;
+}
+
 template <bool kRelease, int kThreads>
 __global__ void __launch_bounds__(kThreads)
 kap_tables_kernel(const TableParams p)
@@ -98,13 +123,13 @@ kap_tables_kernel(const TableParams p)
     const Entry e0 = load_entry<kRelease>(p, tid, seen);
     for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
         const Entry e = b0 == 0 ? e0 : load_entry<kRelease>(p, b0 + tid, seen);
-        bad |= e.bad;
+        bad |= e.bad || (b0 > 0 && e.on_none());
         full |= e.full;
         total = total + Sums{e.pages, e.moved, e.n};
     }
     const Sums mine0 = block_scan<kThreads / 32>(total, all, warp_sums);     // (sums of the sequences themselves, when each has a thread)
-    bad = __syncthreads_or(bad);
-    if (kRelease) full = all.moved > (long long)p.free_capacity - count;
+    bad = __syncthreads_or(bad || e0.on_none());
+    if (kRelease) full = all.moved > INT32_MAX;               // (entries are counted in 32 bits from here on, and no stack takes so many)
     else full = __syncthreads_or(full) || all.moved > count || all.pages > p.bt_capacity || all.rows > p.row_capacity;
     if (bad || full) {                                        // nothing is taken: a step without pages and rows
         if (!kRelease)
@@ -115,43 +140,89 @@ kap_tables_kernel(const TableParams p)
         if (tid == 0 && p.status) atomicOr(p.status, 1 << (bad ? KAP_ERR_DEVICE_INDEX : KAP_ERR_CAPACITY));
         return;
     }
-    // ---- the state and the prefix sums
-    Sums carry{0, 0, 0};
-    if (!kRelease && tid == 0) {
-        p.bt_indptr[0] = 0;
-        if (p.new_indptr) p.new_indptr[0] = 0;
-    }
-    for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
-        const int b = b0 + tid;
-        const Entry e = b0 == 0 ? e0 : load_entry<kRelease>(p, b, nullptr);
-        Sums v = mine0, here = all;
+    // The entries moved by the sequences from b0 on, one for each thread, laid out one after the other: upto, first and request, and their number.
+    Entry e = e0;
+    Sums v = mine0;
+    auto lay_out = [&](int b0) {
+        Sums here = all;
+        e = b0 == 0 ? e0 : load_entry<kRelease>(p, b0 + tid, nullptr);
+        v = mine0;
         if (p.batch > kThreads) v = block_scan<kThreads / 32>(Sums{e.pages, e.moved, e.n}, here, warp_sums);
-        if (b < p.batch) {
-            if (!kRelease) {
-                p.bt_indptr[b + 1] = (int32_t)(carry.pages + v.pages);
-                if (p.new_indptr) p.new_indptr[b + 1] = (int32_t)(carry.rows + v.rows);
-            }
-            if (e.moved > 0) p.pages_held[e.request] = e.pages;
-        }
         upto[tid] = (int32_t)v.moved;
         first[tid] = kRelease ? e.pages : e.held;
         request[tid] = e.request;
         __syncthreads();
-        for (int i = tid; i < (int)here.moved; i += kThreads) {
-            int lo = 0;                                       // the owner: sequences whose pages all come before i
-#pragma unroll
-            for (int d = kThreads / 2; d > 0; d /= 2)
-                if (upto[lo + d - 1] <= i) lo += d;
-            const int before = lo ? upto[lo - 1] : 0;
-            int32_t* entry = p.page_table + request[lo] * p.table_stride + first[lo] + (i - before);
-            // the i-th page moved, in the batch's order, is the i-th from the larger of the two tops
-            if (kRelease) p.free_pages[count + all.moved - 1 - (carry.moved + i)] = *entry;
-            else *entry = p.free_pages[count - 1 - (carry.moved + i)];
+        return here;
+    };
+    auto entry_of = [&](int i) {
+        const int lo = moved_by<kThreads>(upto, i), before = lo ? upto[lo - 1] : 0;
+        return p.page_table + request[lo] * p.table_stride + first[lo] + (i - before);
+    };
+    Sums carry{0, 0, 0};
+    if (kRelease) {
+        // The i-th page, in the batch's order, becomes the i-th from the top of the larger stack.  Entries without a page (negative ones) are rare: every
+        // entry is placed as if there were none (in front of nothing that is on the stack), and placed again, counted one by one, if there were.
+        const long long room = (long long)p.free_capacity - count;
+        bool gone = false;
+        for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
+            const Sums here = lay_out(b0);
+            for (int i = tid; i < (int)here.moved; i += kThreads) {
+                const int32_t page = *entry_of(i);
+                gone |= page < 0;
+                if (all.moved <= room) p.free_pages[count + all.moved - 1 - (carry.moved + i)] = page;
+            }
+            carry = carry + here;
+            if (b0 + kThreads < p.batch) __syncthreads();
         }
+        gone = __syncthreads_or(gone);
+        long long back = all.moved;
+        for (int pass = 0; gone && pass < 2; ++pass) {        // counted, then placed
+            long long before = 0;
+            for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
+                const Sums here = lay_out(b0);
+                for (int i0 = 0; i0 < (int)here.moved; i0 += kThreads) {
+                    const int32_t page = i0 + tid < (int)here.moved ? *entry_of(i0 + tid) : -1;
+                    Sums round;
+                    const Sums upto_here = block_scan<kThreads / 32>(Sums{page >= 0, 0, 0}, round, warp_sums);
+                    if (pass == 1 && page >= 0) p.free_pages[count + back - (before + upto_here.pages)] = page;
+                    before += round.pages;
+                    __syncthreads();
+                }
+                __syncthreads();
+            }
+            back = before;
+            if (back > room) break;
+        }
+        if (back > room) {
+            if (tid == 0 && p.status) atomicOr(p.status, 1 << KAP_ERR_CAPACITY);
+            return;
+        }
+        for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
+            if (b0 > 0 || p.batch > kThreads) e = b0 == 0 ? e0 : load_entry<true>(p, b0 + tid, nullptr);
+            if (e.moved > 0) p.pages_held[e.request] = e.pages;
+        }
+        if (tid == 0 && back > 0) *p.free_count = (int32_t)(count + back);
+        return;
+    }
+    // ---- the state and the prefix sums
+    if (tid == 0) {
+        p.bt_indptr[0] = 0;
+        if (p.new_indptr) p.new_indptr[0] = 0;
+    }
+    for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
+        const Sums here = lay_out(b0);
+        const int b = b0 + tid;
+        if (b < p.batch) {
+            p.bt_indptr[b + 1] = (int32_t)(carry.pages + v.pages);
+            if (p.new_indptr) p.new_indptr[b + 1] = (int32_t)(carry.rows + v.rows);
+            if (e.moved > 0) p.pages_held[e.request] = e.pages;
+        }
+        // the i-th page taken, in the batch's order, is the i-th from the top
+        for (int i = tid; i < (int)here.moved; i += kThreads) *entry_of(i) = p.free_pages[count - 1 - (carry.moved + i)];
         carry = carry + here;
         if (b0 + kThreads < p.batch) __syncthreads();
     }
-    if (tid == 0 && all.moved > 0) *p.free_count = (int32_t)(kRelease ? count + all.moved : count - all.moved);
+    if (tid == 0 && all.moved > 0) *p.free_count = (int32_t)(count - all.moved);
 }
 
 // the last sequence whose entries begin at or before i

@@ -560,7 +560,7 @@ def build_block_tables(ctx_len, page_table, pages_held, free_pages, free_count, 
     """kap_build_block_tables on torch CUDA tensors (int32; slot int64): the CSR block table of the step's sequences
     (request[b], ctx_len[b] tokens cached, n_new[b] new ones; None: row b of page_table, one new token), with the pages it lacks taken
     from free_pages[:free_count].  page_table [requests, pages], pages_held [requests], free_pages and free_count [1] are kept up to
-    date; new_indptr [batch + 1], slot and position [rows] are optional."""
+    date (an entry of page_table whose page the caller has put back on the stack itself is negative); new_indptr [batch + 1], slot and position [rows] are optional."""
     requests, wide, dev = _page_state(page_table, pages_held, free_pages, free_count)
     batch, lists = ctx_len.shape[0], bt_pages.numel()
     if ctx_len.dtype is not _I32 or bt_indptr.dtype is not _I32 or bt_pages.dtype is not _I32 or ctx_len.get_device() != dev or \
@@ -600,7 +600,7 @@ def build_block_tables(ctx_len, page_table, pages_held, free_pages, free_count, 
 def release_pages(request, page_table, pages_held, free_pages, free_count, keep_tokens=None, page_size=16, device_status=None,
                   stream=None):
     """kap_release_pages on torch CUDA tensors: the pages of the requests beyond keep_tokens (None: all) go back to the
-    stack; request None names every row of page_table."""
+    stack; negative entries of page_table, whose pages are there already, are passed over.  request None names every row of page_table."""
     requests, wide, dev = _page_state(page_table, pages_held, free_pages, free_count)
     n, request_at, keep_at, status_at = requests, None, None, None
     if request is not None:
