@@ -5,8 +5,9 @@
 // steps of 80 tokens,
 //     S = Q K^T (128 x 80),   p = 2^(S scale - m),   l += sum p,   O += P V (128 x 128),
 // with a lazy reference m: it moves only when a step's maximum exceeds it by more than 8 (weights stay below 256), and then l and O are rescaled.  P is
-// rounded to bf16 for the product (the tensor core's operand type; 2^-8 of each weight, averaged by the sum); l adds the unrounded weights in fp32, so lse
-// keeps fp32 accuracy.  Parts of a unit leave (m, l, O) in fp32, and states of the same row join as M = max m, l = sum 2^(m_i - M) l_i, O likewise.
+// rounded to bf16 for the product (the tensor core's operand type; 2^-8 of each weight, averaged by the sum); l adds the unrounded weights in fp32.
+// Parts of a unit leave (m, l, O) in fp32, and states of the same row join as M = max m, l = sum 2^(m_i - M) l_i, O likewise.  No part is longer than 2048 steps
+// (see kChunkPartSteps), so l is off by at most 2^-24 (2048 + 22 + the number of parts) of itself, and by far less where errors average.
 //
 // A unit is two tiles of one sequence and KV head (256 rows, a pair), or its last rows if they fit one tile (solo), over the pages that they see: all
 // up to the last row's own, or the sinks' pages and those from the first row's window on.  A pair gives each of two streams a tile and both the same K and V;
@@ -24,7 +25,7 @@
 // burst, 4.2 ms at 1.6 GHz sustained, 1.04 to 1.09 PFLOP/s of 1.37 that a plain product sustains).  Sixteen softmax warps with half a row each took the
 // same time, sixteen with quarter rows (16-lane loads) 1.6 times as long.  A unit costs about 5.2 us beyond its steps of 1.3.
 //
-// Every wait on an mbarrier is bounded, anew for each segment; when one runs out the CTA sets KAP_ERR_TIMEOUT, later waits return at once, the roles run
+// Every wait on an mbarrier is bounded, anew for each part of a segment; when one runs out the CTA sets KAP_ERR_TIMEOUT, later waits return at once, the roles run
 // to their end inside this CTA's shared and tensor memory, copies and products in flight are waited for (bounded again), tensor memory is freed and
 // the kernel returns.
 #pragma once
@@ -51,12 +52,19 @@ constexpr int kChunkQHalfBytes = kChunkTileRows * 128;                 // 128 ro
 constexpr int kChunkQBytes = 2 * kChunkQHalfBytes;
 constexpr int kChunkTmemP = 80, kChunkTmemO = 128;                     // columns of a stream's 256; S from 0
 constexpr int kChunkMaxSegments = 72;                                  // planned at a time
-// A sequence's tokens: a whole unit of so many takes a CTA a second, half of what its waits may take, and steps stay far below the sentinel of chunk_in_step.
+// A sequence's tokens: a whole unit of so many takes a CTA two seconds, and steps stay far below the sentinel of chunk_in_step.
 constexpr int kChunkMostTokens = 1 << 26;
 // What a unit costs, to place the cuts and for nothing else: its tokens and, for the first products and the epilogue, some more, times 2 with two
 // tiles.  (Windowed batch 835 us, with 5 : 3 910, 3 : 1 895; 2 x 4096 on the tape 316 us, with 320 tokens more 327, with 240 341.)
 constexpr int kChunkUnitCost = 400, kChunkPairCost = 2, kChunkSoloCost = 1;
 constexpr int kChunkLeastCost = 640;                                   // of a CTA's share: fewer CTAs work when there is little to do
+
+// One sum over all steps of a long context would lose what is small beside it (2^24 equal weights of 0.37 in a pair: l 0.13 % off, and O, whose products the
+// tensor core adds without rounding to nearest, 9 %; 128K of them 0.0014 % and 0.04 %).  So a segment is done in parts of at most so many steps (163840 tokens),
+// each with fresh sums, whose states join one after the other in memory: l and O are then off by no more than those of 128K, the time is the same to 0.5 %, and
+// waits have their limits for a part of some milliseconds, not for a unit, which may take seconds.
+// (Joined in a function that the loop over the steps calls, prompts took 2 to 3 % longer.)
+constexpr int kChunkPartSteps = 2048;
 
 struct alignas(16) ChunkSegment {                                      // what one CTA does of one unit (query tile pair, KV head)
     int32_t list_at;                                                   // the sequence's first entry in bt_pages
@@ -97,6 +105,19 @@ struct ChunkShared {
     ChunkControl c;
     alignas(16) ChunkSegment segments[kChunkMaxSegments];
 };
+// The next part of segment k, of which `done` steps have been dealt with; moves both on.
+__device__ __forceinline__ ChunkSegment chunk_next_part(const ChunkShared& sh, int& k, int& done) {
+    ChunkSegment s = sh.segments[k];
+    s.step_begin += done;
+    if (s.step_end - s.step_begin > kChunkPartSteps) {
+        s.step_end = s.step_begin + kChunkPartSteps;
+        done += kChunkPartSteps;
+    } else {
+        done = 0;
+        ++k;
+    }
+    return s;
+}
 constexpr int kChunkCtlBytes = 3 * 1024;
 constexpr int kChunkSmemBytes = 2 * kChunkQBytes + kChunkSlots * kChunkSlotBytes + kChunkCtlBytes;
 static_assert(sizeof(ChunkShared) <= kChunkCtlBytes && kChunkSmemBytes <= 232448, "shared memory");
@@ -596,7 +617,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
     pdl_wait();                                                        // nothing of the caller's is read above
     pdl_launch_dependents();
     chunk_plan(p, *c);
-    uint64_t deadline = global_ns() + kWaitBudgetNs;                   // of a segment's waits; every role sets it anew
+    uint64_t deadline = global_ns() + kWaitBudgetNs;                   // of a part's waits; every role sets it anew
     volatile int32_t* const late = &c->timed_out;
     auto wait = [&](unsigned long long& bar, uint32_t parity) {
         return mbar_try_wait(smem_u32(&bar), parity) || wait_slowly(smem_u32(&bar), parity, deadline, late);
@@ -622,8 +643,8 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
         // ---- copies: one warp brings the query tiles and K, another V, which is needed later, so that neither waits for the other's slots.  Up
         // to five a step, issued by one elected lane with warp-uniform coordinates.
         const int v = warp == kChunkSoftmaxWarps ? 0 : 1;
-        for (int k = 0; k < n_segments && ok; ++k) {
-            const ChunkSegment s = sh.segments[k];
+        for (int k = 0, done = 0; k < n_segments && ok;) {
+            const ChunkSegment s = chunk_next_part(sh, k, done);
             deadline = global_ns() + kWaitBudgetNs;
             const int rows = s.rows_head & 0xffff, kv_head = s.rows_head >> 16;
             const ChunkPages g = chunk_pages(p, s.lo, s.lo + (rows >> p.log2_g) - 1);
@@ -690,8 +711,8 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
         const uint64_t q_desc = umma_smem_desc(smem_u32(q_tiles), 16, 1024), k_desc = umma_smem_desc(smem_u32(slots), 16, kChunkGroupBytes);
         // V: 16 tokens (K) x 128 columns (N), N contiguous; columns 64-127 in the other half of a group
         const uint64_t v_desc = umma_smem_desc(smem_u32(slots), kChunkHalfBytes, kChunkGroupBytes);
-        for (int k = 0; k < n_segments; ++k) {
-            const ChunkSegment seg = sh.segments[k];
+        for (int k = 0, done = 0; k < n_segments;) {
+            const ChunkSegment seg = chunk_next_part(sh, k, done);
             deadline = global_ns() + kWaitBudgetNs;
             const int rows = __shfl_sync(0xffffffffu, seg.rows_head & 0xffff, 0);
             const ChunkPages g = chunk_pages(p, seg.lo, seg.lo + (rows >> p.log2_g) - 1);
@@ -771,8 +792,12 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
         const int stream = warp >> 2;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + stream * 256, t_p = t_s + kChunkTmemP, t_o = t_s + kChunkTmemO;
         const float sc = p.scale_log2;
-        for (int k = 0; k < n_segments; ++k) {
-            const ChunkSegment seg = sh.segments[k];
+        for (int k = 0, done = 0; k < n_segments;) {
+            const bool joins = done > 0;                               // to the state that the parts before have left
+            ChunkSegment seg = chunk_next_part(sh, k, done);
+            const bool whole = seg.slot < 0 && done == 0;              // the unit's results, not a state
+            // (of a unit that is not cut: a state that this CTA does not use otherwise, or not before)
+            if (seg.slot < 0) seg.slot = (int)(c->in_step.pieces ? blockIdx.x : 2 * gridDim.x + blockIdx.x);
             deadline = global_ns() + kWaitBudgetNs;
             const int rows = seg.rows_head & 0xffff, kv_head = seg.rows_head >> 16;
             const bool pair = rows > kChunkTileRows;
@@ -870,7 +895,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                 if (lane == 0) mbar_arrive(smem_u32(&c->p_ready[stream]));
                 ++count; ++mine;
             }
-            // ---- the segment's result: the output of a whole unit, a state of a part of one
+            // ---- the part's result: the output of a whole unit, or a state
             if (mine > 0) {
                 wait(c->pv_done[stream], (uint32_t)(count - 1) & 1u);
                 __syncwarp();
@@ -894,14 +919,26 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                 m_ref = m;
                 col0 = stream * (kHeadDim / 2); col1 = col0 + kHeadDim / 2;
             }
+            const long long state = (long long)seg.slot * kChunkUnitRows + R;
+            float factor2 = 0.f;                                       // of the state that it joins
+            if (joins) {
+                float2 prior = make_float2(-INFINITY, 0.f);
+                if (valid) prior = *reinterpret_cast<const float2*>(p.part_ml + state * 2);
+                if (!pair) pair_barrier(1 + (warp & 3));               // both streams have read it
+                const float m = fmaxf(m_ref, prior.x), mu = m == -INFINITY ? 0.f : m, factor = ex2(m_ref - mu);
+                factor2 = ex2(prior.x - mu);
+                factor0 *= factor; factor1 *= factor;
+                l = l * factor + prior.y * factor2;
+                m_ref = m;
+            }
             if (any_valid) {
                 const bool own = mine > 0, both = !pair && n_steps > 1, have = pair ? own : n_steps > 0;
                 const uint32_t t_first = pair ? t_o : t_lane + kChunkTmemO, t_second = t_lane + 256 + kChunkTmemO;
                 const float f0 = pair || stream == 0 ? factor0 : factor1, f1 = stream == 0 ? factor1 : factor0;
                 const bool empty = l == 0.f;                           // (the sum of a query that is not finite is NaN, and so is its result)
-                const float inv = seg.slot >= 0 ? 1.f : empty ? 0.f : 1.f / l;
+                const float inv = !whole ? 1.f : empty ? 0.f : 1.f / l;
                 const int tok = seg.tok0 + (R >> p.log2_g), h = (kv_head << p.log2_g) + (R & (p.G - 1));
-                const long long cell = (long long)tok * p.hq + h, state = (long long)seg.slot * kChunkUnitRows + R;
+                const long long cell = (long long)tok * p.hq + h;
 #pragma unroll 1
                 for (int i = col0; i < col1; i += 32) {
                     float o[32];
@@ -911,7 +948,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                         tmem_ld16_nowait(t_first + i + 16, u[1]);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(u[e >> 4][e & 15]) * (pair ? 1.f : f0);
+                        for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(u[e >> 4][e & 15]) * f0;
                         if (both) {
                             tmem_ld16_nowait(t_second + i, u[0]);
                             tmem_ld16_nowait(t_second + i + 16, u[1]);
@@ -923,7 +960,15 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = 0.f;
                     }
-                    if (valid && seg.slot < 0) {
+                    if (joins && valid) {
+                        const float4* const prior = reinterpret_cast<const float4*>(p.part_o + state * kHeadDim + i);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float4 x = prior[e];
+                            o[4 * e] += x.x * factor2; o[4 * e + 1] += x.y * factor2; o[4 * e + 2] += x.z * factor2; o[4 * e + 3] += x.w * factor2;
+                        }
+                    }
+                    if (valid && whole) {
                         uint32_t v[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) v[e] = empty ? 0u : pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
@@ -942,7 +987,7 @@ kap_chunk_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_consta
                     }
                 }
                 if (valid && (pair || stream == 0)) {
-                    if (seg.slot >= 0) *reinterpret_cast<float2*>(p.part_ml + state * 2) = make_float2(m_ref, l);
+                    if (!whole) *reinterpret_cast<float2*>(p.part_ml + state * 2) = make_float2(m_ref, l);
                     else if (p.lse) p.lse[cell] = empty ? -INFINITY : (m_ref + log2f(l)) * 0.6931471805599453f;
                 }
             }
