@@ -77,8 +77,8 @@ __device__ __forceinline__ LogitRow load_row(const LogitParams& p, int row, bool
     v.r.repetition = rep > 0.f ? rep : 1.f;
     v.r.presence = pres == pres ? pres : 0.f;
     v.r.frequency = freq == freq ? freq : 0.f;
-    if (v.r.repetition == 1.f && v.r.presence == 0.f && v.r.frequency == 0.f) v.h0 = v.h1 = v.h2 = 0;
     if (v.h0 < 0 || v.h1 < v.h0 || v.h2 < v.h1 || v.h2 > p.history_len || v.h2 - v.h0 > (long long)kCountMask) { bad = true; v.h0 = v.h1 = v.h2 = 0; }
+    if (v.r.repetition == 1.f && v.r.presence == 0.f && v.r.frequency == 0.f) v.h0 = v.h1 = v.h2 = 0;      // (checked all the same)
     if (v.b0 < 0 || v.b1 < v.b0 || v.b1 > p.bias_len) { bad = true; v.b0 = v.b1 = 0; }
     v.mask = m >= 0 && m < p.num_masks ? p.allowed + m * p.allowed_stride : nullptr;
     if (m < -1 || m >= p.num_masks) bad = bad || p.allowed;
@@ -329,7 +329,6 @@ extern "C" kap_status kap_adjust_logits(
     p.row_stride = row_stride; p.out_stride = out_stride; p.history_len = history_len; p.bias_len = bias_len; p.allowed_stride = allowed_stride;
     p.rows = rows; p.vocab = vocab; p.num_masks = num_masks;
     const bool needs_words = history_at && (repetition || presence || frequency);
-    if (!needs_words) p.history_at = nullptr;
     // Slices of at most 16384 tokens (64 KiB of words: three CTAs on an SM), and of fewer where there are rows too few to fill the device: every CTA of a
     // row reads its whole history, so no more than that (512 rows of 128256, histories of 2000 to 4000: 8 slices 118 us, 10 120, 12
     // 123; one row with 20000: 8 slices 14 us, 64 8).
