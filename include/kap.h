@@ -772,8 +772,8 @@ enum {
  *   x2 = c > 0 ? x1 - frequency[r] c - presence[r] : x1
  *   x3 = x2 + the sum of the row's biases of t
  *   out = t is allowed ? x3 : -inf
- * in fp32, rounded to the logits' type once.  out may be logits (in place: only logits that change are written); it must not overlap
- * them otherwise.
+ * in fp32, rounded to the logits' type once.  out may be logits (in place: those beside one that changes, up to 16 bytes, may be written again as they
+ * are, and nothing outside the rows); it must not overlap them otherwise.
  *   history_at[r] = {b, a, e}: the prompt is history[b .. a-1], the answer history[a .. e-1]; rows may share tokens (the rows of a verification
  *                   window, each one longer than the one before).  Tokens outside 0 .. vocab-1 are passed over.
  *   bias_indptr     biases bias_indptr[r] .. bias_indptr[r+1]-1 belong to row r, ascending by token; of equal tokens all are added, in order.

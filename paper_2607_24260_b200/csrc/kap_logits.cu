@@ -7,7 +7,7 @@
 // Layout: a row is cut into slices of the vocabulary, a CTA each.  The CTA keeps a 32-bit word for each of its tokens in shared memory (times in the
 // answer; whether in the prompt; whether it has a bias), reads the row's whole history and counts the tokens that are its own, and then passes over its slice
 // once, logits, words and mask together; its first logits are loaded before the history is counted.  Tokens with a bias are left to the biases' pass.
-// Bound: memory without a history (512 rows of 128256: 80 us, a plain copy's rate).  A history of 2000 to 4000 tokens a row makes it 118 us: 40 of the 82
+// Bound: memory without a history (512 rows of 128256: 80 us, a plain copy's rate).  A history of 2000 to 4000 tokens a row makes it 118 us: 57 of the 82
 // million warp instructions are its words' (cleared, counted, found and corrected).  Words in a cluster's shared memory, the history dealt out: 210 us, since
 // frequent tokens meet at one address; a list of touched words corrected after the copy: 158, since their logits are then waited for once more.
 #include <cuda_bf16.h>
@@ -57,7 +57,7 @@ __device__ __forceinline__ float penalised(float x, uint32_t word, const Rules& 
     return x;
 }
 
-// The values of a row that decide what has to be done, the same for its whole cluster.
+// The values of a row that decide what has to be done, the same in all of its CTAs.
 struct LogitRow {
     Rules r;
     long long h0, h1, h2;
@@ -107,7 +107,7 @@ kap_adjust_logits_kernel(const LogitParams p)
     uint4* const dst = reinterpret_cast<uint4*>(out + v0 + head);
     // the word of token v0 + i is words[i], placed so that a vector's words are aligned
     uint32_t* const words = reinterpret_cast<uint32_t*>(word_space) + (kVec - row_head) % kVec;
-    uint4 ahead[kAhead];
+    uint4 ahead[kAhead];                                      // (loaded before it is known whether the row has a mask, whose pass reads for itself)
     if (!in_place) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
@@ -240,7 +240,7 @@ kap_adjust_logits_kernel(const LogitParams p)
                 uint32_t open = __ldg(q.mask + word) >> k;
                 if (k + kVec > 32) open |= __ldg(q.mask + word + 1) << (32 - k);
                 open &= kAllOpen;
-                if (open == 0u) { __stcs(dst + i, minus_inf_vector<T>()); continue; }       // (nothing is read)
+                if (open == 0u) { __stcs(dst + i, minus_inf_vector<T>()); continue; }       // (needs no logits)
                 uint32_t w[kVec], left = 0u, hits = counted ? find(i, w, left) & open : 0u;
                 left &= open;
                 if (open == kAllOpen && hits == 0u && in_place) continue;
@@ -332,7 +332,7 @@ extern "C" kap_status kap_adjust_logits(
     // Slices of at most 16384 tokens (64 KiB of words: three CTAs on an SM), and of fewer where there are rows too few to fill the device: every CTA of a
     // row reads its whole history, so no more than that (512 rows of 128256, histories of 2000 to 4000: 8 slices 118 us, 10 120, 12
     // 123; one row with 20000: 8 slices 14 us, 64 8).
-    constexpr int kOneWave = 148 * 3, kMostSlices = 64;
+    constexpr int kOneWave = 148 * 3, kMostSlices = 64;       // 148 SMs of a B200; only this choice uses it
     const int least = (vocab + kMostSlice - 1) / kMostSlice;
     int slices = least < kMostSlices ? (kOneWave / rows < least ? least : kOneWave / rows > kMostSlices ? kMostSlices : kOneWave / rows) : least;
     p.slice = ((vocab + slices - 1) / slices + 31) / 32 * 32;
