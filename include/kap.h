@@ -779,7 +779,8 @@ enum {
  *   bias_indptr     biases bias_indptr[r] .. bias_indptr[r+1]-1 belong to row r, ascending by token; of equal tokens all are added, in order.
  *                   Tokens outside 0 .. vocab-1 are passed over.
  *   allowed         bit t % 32 of word t / 32 of mask allowed_row[r] (NULL: mask r; -1: every token is allowed) says whether t is allowed
- * A NULL array switches its rule off (history and the bias lists may be NULL with a length of 0, when no row has any); so do, for a row, a repetition that is not above 0 and a NaN presence or frequency.
+ * A NULL array switches its rule off (history and the bias lists may be NULL with a length of 0, when no row has any); so do, for a row, a
+ * repetition that is not above 0 and a NaN presence or frequency.
  * Reported in *device_status (1 << KAP_ERR_DEVICE_INDEX): a history_at that is out of order or leaves 0 .. history_len (or spans 2^30 tokens and
  * more; the row then has no history), a bias_indptr that falls or leaves 0 .. bias_len (the row
  * then has no biases), an allowed_row below -1 or beyond the masks (the row is not masked), biases out of order (the results of such

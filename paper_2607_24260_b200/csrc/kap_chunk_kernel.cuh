@@ -57,7 +57,9 @@ constexpr int kChunkMostTokens = 1 << 26;
 // What a unit costs, to place the cuts and for nothing else: its tokens and, for the first products and the epilogue, some more, times 2 with two
 // tiles.  (Windowed batch 835 us, with 5 : 3 910, 3 : 1 895; 2 x 4096 on the tape 316 us, with 320 tokens more 327, with 240 341.)
 constexpr int kChunkUnitCost = 400, kChunkPairCost = 2, kChunkSoloCost = 1;
-constexpr int kChunkLeastCost = 640;                                   // of a CTA's share: fewer CTAs work when there is little to do
+// Of a CTA's share: fewer CTAs work when there is little to do.  (32 / 8 heads, with 320, 640 and 1280: one token at 100 14.4, 17.8, 22.6 us, at 1K 16.9, 20.3, 22.0, at 4K
+// 23.1, 21.6, 25.6; 16 tokens at 1K 26.6, 26.4, 27.2; 50 rows of 500 21.4, 23.9, 27.3, behind 4K 28.4, 28.5, 31.2.)
+constexpr int kChunkLeastCost = 640;
 
 // One sum over all steps of a long context would lose what is small beside it (2^24 equal weights of 0.37 in a pair: l 0.13 % off, and O, whose products the
 // tensor core adds without rounding to nearest, 9 %; 128K of them 0.0014 % and 0.04 %).  So a segment is done in parts of at most so many steps (163840 tokens),
@@ -187,7 +189,9 @@ __device__ __forceinline__ int chunk_steps(const ChunkParams& p, const ChunkSeq&
 // How one sequence whose rows all see a long context is divided: instead of a range of the tape, which begins anywhere in a unit, CTA i takes the
 // units i, i + n, ... as far as they go round, and of the rest, each cut into pieces, the pieces i, i + n, ... in the order of the context.  All CTAs
 // then walk the same tokens at about the same time, tiles of one head next to each other, so that K and V come from L2, which could not hold the
-// 512 MB of 128K tokens (2048 rows behind them sustained 4.87 ms on the tape, 4.06 so).  Called by one warp.
+// 512 MB of 128K tokens (2048 rows behind them sustained 4.87 ms on the tape, 4.06 so).  Around the limits, bursts, tape / in step: 512 rows behind 12000 (47 MiB of K and
+// V) 117 / 114 us, behind 32K 275 / 285, 64K 551 / 524; 2048 behind 16K 468 / 497, 32K 983 / 961, 64K 2032 / 1864; with eight tokens for each row 4096
+// rows behind 32K 1897 / 1947, with four 8192 rows 3765 / 3819: up to 6 % either way, until the context is well beyond L2.  Called by one warp.
 __device__ __forceinline__ void chunk_in_step(const ChunkParams& p, ChunkControl& c) {
     const int lane = threadIdx.x & 31, n_cta = gridDim.x;
     bool bad;
@@ -212,9 +216,10 @@ __device__ __forceinline__ void chunk_in_step(const ChunkParams& p, ChunkControl
 // Whole units dealt out: where there are many of falling cost, prompts above all, a range of the tape each leaves CTAs with cut units (states, and the join)
 // and with no more even shares than the costs are right.  Instead units are sorted by the tokens that they see, a counting sort in closed form: tile k of a
 // sequence is in class lo / R + 1 + k (lo: its cached tokens, R: tokens of a tile), a solo unit in that of a pair of its cost; and CTA i takes the units at
-// i, 2 n - 1 - i, 2 n + i, ... .  (Prompts of 3 x 5000 231 us, on the tape 250; 2 x 4096 286 and 310; 1 x 4096 158 and 178.)  Not where whole units cannot
-// be shared evenly: the last, incomplete round has to cost less than an eighth of a share (2 x 2048 behind 8K, 3.5 units a CTA: an estimate of 618 us, on the tape
-// 570), the dearest unit less than 3 / 5.
+// i, 2 n - 1 - i, 2 n + i, ... .  (Prompts of 3 x 5000 231 us, on the tape 250; 2 x 4096 286 and 310; 1 x 4096 143 and 161.)  Not where whole units cannot
+// be shared evenly: the last, incomplete round has to cost less than an eighth of a share, the dearest unit less than 3 / 5.  Inside these limits dealing took 0.85 to
+// 1.00 of the tape's time in 20 batches of all kinds.  Outside it may gain or lose.  Last round: 1 x 4400 (0.13 of a share) tape 180, dealt 160 us; 2 x 2048 behind 1K
+// (0.20) 161, 151; behind 4K (0.25) 327, 345; behind 8K (0.27) 559, 604.  Dearest unit: 1 x 2600 (0.78) 85, 72; 64 rows behind 16K beside short prompts (2.1) 148, 344.
 struct ChunkDealt { int32_t base, pairs, solo; };                      // of a lane's sequence: first class and number of pairs, class of the solo unit or -1
 __device__ __forceinline__ ChunkDealt chunk_dealt(const ChunkParams& p, const ChunkControl& c, ChunkSeq& s) {
     int b = -1, rank = threadIdx.x & 31;                               // the rank-th sequence with rows
