@@ -528,8 +528,8 @@ kap_status kap_materialize_view(
  * next (views of one fused projection are fine).  q_out may be q itself (in place); it must not
  * overlap q otherwise, nor k_new or v_new.  q == NULL: only k and v are handled.
  * Rows outside new_indptr[0] .. new_indptr[batch] - 1 belong to no sequence: nothing is written for
- * them.  A token without a page, with a page outside the pool or of a sequence with a negative ctx_len is
- * reported in *device_status (1 << KAP_ERR_DEVICE_INDEX); its k and v are not written, its q_out is.
+ * them.  A token without a page, with a page outside the pool, of a sequence with a negative ctx_len or in
+ * front of its sequence's first row (a new_indptr that falls) is reported in *device_status (1 << KAP_ERR_DEVICE_INDEX); its k and v are not written, its q_out is.
  * With new_indptr == NULL one kernel does everything; with it, advance != 0 adds a second one that
  * moves ctx_len.  Asynchronous on cuda_stream; can be captured into a CUDA graph.
  * Errors: KAP_ERR_UNSUPPORTED (head_dim, page_size; rotary_dim not a multiple of 16 in 16 .. 128),

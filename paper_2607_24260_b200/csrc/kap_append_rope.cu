@@ -178,7 +178,8 @@ kap_append_kv_rope_kernel(const RopeParams p, const NormParams n)
     const long long at = (long long)L + place;      // logical index of the token
     const int list0 = p.bt_indptr[b], n_bt = p.bt_indptr[b + 1] - list0;
     int32_t page = -1;
-    if (L >= 0 && at / kPageSize < n_bt) page = p.bt_pages[list0 + at / kPageSize];
+    if (L >= 0 && place >= 0 && at / kPageSize < n_bt) page =            // (place < 0: offsets that fall)
+        p.bt_pages[list0 + at / kPageSize];
     const bool stored = page >= 0 && page < p.num_pool_pages;
     if (!stored && tid == 0 && p.status) atomicOr(p.status, 1 << KAP_ERR_DEVICE_INDEX);
     if (tid < p.half) {

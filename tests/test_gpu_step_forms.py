@@ -95,3 +95,27 @@ def test_tables_without_the_optional_arrays():
     assert pg.tolist() == [first, s.table[1, 0], s.table[1, 1], s.table[2, 0], s.table[2, 1], third, -9, -9]
     s.expect_state()
     assert int(s.status[0]) == 0
+
+
+@pytest.mark.parametrize("norms", [False, True])
+@pytest.mark.parametrize("indptr,length", [([0, 10, 4, 12], 0), ([0, 10, 4, 12], 3), ([0, 40, 1, 42], 0)])
+def test_offsets_that_fall_write_nothing_in_front(indptr, length, norms):
+    # rows that lie in front of their sequence's first one; the sequences' pages are in the middle of the pool, all others stay
+    hq, hkv, rows, g = 8, 2, indptr[-1], torch.Generator(device=gu.DEV).manual_seed(30)
+    rand = lambda heads: torch.randn((rows, heads, D), device=gu.DEV, generator=g).to(torch.bfloat16)      # noqa: E731
+    q, k, v = rand(hq), rand(hkv), rand(hkv)
+    pool = torch.full((40, 2, hkv, PAGE, D), 3.0, dtype=torch.bfloat16, device=gu.DEV)
+    pages = np.arange(20, 29)                                       # three a sequence
+    status = torch.zeros(1, dtype=torch.int32, device=gu.DEV)
+    inv = torch.ones(D // 2, device=gu.DEV)
+    call = kap.append_kv_norm_rope if norms else kap.append_kv_rope
+    call(q, k, v, pool, gu.i32([0, 3, 6, 9]), gu.i32(pages), gu.i32([length] * 3), inv, q_out=torch.empty_like(q), new_indptr=gu.i32(indptr), advance=False, device_status=status)
+    assert int(status[0]) == 1 << kap.ERR_DEVICE_INDEX
+    keep = torch.ones(40, dtype=torch.bool, device=gu.DEV)
+    keep[20:29] = False
+    assert bool((pool[keep] == 3.0).all())
+    # v of the rows that have an owner: those of the first sequence and of the last, whose first row is the offset's
+    heads = pool.permute(0, 1, 3, 2, 4)
+    for b, row in ((0, 0), (2, rows - 1)):
+        pos = length + row - indptr[b]
+        assert torch.equal(heads[20 + 3 * b + pos // PAGE, 1, pos % PAGE], v[row])
