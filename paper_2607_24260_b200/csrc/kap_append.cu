@@ -38,8 +38,8 @@ kap_append_kv_kernel(const uint4* __restrict__ k_new, const uint4* __restrict__ 
         const int j = i / (kRowVec * hkv * 2);
         const long long pos = (long long)L + j;
         const long long lp = pos / kPageSize;
-        int32_t page = lp < n_bt ? bt_pages[bt_indptr[b] + lp] : -1;
-        if (L < 0 || page < 0 || page >= num_pool_pages) {       // report, never write out of range
+        int32_t page = L >= 0 && lp < n_bt ? bt_pages[bt_indptr[b] + lp] : -1;
+        if (page < 0 || page >= num_pool_pages) {       // report, never write out of range
             if (status) atomicOr(status, 1 << KAP_ERR_DEVICE_INDEX);
             continue;
         }
