@@ -6,8 +6,8 @@
 // page table is a page that its request has given back: a release passes it over, and a new row may not lie on it.
 // Layout: one CTA does the sums, the checks and the state (page table, held pages, stack), all or nothing; a second kernel, started while
 // the first runs, copies the lists and writes the slots, a CTA for each 2048 entries, whose owners it finds by bisection.
-// Bound: latency.  A step and its release are three kernels, each a chain of look-ups: 11 us for 64 sequences at 16K, 19 us for 512 of up to 128K (the bytes
-// alone 0.03 and 1.5 us); of the 19, 0.7 look at the pages that first rows lie on and 0.4 at the released entries for negative ones.
+// Bound: latency.  A step and its release are three kernels, each a chain of look-ups: 10.4 us for 64 sequences at 16K, 18.3 us for 512 of up to 128K (the bytes
+// alone 0.03 and 1.5 us); of the 18.3, 0.7 look at the pages that first rows lie on.  Each alone (cold): sums 5.7 and 7, lists and slots 9.5 and 13, release 5 and 7.
 #include <cuda_runtime.h>
 
 #include "kap_internal.h"
@@ -66,6 +66,7 @@ __device__ __forceinline__ Entry load_entry(const TableParams& p, int b, uint32_
         if (seen && e.n > 0) {                                // new rows on pages held: not on entries that the caller has given back
             const int end = min(e.held, e.pages);
             e.on_held = first < end;
+            // (64 chunks of 512 on pages held 9 us, of 8192 17, one of 131072 111: by whole warps 10, 54, 20)
             for (int i = first + 1; i < end; ++i) e.bad |= row[i] < 0;
         }
     }

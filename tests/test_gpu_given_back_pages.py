@@ -95,6 +95,29 @@ def test_new_rows_need_a_page(batch):
             s.expect_build(got, ctx + tail, *rest)
 
 
+def test_long_chunks_on_pages_held():
+    # every place of a chunk's pages, of several chunks in one step
+    s = Server(40, 500, 19000)                                     # 18073 pages are needed
+    ctx, new = np.arange(40) * 37, np.full(40, 6500)
+    s.step(ctx, new)                                               # more than 400 pages each
+    s.step(ctx, new)                                               # the same rows again: nothing is taken
+    for r, i in ((0, 0), (1, 2), (7, 1 + (7 * 37) // 16), (7, 34), (7, 200), (33, 300), (39, 400), (39, 496), (38, 493)):
+        was, held = int(s.table[r, i]), bool(i < s.held[r])
+        s.table[r, i] = -1
+        s.dev["page_table"].copy_(gu.i32(s.table))
+        s.status.zero_()
+        needed = ctx[r] // 16 <= i < (ctx[r] + 6500 + 15) // 16
+        got, *rest = s.build(ctx, new)
+        assert held and int(s.status[0]) == (INDEX if needed else 0)
+        if not needed:
+            s.expect_build(got, ctx, *rest)
+        s.expect_state()
+        s.table[r, i] = was
+        s.dev["page_table"].copy_(gu.i32(s.table))
+    s.status.zero_()
+    s.step(ctx, new)
+
+
 def test_an_index_beyond_the_row_is_not_followed():
     # the look-up of the first row's page stays inside the table; such a step is refused
     s = Server(3, 12, 40)
