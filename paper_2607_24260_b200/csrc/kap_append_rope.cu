@@ -20,7 +20,7 @@
 // A head's eight threads are neighbours and exchange their sums of squares (three shuffles).  Bound: 2 x 8192 rows of 32 / 8 heads take 77 us, 5.2 TB/s,
 // at 64 % of the issue slots; without norms 66.  Arithmetic on pairs of values (55.7 million warp instructions, 69.9 without), values loaded a task
 // ahead, the first ones before the look-ups, 8 CTAs on an SM (the first ones behind the look-ups 79 us, only those ahead 84; 7 CTAs 76, but 83 instead of 79 with
-// half of a head rotated; 9 and 10 CTAs without loads ahead 79 and 84).  64 single rows: 4.6 us.
+// half of a head rotated; 9 and 10 CTAs without loads ahead 79 and 84).  64 single rows: 4.5 us.
 #include "kap_ptx.cuh"
 
 namespace kap {
